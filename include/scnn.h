@@ -235,6 +235,98 @@ int density_regulariser(const float* out_feats, int64_t rows, const int64_t* row
  * {weights removed by this call, non-zero weights left}. */
 int prune_weights(float* w, unsigned char* warned, int64_t n_w, float eps, int64_t* counts, void* hip_stream);
 
+/* ---------------------------------------------------------------- layers on rows of values
+ * Linear layers and layer norm act on row-major arrays [rows, channels]: the
+ * value rows of a sparse tensor (one layer for every occupied site), or the
+ * flattened dense maps behind sparse_to_dense.  Rows are contiguous; arrays are
+ * aligned to their element and start anywhere.  `dtype` (SCNN_F32, SCNN_BF16,
+ * SCNN_F16) is the type of all arrays of a call but those named fp32 or fp64;
+ * sums and statistics are fp32 or wider and results are rounded once.  A value
+ * that is exactly 0 is an ordinary 0 here, not an absent entry.  `rows` is a
+ * host number; with rows_dev (nullable, device) the count is read from there
+ * (0 .. rows; less counts as 0, more as rows), so that a call follows
+ * sparse_conv_fwd without a host read: rows past the count are neither read nor
+ * written, in outputs too.  An array that a call writes may overlap no other
+ * array of the call, the workspace included (refused; see linear_fwd's residual).
+ * The calls allocate nothing, wait for nothing,
+ * contain no memset and can be captured in a HIP graph; calls that run at the
+ * same time need workspaces of their own. */
+#define SCNN_F32 0
+#define SCNN_BF16 1
+#define SCNN_F16 2
+
+#define SCNN_ACT_NONE 0
+#define SCNN_ACT_RELU 1 /* z where z > 0, else 0 (derivative at 0: 0) */
+#define SCNN_ACT_GELU 2 /* z Phi(z), Phi the normal distribution function (erf, no approximation) */
+#define SCNN_ACT_SILU 3 /* z / (1 + exp(-z)) */
+
+/* Linear layer:  z = x w + bias,  out = act(z) + residual.
+ * x [rows, c_in], w [c_in, c_out] (one tap of a filter as sparse_conv_fwd takes
+ * it), bias [c_out] (nullable), residual [rows, c_out] (nullable), out
+ * [rows, c_out]; pre [rows, c_out] (nullable) receives z, which linear_bwd needs
+ * where act is not SCNN_ACT_NONE.  out and residual may be the same array.
+ * fp32 products are formed by splitting both operands into three bf16 numbers
+ * (as sparse_conv_fwd's split kernels do); a tile of outputs that meets a value
+ * these do not hold - infinities, NaN, non-zero magnitudes below 2^-109 or from
+ * 2^58 up - is summed with fp32 products instead, several times as slowly.  The
+ * error of an fp32 result is a few 2^-24 of the sum of |x w| behind it, as with
+ * fp32 products.  Repeated calls give identical bits. */
+size_t linear_fwd_workspace(int dtype, int64_t rows, int64_t c_in, int64_t c_out);
+int linear_fwd(int dtype, const void* x, int64_t rows, const int64_t* rows_dev, int64_t c_in, const void* w,
+               const void* bias, int64_t c_out, int act, const void* residual, void* out, void* pre, void* workspace,
+               size_t workspace_bytes, void* hip_stream);
+
+/* Gradients of a linear layer from g [rows, c_out], the gradient of out:
+ *   dz = g act'(z),  dx = dz w^T,  dw = x^T dz,  dbias = sum over rows of dz
+ * (the gradient of residual is g itself).  pre: z as linear_fwd gave it; only
+ * read where act is not SCNN_ACT_NONE.  dx [rows, c_in], dw [c_in, c_out], dbias
+ * [c_out]: each nullable.  With 16-bit types dz is rounded to the type for the
+ * two products (not for dbias), which adds an error of the size of the results'
+ * own rounding.  With no rows dw and dbias are 0.  x may be null without dw, w
+ * without dx. */
+size_t linear_bwd_workspace(int dtype, int64_t rows, int64_t c_in, int64_t c_out, int act);
+int linear_bwd(int dtype, const void* x, int64_t rows, const int64_t* rows_dev, int64_t c_in, const void* w,
+               int64_t c_out, int act, const void* pre, const void* g, void* dx, void* dw, void* dbias, void* workspace,
+               size_t workspace_bytes, void* hip_stream);
+
+/* Layer norm over the channels of each row:
+ *   mean = sum x / C,  var = sum (x - mean)^2 / C,  rstd = 1 / sqrt(var + eps),
+ *   out = (x - mean) rstd gamma + beta
+ * gamma, beta [channels] (nullable: 1 and 0); mean, rstd fp32 [rows] (nullable)
+ * are what layer_norm_bwd needs.  eps >= 0; with eps 0 a row of equal values
+ * gives NaN, as the formula does.  channels up to 2^28. */
+int layer_norm_fwd(int dtype, const void* x, int64_t rows, const int64_t* rows_dev, int64_t channels, const void* gamma,
+                   const void* beta, double eps, void* out, float* mean, float* rstd, void* hip_stream);
+
+/* Gradients of layer norm from g [rows, channels], the gradient of out; with
+ * xh = (x - mean) rstd and h = g gamma:
+ *   dx = rstd (h - sum(h) / C - xh sum(h xh) / C)   (sums over the row),
+ *   dgamma = sum over rows of g xh,  dbeta = sum over rows of g.
+ * dx, dgamma, dbeta: each nullable.  Sums over rows are added in a fixed order:
+ * repeated calls give identical bits.  With no rows dgamma and dbeta are 0. */
+size_t layer_norm_bwd_workspace(int dtype, int64_t rows, int64_t channels);
+int layer_norm_bwd(int dtype, const void* x, const void* g, int64_t rows, const int64_t* rows_dev, int64_t channels,
+                   const void* gamma, const float* mean, const float* rstd, void* dx, void* dgamma, void* dbeta,
+                   void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Global norm of the gradients of a network, and clipping by it:
+ *   norm = sqrt(sum of squares of all entries of all tensors),
+ *   scale = max_norm / (norm + 1e-6), at most 1;  every entry times scale.
+ * n tensors; grads, outs (host arrays of device pointers), counts (host,
+ * entries of each; 0 is skipped, its pointers may be null), dtypes (host,
+ * SCNN_F32 / BF16 / F16 of each).  outs[i] (of grads[i]'s type) receives the
+ * scaled entries; outs[i] == grads[i] scales in place, and nothing is written
+ * there when scale is 1.  outs null: the norm alone.  Apart from outs[i] ==
+ * grads[i] no output may overlap an output or a gradient, which the call checks
+ * (a tensor listed twice is refused; with outs null it counts twice).  The host
+ * arrays are read before the call returns.  result (device, double[2]) =
+ * {norm, scale}; a NaN or infinity among the entries shows there and in what is
+ * scaled, as the formulas have it.  Sums in fp64 in a fixed order.  max_norm >= 0
+ * (infinity: scale 1). */
+size_t grad_clip_workspace(int n, const int64_t* counts);
+int grad_clip(int n, const void* const* grads, void* const* outs, const int64_t* counts, const int* dtypes,
+              double max_norm, double* result, void* workspace, size_t workspace_bytes, void* hip_stream);
+
 /* Optional precondition check of a coordinate list (synchronises the stream):
  * SCNN_OK, SCNN_EINVAL (coordinate outside the grid) or SCNN_EUNSORTED (rows
  * not strictly ascending by (b, lin)).  workspace: at least 256 bytes. */

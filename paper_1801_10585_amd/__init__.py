@@ -7,6 +7,8 @@ anywhere, calling an operator without the built library or without a GPU raises.
 """
 from .binding import (  # noqa: F401
     ABS,
+    ACTIVATIONS,
+    DTYPES,
     SIGNED,
     FLAG_BAD_COORD,
     FLAG_CAND_OVERFLOW,
@@ -16,7 +18,17 @@ from .binding import (  # noqa: F401
     ChainedLayer,
     attention_topk,
     calibration_copy,
+    clip_grad_norm,
     density_regulariser,
+    grad_clip_workspace,
+    grad_norm,
+    layer_norm_bwd,
+    layer_norm_bwd_workspace,
+    layer_norm_fwd,
+    linear_bwd,
+    linear_bwd_workspace,
+    linear_fwd,
+    linear_fwd_workspace,
     prune_weights,
     k_from_rho,
     library_path,

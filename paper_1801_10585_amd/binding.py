@@ -15,6 +15,8 @@ ABS, SIGNED = 0, 1
 FUSE_RELU, FUSE_MAXPOOL2 = 1, 2
 FLAG_CAND_OVERFLOW, FLAG_OUT_OVERFLOW, FLAG_BAD_COORD, FLAG_UNSORTED = 1, 2, 4, 8
 NNZ_LEN = 4
+DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
 
 EXPORTED_SYMBOLS = [
     "scnn_last_error", "scnn_version", "scnn_k_from_rho", "sparse_conv_fwd_max_rows", "sparse_conv_fwd_workspace",
@@ -24,6 +26,8 @@ EXPORTED_SYMBOLS = [
     "sparse_conv_bwd_workspace", "sparse_conv_bwd", "sparse_to_dense",
     "density_regulariser_workspace", "density_regulariser", "prune_weights", "sparse_conv_fwd_chained",
     "sparse_relu_static_max_rows", "sparse_relu_static", "scnn_last_conv_kernel",
+    "linear_fwd_workspace", "linear_fwd", "linear_bwd_workspace", "linear_bwd", "layer_norm_fwd",
+    "layer_norm_bwd_workspace", "layer_norm_bwd", "grad_clip_workspace", "grad_clip",
 ]
 
 
@@ -91,6 +95,25 @@ def load_library():
     L.density_regulariser.argtypes = [vp, i64, vp, ci, i64, dbl, dbl, dbl, dbl, dbl, vp, i64, vp, vp, vp, sz, vp]
     L.prune_weights.restype = ci
     L.prune_weights.argtypes = [vp, vp, i64, ctypes.c_float, vp, vp]
+    L.linear_fwd_workspace.restype = sz
+    L.linear_fwd_workspace.argtypes = [ci, i64, i64, i64]
+    L.linear_fwd.restype = ci
+    L.linear_fwd.argtypes = [ci, vp, i64, vp, i64, vp, vp, i64, ci, vp, vp, vp, vp, sz, vp]
+    L.linear_bwd_workspace.restype = sz
+    L.linear_bwd_workspace.argtypes = [ci, i64, i64, i64, ci]
+    L.linear_bwd.restype = ci
+    L.linear_bwd.argtypes = [ci, vp, i64, vp, i64, vp, i64, ci, vp, vp, vp, vp, vp, vp, sz, vp]
+    L.layer_norm_fwd.restype = ci
+    L.layer_norm_fwd.argtypes = [ci, vp, i64, vp, i64, vp, vp, dbl, vp, vp, vp, vp]
+    L.layer_norm_bwd_workspace.restype = sz
+    L.layer_norm_bwd_workspace.argtypes = [ci, i64, i64]
+    L.layer_norm_bwd.restype = ci
+    L.layer_norm_bwd.argtypes = [ci, vp, vp, i64, vp, i64, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    L.grad_clip_workspace.restype = sz
+    L.grad_clip_workspace.argtypes = [ci, ctypes.POINTER(i64)]
+    L.grad_clip.restype = ci
+    L.grad_clip.argtypes = [ci, ctypes.POINTER(vp), ctypes.POINTER(vp), ctypes.POINTER(i64), ctypes.POINTER(ci), dbl, vp, vp,
+                            sz, vp]
     L.scnn_validate_rows.restype = ci
     L.scnn_validate_rows.argtypes = [ci, i32p, ci, vp, i64, vp, sz, vp]
     L.scnn_calibration_copy.restype = ci
@@ -451,6 +474,282 @@ def prune_weights(w, warned, eps, *, stream=None):
     counts = torch.zeros(2, dtype=torch.int64, device=w.device)
     _check(L, L.prune_weights(_ptr(w), _ptr(warned), w.numel(), float(eps), _ptr(counts), _stream(stream)))
     return counts
+
+
+# Layers on rows of values.  All tensors of a call live on one device, which need not be the current one.  With `stream`
+# the call runs there and its new tensors belong to that stream: the caller orders other streams behind it.
+
+class _On:
+    """Makes `dev`, and `stream` where one is given, current while a call allocates and launches."""
+
+    def __init__(self, dev, stream, tensors):
+        if stream is not None:
+            if stream.device != dev:
+                raise ValueError("the stream belongs to another device than the tensors")
+            if stream != torch.cuda.current_stream(dev):
+                for t in tensors:  # (their memory may not be handed out again before the stream is done with them)
+                    if t is not None:
+                        t.record_stream(stream)
+            self.scope = torch.cuda.stream(stream)
+        else:
+            self.scope = None if dev.index == torch.cuda.current_device() else torch.cuda.device(dev)
+
+    def __enter__(self):
+        if self.scope is not None:
+            self.scope.__enter__()
+
+    def __exit__(self, *exc):
+        if self.scope is not None:
+            self.scope.__exit__(*exc)
+
+
+def _same(t, like: torch.Tensor, shape, name: str, dtype=None):
+    """An optional input of a given shape, of like's device and (without dtype) type."""
+    if t is None:
+        return None
+    if t.device != like.device:
+        raise ValueError(f"{name} must live on the GPU of the other tensors")
+    if t.dtype != (dtype or like.dtype):
+        raise ValueError(f"{name} must be {dtype or like.dtype}")
+    if tuple(t.shape) != shape:
+        raise ValueError(f"{name} must be of shape {list(shape)}, not {list(t.shape)}")
+    return t
+
+
+def _result(t, like: torch.Tensor, shape, name: str, dtype=None) -> torch.Tensor:
+    """An output: the caller's, which must be contiguous, or a new one."""
+    if t is None:
+        return torch.empty(shape, dtype=dtype or like.dtype, device=like.device)
+    if not _same(t, like, shape, name, dtype).is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t
+
+
+def _rows_of(x: torch.Tensor, name: str) -> Tuple[int, int, int]:
+    if not x.is_cuda:
+        raise ValueError(f"{name} must live on the GPU")
+    if x.dtype not in DTYPES:
+        raise ValueError(f"{name} must be float32, bfloat16 or float16")
+    if x.dim() != 2:
+        raise ValueError(f"{name} must be [rows, channels]")
+    return DTYPES[x.dtype], x.shape[0], x.shape[1]
+
+
+def _rows_dev(rows_dev, like: torch.Tensor):
+    if rows_dev is None:
+        return None
+    if rows_dev.device != like.device or rows_dev.dtype != torch.int64 or rows_dev.numel() < 1:
+        raise ValueError("rows_dev must be an int64 tensor on the GPU of the rows")
+    return rows_dev
+
+
+def _activation(act: str) -> int:
+    if act not in ACTIVATIONS:
+        raise ValueError(f"act must be one of {', '.join(ACTIVATIONS)}")
+    return ACTIVATIONS[act]
+
+
+def _scratch(workspace, need: int, like: torch.Tensor) -> torch.Tensor:
+    if need == 0:
+        raise ScnnError(-1, load_library().scnn_last_error().decode())
+    if workspace is None:
+        return torch.empty(need, dtype=torch.uint8, device=like.device)
+    if workspace.device != like.device or workspace.dtype != torch.uint8 or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous uint8 tensor on the GPU of the rows")
+    return workspace
+
+
+def _cont(t: Optional[torch.Tensor]) -> Optional[torch.Tensor]:
+    return None if t is None else t.contiguous()
+
+
+def linear_fwd_workspace(dtype: torch.dtype, rows: int, c_in: int, c_out: int) -> int:
+    L = load_library()
+    r = int(L.linear_fwd_workspace(DTYPES[dtype], int(rows), int(c_in), int(c_out)))
+    if r == 0:
+        raise ScnnError(-1, L.scnn_last_error().decode())
+    return r
+
+
+def linear_fwd(x, w, bias=None, *, act="none", residual=None, keep_pre=False, rows_dev=None, out=None, pre=None,
+               workspace=None, stream=None):
+    """out = act(x w + bias) + residual on rows x [rows, c_in], w [c_in, c_out]; act: "none", "relu", "gelu" or "silu".
+    Returns out, or (out, pre) with keep_pre (or a tensor given as pre): pre = x w + bias is what linear_bwd needs."""
+    L = load_library()
+    dt, rows, c_in = _rows_of(x, "x")
+    if w.dim() != 2 or w.shape[0] != c_in:
+        raise ValueError("w must be [c_in, c_out]")
+    c_out = w.shape[1]
+    _same(w, x, (c_in, c_out), "w")
+    _same(bias, x, (c_out,), "bias")
+    _same(residual, x, (rows, c_out), "residual")
+    code = _activation(act)
+    rows_dev = _rows_dev(rows_dev, x)
+    with _On(x.device, stream, (x, w, bias, residual, rows_dev, out, pre, workspace)):
+        x, w, bias, residual = x.contiguous(), w.contiguous(), _cont(bias), _cont(residual)
+        keep = keep_pre or pre is not None
+        out = _result(out, x, (rows, c_out), "out")
+        if keep:
+            pre = _result(pre, x, (rows, c_out), "pre")
+        workspace = _scratch(workspace, int(L.linear_fwd_workspace(dt, rows, c_in, c_out)), x)
+        _check(L, L.linear_fwd(dt, _ptr(x), rows, _ptr(rows_dev), c_in, _ptr(w), _ptr(bias), c_out, code, _ptr(residual),
+                               _ptr(out), _ptr(pre), _ptr(workspace), workspace.numel(), _stream(None)))
+    return (out, pre) if keep else out
+
+
+def linear_bwd_workspace(dtype: torch.dtype, rows: int, c_in: int, c_out: int, act="none") -> int:
+    L = load_library()
+    r = int(L.linear_bwd_workspace(DTYPES[dtype], int(rows), int(c_in), int(c_out), _activation(act)))
+    if r == 0:
+        raise ScnnError(-1, L.scnn_last_error().decode())
+    return r
+
+
+def linear_bwd(x, w, g, *, act="none", pre=None, want=(True, True, True), rows_dev=None, out=None, workspace=None,
+               stream=None):
+    """Gradients of linear_fwd from g [rows, c_out], the gradient of its result (which is the residual's gradient too).
+    pre: as linear_fwd gave it (not read with act "none").  Returns (dx, dw, dbias), None where `want` is False; `out`:
+    tensors to put them in."""
+    L = load_library()
+    dt, rows, c_in = _rows_of(x, "x")
+    if w.dim() != 2 or w.shape[0] != c_in:
+        raise ValueError("w must be [c_in, c_out]")
+    c_out = w.shape[1]
+    _same(w, x, (c_in, c_out), "w")
+    _same(g, x, (rows, c_out), "g")
+    code = _activation(act)
+    if code and pre is None:
+        raise ValueError("the activation's gradient needs pre")
+    pre = _same(pre, x, (rows, c_out), "pre") if code else None
+    rows_dev = _rows_dev(rows_dev, x)
+    dx, dw, dbias = out if out is not None else (None, None, None)
+    with _On(x.device, stream, (x, w, g, pre, rows_dev, dx, dw, dbias, workspace)):
+        x, w, g, pre = x.contiguous(), w.contiguous(), g.contiguous(), _cont(pre)
+        dx = _result(dx, x, (rows, c_in), "dx") if want[0] else None
+        dw = _result(dw, x, (c_in, c_out), "dw") if want[1] else None
+        dbias = _result(dbias, x, (c_out,), "dbias") if want[2] else None
+        workspace = _scratch(workspace, int(L.linear_bwd_workspace(dt, rows, c_in, c_out, code)), x)
+        _check(L, L.linear_bwd(dt, _ptr(x), rows, _ptr(rows_dev), c_in, _ptr(w), c_out, code, _ptr(pre), _ptr(g), _ptr(dx),
+                               _ptr(dw), _ptr(dbias), _ptr(workspace), workspace.numel(), _stream(None)))
+    return dx, dw, dbias
+
+
+def layer_norm_fwd(x, gamma=None, beta=None, *, eps=1e-5, rows_dev=None, out=None, stream=None):
+    """Layer norm over the channels of each row of x [rows, channels].  Returns (out, mean, rstd), the statistics fp32
+    [rows], which layer_norm_bwd needs; `out`: three tensors to put them in."""
+    L = load_library()
+    dt, rows, ch = _rows_of(x, "x")
+    _same(gamma, x, (ch,), "gamma")
+    _same(beta, x, (ch,), "beta")
+    rows_dev = _rows_dev(rows_dev, x)
+    y, mean, rstd = out if out is not None else (None, None, None)
+    with _On(x.device, stream, (x, gamma, beta, rows_dev, y, mean, rstd)):
+        x, gamma, beta = x.contiguous(), _cont(gamma), _cont(beta)
+        y = _result(y, x, (rows, ch), "out")
+        mean = _result(mean, x, (rows,), "mean", torch.float32)
+        rstd = _result(rstd, x, (rows,), "rstd", torch.float32)
+        _check(L, L.layer_norm_fwd(dt, _ptr(x), rows, _ptr(rows_dev), ch, _ptr(gamma), _ptr(beta), float(eps), _ptr(y),
+                                   _ptr(mean), _ptr(rstd), _stream(None)))
+    return y, mean, rstd
+
+
+def layer_norm_bwd_workspace(dtype: torch.dtype, rows: int, channels: int) -> int:
+    L = load_library()
+    r = int(L.layer_norm_bwd_workspace(DTYPES[dtype], int(rows), int(channels)))
+    if r == 0:
+        raise ScnnError(-1, L.scnn_last_error().decode())
+    return r
+
+
+def layer_norm_bwd(x, g, gamma, mean, rstd, *, want=(True, True, True), rows_dev=None, out=None, workspace=None,
+                   stream=None):
+    """Gradients of layer_norm_fwd from g [rows, channels], the gradient of its result; gamma may be None, mean and rstd as
+    layer_norm_fwd gave them.  Returns (dx, dgamma, dbeta), None where `want` is False; `out`: tensors to put them in."""
+    L = load_library()
+    dt, rows, ch = _rows_of(x, "x")
+    _same(g, x, (rows, ch), "g")
+    _same(gamma, x, (ch,), "gamma")
+    _same(mean, x, (rows,), "mean", torch.float32)
+    _same(rstd, x, (rows,), "rstd", torch.float32)
+    rows_dev = _rows_dev(rows_dev, x)
+    dx, dgamma, dbeta = out if out is not None else (None, None, None)
+    with _On(x.device, stream, (x, g, gamma, mean, rstd, rows_dev, dx, dgamma, dbeta, workspace)):
+        x, g, gamma, mean, rstd = x.contiguous(), g.contiguous(), _cont(gamma), mean.contiguous(), rstd.contiguous()
+        dx = _result(dx, x, (rows, ch), "dx") if want[0] else None
+        dgamma = _result(dgamma, x, (ch,), "dgamma") if want[1] else None
+        dbeta = _result(dbeta, x, (ch,), "dbeta") if want[2] else None
+        workspace = _scratch(workspace, int(L.layer_norm_bwd_workspace(dt, rows, ch)), x)
+        _check(L, L.layer_norm_bwd(dt, _ptr(x), _ptr(g), rows, _ptr(rows_dev), ch, _ptr(gamma), _ptr(mean), _ptr(rstd),
+                                   _ptr(dx), _ptr(dgamma), _ptr(dbeta), _ptr(workspace), workspace.numel(), _stream(None)))
+    return dx, dgamma, dbeta
+
+
+def _dense(t: torch.Tensor) -> bool:
+    """The tensor's entries fill one stretch of memory, in any order of its axes."""
+    if t.is_contiguous():
+        return True
+    step = 1
+    for stride, size in sorted((st, sz) for st, sz in zip(t.stride(), t.shape) if sz != 1):
+        if stride != step:
+            return False
+        step *= size
+    return True
+
+
+def _grad_clip(grads, max_norm, outs, workspace, stream):
+    L = load_library()
+    grads = list(grads)
+    if outs is not None:
+        outs = list(outs)
+        if len(outs) != len(grads):
+            raise ValueError("outs must hold a tensor for every gradient")
+    if not grads:
+        raise ValueError("no gradients")
+    like = grads[0]
+    dev = like.device
+    for t in grads:
+        if not t.is_cuda or t.device != dev:
+            raise ValueError("the gradients must live on one GPU")
+        if t.dtype not in DTYPES:
+            raise ValueError("gradients must be float32, bfloat16 or float16")
+        if not _dense(t):
+            raise ValueError("a gradient must fill one stretch of memory")
+    if outs is not None and outs is not grads:
+        for t, o in zip(grads, outs):
+            if o.device != dev or o.dtype != t.dtype or o.shape != t.shape or o.stride() != t.stride():
+                raise ValueError("an output must be like its gradient (device, type, shape and strides)")
+    n = len(grads)
+    counts = (ctypes.c_int64 * n)(*[t.numel() for t in grads])
+    types = (ctypes.c_int * n)(*[DTYPES[t.dtype] for t in grads])
+    src = (ctypes.c_void_p * n)(*[t.data_ptr() for t in grads])
+    dst = None if outs is None else (ctypes.c_void_p * n)(*[t.data_ptr() for t in outs])
+    with _On(dev, stream, (*grads, *(outs or ()), workspace)):
+        result = torch.empty(2, dtype=torch.float64, device=dev)
+        workspace = _scratch(workspace, int(L.grad_clip_workspace(n, counts)), like)
+        _check(L, L.grad_clip(n, src, dst, counts, types, float(max_norm), _ptr(result), _ptr(workspace), workspace.numel(),
+                              _stream(None)))
+    return result
+
+
+def clip_grad_norm(grads, max_norm, *, outs=None, workspace=None, stream=None):
+    """Scales all gradients by min(1, max_norm / (norm + 1e-6)), norm = their global 2-norm: in place, or into `outs`.
+    Returns double[2] = {norm, scale} on the device."""
+    grads = list(grads)
+    return _grad_clip(grads, max_norm, grads if outs is None else outs, workspace, stream)
+
+
+def grad_norm(grads, *, workspace=None, stream=None):
+    """Global 2-norm of a list of gradients: a double on the device."""
+    return _grad_clip(grads, float("inf"), None, workspace, stream)[0]
+
+
+def grad_clip_workspace(counts) -> int:
+    """Bytes of workspace of clip_grad_norm and grad_norm for tensors of these numbers of entries."""
+    L = load_library()
+    r = int(L.grad_clip_workspace(len(counts), (ctypes.c_int64 * len(counts))(*[int(c) for c in counts])))
+    if r == 0:
+        raise ScnnError(-1, L.scnn_last_error().decode())
+    return r
 
 
 def validate_rows(extent, batch, coords, stream=None) -> None:

@@ -14,7 +14,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libscnn.so")
-SOURCES = ["scnn_index.hip", "scnn_conv.hip", "scnn_conv_quad.hip", "scnn_conv_split.hip", "scnn_topk.hip", "scnn_rows.hip", "scnn_bwd.hip", "scnn_train.hip", "scnn_tiny.hip", "scnn_api.hip"]
+SOURCES = ["scnn_index.hip", "scnn_conv.hip", "scnn_conv_quad.hip", "scnn_conv_split.hip", "scnn_topk.hip", "scnn_rows.hip", "scnn_bwd.hip", "scnn_train.hip", "scnn_tiny.hip",
+           "scnn_linear.hip", "scnn_norm.hip", "scnn_clip.hip", "scnn_api.hip"]
 # packed fp32 VALU ops are switched off on purpose (they have misbehaved on the target machines)
 FLAGS = ["--offload-arch=gfx950", "-O3", "-fPIC", "-std=c++17", "-Xclang", "-target-feature", "-Xclang",
          "-packed-fp32-ops", "-Wno-unused-command-line-argument",
@@ -35,8 +36,8 @@ def is_stale() -> bool:
 def _compile(src: str, force: bool) -> str:
     obj = os.path.join(BUILD, src.replace(".hip", ".o"))
     src_path = os.path.join(CSRC, src)
-    hdr_m = max(os.path.getmtime(os.path.join(CSRC, "scnn_internal.h")),
-                os.path.getmtime(os.path.join(HERE, "..", "include", "scnn.h")))
+    hdr_m = max(os.path.getmtime(p) for p in [os.path.join(CSRC, "scnn_internal.h"), os.path.join(CSRC, "scnn_dense.h"),
+                                              os.path.join(HERE, "..", "include", "scnn.h")])
     if not force and os.path.exists(obj) and os.path.getmtime(obj) >= max(os.path.getmtime(src_path), hdr_m):
         return obj
     cmd = ["hipcc", *FLAGS, "-c", src_path, "-o", obj]

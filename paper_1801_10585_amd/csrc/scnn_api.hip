@@ -1,14 +1,17 @@
 // Host side of the C ABI: argument checks, workspace layout, launch sequences.
 // Nothing here touches values; every step of the layer runs in the kernels.
 #include <atomic>
+#include <algorithm>
 #include <cmath>
 #include <cstddef>
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
+#include <initializer_list>
 #include <mutex>
 #include <vector>
 
+#include "scnn_dense.h"
 #include "scnn_internal.h"
 
 namespace scnn {
@@ -1090,6 +1093,232 @@ int prune_weights(float* w, unsigned char* warned, int64_t n_w, float eps, int64
     if (!(eps >= 0.0f)) return fail(SCNN_EINVAL, "eps must be >= 0");
     if (!counts || (n_w > 0 && (!w || !warned))) return fail(SCNN_EINVAL, "null pointer");
     SCNN_TRY(launch_prune(w, warned, n_w, eps, (unsigned long long*)counts, (hipStream_t)hip_stream));
+    return SCNN_OK;
+}
+
+// ---------------------------------------------------------------- layers on rows of values
+static constexpr long long kMaxWidth = 1LL << 28;  // channels of a row: tiles and vectors of one row are counted in 31 bits
+
+static int check_rows(int dtype, int64_t rows) {
+    if (dtype != SCNN_F32 && dtype != SCNN_BF16 && dtype != SCNN_F16) return fail(SCNN_EINVAL, "unknown dtype %d", dtype);
+    if (rows < 0) return fail(SCNN_EINVAL, "rows = %lld", (long long)rows);
+    if (rows > kMaxIndex) return fail(SCNN_ECAPACITY, "more than 2^31-1 rows");
+    return SCNN_OK;
+}
+static int check_width(int64_t channels, const char* name) {
+    if (channels < 1) return fail(SCNN_EINVAL, "%s = %lld", name, (long long)channels);
+    if (channels > kMaxWidth) return fail(SCNN_ECAPACITY, "%s = %lld exceeds 2^28", name, (long long)channels);
+    return SCNN_OK;
+}
+static size_t dtype_size(int dtype) { return dtype == SCNN_F32 ? 4 : 2; }
+static bool element_aligned(int dtype, const void* p) { return ((uintptr_t)p & (dtype_size(dtype) - 1)) == 0; }
+static int check_workspace(const void* workspace, size_t bytes, size_t need) {
+    if (!workspace || ((uintptr_t)workspace & 255) != 0 || bytes < need)
+        return fail(SCNN_EWORKSPACE, "workspace too small (%zu of %zu bytes) or misaligned", bytes, need);
+    return SCNN_OK;
+}
+
+// What a call writes may overlap nothing else of the call; `may` is an input that an output may be, as a whole.
+struct Span { const void* p; size_t bytes; };
+static int check_apart(std::initializer_list<Span> outs, std::initializer_list<Span> ins, const void* may = nullptr) {
+    auto meet = [](const Span& a, const Span& b) {
+        return a.p && b.p && (uintptr_t)a.p < (uintptr_t)b.p + b.bytes && (uintptr_t)b.p < (uintptr_t)a.p + a.bytes;
+    };
+    for (const Span* o = outs.begin(); o != outs.end(); ++o) {
+        for (const Span* q = o + 1; q != outs.end(); ++q)
+            if (meet(*o, *q)) return fail(SCNN_EINVAL, "two outputs overlap");
+        for (const Span& i : ins)
+            if (meet(*o, i) && !(i.p == may && o->p == may)) return fail(SCNN_EINVAL, "an output overlaps an input");
+    }
+    return SCNN_OK;
+}
+
+static int check_linear(int dtype, int64_t rows, int64_t c_in, int64_t c_out) {
+    int rc = check_rows(dtype, rows);
+    if (rc == SCNN_OK) rc = check_width(c_in, "c_in");
+    if (rc == SCNN_OK) rc = check_width(c_out, "c_out");
+    if (rc != SCNN_OK) return rc;
+    // (arrays of more bytes than an address has bits for, and tiles past what a launch counts)
+    if ((double)rows * (double)(c_in > c_out ? c_in : c_out) > 0x1p42 || (double)c_in * (double)c_out > 0x1p42)
+        return fail(SCNN_ECAPACITY, "more than 2^42 values in an array");
+    return SCNN_OK;
+}
+
+size_t linear_fwd_workspace(int dtype, int64_t rows, int64_t c_in, int64_t c_out) {
+    if (check_linear(dtype, rows, c_in, c_out) != SCNN_OK) return 0;
+    return 256 + linear_fwd_part_bytes(rows, c_in, c_out);
+}
+
+int linear_fwd(int dtype, const void* x, int64_t rows, const int64_t* rows_dev, int64_t c_in, const void* w,
+               const void* bias, int64_t c_out, int act, const void* residual, void* out, void* pre, void* workspace,
+               size_t workspace_bytes, void* hip_stream) {
+    int rc = check_linear(dtype, rows, c_in, c_out);
+    if (rc != SCNN_OK) return rc;
+    if (act < SCNN_ACT_NONE || act > SCNN_ACT_SILU) return fail(SCNN_EINVAL, "unknown activation %d", act);
+    if (rows == 0) return SCNN_OK;
+    if (!x || !w || !out) return fail(SCNN_EINVAL, "null pointer");
+    for (const void* q : {x, w, bias, residual, (const void*)out, (const void*)pre})
+        if (!element_aligned(dtype, q)) return fail(SCNN_EINVAL, "an array is not aligned to its element");
+    const size_t need = linear_fwd_workspace(dtype, rows, c_in, c_out), e = dtype_size(dtype);
+    rc = check_workspace(workspace, workspace_bytes, need);
+    if (rc != SCNN_OK) return rc;
+    const size_t in = (size_t)rows * c_in * e, of = (size_t)rows * c_out * e;
+    rc = check_apart({{out, of}, {pre, of}, {workspace, need}},
+                     {{x, in}, {w, (size_t)c_in * c_out * e}, {bias, (size_t)c_out * e}, {residual, of}}, out == residual ? out : nullptr);
+    if (rc != SCNN_OK) return rc;
+    LinearCall c = {};
+    c.x = x; c.w = w; c.bias = bias; c.residual = residual; c.out = out; c.pre = pre;
+    c.rows = rows; c.c_in = c_in; c.c_out = c_out;
+    c.rows_dev = (const long long*)rows_dev;
+    c.act = act;
+    c.workspace = workspace;
+    SCNN_TRY(launch_linear_fwd(dtype, c, (hipStream_t)hip_stream));
+    return SCNN_OK;
+}
+
+size_t linear_bwd_workspace(int dtype, int64_t rows, int64_t c_in, int64_t c_out, int act) {
+    if (check_linear(dtype, rows, c_in, c_out) != SCNN_OK) return 0;
+    if (act < SCNN_ACT_NONE || act > SCNN_ACT_SILU) { fail(SCNN_EINVAL, "unknown activation %d", act); return 0; }
+    return 256 + linear_bwd_bytes(dtype, rows, c_in, c_out, act);
+}
+
+int linear_bwd(int dtype, const void* x, int64_t rows, const int64_t* rows_dev, int64_t c_in, const void* w,
+               int64_t c_out, int act, const void* pre, const void* g, void* dx, void* dw, void* dbias, void* workspace,
+               size_t workspace_bytes, void* hip_stream) {
+    int rc = check_linear(dtype, rows, c_in, c_out);
+    if (rc != SCNN_OK) return rc;
+    if (act < SCNN_ACT_NONE || act > SCNN_ACT_SILU) return fail(SCNN_EINVAL, "unknown activation %d", act);
+    if (rows > 0) {
+        if (!g) return fail(SCNN_EINVAL, "null gradient");
+        if (act != SCNN_ACT_NONE && !pre) return fail(SCNN_EINVAL, "the activation's gradient needs pre");
+        if ((dw && !x) || (dx && !w)) return fail(SCNN_EINVAL, "null pointer");
+    }
+    for (const void* q : {x, w, pre, g, (const void*)dx, (const void*)dw, (const void*)dbias})
+        if (!element_aligned(dtype, q)) return fail(SCNN_EINVAL, "an array is not aligned to its element");
+    const size_t need = linear_bwd_workspace(dtype, rows, c_in, c_out, act), e = dtype_size(dtype);
+    rc = check_workspace(workspace, workspace_bytes, need);
+    if (rc != SCNN_OK) return rc;
+    const size_t in = (size_t)rows * c_in * e, of = (size_t)rows * c_out * e, filter = (size_t)c_in * c_out * e;
+    rc = check_apart({{dx, in}, {dw, filter}, {dbias, (size_t)c_out * e}, {workspace, need}},
+                     {{x, in}, {w, filter}, {act == SCNN_ACT_NONE ? nullptr : pre, of}, {g, of}});
+    if (rc != SCNN_OK) return rc;
+    LinearCall c = {};
+    c.x = x; c.w = w; c.pre_in = pre; c.g = g; c.dx = dx; c.dw = dw; c.dbias = dbias;
+    c.rows = rows; c.c_in = c_in; c.c_out = c_out;
+    c.rows_dev = (const long long*)rows_dev;
+    c.act = act;
+    c.workspace = workspace;
+    SCNN_TRY(launch_linear_bwd(dtype, c, (hipStream_t)hip_stream));
+    return SCNN_OK;
+}
+
+int layer_norm_fwd(int dtype, const void* x, int64_t rows, const int64_t* rows_dev, int64_t channels, const void* gamma,
+                   const void* beta, double eps, void* out, float* mean, float* rstd, void* hip_stream) {
+    int rc = check_rows(dtype, rows);
+    if (rc == SCNN_OK) rc = check_width(channels, "channels");
+    if (rc != SCNN_OK) return rc;
+    if (!(eps >= 0.0) || std::isinf((float)eps)) return fail(SCNN_EINVAL, "eps = %g", eps);
+    if (rows == 0) return SCNN_OK;
+    if (!x || !out) return fail(SCNN_EINVAL, "null pointer");
+    for (const void* q : {x, gamma, beta, (const void*)out})
+        if (!element_aligned(dtype, q)) return fail(SCNN_EINVAL, "an array is not aligned to its element");
+    const size_t e = dtype_size(dtype), all = (size_t)rows * channels * e;
+    rc = check_apart({{out, all}, {mean, (size_t)rows * 4}, {rstd, (size_t)rows * 4}},
+                     {{x, all}, {gamma, (size_t)channels * e}, {beta, (size_t)channels * e}});
+    if (rc != SCNN_OK) return rc;
+    SCNN_TRY(launch_norm_fwd(x, rows, (const long long*)rows_dev, (int)channels, gamma, beta, (float)eps, out, mean, rstd,
+                             dtype, (hipStream_t)hip_stream));
+    return SCNN_OK;
+}
+
+size_t layer_norm_bwd_workspace(int dtype, int64_t rows, int64_t channels) {
+    if (check_rows(dtype, rows) != SCNN_OK || check_width(channels, "channels") != SCNN_OK) return 0;
+    return 256 + norm_bwd_part_bytes(rows, (int)channels, dtype);
+}
+
+int layer_norm_bwd(int dtype, const void* x, const void* g, int64_t rows, const int64_t* rows_dev, int64_t channels,
+                   const void* gamma, const float* mean, const float* rstd, void* dx, void* dgamma, void* dbeta,
+                   void* workspace, size_t workspace_bytes, void* hip_stream) {
+    int rc = check_rows(dtype, rows);
+    if (rc == SCNN_OK) rc = check_width(channels, "channels");
+    if (rc != SCNN_OK) return rc;
+    if (rows > 0 && (!x || !g || !mean || !rstd)) return fail(SCNN_EINVAL, "null pointer");
+    for (const void* q : {x, g, gamma, (const void*)dx, (const void*)dgamma, (const void*)dbeta})
+        if (!element_aligned(dtype, q)) return fail(SCNN_EINVAL, "an array is not aligned to its element");
+    const size_t need = layer_norm_bwd_workspace(dtype, rows, channels), e = dtype_size(dtype), row = (size_t)channels * e;
+    rc = check_workspace(workspace, workspace_bytes, need);
+    if (rc != SCNN_OK) return rc;
+    rc = check_apart({{dx, rows * row}, {dgamma, row}, {dbeta, row}, {workspace, need}},
+                     {{x, rows * row}, {g, rows * row}, {gamma, row}, {mean, (size_t)rows * 4}, {rstd, (size_t)rows * 4}});
+    if (rc != SCNN_OK) return rc;
+    SCNN_TRY(launch_norm_bwd(x, g, rows, (const long long*)rows_dev, (int)channels, gamma, mean, rstd, dx, dgamma, dbeta,
+                             (float*)workspace, dtype, (hipStream_t)hip_stream));
+    return SCNN_OK;
+}
+
+// ---------------------------------------------------------------- gradient clipping
+static int check_counts(int n, const int64_t* counts) {
+    if (n < 0 || (n > 0 && !counts)) return fail(SCNN_EINVAL, "bad tensor list");
+    long long total = 0;
+    for (int i = 0; i < n; ++i) {
+        if (counts[i] < 0) return fail(SCNN_EINVAL, "counts[%d] = %lld", i, (long long)counts[i]);
+        if (counts[i] > (1LL << 42) - total) return fail(SCNN_ECAPACITY, "more than 2^42 gradient entries");
+        total += counts[i];
+    }
+    return SCNN_OK;
+}
+
+size_t grad_clip_workspace(int n, const int64_t* counts) {
+    if (check_counts(n, counts) != SCNN_OK) return 0;
+    return 256 + (size_t)grad_norm_parts(n, counts) * sizeof(double);
+}
+
+// Outputs that overlap an output, or a gradient other than their own: 1; no memory for the list: -1.
+static int outputs_overlap(int n, const void* const* grads, void* const* outs, const int64_t* counts, const int* dtypes) try {
+    struct Range { uintptr_t from, to; int i; bool out; };
+    std::vector<Range> r;
+    r.reserve(2 * (size_t)n);
+    for (int i = 0; i < n; ++i) {
+        const size_t bytes = (size_t)counts[i] * dtype_size(dtypes[i]);
+        if (bytes == 0) continue;
+        r.push_back({(uintptr_t)outs[i], (uintptr_t)outs[i] + bytes, i, true});
+        if (outs[i] != grads[i]) r.push_back({(uintptr_t)grads[i], (uintptr_t)grads[i] + bytes, i, false});
+    }
+    std::sort(r.begin(), r.end(), [](const Range& a, const Range& b) { return a.from < b.from; });
+    // ends of the outputs and of all ranges so far: a range may begin before neither (outputs), or not before the former
+    uintptr_t out_end = 0, any_end = 0;
+    for (const Range& q : r) {
+        if (q.from < (q.out ? any_end : out_end)) return 1;
+        if (q.out) out_end = std::max(out_end, q.to);
+        any_end = std::max(any_end, q.to);
+    }
+    return 0;
+} catch (...) {
+    return -1;
+}
+
+int grad_clip(int n, const void* const* grads, void* const* outs, const int64_t* counts, const int* dtypes,
+              double max_norm, double* result, void* workspace, size_t workspace_bytes, void* hip_stream) {
+    int rc = check_counts(n, counts);
+    if (rc != SCNN_OK) return rc;
+    if (!(max_norm >= 0.0)) return fail(SCNN_EINVAL, "max_norm = %g must be >= 0", max_norm);
+    if (!result || (n > 0 && (!grads || !dtypes))) return fail(SCNN_EINVAL, "null pointer");
+    for (int i = 0; i < n; ++i) {
+        if (dtypes[i] != SCNN_F32 && dtypes[i] != SCNN_BF16 && dtypes[i] != SCNN_F16)
+            return fail(SCNN_EINVAL, "dtypes[%d] = %d", i, dtypes[i]);
+        if (counts[i] == 0) continue;
+        if (!grads[i] || (outs && !outs[i])) return fail(SCNN_EINVAL, "null tensor %d", i);
+        if (!element_aligned(dtypes[i], grads[i]) || (outs && !element_aligned(dtypes[i], outs[i])))
+            return fail(SCNN_EINVAL, "tensor %d is not aligned to its element", i);
+    }
+    if (outs) {
+        const int over = outputs_overlap(n, grads, outs, counts, dtypes);
+        if (over < 0) return fail(SCNN_ECAPACITY, "no host memory for the list of tensors");
+        if (over > 0) return fail(SCNN_EINVAL, "an output overlaps another tensor of the list");
+    }
+    rc = check_workspace(workspace, workspace_bytes, grad_clip_workspace(n, counts));
+    if (rc != SCNN_OK) return rc;
+    SCNN_TRY(launch_grad_clip(n, grads, outs, counts, dtypes, max_norm, result, (double*)workspace, (hipStream_t)hip_stream));
     return SCNN_OK;
 }
 

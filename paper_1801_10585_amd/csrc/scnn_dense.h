@@ -1,0 +1,135 @@
+// Shared by the layers on plain rows of values (linear layers, layer norm) and by gradient clipping: element types,
+// vectors of them at any alignment, activations, sums across lanes.
+#pragma once
+#include <type_traits>
+
+#include "scnn_internal.h"
+
+namespace scnn {
+
+template <int DTYPE> struct DenseType;
+template <> struct DenseType<SCNN_F32> { using type = float; };
+template <> struct DenseType<SCNN_BF16> { using type = __bf16; };
+template <> struct DenseType<SCNN_F16> { using type = _Float16; };
+
+// Elements of one 16-byte access.
+template <typename T> constexpr int kVec = 16 / (int)sizeof(T);
+template <typename T, int N> using VecOf = T __attribute__((ext_vector_type(N)));
+
+// Sixteen bytes from an address aligned to the element only (rows of odd widths start anywhere): the compiler makes one
+// global access of 16 bytes of it, which the hardware takes at any address.  The first `n` elements, the rest 0.
+template <typename T>
+__device__ __forceinline__ void load_elems(const T* __restrict__ p, int n, float (&v)[kVec<T>]) {
+    if (n >= kVec<T>) {
+        VecOf<T, kVec<T>> r;
+        __builtin_memcpy(&r, p, sizeof(r));
+#pragma unroll
+        for (int i = 0; i < kVec<T>; ++i) v[i] = (float)r[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < kVec<T>; ++i) v[i] = i < n ? (float)p[i] : 0.0f;
+    }
+}
+
+// Rounded once, to nearest even.
+template <typename T>
+__device__ __forceinline__ void store_elems(T* __restrict__ p, int n, const float (&v)[kVec<T>]) {
+    if (n >= kVec<T>) {
+        VecOf<T, kVec<T>> r;
+#pragma unroll
+        for (int i = 0; i < kVec<T>; ++i) r[i] = (T)v[i];
+        __builtin_memcpy(p, &r, sizeof(r));
+    } else {
+#pragma unroll
+        for (int i = 0; i < kVec<T>; ++i)
+            if (i < n) p[i] = (T)v[i];
+    }
+}
+
+// Rows of a call: the host's count, or the device's, held to the arrays' capacity.
+__device__ __forceinline__ long long rows_of(long long rows, const long long* __restrict__ rows_dev) {
+    if (!rows_dev) return rows;
+    const long long n = *rows_dev;
+    return n < 0 ? 0 : (n < rows ? n : rows);
+}
+
+__device__ __forceinline__ float activate(float z, int act) {
+    switch (act) {
+        case SCNN_ACT_RELU: return z < 0.0f ? 0.0f : z;  // (a NaN stays one)
+        case SCNN_ACT_GELU: return 0.5f * z * erfcf(z * -0.70710678118654752f);
+        case SCNN_ACT_SILU: return z / (1.0f + expf(-z));
+        default: return z;
+    }
+}
+
+// g * d act(z) / dz
+__device__ __forceinline__ float activate_back(float g, float z, int act) {
+    switch (act) {
+        case SCNN_ACT_RELU: return z <= 0.0f ? 0.0f : g;
+        case SCNN_ACT_GELU:
+            return g * (0.5f * erfcf(z * -0.70710678118654752f) + z * expf(-0.5f * z * z) * 0.39894228040143268f);
+        case SCNN_ACT_SILU: {
+            const float s = 1.0f / (1.0f + expf(-z));
+            return g * (s * (1.0f + z * (1.0f - s)));
+        }
+        default: return g;
+    }
+}
+
+// Sum over groups of P lanes of a wave (P a power of two), the same bits in each of the group's lanes.
+template <int P, typename F>
+__device__ __forceinline__ F lanes_add(F v) {
+#pragma unroll
+    for (int d = 1; d < P; d <<= 1) v += __shfl_xor(v, d, 64);
+    return v;
+}
+
+// out[c] = sum over p < parts of part[p * cols + c], in a fixed order, rounded once; columns [0, split) go to out0, the
+// rest to out1 (either may be null).
+hipError_t launch_column_sums(const float* part, int parts, long long cols, long long split, void* out0, void* out1,
+                              int dtype, hipStream_t s);
+
+// Tensors of a gradient list, as the kernels' argument: 120 of them fit the 4096 bytes that a launch may carry.
+constexpr int kClipTensors = 120;
+struct ClipTensor {
+    const void* src;
+    void* dst;
+    long long count;
+    unsigned first;  // first workgroup
+    int dtype;
+};
+struct ClipTable {
+    ClipTensor t[kClipTensors];
+    long long chunk;  // entries a workgroup
+    int n;
+    int slot;         // the launch's first partial sum
+};
+static_assert(sizeof(ClipTable) + 64 <= 4096, "kernel arguments of one launch");
+
+long long grad_norm_parts(int n, const int64_t* counts);  // partial sums (double) of a call
+hipError_t launch_grad_clip(int n, const void* const* src, void* const* dst, const int64_t* counts, const int* dtypes,
+                            double max_norm, double* result, double* part, hipStream_t s);
+
+size_t norm_bwd_part_bytes(long long rows, int channels, int dtype);
+hipError_t launch_norm_fwd(const void* x, long long rows, const long long* rows_dev, int channels, const void* gamma,
+                           const void* beta, float eps, void* out, float* mean, float* rstd, int dtype, hipStream_t s);
+hipError_t launch_norm_bwd(const void* x, const void* g, long long rows, const long long* rows_dev, int channels,
+                           const void* gamma, const float* mean, const float* rstd, void* dx, void* dgamma, void* dbeta,
+                           float* part, int dtype, hipStream_t s);
+
+// A linear layer's call, forward (x, w, bias, residual, out, pre) or backward (x, w, pre, g, dx, dw, dbias).
+struct LinearCall {
+    const void *x, *w, *bias, *residual, *g;
+    const void* pre_in;
+    void *out, *pre, *dx, *dw, *dbias;
+    long long rows, c_in, c_out;
+    const long long* rows_dev;
+    int act;
+    void* workspace;
+};
+size_t linear_fwd_part_bytes(long long rows, long long c_in, long long c_out);
+size_t linear_bwd_bytes(int dtype, long long rows, long long c_in, long long c_out, int act);
+hipError_t launch_linear_fwd(int dtype, const LinearCall& c, hipStream_t s);
+hipError_t launch_linear_bwd(int dtype, const LinearCall& c, hipStream_t s);
+
+}  // namespace scnn

@@ -1,0 +1,558 @@
+// Linear layers on rows: out = act(x w + bias) + residual, and the gradients of x, w and bias.
+//
+//   forward   z [R, N] = x [R, K] w [K, N] + bias,  out = act(z) + residual
+//   backward  dz = g act'(z),  dx [R, K] = dz w^T,  dw [K, N] = x^T dz,  dbias = sum_r dz
+//
+// All three products run through one tiled kernel (k_linear_tile): D [M, N] = sum_k A(m, k) B(k, n), where either operand
+// lies in memory with k or with its other index contiguous.  A tile is staged in LDS the way it lies in memory; an operand
+// whose k is contiguous is read from there in pieces of eight k a lane, the other by transposing LDS reads
+// (ds_read_b64_tr_b16: sixteen lanes read four rows of sixteen values and each receives one column), so that no operand
+// is laid out anew.  16-bit operands multiply as they are; fp32 operands are split into three bf16 numbers each while they
+// are staged, and six of the nine products are multiplied (split8, split_products: as close to the exact sum as fp32
+// products), at 2.6 times the rate of fp32 instructions.  All sums are fp32.
+#include "scnn_dense.h"
+
+namespace scnn {
+
+typedef float f4 __attribute__((ext_vector_type(4)));
+typedef _Float16 h8 __attribute__((ext_vector_type(8)));
+typedef short s4 __attribute__((ext_vector_type(4)));
+
+// Byte offset of 16-byte piece c of row r of a staged tile.  K_CONTIG: rows of BK k (a row is one m or n); else rows of W
+// values of one k.  Pieces are permuted within a row so that the lanes of a read hit different banks: by the row number
+// for rows of k; in pairs (the 32 bytes that four lanes of a transposing read share) by the k for the others, of which one
+// read takes the rows 8q .. 8q + 3, q < 4.
+template <bool K_CONTIG, int W>
+__device__ __forceinline__ int staged(int r, int c) {
+    constexpr int CH = W / 8;
+    if constexpr (K_CONTIG) {
+        const int sw = CH >= 8 ? (r & 7) : ((r >> 1) & 3);
+        return (r * CH + (c ^ sw)) * 16;
+    } else {
+        const int sw = ((r & 3) | ((r >> 1) & 4)) & (CH / 2 - 1);
+        return (r * CH + (c ^ (sw << 1))) * 16;
+    }
+}
+
+// Eight k (32 kk + 8 q .. + 7, q = lane / 16) of row or column `base` + lane % 16.
+template <bool K_CONTIG, int W>
+__device__ __forceinline__ u32x4 fragment(const char* tile, int base, int kk) {
+    const int lane = threadIdx.x & 63, q = lane >> 4, i = lane & 15;
+    if constexpr (K_CONTIG) {
+        return *(const u32x4*)(tile + staged<true, W>(base + i, kk * 4 + q));
+    } else {
+        typedef __attribute__((address_space(3))) s4 lds_s4;
+        const int k = kk * 32 + 8 * q + (i >> 2);
+        const int c = (base >> 3) + ((i & 3) >> 1), in = (i & 1) * 8;
+        union { s4 half[2]; u32x4 all; } r;
+        r.half[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4*)(tile + staged<false, W>(k, c) + in));
+        r.half[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4*)(tile + staged<false, W>(k + 4, c) + in));
+        return r.all;
+    }
+}
+
+// What a call multiplies.  `rows_k`: the device's row count bounds k (the filter's gradient), else m.
+struct LinearArgs {
+    const void* a;
+    const void* b;
+    long long m, n, k;
+    const long long* rows_dev;
+    const void* bias;
+    const void* residual;
+    void* out;
+    void* pre;
+    float* part;       // [splits][m][n], joined by k_linear_join; null: the tile ends the call itself
+    long long k_split; // k a workgroup sums, a multiple of 64
+    int act;
+    int rows_k;
+};
+
+// Epilogue of four neighbouring columns: bias, activation, residual.
+template <typename T>
+__device__ __forceinline__ void finish4(const LinearArgs& p, long long m, long long n, float (&z)[4]) {
+    const long long at = m * p.n + n;
+    const int w = (int)(p.n - n < 4 ? p.n - n : 4);
+    auto load4 = [&](const void* from, long long i, float (&v)[4]) {
+        const T* f = (const T*)from + i;
+        if (w == 4) {
+            VecOf<T, 4> r;
+            __builtin_memcpy(&r, f, sizeof(r));
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] = (float)r[j];
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] = j < w ? (float)f[j] : 0.0f;
+        }
+    };
+    auto store4 = [&](void* to, const float (&v)[4]) {
+        T* f = (T*)to + at;
+        if (w == 4) {
+            VecOf<T, 4> r;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) r[j] = (T)v[j];
+            __builtin_memcpy(f, &r, sizeof(r));
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (j < w) f[j] = (T)v[j];
+        }
+    };
+    float t[4];
+    if (p.bias) {
+        load4(p.bias, n, t);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) z[j] += t[j];
+    }
+    if (p.pre) store4(p.pre, z);
+    if (p.act != SCNN_ACT_NONE)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) z[j] = activate(z[j], p.act);
+    if (p.residual) {
+        load4(p.residual, at, t);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) z[j] += t[j];
+    }
+    store4(p.out, z);
+}
+
+// Eight neighbouring values of a tile's row, 0 past the array's end.
+template <typename T>
+__device__ __forceinline__ VecOf<T, 8> load8(const T* __restrict__ base, long long row, long long rows, long long col, long long cols) {
+    VecOf<T, 8> v = {};
+    if (row < rows) {
+        const T* __restrict__ p = base + row * cols + col;
+        if (col + 8 <= cols) {
+            __builtin_memcpy(&v, p, sizeof(v));
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (col + i < cols) v[i] = p[i];
+        }
+    }
+    return v;
+}
+
+// BM x BN outputs a workgroup of WM x WN waves, BK values of k a step.  The operands swap places at the instruction: its
+// rows are the tile's columns n, so that a lane ends with four neighbouring n of one m (16 or 8 bytes a store).
+template <typename T, bool AK, bool BK_, int BM, int BN, int BK, int WM, int WN>
+__global__ __launch_bounds__(64 * WM * WN) void k_linear_tile(LinearArgs p) {
+    constexpr bool SPLIT = std::is_same<T, float>::value;
+    constexpr int PARTS = SPLIT ? 3 : 1, NT = 64 * WM * WN;
+    constexpr int AW = AK ? BK : BM, BW = BK_ ? BK : BN;          // values of a staged row
+    constexpr int A8 = BM * BK / 8, B8 = BN * BK / 8;             // pieces of eight values
+    constexpr int AN = (A8 + NT - 1) / NT, BN8 = (B8 + NT - 1) / NT;
+    constexpr int TM = BM / WM / 16, TN = BN / WN / 16;
+    __shared__ __align__(16) char s_a[PARTS * A8 * 16];
+    __shared__ __align__(16) char s_b[PARTS * B8 * 16];
+    const long long rows = rows_of(p.rows_k ? p.k : p.m, p.rows_dev);
+    const long long m_end = p.rows_k ? p.m : rows, k_all = p.rows_k ? rows : p.k;
+    const unsigned tiles_n = (unsigned)((p.n + BN - 1) / BN);
+    const long long m0 = (long long)(blockIdx.x / tiles_n) * BM, n0 = (long long)(blockIdx.x % tiles_n) * BN;
+    if (m0 >= m_end) return;
+    const long long k_first = (long long)blockIdx.y * p.k_split;
+    const long long k_end = k_first + p.k_split < k_all ? k_first + p.k_split : k_all;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int wm = (wave / WN) * (TM * 16), wn = (wave % WN) * (TN * 16);
+
+    f4 acc[TM][TN];
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j) acc[i][j] = f4{0.f, 0.f, 0.f, 0.f};
+
+    VecOf<T, 8> ra[AN], rb[BN8];
+    auto fetch = [&](long long k) {
+#pragma unroll
+        for (int i = 0; i < AN; ++i) {
+            const int e = i * NT + tid, r = e / (AW / 8), c = e % (AW / 8) * 8;
+            if (A8 % NT == 0 || e < A8)
+                ra[i] = AK ? load8<T>((const T*)p.a, m0 + r, m_end, k + c, p.k)
+                           : load8<T>((const T*)p.a, k + r, k_end, m0 + c, p.m);
+        }
+#pragma unroll
+        for (int i = 0; i < BN8; ++i) {
+            const int e = i * NT + tid, r = e / (BW / 8), c = e % (BW / 8) * 8;
+            if (B8 % NT == 0 || e < B8)
+                rb[i] = BK_ ? load8<T>((const T*)p.b, n0 + r, p.n, k + c, p.k)
+                            : load8<T>((const T*)p.b, k + r, k_end, n0 + c, p.n);
+        }
+    };
+    int odd = 0;
+    auto put = [&](char* tile, int pieces, int at, const VecOf<T, 8>& v) {
+        if constexpr (SPLIT) {
+            u32x4 x[2], part[3];
+            __builtin_memcpy(x, &v, 32);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) odd |= split_exact(x[i >> 2][i & 3]) ? 0 : 1;
+            split8(x, part);
+#pragma unroll
+            for (int q = 0; q < 3; ++q) *(u32x4*)(tile + q * pieces * 16 + at) = part[q];
+        } else {
+            *(u32x4*)(tile + at) = __builtin_bit_cast(u32x4, v);
+        }
+    };
+    auto stage = [&]() {
+#pragma unroll
+        for (int i = 0; i < AN; ++i) {
+            const int e = i * NT + tid;
+            if (A8 % NT == 0 || e < A8) put(s_a, A8, staged<AK, AW>(e / (AW / 8), e % (AW / 8)), ra[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < BN8; ++i) {
+            const int e = i * NT + tid;
+            if (B8 % NT == 0 || e < B8) put(s_b, B8, staged<BK_, BW>(e / (BW / 8), e % (BW / 8)), rb[i]);
+        }
+    };
+    fetch(k_first);
+    for (long long k = k_first; k < k_end; k += BK) {
+        __syncthreads();
+        stage();
+        __syncthreads();
+        if (k + BK < k_end) fetch(k + BK);
+#pragma unroll
+        for (int kk = 0; kk < BK / 32; ++kk) {
+            u32x4 fa[TM][PARTS];
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+                for (int q = 0; q < PARTS; ++q) fa[i][q] = fragment<AK, AW>(s_a + q * A8 * 16, wm + i * 16, kk);
+#pragma unroll
+            for (int j = 0; j < TN; ++j) {
+                u32x4 fb[PARTS];
+#pragma unroll
+                for (int q = 0; q < PARTS; ++q) fb[q] = fragment<BK_, BW>(s_b + q * B8 * 16, wn + j * 16, kk);
+#pragma unroll
+                for (int i = 0; i < TM; ++i) {
+                    if constexpr (SPLIT) {
+                        f4 large, small;
+                        split_products(fb, fa[i][0], fa[i][1], fa[i][2], large, small);
+                        acc[i][j] += large + small;
+                    } else if constexpr (std::is_same<T, __bf16>::value) {
+                        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, fb[0]),
+                                                                            __builtin_bit_cast(bf16x8, fa[i][0]), acc[i][j], 0, 0, 0);
+                    } else {
+                        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, fb[0]),
+                                                                           __builtin_bit_cast(h8, fa[i][0]), acc[i][j], 0, 0, 0);
+                    }
+                }
+            }
+        }
+    }
+    if constexpr (SPLIT) {
+        // A value that the parts do not hold (infinities, NaN, magnitudes below 2^-109 or from 2^58 up) was among this
+        // workgroup's: its outputs are summed anew with fp32 products.
+        if (__syncthreads_or(odd)) {
+            const int q = lane >> 4, i16 = lane & 15;
+            auto at_a = [&](long long m, long long k) {
+                return m < m_end && k < k_end ? (float)((const T*)p.a)[AK ? m * p.k + k : k * p.m + m] : 0.0f;
+            };
+            auto at_b = [&](long long n, long long k) {
+                return n < p.n && k < k_end ? (float)((const T*)p.b)[BK_ ? n * p.k + k : k * p.n + n] : 0.0f;
+            };
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+                for (int j = 0; j < TN; ++j) acc[i][j] = f4{0.f, 0.f, 0.f, 0.f};
+            for (long long k = k_first; k < k_end; k += 4)
+#pragma unroll
+                for (int i = 0; i < TM; ++i) {
+                    const float va = at_a(m0 + wm + i * 16 + i16, k + q);
+#pragma unroll
+                    for (int j = 0; j < TN; ++j)
+                        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(at_b(n0 + wn + j * 16 + i16, k + q), va, acc[i][j], 0, 0, 0);
+                }
+        }
+    }
+    // lane: row m = lane % 16, columns n = 4 (lane / 16) .. + 3 of each block
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+        const long long m = m0 + wm + i * 16 + (lane & 15);
+        if (m >= m_end) continue;
+#pragma unroll
+        for (int j = 0; j < TN; ++j) {
+            const long long n = n0 + wn + j * 16 + 4 * (lane >> 4);
+            if (n >= p.n) continue;
+            float z[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
+            if (p.part) {
+                float* __restrict__ to = p.part + ((long long)blockIdx.y * p.m + m) * p.n + n;
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+                    if (n + c < p.n) to[c] = z[c];
+            } else {
+                finish4<T>(p, m, n, z);
+            }
+        }
+    }
+}
+
+// Joins the partial sums of a split k in order and ends the call; four neighbouring columns a thread.
+template <typename T>
+__global__ __launch_bounds__(256) void k_linear_join(LinearArgs p, int splits) {
+    const long long m_end = p.rows_k ? p.m : rows_of(p.m, p.rows_dev);
+    const long long quads = (p.n + 3) / 4;
+    const long long id = (long long)blockIdx.x * 256 + threadIdx.x;
+    const long long m = id / quads, n = id % quads * 4;
+    if (m >= m_end) return;
+    const int w = (int)(p.n - n < 4 ? p.n - n : 4);
+    float z[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int s = 0; s < splits; ++s) {
+        const float* __restrict__ f = p.part + ((long long)s * p.m + m) * p.n + n;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (j < w) z[j] += f[j];
+    }
+    finish4<T>(p, m, n, z);
+}
+
+// dz = g act'(pre) rounded to the operands' type (what the matrix instructions take), and this workgroup's column sums of
+// the dz before that rounding: part [gridDim.y][cols].  A block is 256 / TR threads wide, each a 16-byte vector of columns.
+template <typename T>
+__global__ __launch_bounds__(256) void k_act_back(const T* __restrict__ g, const T* __restrict__ pre, long long rows_cap,
+                                                  const long long* __restrict__ rows_dev, long long cols, int act, int tn,
+                                                  T* __restrict__ dz, float* __restrict__ part) {
+    constexpr int V = kVec<T>;
+    __shared__ float s_sum[256][V];
+    const long long rows = rows_of(rows_cap, rows_dev);
+    const int tc = threadIdx.x % tn, tr = threadIdx.x / tn, nr = 256 / tn;
+    const long long c = ((long long)blockIdx.x * tn + tc) * V;
+    const int n = (int)(cols - c < V ? cols - c : V);
+    float sum[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) sum[i] = 0.0f;
+    if (n > 0)
+        for (long long row = (long long)blockIdx.y * nr + tr; row < rows; row += (long long)gridDim.y * nr) {
+            float v[V], z[V];
+            load_elems<T>(g + row * cols + c, n, v);
+            if (act != SCNN_ACT_NONE) {
+                load_elems<T>(pre + row * cols + c, n, z);
+#pragma unroll
+                for (int i = 0; i < V; ++i) v[i] = activate_back(v[i], z[i], act);
+                store_elems<T>(dz + row * cols + c, n, v);
+            }
+#pragma unroll
+            for (int i = 0; i < V; ++i) sum[i] += v[i];
+        }
+    if (!part) return;
+#pragma unroll
+    for (int i = 0; i < V; ++i) s_sum[threadIdx.x][i] = sum[i];
+    __syncthreads();
+    for (int e = threadIdx.x; e < tn * V; e += 256) {
+        const int col = e / V, i = e % V;
+        const long long at = ((long long)blockIdx.x * tn + col) * V + i;
+        if (at >= cols) continue;
+        float t = 0.0f;
+        for (int r = 0; r < nr; ++r) t += s_sum[r * tn + col][i];
+        part[(long long)blockIdx.y * cols + at] = t;
+    }
+}
+
+// One to eight rows: bound by reading w once.  A workgroup owns sixteen columns; its threads, four or two side by side on a row of w,
+// share k; fp32 products; the threads' sums meet in LDS.
+template <typename T, int R>
+__global__ __launch_bounds__(256) void k_linear_few(LinearArgs p, int row0) {
+    constexpr int V = kVec<T>, TC = 16 / V, TK = 256 / TC;
+    __shared__ float s_sum[4][R][16];
+    const long long m_end = rows_of(p.m, p.rows_dev);
+    const int tc = threadIdx.x % TC, tk = threadIdx.x / TC, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const long long n = (long long)blockIdx.x * 16 + tc * V;
+    const int w = (int)(p.n - n < V ? p.n - n : V);
+    float acc[R][V];
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int i = 0; i < V; ++i) acc[r][i] = 0.0f;
+    const T* __restrict__ x = (const T*)p.a;
+    const T* __restrict__ wt = (const T*)p.b;
+#pragma unroll 4
+    for (long long k = tk; k < p.k; k += TK) {
+        float wv[V];
+        load_elems<T>(wt + k * p.n + n, w, wv);
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const float xv = row0 + r < m_end ? (float)x[(row0 + r) * p.k + k] : 0.0f;
+#pragma unroll
+            for (int i = 0; i < V; ++i) acc[r][i] += xv * wv[i];
+        }
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            float v = acc[r][i];
+#pragma unroll
+            for (int d = TC; d < 64; d <<= 1) v += __shfl_xor(v, d, 64);
+            if (lane < TC) s_sum[wave][r][tc * V + i] = v;
+        }
+    __syncthreads();
+    if (threadIdx.x >= R * 4) return;
+    const int r = threadIdx.x >> 2, c = (threadIdx.x & 3) * 4;
+    const long long col = (long long)blockIdx.x * 16 + c;
+    if (row0 + r >= m_end || col >= p.n) return;
+    float z[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) z[j] = (s_sum[0][r][c + j] + s_sum[1][r][c + j]) + (s_sum[2][r][c + j] + s_sum[3][r][c + j]);
+    finish4<T>(p, row0 + r, col, z);
+}
+
+// ------------------------------------------------------------------ host side
+struct TilePlan {
+    int splits;
+    long long k_split;
+    bool few;
+};
+constexpr int kTileM = 64, kTileN = 64;
+
+// The most k that one chain of 16-bit matrix instructions sums: the instruction cuts its sum off downwards at every step
+// of 32 k, half a last bit on average, so that 65536 k may leave 2^10 last bits of 2^-24, an eighth of a last bit of fp16.
+constexpr long long kChain = 65536;
+
+// k is split where the output has too few tiles to fill the card, and into chains of at most kChain.
+static TilePlan tile_plan(long long m, long long n, long long k, bool forward) {
+    TilePlan t = {1, round_up(k < 1 ? 1 : k, 64), false};
+    if (m < 1) return t;
+    if (forward && m <= 8) {
+        t.few = true;
+        return t;
+    }
+    const long long tiles = ((m + kTileM - 1) / kTileM) * ((n + kTileN - 1) / kTileN);
+    const long long want = 2LL * device_cu_count();
+    if (tiles < want) {
+        long long s = want / tiles, most = (k + 255) / 256;
+        if (s > most) s = most;
+        if (s > 1) t.k_split = round_up((k + s - 1) / s, 64);
+    }
+    if (t.k_split > kChain) t.k_split = kChain;
+    t.splits = (int)((k + t.k_split - 1) / t.k_split);
+    if (t.splits < 1) t.splits = 1;
+    return t;
+}
+
+static size_t part_bytes(const TilePlan& t, long long m, long long n) {
+    return t.splits > 1 ? (size_t)round_up((long long)t.splits * m * n * 4, 256) : 0;
+}
+
+template <typename T, bool AK, bool BK_>
+static hipError_t product(LinearArgs p, const TilePlan& t, hipStream_t s) {
+    constexpr int BK = std::is_same<T, float>::value ? 32 : 64;
+    p.k_split = t.k_split;
+    if (t.splits <= 1) p.part = nullptr;
+    const dim3 grid((unsigned)(((p.n + kTileN - 1) / kTileN) * ((p.m + kTileM - 1) / kTileM)), (unsigned)t.splits);
+    hipLaunchKernelGGL((k_linear_tile<T, AK, BK_, kTileM, kTileN, BK, 2, 2>), grid, dim3(256), 0, s, p);
+    if (t.splits > 1) {
+        const long long threads = p.m * ((p.n + 3) / 4);
+        hipLaunchKernelGGL((k_linear_join<T>), dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, s, p, t.splits);
+    }
+    return hipGetLastError();
+}
+
+template <typename T>
+static hipError_t few_rows(const LinearArgs& p, hipStream_t s) {
+    const dim3 grid((unsigned)((p.n + 15) / 16));
+    if (p.m == 1) hipLaunchKernelGGL((k_linear_few<T, 1>), grid, dim3(256), 0, s, p, 0);
+    else if (p.m <= 4) hipLaunchKernelGGL((k_linear_few<T, 4>), grid, dim3(256), 0, s, p, 0);
+    else hipLaunchKernelGGL((k_linear_few<T, 8>), grid, dim3(256), 0, s, p, 0);
+    return hipGetLastError();
+}
+
+size_t linear_fwd_part_bytes(long long rows, long long c_in, long long c_out) {
+    return part_bytes(tile_plan(rows, c_out, c_in, true), rows, c_out);
+}
+
+hipError_t launch_linear_fwd(int dtype, const LinearCall& c, hipStream_t s) {
+    if (c.rows < 1) return hipSuccess;
+    LinearArgs p = {};
+    p.a = c.x; p.b = c.w;
+    p.m = c.rows; p.n = c.c_out; p.k = c.c_in;
+    p.rows_dev = c.rows_dev;
+    p.bias = c.bias; p.residual = c.residual; p.out = c.out; p.pre = c.pre;
+    p.part = (float*)c.workspace;
+    p.act = c.act;
+    const TilePlan t = tile_plan(p.m, p.n, p.k, true);
+    switch (dtype) {
+        case SCNN_F32: return t.few ? few_rows<float>(p, s) : product<float, true, false>(p, t, s);
+        case SCNN_BF16: return t.few ? few_rows<__bf16>(p, s) : product<__bf16, true, false>(p, t, s);
+        default: return t.few ? few_rows<_Float16>(p, s) : product<_Float16, true, false>(p, t, s);
+    }
+}
+
+// Row slices of k_act_back and its block's width in threads.
+struct BackPlan { int tn, parts; };
+static BackPlan back_plan(long long rows, long long cols, int dtype) {
+    const int v = dtype == SCNN_F32 ? 4 : 8;
+    BackPlan b = {1, 1};
+    while (b.tn < 64 && (long long)b.tn * v < cols) b.tn <<= 1;
+    const long long strips = (cols + (long long)b.tn * v - 1) / ((long long)b.tn * v), nr = 256 / b.tn;
+    long long parts = 4LL * device_cu_count() / strips;
+    const long long need = (rows + nr - 1) / nr;
+    if (parts > need) parts = need;
+    b.parts = (int)(parts < 1 ? 1 : parts);
+    return b;
+}
+
+struct BackSpace { size_t dz, sums, dx, dw, total; };
+static BackSpace back_space(int dtype, long long rows, long long c_in, long long c_out, int act) {
+    BackSpace b = {};
+    const size_t e = dtype == SCNN_F32 ? 4 : 2;
+    size_t at = 0;
+    b.dz = at;
+    if (act != SCNN_ACT_NONE) at += (size_t)round_up(rows * c_out * (long long)e, 256);
+    b.sums = at;
+    at += (size_t)round_up((long long)back_plan(rows, c_out, dtype).parts * c_out * 4, 256);
+    b.dx = b.dw = at;  // (the two products run one after the other and share their partial sums' place)
+    const size_t dx = part_bytes(tile_plan(rows, c_in, c_out, false), rows, c_in);
+    const size_t dw = part_bytes(tile_plan(c_in, c_out, rows, false), c_in, c_out);
+    b.total = at + (dx > dw ? dx : dw);
+    return b;
+}
+
+size_t linear_bwd_bytes(int dtype, long long rows, long long c_in, long long c_out, int act) {
+    return back_space(dtype, rows, c_in, c_out, act).total;
+}
+
+template <typename T>
+static hipError_t linear_bwd_typed(int dtype, const LinearCall& c, hipStream_t s) {
+    const BackSpace at = back_space(dtype, c.rows, c.c_in, c.c_out, c.act);
+    char* const ws = (char*)c.workspace;
+    const void* dz = c.g;
+    if (c.act != SCNN_ACT_NONE) dz = ws + at.dz;
+    const bool products = c.dx || c.dw;
+    if (c.dbias || (products && c.act != SCNN_ACT_NONE)) {
+        const BackPlan b = back_plan(c.rows, c.c_out, dtype);
+        const long long wide = (long long)b.tn * kVec<T>;
+        float* const sums = c.dbias ? (float*)(ws + at.sums) : nullptr;
+        hipLaunchKernelGGL((k_act_back<T>), dim3((unsigned)((c.c_out + wide - 1) / wide), (unsigned)b.parts), dim3(256), 0, s,
+                           (const T*)c.g, (const T*)c.pre_in, c.rows, c.rows_dev, c.c_out, c.act, b.tn, (T*)(ws + at.dz), sums);
+        if (c.dbias) {
+            const hipError_t e = launch_column_sums(sums, b.parts, c.c_out, c.c_out, c.dbias, nullptr, dtype, s);
+            if (e != hipSuccess) return e;
+        }
+    }
+    LinearArgs p = {};
+    p.rows_dev = c.rows_dev;
+    p.act = SCNN_ACT_NONE;
+    if (c.dx && c.rows > 0) {
+        p.a = dz; p.b = c.w; p.out = c.dx;
+        p.m = c.rows; p.n = c.c_in; p.k = c.c_out;
+        p.part = (float*)(ws + at.dx);
+        const hipError_t e = product<T, true, true>(p, tile_plan(p.m, p.n, p.k, false), s);
+        if (e != hipSuccess) return e;
+    }
+    if (c.dw) {
+        p.a = c.x; p.b = dz; p.out = c.dw;
+        p.m = c.c_in; p.n = c.c_out; p.k = c.rows;
+        p.rows_k = 1;
+        p.part = (float*)(ws + at.dw);
+        return product<T, false, false>(p, tile_plan(p.m, p.n, p.k, false), s);
+    }
+    return hipGetLastError();
+}
+
+hipError_t launch_linear_bwd(int dtype, const LinearCall& c, hipStream_t s) {
+    switch (dtype) {
+        case SCNN_F32: return linear_bwd_typed<float>(dtype, c, s);
+        case SCNN_BF16: return linear_bwd_typed<__bf16>(dtype, c, s);
+        default: return linear_bwd_typed<_Float16>(dtype, c, s);
+    }
+}
+
+}  // namespace scnn

@@ -1,0 +1,483 @@
+// Layer norm over the channels of rows [rows, C], forward and backward.
+//
+//   mean = sum_c x / C,  var = sum_c (x - mean)^2 / C,  rstd = 1 / sqrt(var + eps),  xh = (x - mean) rstd
+//   out = xh gamma + beta
+//   h = g gamma,  dx = rstd (h - sum_c(h) / C - xh sum_c(h xh) / C),  dgamma = sum_r g xh,  dbeta = sum_r g
+//
+// Both directions are bound by memory: a row is read once and kept in registers between its sums and its result (the
+// deviations are summed around the mean that is already known, so nothing cancels).  The mean is summed in fp64, so that it
+// is the exact one rounded, and a row of equal values, however large, has deviations of exactly 0; the other sums in fp32.
+// The sums over rows
+// behind dgamma and dbeta are formed a column a lane in registers while the rows go by, joined within the workgroup, and
+// the workgroups' sums are added by a second launch in a fixed order: no atomics, the same bits every time.
+#include "scnn_dense.h"
+
+namespace scnn {
+
+// P threads hold a row (a group of lanes of a wave, or a whole workgroup from 256 on), VPL 16-byte vectors each.
+template <int P> constexpr int kNormBlock = P <= 64 ? 256 : P;
+
+// Sum over the P threads of a row; s_part holds one value a wave.  From 256 threads on every thread of the block calls it.
+template <int P, typename F>
+__device__ __forceinline__ F row_add(F v, F* s_part) {
+    if constexpr (P <= 64) {
+        return lanes_add<P>(v);
+    } else {
+        v = lanes_add<64>(v);
+        __syncthreads();  // (the sum before this one has been read)
+        if ((threadIdx.x & 63) == 0) s_part[threadIdx.x >> 6] = v;
+        __syncthreads();
+        F t = 0;
+#pragma unroll
+        for (int i = 0; i < P / 64; ++i) t += s_part[i];
+        return t;
+    }
+}
+
+template <typename T, int P, int VPL>
+__global__ __launch_bounds__(kNormBlock<P>) void k_norm_fwd(const T* __restrict__ x, long long rows_cap,
+                                                            const long long* __restrict__ rows_dev, int channels,
+                                                            const T* __restrict__ gamma, const T* __restrict__ beta,
+                                                            float eps, T* __restrict__ out, float* __restrict__ mean_out,
+                                                            float* __restrict__ rstd_out) {
+    constexpr int V = kVec<T>, G = kNormBlock<P> / P;
+    __shared__ float s_part[P <= 64 ? 1 : P / 64];
+    __shared__ double s_mean[P <= 64 ? 1 : P / 64];
+    const long long rows = rows_of(rows_cap, rows_dev);
+    const int t = threadIdx.x % P;
+    const float inv_c = 1.0f / (float)channels;
+    const double inv_c64 = 1.0 / (double)channels;
+    for (long long row = (long long)blockIdx.x * G + threadIdx.x / P; row < rows; row += (long long)gridDim.x * G) {
+        const T* __restrict__ xr = x + row * channels;
+        float v[VPL][V];
+        double sum = 0.0;
+#pragma unroll
+        for (int j = 0; j < VPL; ++j) {
+            const int c = (j * P + t) * V;
+            load_elems<T>(xr + c, channels - c, v[j]);
+#pragma unroll
+            for (int i = 0; i < V; ++i) sum += (double)v[j][i];
+        }
+        const float mean = (float)(row_add<P>(sum, s_mean) * inv_c64);
+        float sq = 0.0f;
+#pragma unroll
+        for (int j = 0; j < VPL; ++j) {
+            const int c = (j * P + t) * V;
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                v[j][i] = c + i < channels ? v[j][i] - mean : 0.0f;
+                sq += v[j][i] * v[j][i];
+            }
+        }
+        const float rstd = 1.0f / sqrtf(row_add<P>(sq, s_part) * inv_c + eps);
+        T* __restrict__ yr = out + row * channels;
+#pragma unroll
+        for (int j = 0; j < VPL; ++j) {
+            const int c = (j * P + t) * V;
+            float ga[V], be[V];
+            if (gamma) load_elems<T>(gamma + c, channels - c, ga);
+            if (beta) load_elems<T>(beta + c, channels - c, be);
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                v[j][i] *= rstd;
+                if (gamma) v[j][i] *= ga[i];
+                if (beta) v[j][i] += be[i];
+            }
+            store_elems<T>(yr + c, channels - c, v[j]);
+        }
+        if (t == 0) {
+            if (mean_out) mean_out[row] = mean;
+            if (rstd_out) rstd_out[row] = rstd;
+        }
+    }
+}
+
+// Rows too long for a workgroup's registers: read three times, the second and third time mostly from the L2.
+template <typename T>
+__global__ __launch_bounds__(1024) void k_norm_fwd_long(const T* __restrict__ x, long long rows_cap,
+                                                        const long long* __restrict__ rows_dev, int channels,
+                                                        const T* __restrict__ gamma, const T* __restrict__ beta, float eps,
+                                                        T* __restrict__ out, float* __restrict__ mean_out,
+                                                        float* __restrict__ rstd_out) {
+    constexpr int V = kVec<T>, P = 1024;
+    __shared__ float s_part[P / 64];
+    __shared__ double s_mean[P / 64];
+    const long long rows = rows_of(rows_cap, rows_dev);
+    const float inv_c = 1.0f / (float)channels;
+    const double inv_c64 = 1.0 / (double)channels;
+    for (long long row = blockIdx.x; row < rows; row += gridDim.x) {
+        const T* __restrict__ xr = x + row * channels;
+        T* __restrict__ yr = out + row * channels;
+        double sum = 0.0;
+        float sq = 0.0f;
+        for (long long c = (long long)threadIdx.x * V; c < channels; c += P * V) {
+            float v[V];
+            load_elems<T>(xr + c, channels - (int)c, v);
+#pragma unroll
+            for (int i = 0; i < V; ++i) sum += (double)v[i];
+        }
+        const float mean = (float)(row_add<P>(sum, s_mean) * inv_c64);
+        for (long long c = (long long)threadIdx.x * V; c < channels; c += P * V) {
+            float v[V];
+            load_elems<T>(xr + c, channels - (int)c, v);
+#pragma unroll
+            for (int i = 0; i < V; ++i) sq += c + i < channels ? (v[i] - mean) * (v[i] - mean) : 0.0f;
+        }
+        const float rstd = 1.0f / sqrtf(row_add<P>(sq, s_part) * inv_c + eps);
+        for (long long c = (long long)threadIdx.x * V; c < channels; c += P * V) {
+            const int n = channels - (int)c;
+            float v[V], ga[V], be[V];
+            load_elems<T>(xr + c, n, v);
+            if (gamma) load_elems<T>(gamma + c, n, ga);
+            if (beta) load_elems<T>(beta + c, n, be);
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                v[i] = (v[i] - mean) * rstd;
+                if (gamma) v[i] *= ga[i];
+                if (beta) v[i] += be[i];
+            }
+            store_elems<T>(yr + c, n, v);
+        }
+        if (threadIdx.x == 0) {
+            if (mean_out) mean_out[row] = mean;
+            if (rstd_out) rstd_out[row] = rstd;
+        }
+    }
+}
+
+// part [gridDim.x][2][channels]: this workgroup's sums of g xh and of g (not written where part is null).
+template <typename T, int P, int VPL>
+__global__ __launch_bounds__(kNormBlock<P>) void k_norm_bwd(const T* __restrict__ x, const T* __restrict__ g,
+                                                            long long rows_cap, const long long* __restrict__ rows_dev,
+                                                            int channels, const T* __restrict__ gamma,
+                                                            const float* __restrict__ mean_in,
+                                                            const float* __restrict__ rstd_in, T* __restrict__ dx,
+                                                            float* __restrict__ part) {
+    constexpr int V = kVec<T>, G = kNormBlock<P> / P;
+    __shared__ float s_part[P <= 64 ? 1 : P / 64];
+    const long long rows = rows_of(rows_cap, rows_dev);
+    const int t = threadIdx.x % P;
+    const float inv_c = 1.0f / (float)channels;
+    float ga[VPL][V], d_gamma[VPL][V], d_beta[VPL][V];
+#pragma unroll
+    for (int j = 0; j < VPL; ++j) {
+        const int c = (j * P + t) * V;
+        if (gamma) load_elems<T>(gamma + c, channels - c, ga[j]);
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            d_gamma[j][i] = d_beta[j][i] = 0.0f;
+            if (!gamma) ga[j][i] = 1.0f;
+        }
+    }
+    for (long long row = (long long)blockIdx.x * G + threadIdx.x / P; row < rows; row += (long long)gridDim.x * G) {
+        const float mean = mean_in[row], rstd = rstd_in[row];
+        float xh[VPL][V], gr[VPL][V];
+        float s_h = 0.0f, s_hx = 0.0f;
+#pragma unroll
+        for (int j = 0; j < VPL; ++j) {
+            const int c = (j * P + t) * V;
+            load_elems<T>(x + row * channels + c, channels - c, xh[j]);
+            load_elems<T>(g + row * channels + c, channels - c, gr[j]);
+        }
+#pragma unroll
+        for (int j = 0; j < VPL; ++j)
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                // (past the row's end g is 0, and so is everything below; xh there is finite with the row's own mean)
+                const bool in = (j * P + t) * V + i < channels;
+                xh[j][i] = in ? (xh[j][i] - mean) * rstd : 0.0f;
+                d_gamma[j][i] += gr[j][i] * xh[j][i];
+                d_beta[j][i] += gr[j][i];
+                gr[j][i] *= ga[j][i];
+                s_h += gr[j][i];
+                s_hx += gr[j][i] * xh[j][i];
+            }
+        if (!dx) continue;
+        const float m_h = row_add<P>(s_h, s_part) * inv_c, m_hx = row_add<P>(s_hx, s_part) * inv_c;
+#pragma unroll
+        for (int j = 0; j < VPL; ++j) {
+            const int c = (j * P + t) * V;
+#pragma unroll
+            for (int i = 0; i < V; ++i) gr[j][i] = rstd * (gr[j][i] - m_h - xh[j][i] * m_hx);
+            store_elems<T>(dx + row * channels + c, channels - c, gr[j]);
+        }
+    }
+    if (!part) return;
+    float* __restrict__ mine = part + (long long)blockIdx.x * 2 * channels;
+    if constexpr (P > 64) {
+#pragma unroll
+        for (int j = 0; j < VPL; ++j)
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const int c = (j * P + t) * V + i;
+                if (c < channels) {
+                    mine[c] = d_gamma[j][i];
+                    mine[channels + c] = d_beta[j][i];
+                }
+            }
+    } else {
+        // the groups of a wave by lane exchanges, the four waves in LDS
+        __shared__ float s_col[4][2][P * V];
+        const int wave = threadIdx.x >> 6;
+#pragma unroll
+        for (int j = 0; j < VPL; ++j) {
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                float a = d_gamma[j][i], b = d_beta[j][i];
+#pragma unroll
+                for (int d = P; d < 64; d <<= 1) {
+                    a += __shfl_xor(a, d, 64);
+                    b += __shfl_xor(b, d, 64);
+                }
+                if ((threadIdx.x & 63) < P) {
+                    s_col[wave][0][t * V + i] = a;
+                    s_col[wave][1][t * V + i] = b;
+                }
+            }
+            __syncthreads();
+            for (int c = threadIdx.x; c < P * V; c += 256) {
+                const int cc = j * P * V + c;
+                if (cc < channels) {
+                    mine[cc] = (s_col[0][0][c] + s_col[1][0][c]) + (s_col[2][0][c] + s_col[3][0][c]);
+                    mine[channels + cc] = (s_col[0][1][c] + s_col[1][1][c]) + (s_col[2][1][c] + s_col[3][1][c]);
+                }
+            }
+        }
+    }
+}
+
+// dx of rows too long for a workgroup's registers; their dgamma and dbeta come from k_norm_cols_long.
+template <typename T>
+__global__ __launch_bounds__(1024) void k_norm_bwd_long(const T* __restrict__ x, const T* __restrict__ g,
+                                                        long long rows_cap, const long long* __restrict__ rows_dev,
+                                                        int channels, const T* __restrict__ gamma,
+                                                        const float* __restrict__ mean_in,
+                                                        const float* __restrict__ rstd_in, T* __restrict__ dx) {
+    constexpr int V = kVec<T>, P = 1024;
+    __shared__ float s_part[P / 64];
+    const long long rows = rows_of(rows_cap, rows_dev);
+    const float inv_c = 1.0f / (float)channels;
+    for (long long row = blockIdx.x; row < rows; row += gridDim.x) {
+        const float mean = mean_in[row], rstd = rstd_in[row];
+        const T* __restrict__ xr = x + row * channels;
+        const T* __restrict__ gr = g + row * channels;
+        float s_h = 0.0f, s_hx = 0.0f;
+        for (int pass = 0; pass < 2; ++pass) {
+            float m_h = 0.0f, m_hx = 0.0f;
+            if (pass) {
+                m_h = row_add<P>(s_h, s_part) * inv_c;
+                m_hx = row_add<P>(s_hx, s_part) * inv_c;
+            }
+            for (long long c = (long long)threadIdx.x * V; c < channels; c += P * V) {
+                const int n = channels - (int)c;
+                float v[V], h[V], ga[V];
+                load_elems<T>(xr + c, n, v);
+                load_elems<T>(gr + c, n, h);
+                if (gamma) load_elems<T>(gamma + c, n, ga);
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    v[i] = i < n ? (v[i] - mean) * rstd : 0.0f;
+                    if (gamma) h[i] *= ga[i];
+                    if (pass) {
+                        h[i] = rstd * (h[i] - m_h - v[i] * m_hx);
+                    } else {
+                        s_h += h[i];
+                        s_hx += h[i] * v[i];
+                    }
+                }
+                if (pass) store_elems<T>(dx + row * channels + c, n, h);
+            }
+        }
+    }
+}
+
+// part [gridDim.y][2][channels]: column sums of g xh and g over this workgroup's rows, a vector of columns a thread.
+template <typename T>
+__global__ __launch_bounds__(256) void k_norm_cols_long(const T* __restrict__ x, const T* __restrict__ g, long long rows_cap,
+                                                        const long long* __restrict__ rows_dev, int channels,
+                                                        const float* __restrict__ mean_in,
+                                                        const float* __restrict__ rstd_in, float* __restrict__ part) {
+    constexpr int V = kVec<T>;
+    const long long rows = rows_of(rows_cap, rows_dev);
+    const long long c = ((long long)blockIdx.x * 256 + threadIdx.x) * V;
+    if (c >= channels) return;
+    const int n = channels - (int)c;
+    float d_gamma[V], d_beta[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) d_gamma[i] = d_beta[i] = 0.0f;
+    for (long long row = blockIdx.y; row < rows; row += gridDim.y) {
+        const float mean = mean_in[row], rstd = rstd_in[row];
+        float v[V], h[V];
+        load_elems<T>(x + row * channels + c, n, v);
+        load_elems<T>(g + row * channels + c, n, h);
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            d_gamma[i] += i < n ? h[i] * ((v[i] - mean) * rstd) : 0.0f;
+            d_beta[i] += h[i];
+        }
+    }
+    float* __restrict__ mine = part + (long long)blockIdx.y * 2 * channels;
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+        if (i < n) {
+            mine[c + i] = d_gamma[i];
+            mine[channels + c + i] = d_beta[i];
+        }
+}
+
+// Sixteen columns a workgroup, sixteen threads a column, each over every sixteenth part; their sums joined in order.
+template <typename T>
+__global__ __launch_bounds__(256) void k_column_sums(const float* __restrict__ part, int parts, long long cols,
+                                                     long long split, T* __restrict__ out0, T* __restrict__ out1) {
+    __shared__ double s_sum[16][17];
+    const int tc = threadIdx.x & 15, tp = threadIdx.x >> 4;
+    const long long c = (long long)blockIdx.x * 16 + tc;
+    double sum = 0.0;
+    if (c < cols)
+        for (int p = tp; p < parts; p += 16) sum += (double)part[(long long)p * cols + c];
+    s_sum[tp][tc] = sum;
+    __syncthreads();
+    if (tp != 0 || c >= cols) return;
+    sum = 0.0;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) sum += s_sum[i][tc];
+    if (c < split) {
+        if (out0) out0[c] = (T)(float)sum;
+    } else if (out1) {
+        out1[c - split] = (T)(float)sum;
+    }
+}
+
+template <typename T>
+static hipError_t column_sums(const float* part, int parts, long long cols, long long split, void* out0, void* out1,
+                              hipStream_t s) {
+    hipLaunchKernelGGL((k_column_sums<T>), dim3((unsigned)((cols + 15) / 16)), dim3(256), 0, s, part, parts, cols, split,
+                       (T*)out0, (T*)out1);
+    return hipGetLastError();
+}
+
+hipError_t launch_column_sums(const float* part, int parts, long long cols, long long split, void* out0, void* out1,
+                              int dtype, hipStream_t s) {
+    if (cols < 1 || (!out0 && !out1)) return hipSuccess;
+    switch (dtype) {
+        case SCNN_F32: return column_sums<float>(part, parts, cols, split, out0, out1, s);
+        case SCNN_BF16: return column_sums<__bf16>(part, parts, cols, split, out0, out1, s);
+        default: return column_sums<_Float16>(part, parts, cols, split, out0, out1, s);
+    }
+}
+
+static int dtype_vec(int dtype) { return dtype == SCNN_F32 ? 4 : 8; }
+
+// Threads a row and vectors a thread: the fewest threads that hold the row with one vector each up to a wave, then up to
+// four vectors a lane, then a workgroup.  `most` = vectors a thread may hold in a workgroup of 1024 (the backward pass
+// keeps six values an element).
+struct NormShape { int p, vpl; };
+static NormShape norm_shape(int channels, int dtype, int most) {
+    const int units = (int)(((long long)channels + dtype_vec(dtype) - 1) / dtype_vec(dtype));
+    for (int p = 1; p <= 64; p <<= 1)
+        if (units <= p) return {p, 1};
+    if (units <= 128) return {64, 2};
+    if (units <= 256) return {256, 1};
+    if (units <= 512) return {256, 2};
+    if (units <= 1024) return {1024, 1};
+    if (units <= 2048) return {1024, 2};
+    if (units <= 4096 && most >= 4) return {1024, 4};
+    return {0, 0};
+}
+
+// Workgroups of the backward pass: each leaves 2 * channels sums, which are written and read again, so that at least 32
+// rows stand behind one (the sums are then a sixteenth of the bytes of 16-bit rows, less of others), but the card is filled.
+static int norm_parts(long long rows, int channels, int dtype) {
+    const NormShape n = norm_shape(channels, dtype, 2);
+    if (n.p == 0) return (int)(rows < 1 ? 1 : (rows < 256 ? rows : 256));
+    const long long per = n.p <= 64 ? 256 / n.p : 1;
+    long long parts = rows / (32 * per) > 256 ? rows / (32 * per) : 256;
+    if (parts > 1024) parts = 1024;
+    const long long need = (rows + per - 1) / per;
+    if (parts > need) parts = need;
+    return (int)(parts < 1 ? 1 : parts);
+}
+
+size_t norm_bwd_part_bytes(long long rows, int channels, int dtype) {
+    return (size_t)norm_parts(rows, channels, dtype) * 2 * (size_t)channels * sizeof(float);
+}
+
+#define SCNN_NORM_SHAPES(F)                                                                                             \
+    F(1, 1) F(2, 1) F(4, 1) F(8, 1) F(16, 1) F(32, 1) F(64, 1) F(64, 2) F(256, 1) F(256, 2) F(1024, 1) F(1024, 2)
+
+template <typename T>
+static hipError_t norm_fwd(const void* x, long long rows, const long long* rows_dev, int channels, const void* gamma,
+                           const void* beta, float eps, void* out, float* mean, float* rstd, int dtype, hipStream_t s) {
+    const NormShape n = norm_shape(channels, dtype, 4);
+    const long long per = n.p > 0 && n.p <= 64 ? 256 / n.p : 1;
+    const int threads = n.p == 0 ? 1024 : (n.p <= 64 ? 256 : n.p);
+    long long blocks = (rows + per - 1) / per;
+    const long long most = (long long)device_cu_count() * (2048 / threads);
+    if (blocks > most) blocks = most;
+#define F(P, VPL)                                                                                                      \
+    if (n.p == P && n.vpl == VPL)                                                                                      \
+        hipLaunchKernelGGL((k_norm_fwd<T, P, VPL>), dim3((unsigned)blocks), dim3(kNormBlock<P>), 0, s, (const T*)x, rows,    \
+                           rows_dev, channels, (const T*)gamma, (const T*)beta, eps, (T*)out, mean, rstd);
+    SCNN_NORM_SHAPES(F) F(1024, 4)
+#undef F
+    if (n.p == 0)
+        hipLaunchKernelGGL((k_norm_fwd_long<T>), dim3((unsigned)blocks), dim3(1024), 0, s, (const T*)x, rows, rows_dev,
+                           channels, (const T*)gamma, (const T*)beta, eps, (T*)out, mean, rstd);
+    return hipGetLastError();
+}
+
+hipError_t launch_norm_fwd(const void* x, long long rows, const long long* rows_dev, int channels, const void* gamma,
+                           const void* beta, float eps, void* out, float* mean, float* rstd, int dtype, hipStream_t s) {
+    if (rows < 1) return hipSuccess;
+    switch (dtype) {
+        case SCNN_F32: return norm_fwd<float>(x, rows, rows_dev, channels, gamma, beta, eps, out, mean, rstd, dtype, s);
+        case SCNN_BF16: return norm_fwd<__bf16>(x, rows, rows_dev, channels, gamma, beta, eps, out, mean, rstd, dtype, s);
+        default: return norm_fwd<_Float16>(x, rows, rows_dev, channels, gamma, beta, eps, out, mean, rstd, dtype, s);
+    }
+}
+
+template <typename T>
+static hipError_t norm_bwd(const void* x, const void* g, long long rows, const long long* rows_dev, int channels,
+                           const void* gamma, const float* mean, const float* rstd, void* dx, void* dgamma, void* dbeta,
+                           float* part, int dtype, hipStream_t s) {
+    const NormShape n = norm_shape(channels, dtype, 2);
+    const int parts = norm_parts(rows, channels, dtype);
+    float* const sums = dgamma || dbeta ? part : nullptr;
+#define F(P, VPL)                                                                                                      \
+    if (n.p == P && n.vpl == VPL)                                                                                      \
+        hipLaunchKernelGGL((k_norm_bwd<T, P, VPL>), dim3((unsigned)parts), dim3(kNormBlock<P>), 0, s, (const T*)x,      \
+                           (const T*)g, rows, rows_dev, channels, (const T*)gamma, mean, rstd, (T*)dx, sums);
+    SCNN_NORM_SHAPES(F)
+#undef F
+    if (n.p == 0) {
+        if (dx) {
+            const long long blocks = rows < 2 * device_cu_count() ? (rows < 1 ? 1 : rows) : 2 * device_cu_count();
+            hipLaunchKernelGGL((k_norm_bwd_long<T>), dim3((unsigned)blocks), dim3(1024), 0, s, (const T*)x, (const T*)g,
+                               rows, rows_dev, channels, (const T*)gamma, mean, rstd, (T*)dx);
+        }
+        if (sums) {
+            const int wide = 256 * dtype_vec(dtype);
+            hipLaunchKernelGGL((k_norm_cols_long<T>), dim3((unsigned)(((long long)channels + wide - 1) / wide), (unsigned)parts),
+                               dim3(256), 0, s, (const T*)x, (const T*)g, rows, rows_dev, channels, mean, rstd, sums);
+        }
+    }
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || !sums) return e;
+    return launch_column_sums(sums, parts, 2LL * channels, channels, dgamma, dbeta, dtype, s);
+}
+
+hipError_t launch_norm_bwd(const void* x, const void* g, long long rows, const long long* rows_dev, int channels,
+                           const void* gamma, const float* mean, const float* rstd, void* dx, void* dgamma, void* dbeta,
+                           float* part, int dtype, hipStream_t s) {
+    switch (dtype) {
+        case SCNN_F32:
+            return norm_bwd<float>(x, g, rows, rows_dev, channels, gamma, mean, rstd, dx, dgamma, dbeta, part, dtype, s);
+        case SCNN_BF16:
+            return norm_bwd<__bf16>(x, g, rows, rows_dev, channels, gamma, mean, rstd, dx, dgamma, dbeta, part, dtype, s);
+        default:
+            return norm_bwd<_Float16>(x, g, rows, rows_dev, channels, gamma, mean, rstd, dx, dgamma, dbeta, part, dtype, s);
+    }
+}
+
+}  // namespace scnn
