@@ -479,28 +479,34 @@ def prune_weights(w, warned, eps, *, stream=None):
 # Layers on rows of values.  All tensors of a call live on one device, which need not be the current one.  With `stream`
 # the call runs there and its new tensors belong to that stream: the caller orders other streams behind it.
 
-class _On:
-    """Makes `dev`, and `stream` where one is given, current while a call allocates and launches."""
-
-    def __init__(self, dev, stream, tensors):
-        if stream is not None:
-            if stream.device != dev:
-                raise ValueError("the stream belongs to another device than the tensors")
-            if stream != torch.cuda.current_stream(dev):
-                for t in tensors:  # (their memory may not be handed out again before the stream is done with them)
-                    if t is not None:
-                        t.record_stream(stream)
-            self.scope = torch.cuda.stream(stream)
-        else:
-            self.scope = None if dev.index == torch.cuda.current_device() else torch.cuda.device(dev)
+class _Here:
+    """The current device and stream: nothing to change."""
 
     def __enter__(self):
-        if self.scope is not None:
-            self.scope.__enter__()
+        pass
 
     def __exit__(self, *exc):
-        if self.scope is not None:
-            self.scope.__exit__(*exc)
+        pass
+
+
+_HERE = _Here()
+
+
+def _on(dev, stream, tensors):
+    """Makes `dev`, and `stream` where one is given, current while a call allocates and launches."""
+    if stream is None:
+        return _HERE if dev.index == torch.cuda.current_device() else torch.cuda.device(dev)
+    if stream.device != dev:
+        raise ValueError("the stream belongs to another device than the tensors")
+    if stream != torch.cuda.current_stream(dev):
+        for t in tensors:  # (their memory may not be handed out again before the stream is done with them)
+            if t is not None:
+                t.record_stream(stream)
+    return torch.cuda.stream(stream)
+
+
+def _at(t: Optional[torch.Tensor]) -> Optional[int]:
+    return None if t is None else t.data_ptr()
 
 
 def _same(t, like: torch.Tensor, shape, name: str, dtype=None):
@@ -511,7 +517,7 @@ def _same(t, like: torch.Tensor, shape, name: str, dtype=None):
         raise ValueError(f"{name} must live on the GPU of the other tensors")
     if t.dtype != (dtype or like.dtype):
         raise ValueError(f"{name} must be {dtype or like.dtype}")
-    if tuple(t.shape) != shape:
+    if t.shape != shape:
         raise ValueError(f"{name} must be of shape {list(shape)}, not {list(t.shape)}")
     return t
 
@@ -585,15 +591,15 @@ def linear_fwd(x, w, bias=None, *, act="none", residual=None, keep_pre=False, ro
     _same(residual, x, (rows, c_out), "residual")
     code = _activation(act)
     rows_dev = _rows_dev(rows_dev, x)
-    with _On(x.device, stream, (x, w, bias, residual, rows_dev, out, pre, workspace)):
+    with _on(x.device, stream, (x, w, bias, residual, rows_dev, out, pre, workspace)):
         x, w, bias, residual = x.contiguous(), w.contiguous(), _cont(bias), _cont(residual)
         keep = keep_pre or pre is not None
         out = _result(out, x, (rows, c_out), "out")
         if keep:
             pre = _result(pre, x, (rows, c_out), "pre")
         workspace = _scratch(workspace, int(L.linear_fwd_workspace(dt, rows, c_in, c_out)), x)
-        _check(L, L.linear_fwd(dt, _ptr(x), rows, _ptr(rows_dev), c_in, _ptr(w), _ptr(bias), c_out, code, _ptr(residual),
-                               _ptr(out), _ptr(pre), _ptr(workspace), workspace.numel(), _stream(None)))
+        _check(L, L.linear_fwd(dt, _at(x), rows, _at(rows_dev), c_in, _at(w), _at(bias), c_out, code, _at(residual),
+                               _at(out), _at(pre), _at(workspace), workspace.numel(), torch.cuda.current_stream().cuda_stream))
     return (out, pre) if keep else out
 
 
@@ -623,14 +629,14 @@ def linear_bwd(x, w, g, *, act="none", pre=None, want=(True, True, True), rows_d
     pre = _same(pre, x, (rows, c_out), "pre") if code else None
     rows_dev = _rows_dev(rows_dev, x)
     dx, dw, dbias = out if out is not None else (None, None, None)
-    with _On(x.device, stream, (x, w, g, pre, rows_dev, dx, dw, dbias, workspace)):
+    with _on(x.device, stream, (x, w, g, pre, rows_dev, dx, dw, dbias, workspace)):
         x, w, g, pre = x.contiguous(), w.contiguous(), g.contiguous(), _cont(pre)
         dx = _result(dx, x, (rows, c_in), "dx") if want[0] else None
         dw = _result(dw, x, (c_in, c_out), "dw") if want[1] else None
         dbias = _result(dbias, x, (c_out,), "dbias") if want[2] else None
         workspace = _scratch(workspace, int(L.linear_bwd_workspace(dt, rows, c_in, c_out, code)), x)
-        _check(L, L.linear_bwd(dt, _ptr(x), rows, _ptr(rows_dev), c_in, _ptr(w), c_out, code, _ptr(pre), _ptr(g), _ptr(dx),
-                               _ptr(dw), _ptr(dbias), _ptr(workspace), workspace.numel(), _stream(None)))
+        _check(L, L.linear_bwd(dt, _at(x), rows, _at(rows_dev), c_in, _at(w), c_out, code, _at(pre), _at(g), _at(dx),
+                               _at(dw), _at(dbias), _at(workspace), workspace.numel(), torch.cuda.current_stream().cuda_stream))
     return dx, dw, dbias
 
 
@@ -643,13 +649,13 @@ def layer_norm_fwd(x, gamma=None, beta=None, *, eps=1e-5, rows_dev=None, out=Non
     _same(beta, x, (ch,), "beta")
     rows_dev = _rows_dev(rows_dev, x)
     y, mean, rstd = out if out is not None else (None, None, None)
-    with _On(x.device, stream, (x, gamma, beta, rows_dev, y, mean, rstd)):
+    with _on(x.device, stream, (x, gamma, beta, rows_dev, y, mean, rstd)):
         x, gamma, beta = x.contiguous(), _cont(gamma), _cont(beta)
         y = _result(y, x, (rows, ch), "out")
         mean = _result(mean, x, (rows,), "mean", torch.float32)
         rstd = _result(rstd, x, (rows,), "rstd", torch.float32)
-        _check(L, L.layer_norm_fwd(dt, _ptr(x), rows, _ptr(rows_dev), ch, _ptr(gamma), _ptr(beta), float(eps), _ptr(y),
-                                   _ptr(mean), _ptr(rstd), _stream(None)))
+        _check(L, L.layer_norm_fwd(dt, _at(x), rows, _at(rows_dev), ch, _at(gamma), _at(beta), float(eps), _at(y),
+                                   _at(mean), _at(rstd), torch.cuda.current_stream().cuda_stream))
     return y, mean, rstd
 
 
@@ -673,14 +679,14 @@ def layer_norm_bwd(x, g, gamma, mean, rstd, *, want=(True, True, True), rows_dev
     _same(rstd, x, (rows,), "rstd", torch.float32)
     rows_dev = _rows_dev(rows_dev, x)
     dx, dgamma, dbeta = out if out is not None else (None, None, None)
-    with _On(x.device, stream, (x, g, gamma, mean, rstd, rows_dev, dx, dgamma, dbeta, workspace)):
+    with _on(x.device, stream, (x, g, gamma, mean, rstd, rows_dev, dx, dgamma, dbeta, workspace)):
         x, g, gamma, mean, rstd = x.contiguous(), g.contiguous(), _cont(gamma), mean.contiguous(), rstd.contiguous()
         dx = _result(dx, x, (rows, ch), "dx") if want[0] else None
         dgamma = _result(dgamma, x, (ch,), "dgamma") if want[1] else None
         dbeta = _result(dbeta, x, (ch,), "dbeta") if want[2] else None
         workspace = _scratch(workspace, int(L.layer_norm_bwd_workspace(dt, rows, ch)), x)
-        _check(L, L.layer_norm_bwd(dt, _ptr(x), _ptr(g), rows, _ptr(rows_dev), ch, _ptr(gamma), _ptr(mean), _ptr(rstd),
-                                   _ptr(dx), _ptr(dgamma), _ptr(dbeta), _ptr(workspace), workspace.numel(), _stream(None)))
+        _check(L, L.layer_norm_bwd(dt, _at(x), _at(g), rows, _at(rows_dev), ch, _at(gamma), _at(mean), _at(rstd),
+                                   _at(dx), _at(dgamma), _at(dbeta), _at(workspace), workspace.numel(), torch.cuda.current_stream().cuda_stream))
     return dx, dgamma, dbeta
 
 
@@ -723,11 +729,11 @@ def _grad_clip(grads, max_norm, outs, workspace, stream):
     types = (ctypes.c_int * n)(*[DTYPES[t.dtype] for t in grads])
     src = (ctypes.c_void_p * n)(*[t.data_ptr() for t in grads])
     dst = None if outs is None else (ctypes.c_void_p * n)(*[t.data_ptr() for t in outs])
-    with _On(dev, stream, (*grads, *(outs or ()), workspace)):
+    with _on(dev, stream, (*grads, *(outs or ()), workspace)):
         result = torch.empty(2, dtype=torch.float64, device=dev)
         workspace = _scratch(workspace, int(L.grad_clip_workspace(n, counts)), like)
-        _check(L, L.grad_clip(n, src, dst, counts, types, float(max_norm), _ptr(result), _ptr(workspace), workspace.numel(),
-                              _stream(None)))
+        _check(L, L.grad_clip(n, src, dst, counts, types, float(max_norm), _at(result), _at(workspace), workspace.numel(),
+                              torch.cuda.current_stream().cuda_stream))
     return result
 
 

@@ -19,16 +19,22 @@ template <typename T, int N> using VecOf = T __attribute__((ext_vector_type(N)))
 // Sixteen bytes from an address aligned to the element only (rows of odd widths start anywhere): the compiler makes one
 // global access of 16 bytes of it, which the hardware takes at any address.  The first `n` elements, the rest 0.
 template <typename T>
-__device__ __forceinline__ void load_elems(const T* __restrict__ p, int n, float (&v)[kVec<T>]) {
+__device__ __forceinline__ VecOf<T, kVec<T>> load_raw(const T* __restrict__ p, int n) {
+    VecOf<T, kVec<T>> r = {};
     if (n >= kVec<T>) {
-        VecOf<T, kVec<T>> r;
         __builtin_memcpy(&r, p, sizeof(r));
-#pragma unroll
-        for (int i = 0; i < kVec<T>; ++i) v[i] = (float)r[i];
     } else {
 #pragma unroll
-        for (int i = 0; i < kVec<T>; ++i) v[i] = i < n ? (float)p[i] : 0.0f;
+        for (int i = 0; i < kVec<T>; ++i)
+            if (i < n) r[i] = p[i];
     }
+    return r;
+}
+template <typename T>
+__device__ __forceinline__ void load_elems(const T* __restrict__ p, int n, float (&v)[kVec<T>]) {
+    const VecOf<T, kVec<T>> r = load_raw<T>(p, n);
+#pragma unroll
+    for (int i = 0; i < kVec<T>; ++i) v[i] = (float)r[i];
 }
 
 // Rounded once, to nearest even.
@@ -80,7 +86,16 @@ __device__ __forceinline__ float activate_back(float g, float z, int act) {
 template <int P, typename F>
 __device__ __forceinline__ F lanes_add(F v) {
 #pragma unroll
-    for (int d = 1; d < P; d <<= 1) v += __shfl_xor(v, d, 64);
+    for (int d = 1; d < P; d <<= 1) {
+        if constexpr (sizeof(F) == 8 && !std::is_same<F, double>::value) {  // (a pair of floats)
+            F o;
+            o.x = __shfl_xor(v.x, d, 64);
+            o.y = __shfl_xor(v.y, d, 64);
+            v += o;
+        } else {
+            v += __shfl_xor(v, d, 64);
+        }
+    }
     return v;
 }
 

@@ -14,22 +14,24 @@
 
 namespace scnn {
 
-// P threads hold a row (a group of lanes of a wave, or a whole workgroup from 256 on), VPL 16-byte vectors each.
+// P threads hold a row (a group of lanes of a wave, or whole waves from 256 on), VPL 16-byte vectors each.
 template <int P> constexpr int kNormBlock = P <= 64 ? 256 : P;
+// The backward pass takes four rows of 256 threads at once: sixteen waves of loads in flight, and one set of sums.
+template <int P> constexpr int kBackBlock = P <= 64 ? 256 : 1024;
 
-// Sum over the P threads of a row; s_part holds one value a wave.  From 256 threads on every thread of the block calls it.
+// Sum over the P threads of a row.  Up to 64: lane exchanges.  Else s_part holds a value a wave of the workgroup, all of
+// whose threads call it; two arrays in turn make one barrier a sum enough.
 template <int P, typename F>
 __device__ __forceinline__ F row_add(F v, F* s_part) {
     if constexpr (P <= 64) {
         return lanes_add<P>(v);
     } else {
         v = lanes_add<64>(v);
-        __syncthreads();  // (the sum before this one has been read)
         if ((threadIdx.x & 63) == 0) s_part[threadIdx.x >> 6] = v;
         __syncthreads();
         F t = 0;
 #pragma unroll
-        for (int i = 0; i < P / 64; ++i) t += s_part[i];
+        for (int i = 0; i < P / 64; ++i) t += s_part[threadIdx.x / P * (P / 64) + i];
         return t;
     }
 }
@@ -147,104 +149,123 @@ __global__ __launch_bounds__(1024) void k_norm_fwd_long(const T* __restrict__ x,
 
 // part [gridDim.x][2][channels]: this workgroup's sums of g xh and of g (not written where part is null).
 template <typename T, int P, int VPL>
-__global__ __launch_bounds__(kNormBlock<P>) void k_norm_bwd(const T* __restrict__ x, const T* __restrict__ g,
+__global__ __launch_bounds__(kBackBlock<P>) void k_norm_bwd(const T* __restrict__ x, const T* __restrict__ g,
                                                             long long rows_cap, const long long* __restrict__ rows_dev,
                                                             int channels, const T* __restrict__ gamma,
                                                             const float* __restrict__ mean_in,
                                                             const float* __restrict__ rstd_in, T* __restrict__ dx,
                                                             float* __restrict__ part) {
-    constexpr int V = kVec<T>, G = kNormBlock<P> / P;
-    __shared__ float s_part[P <= 64 ? 1 : P / 64];
+    constexpr int V = kVec<T>, B = kBackBlock<P>, G = B / P;
+    typedef float f2 __attribute__((ext_vector_type(2)));
+    __shared__ f2 s_part[2][P <= 64 ? 1 : B / 64];
     const long long rows = rows_of(rows_cap, rows_dev);
-    const int t = threadIdx.x % P;
+    const int t = threadIdx.x % P, group = threadIdx.x / P;
     const float inv_c = 1.0f / (float)channels;
-    float ga[VPL][V], d_gamma[VPL][V], d_beta[VPL][V];
+    float d_gamma[VPL][V], d_beta[VPL][V];
+    VecOf<T, V> ga[VPL];
 #pragma unroll
     for (int j = 0; j < VPL; ++j) {
         const int c = (j * P + t) * V;
-        if (gamma) load_elems<T>(gamma + c, channels - c, ga[j]);
+        ga[j] = VecOf<T, V>{};
+        if (gamma) ga[j] = load_raw<T>(gamma + c, channels - c);
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-            d_gamma[j][i] = d_beta[j][i] = 0.0f;
-            if (!gamma) ga[j][i] = 1.0f;
-        }
+        for (int i = 0; i < V; ++i) d_gamma[j][i] = d_beta[j][i] = 0.0f;
     }
-    for (long long row = (long long)blockIdx.x * G + threadIdx.x / P; row < rows; row += (long long)gridDim.x * G) {
-        const float mean = mean_in[row], rstd = rstd_in[row];
-        float xh[VPL][V], gr[VPL][V];
-        float s_h = 0.0f, s_hx = 0.0f;
+    int turn = 0;
+    // Rows as they lie in memory (half the registers with 16-bit types), the next one on its way while this one is summed
+    // where the registers last.
+    constexpr bool AHEAD = VPL == 1;
+    VecOf<T, V> xr[VPL], gr[VPL], x_next[VPL], g_next[VPL];
+    float mean_next = 0.0f, rstd_next = 0.0f;
+    auto fetch = [&](long long row) {
+        const bool live = row < rows;
+        if (live) {
+            mean_next = mean_in[row];
+            rstd_next = rstd_in[row];
+        }
 #pragma unroll
         for (int j = 0; j < VPL; ++j) {
             const int c = (j * P + t) * V;
-            load_elems<T>(x + row * channels + c, channels - c, xh[j]);
-            load_elems<T>(g + row * channels + c, channels - c, gr[j]);
+            x_next[j] = load_raw<T>(x + row * channels + c, live ? channels - c : 0);
+            g_next[j] = load_raw<T>(g + row * channels + c, live ? channels - c : 0);
         }
+    };
+    if (AHEAD) fetch((long long)blockIdx.x * G + group);
+    // (all groups of the workgroup go round together: row_add holds a barrier)
+    for (long long row0 = (long long)blockIdx.x * G; row0 < rows; row0 += (long long)gridDim.x * G, turn ^= 1) {
+        const long long row = row0 + group;
+        const bool live = row < rows;
+        if (!AHEAD) fetch(row);
+        const float mean = mean_next, rstd = rstd_next;
+        f2 sums = {0.0f, 0.0f};
+#pragma unroll
+        for (int j = 0; j < VPL; ++j) {
+            xr[j] = x_next[j];
+            gr[j] = g_next[j];
+        }
+        if (AHEAD) fetch(row + (long long)gridDim.x * G);
 #pragma unroll
         for (int j = 0; j < VPL; ++j)
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-                // (past the row's end g is 0, and so is everything below; xh there is finite with the row's own mean)
-                const bool in = (j * P + t) * V + i < channels;
-                xh[j][i] = in ? (xh[j][i] - mean) * rstd : 0.0f;
-                d_gamma[j][i] += gr[j][i] * xh[j][i];
-                d_beta[j][i] += gr[j][i];
-                gr[j][i] *= ga[j][i];
-                s_h += gr[j][i];
-                s_hx += gr[j][i] * xh[j][i];
+                // (past the row's end g is 0, and so is everything below)
+                const float xh = (j * P + t) * V + i < channels ? ((float)xr[j][i] - mean) * rstd : 0.0f;
+                const float gi = (float)gr[j][i], h = gamma ? gi * (float)ga[j][i] : gi;
+                d_gamma[j][i] += gi * xh;
+                d_beta[j][i] += gi;
+                sums.x += h;
+                sums.y += h * xh;
             }
         if (!dx) continue;
-        const float m_h = row_add<P>(s_h, s_part) * inv_c, m_hx = row_add<P>(s_hx, s_part) * inv_c;
+        sums = row_add<P>(sums, s_part[turn]) * inv_c;
+        if constexpr (sizeof(T) == 2) {
+            // the compiler would keep the products of the first half in twice the registers: it may not know these values
+            // any more
 #pragma unroll
-        for (int j = 0; j < VPL; ++j) {
-            const int c = (j * P + t) * V;
-#pragma unroll
-            for (int i = 0; i < V; ++i) gr[j][i] = rstd * (gr[j][i] - m_h - xh[j][i] * m_hx);
-            store_elems<T>(dx + row * channels + c, channels - c, gr[j]);
+            for (int j = 0; j < VPL; ++j) asm volatile("" : "+v"(xr[j]), "+v"(gr[j]));
         }
+        if (live)
+#pragma unroll
+            for (int j = 0; j < VPL; ++j) {
+                const int c = (j * P + t) * V;
+                float v[V];
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    const float gi = (float)gr[j][i], h = gamma ? gi * (float)ga[j][i] : gi;
+                    v[i] = rstd * (h - sums.x - ((float)xr[j][i] - mean) * rstd * sums.y);
+                }
+                store_elems<T>(dx + row * channels + c, channels - c, v);
+            }
     }
     if (!part) return;
     float* __restrict__ mine = part + (long long)blockIdx.x * 2 * channels;
-    if constexpr (P > 64) {
+    // the rows of a wave by lane exchanges, those of different waves in LDS
+    constexpr int L = P <= 64 ? 4 : G;
+    __shared__ float s_col[L][P * V];
+    const int set = P <= 64 ? threadIdx.x >> 6 : group;
 #pragma unroll
-        for (int j = 0; j < VPL; ++j)
+    for (int j = 0; j < VPL; ++j)
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const int c = (j * P + t) * V + i;
-                if (c < channels) {
-                    mine[c] = d_gamma[j][i];
-                    mine[channels + c] = d_beta[j][i];
-                }
-            }
-    } else {
-        // the groups of a wave by lane exchanges, the four waves in LDS
-        __shared__ float s_col[4][2][P * V];
-        const int wave = threadIdx.x >> 6;
-#pragma unroll
-        for (int j = 0; j < VPL; ++j) {
+        for (int k = 0; k < 2; ++k) {
             __syncthreads();
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-                float a = d_gamma[j][i], b = d_beta[j][i];
+                float a = k ? d_beta[j][i] : d_gamma[j][i];
+                if constexpr (P < 64)
 #pragma unroll
-                for (int d = P; d < 64; d <<= 1) {
-                    a += __shfl_xor(a, d, 64);
-                    b += __shfl_xor(b, d, 64);
-                }
-                if ((threadIdx.x & 63) < P) {
-                    s_col[wave][0][t * V + i] = a;
-                    s_col[wave][1][t * V + i] = b;
-                }
+                    for (int d = P; d < 64; d <<= 1) a += __shfl_xor(a, d, 64);
+                if (P > 64 || (threadIdx.x & 63) < P) s_col[set][t * V + i] = a;
             }
             __syncthreads();
-            for (int c = threadIdx.x; c < P * V; c += 256) {
+            for (int c = threadIdx.x; c < P * V; c += B) {
                 const int cc = j * P * V + c;
-                if (cc < channels) {
-                    mine[cc] = (s_col[0][0][c] + s_col[1][0][c]) + (s_col[2][0][c] + s_col[3][0][c]);
-                    mine[channels + cc] = (s_col[0][1][c] + s_col[1][1][c]) + (s_col[2][1][c] + s_col[3][1][c]);
-                }
+                if (cc >= channels) break;
+                float sum = s_col[0][c];
+#pragma unroll
+                for (int q = 1; q < L; ++q) sum += s_col[q][c];
+                mine[(long long)k * channels + cc] = sum;
             }
         }
-    }
 }
 
 // dx of rows too long for a workgroup's registers; their dgamma and dbeta come from k_norm_cols_long.
@@ -255,7 +276,7 @@ __global__ __launch_bounds__(1024) void k_norm_bwd_long(const T* __restrict__ x,
                                                         const float* __restrict__ mean_in,
                                                         const float* __restrict__ rstd_in, T* __restrict__ dx) {
     constexpr int V = kVec<T>, P = 1024;
-    __shared__ float s_part[P / 64];
+    __shared__ float s_part[2][P / 64];
     const long long rows = rows_of(rows_cap, rows_dev);
     const float inv_c = 1.0f / (float)channels;
     for (long long row = blockIdx.x; row < rows; row += gridDim.x) {
@@ -266,8 +287,8 @@ __global__ __launch_bounds__(1024) void k_norm_bwd_long(const T* __restrict__ x,
         for (int pass = 0; pass < 2; ++pass) {
             float m_h = 0.0f, m_hx = 0.0f;
             if (pass) {
-                m_h = row_add<P>(s_h, s_part) * inv_c;
-                m_hx = row_add<P>(s_hx, s_part) * inv_c;
+                m_h = row_add<P>(s_h, s_part[0]) * inv_c;
+                m_hx = row_add<P>(s_hx, s_part[1]) * inv_c;
             }
             for (long long c = (long long)threadIdx.x * V; c < channels; c += P * V) {
                 const int n = channels - (int)c;
@@ -326,22 +347,27 @@ __global__ __launch_bounds__(256) void k_norm_cols_long(const T* __restrict__ x,
         }
 }
 
-// Sixteen columns a workgroup, sixteen threads a column, each over every sixteenth part; their sums joined in order.
+// Sixteen columns a workgroup, 64 threads a column, each over every 64th part; their sums joined in order.  (The parts are
+// some hundred to two thousand; with sixteen threads a column 820 parts took 13.7 us, a load behind the other.)
 template <typename T>
-__global__ __launch_bounds__(256) void k_column_sums(const float* __restrict__ part, int parts, long long cols,
-                                                     long long split, T* __restrict__ out0, T* __restrict__ out1) {
-    __shared__ double s_sum[16][17];
+__global__ __launch_bounds__(1024) void k_column_sums(const float* __restrict__ part, int parts, long long cols,
+                                                      long long split, T* __restrict__ out0, T* __restrict__ out1) {
+    __shared__ double s_sum[64][17];
     const int tc = threadIdx.x & 15, tp = threadIdx.x >> 4;
     const long long c = (long long)blockIdx.x * 16 + tc;
     double sum = 0.0;
     if (c < cols)
-        for (int p = tp; p < parts; p += 16) sum += (double)part[(long long)p * cols + c];
+#pragma unroll 8
+        for (int p = tp; p < parts; p += 64) sum += (double)part[(long long)p * cols + c];
     s_sum[tp][tc] = sum;
     __syncthreads();
-    if (tp != 0 || c >= cols) return;
-    sum = 0.0;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) sum += s_sum[i][tc];
+    for (int d = 32; d >= 4; d >>= 1) {
+        if (tp < d) s_sum[tp][tc] += s_sum[tp + d][tc];
+        __syncthreads();
+    }
+    if (tp != 0 || c >= cols) return;
+    sum = (s_sum[0][tc] + s_sum[1][tc]) + (s_sum[2][tc] + s_sum[3][tc]);
     if (c < split) {
         if (out0) out0[c] = (T)(float)sum;
     } else if (out1) {
@@ -352,7 +378,7 @@ __global__ __launch_bounds__(256) void k_column_sums(const float* __restrict__ p
 template <typename T>
 static hipError_t column_sums(const float* part, int parts, long long cols, long long split, void* out0, void* out1,
                               hipStream_t s) {
-    hipLaunchKernelGGL((k_column_sums<T>), dim3((unsigned)((cols + 15) / 16)), dim3(256), 0, s, part, parts, cols, split,
+    hipLaunchKernelGGL((k_column_sums<T>), dim3((unsigned)((cols + 15) / 16)), dim3(1024), 0, s, part, parts, cols, split,
                        (T*)out0, (T*)out1);
     return hipGetLastError();
 }
@@ -379,21 +405,26 @@ static NormShape norm_shape(int channels, int dtype, int most) {
         if (units <= p) return {p, 1};
     if (units <= 128) return {64, 2};
     if (units <= 256) return {256, 1};
-    if (units <= 512) return {256, 2};
+    if (units <= 512) return {512, 1};
     if (units <= 1024) return {1024, 1};
     if (units <= 2048) return {1024, 2};
     if (units <= 4096 && most >= 4) return {1024, 4};
     return {0, 0};
 }
 
-// Workgroups of the backward pass: each leaves 2 * channels sums, which are written and read again, so that at least 32
-// rows stand behind one (the sums are then a sixteenth of the bytes of 16-bit rows, less of others), but the card is filled.
+// Workgroups of the backward pass.  Each leaves 2 * channels sums, written and read again in fp32: at most about a sixteenth
+// of the bytes that the rows take in and out, but enough to fill the card with one workgroup a compute unit, and no more
+// than eight of four waves.
 static int norm_parts(long long rows, int channels, int dtype) {
     const NormShape n = norm_shape(channels, dtype, 2);
-    if (n.p == 0) return (int)(rows < 1 ? 1 : (rows < 256 ? rows : 256));
-    const long long per = n.p <= 64 ? 256 / n.p : 1;
-    long long parts = rows / (32 * per) > 256 ? rows / (32 * per) : 256;
-    if (parts > 1024) parts = 1024;
+    const long long cus = device_cu_count();
+    if (n.p == 0) return (int)(rows < 1 ? 1 : (rows < cus ? rows : cus));
+    const long long per = (n.p <= 64 ? 256 : 1024) / n.p;
+    const long long e = dtype == SCNN_F32 ? 4 : 2;
+    long long parts = rows * 3 * e / (16 * 16);
+    if (parts > 8 * cus) parts = 8 * cus;
+    if (n.p > 64) parts = cus;
+    if (parts < cus) parts = cus;
     const long long need = (rows + per - 1) / per;
     if (parts > need) parts = need;
     return (int)(parts < 1 ? 1 : parts);
@@ -404,7 +435,7 @@ size_t norm_bwd_part_bytes(long long rows, int channels, int dtype) {
 }
 
 #define SCNN_NORM_SHAPES(F)                                                                                             \
-    F(1, 1) F(2, 1) F(4, 1) F(8, 1) F(16, 1) F(32, 1) F(64, 1) F(64, 2) F(256, 1) F(256, 2) F(1024, 1) F(1024, 2)
+    F(1, 1) F(2, 1) F(4, 1) F(8, 1) F(16, 1) F(32, 1) F(64, 1) F(64, 2) F(256, 1) F(512, 1) F(1024, 1) F(1024, 2)
 
 template <typename T>
 static hipError_t norm_fwd(const void* x, long long rows, const long long* rows_dev, int channels, const void* gamma,
@@ -446,7 +477,7 @@ static hipError_t norm_bwd(const void* x, const void* g, long long rows, const l
     float* const sums = dgamma || dbeta ? part : nullptr;
 #define F(P, VPL)                                                                                                      \
     if (n.p == P && n.vpl == VPL)                                                                                      \
-        hipLaunchKernelGGL((k_norm_bwd<T, P, VPL>), dim3((unsigned)parts), dim3(kNormBlock<P>), 0, s, (const T*)x,      \
+        hipLaunchKernelGGL((k_norm_bwd<T, P, VPL>), dim3((unsigned)parts), dim3(kBackBlock<P>), 0, s, (const T*)x,      \
                            (const T*)g, rows, rows_dev, channels, (const T*)gamma, mean, rstd, (T*)dx, sums);
     SCNN_NORM_SHAPES(F)
 #undef F
