@@ -248,7 +248,8 @@ int prune_weights(float* w, unsigned char* warned, int64_t n_w, float eps, int64
  * sparse_conv_fwd without a host read: rows past the count are neither read nor
  * written, in outputs too.  An array that a call writes may overlap no other
  * array of the call, the workspace included (refused; see linear_fwd's residual).
- * The calls allocate nothing, wait for nothing,
+ * Where a workspace query answers 256 the call
+ * uses none and takes a null one too.  The calls allocate nothing, wait for nothing,
  * contain no memset and can be captured in a HIP graph; calls that run at the
  * same time need workspaces of their own. */
 #define SCNN_F32 0

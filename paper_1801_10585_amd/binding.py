@@ -2,6 +2,7 @@
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from typing import Optional, Sequence, Tuple
 
@@ -555,14 +556,32 @@ def _activation(act: str) -> int:
     return ACTIVATIONS[act]
 
 
-def _scratch(workspace, need: int, like: torch.Tensor) -> torch.Tensor:
-    if need == 0:
-        raise ScnnError(-1, load_library().scnn_last_error().decode())
+@functools.lru_cache(maxsize=4096)
+def _need(query: str, *sizes) -> int:
+    """Answer of a workspace query, which depends on its arguments alone."""
+    L = load_library()
+    r = int(getattr(L, query)(*sizes))
+    if r == 0:
+        raise ScnnError(-1, L.scnn_last_error().decode())
+    return r
+
+
+def _scratch(workspace, need: int, like: torch.Tensor) -> Optional[torch.Tensor]:
     if workspace is None:
-        return torch.empty(need, dtype=torch.uint8, device=like.device)
+        # (a call that needs the least amount uses none)
+        return None if need <= 256 else torch.empty(need, dtype=torch.uint8, device=like.device)
     if workspace.device != like.device or workspace.dtype != torch.uint8 or not workspace.is_contiguous():
         raise ValueError("workspace must be a contiguous uint8 tensor on the GPU of the rows")
     return workspace
+
+
+def _bytes(workspace) -> int:
+    return 0 if workspace is None else workspace.numel()
+
+
+def _current() -> int:
+    """The current device's current stream."""
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
 def _cont(t: Optional[torch.Tensor]) -> Optional[torch.Tensor]:
@@ -570,11 +589,7 @@ def _cont(t: Optional[torch.Tensor]) -> Optional[torch.Tensor]:
 
 
 def linear_fwd_workspace(dtype: torch.dtype, rows: int, c_in: int, c_out: int) -> int:
-    L = load_library()
-    r = int(L.linear_fwd_workspace(DTYPES[dtype], int(rows), int(c_in), int(c_out)))
-    if r == 0:
-        raise ScnnError(-1, L.scnn_last_error().decode())
-    return r
+    return _need("linear_fwd_workspace", DTYPES[dtype], int(rows), int(c_in), int(c_out))
 
 
 def linear_fwd(x, w, bias=None, *, act="none", residual=None, keep_pre=False, rows_dev=None, out=None, pre=None,
@@ -597,18 +612,14 @@ def linear_fwd(x, w, bias=None, *, act="none", residual=None, keep_pre=False, ro
         out = _result(out, x, (rows, c_out), "out")
         if keep:
             pre = _result(pre, x, (rows, c_out), "pre")
-        workspace = _scratch(workspace, int(L.linear_fwd_workspace(dt, rows, c_in, c_out)), x)
+        workspace = _scratch(workspace, _need("linear_fwd_workspace", dt, rows, c_in, c_out), x)
         _check(L, L.linear_fwd(dt, _at(x), rows, _at(rows_dev), c_in, _at(w), _at(bias), c_out, code, _at(residual),
-                               _at(out), _at(pre), _at(workspace), workspace.numel(), torch.cuda.current_stream().cuda_stream))
+                               _at(out), _at(pre), _at(workspace), _bytes(workspace), _current()))
     return (out, pre) if keep else out
 
 
 def linear_bwd_workspace(dtype: torch.dtype, rows: int, c_in: int, c_out: int, act="none") -> int:
-    L = load_library()
-    r = int(L.linear_bwd_workspace(DTYPES[dtype], int(rows), int(c_in), int(c_out), _activation(act)))
-    if r == 0:
-        raise ScnnError(-1, L.scnn_last_error().decode())
-    return r
+    return _need("linear_bwd_workspace", DTYPES[dtype], int(rows), int(c_in), int(c_out), _activation(act))
 
 
 def linear_bwd(x, w, g, *, act="none", pre=None, want=(True, True, True), rows_dev=None, out=None, workspace=None,
@@ -634,9 +645,9 @@ def linear_bwd(x, w, g, *, act="none", pre=None, want=(True, True, True), rows_d
         dx = _result(dx, x, (rows, c_in), "dx") if want[0] else None
         dw = _result(dw, x, (c_in, c_out), "dw") if want[1] else None
         dbias = _result(dbias, x, (c_out,), "dbias") if want[2] else None
-        workspace = _scratch(workspace, int(L.linear_bwd_workspace(dt, rows, c_in, c_out, code)), x)
+        workspace = _scratch(workspace, _need("linear_bwd_workspace", dt, rows, c_in, c_out, code), x)
         _check(L, L.linear_bwd(dt, _at(x), rows, _at(rows_dev), c_in, _at(w), c_out, code, _at(pre), _at(g), _at(dx),
-                               _at(dw), _at(dbias), _at(workspace), workspace.numel(), torch.cuda.current_stream().cuda_stream))
+                               _at(dw), _at(dbias), _at(workspace), _bytes(workspace), _current()))
     return dx, dw, dbias
 
 
@@ -655,16 +666,12 @@ def layer_norm_fwd(x, gamma=None, beta=None, *, eps=1e-5, rows_dev=None, out=Non
         mean = _result(mean, x, (rows,), "mean", torch.float32)
         rstd = _result(rstd, x, (rows,), "rstd", torch.float32)
         _check(L, L.layer_norm_fwd(dt, _at(x), rows, _at(rows_dev), ch, _at(gamma), _at(beta), float(eps), _at(y),
-                                   _at(mean), _at(rstd), torch.cuda.current_stream().cuda_stream))
+                                   _at(mean), _at(rstd), _current()))
     return y, mean, rstd
 
 
 def layer_norm_bwd_workspace(dtype: torch.dtype, rows: int, channels: int) -> int:
-    L = load_library()
-    r = int(L.layer_norm_bwd_workspace(DTYPES[dtype], int(rows), int(channels)))
-    if r == 0:
-        raise ScnnError(-1, L.scnn_last_error().decode())
-    return r
+    return _need("layer_norm_bwd_workspace", DTYPES[dtype], int(rows), int(channels))
 
 
 def layer_norm_bwd(x, g, gamma, mean, rstd, *, want=(True, True, True), rows_dev=None, out=None, workspace=None,
@@ -684,9 +691,9 @@ def layer_norm_bwd(x, g, gamma, mean, rstd, *, want=(True, True, True), rows_dev
         dx = _result(dx, x, (rows, ch), "dx") if want[0] else None
         dgamma = _result(dgamma, x, (ch,), "dgamma") if want[1] else None
         dbeta = _result(dbeta, x, (ch,), "dbeta") if want[2] else None
-        workspace = _scratch(workspace, int(L.layer_norm_bwd_workspace(dt, rows, ch)), x)
+        workspace = _scratch(workspace, _need("layer_norm_bwd_workspace", dt, rows, ch), x)
         _check(L, L.layer_norm_bwd(dt, _at(x), _at(g), rows, _at(rows_dev), ch, _at(gamma), _at(mean), _at(rstd),
-                                   _at(dx), _at(dgamma), _at(dbeta), _at(workspace), workspace.numel(), torch.cuda.current_stream().cuda_stream))
+                                   _at(dx), _at(dgamma), _at(dbeta), _at(workspace), _bytes(workspace), _current()))
     return dx, dgamma, dbeta
 
 
@@ -732,8 +739,8 @@ def _grad_clip(grads, max_norm, outs, workspace, stream):
     with _on(dev, stream, (*grads, *(outs or ()), workspace)):
         result = torch.empty(2, dtype=torch.float64, device=dev)
         workspace = _scratch(workspace, int(L.grad_clip_workspace(n, counts)), like)
-        _check(L, L.grad_clip(n, src, dst, counts, types, float(max_norm), _at(result), _at(workspace), workspace.numel(),
-                              torch.cuda.current_stream().cuda_stream))
+        _check(L, L.grad_clip(n, src, dst, counts, types, float(max_norm), _at(result), _at(workspace), _bytes(workspace),
+                              _current()))
     return result
 
 

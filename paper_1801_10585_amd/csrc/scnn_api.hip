@@ -1113,6 +1113,7 @@ static int check_width(int64_t channels, const char* name) {
 static size_t dtype_size(int dtype) { return dtype == SCNN_F32 ? 4 : 2; }
 static bool element_aligned(int dtype, const void* p) { return ((uintptr_t)p & (dtype_size(dtype) - 1)) == 0; }
 static int check_workspace(const void* workspace, size_t bytes, size_t need) {
+    if (!workspace && need == 256) return SCNN_OK;  // (the least that a query answers: the call uses none)
     if (!workspace || ((uintptr_t)workspace & 255) != 0 || bytes < need)
         return fail(SCNN_EWORKSPACE, "workspace too small (%zu of %zu bytes) or misaligned", bytes, need);
     return SCNN_OK;
@@ -1146,7 +1147,7 @@ static int check_linear(int dtype, int64_t rows, int64_t c_in, int64_t c_out) {
 
 size_t linear_fwd_workspace(int dtype, int64_t rows, int64_t c_in, int64_t c_out) {
     if (check_linear(dtype, rows, c_in, c_out) != SCNN_OK) return 0;
-    return 256 + linear_fwd_part_bytes(rows, c_in, c_out);
+    return 256 + linear_fwd_part_bytes(dtype, rows, c_in, c_out);
 }
 
 int linear_fwd(int dtype, const void* x, int64_t rows, const int64_t* rows_dev, int64_t c_in, const void* w,

@@ -285,6 +285,161 @@ __global__ __launch_bounds__(64 * WM * WN) void k_linear_tile(LinearArgs p) {
     }
 }
 
+// Tiles of a launch in the order of its workgroups.  Workgroup i runs on XCD i % 8: each XCD takes one run of neighbouring
+// tiles, and within a run eight rows of tiles go side by side, so that the tiles that an L2 works on share their operands.
+__device__ __forceinline__ void tile_at(unsigned block, unsigned tiles_m, unsigned tiles_n, unsigned& tm, unsigned& tn) {
+    const unsigned all = tiles_m * tiles_n, each = all / kXcds, more = all % kXcds;
+    const unsigned xcd = block % kXcds, i = block / kXcds;
+    const unsigned at = xcd * each + (xcd < more ? xcd : more) + i;
+    constexpr unsigned kSide = 8;
+    const unsigned group = at / (kSide * tiles_n), in = at % (kSide * tiles_n);
+    const unsigned side = tiles_m - group * kSide < kSide ? tiles_m - group * kSide : kSide;
+    // (divisions leave the vector unit: the addresses that follow from these are to be scalar)
+    tm = (unsigned)__builtin_amdgcn_readfirstlane((int)(group * kSide + in % side));
+    tn = (unsigned)__builtin_amdgcn_readfirstlane((int)(in / side));
+}
+
+// Sixteen bytes a lane straight from memory to LDS: lane l's to lds + 16 l.
+__device__ __forceinline__ void copy_to_lds(const void* base, unsigned offset, unsigned lds) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(base) : "memory");
+}
+// Waits until at most N of this wave's copies are on their way and its LDS reads have arrived, then for the workgroup's
+// other waves.
+template <int N>
+__device__ __forceinline__ void copies_and_barrier() {
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+}
+
+// The same product for 16-bit operands whose rows begin on 16 bytes: tiles of BM x BN x BK go from memory to LDS without
+// passing through registers, into a ring of STAGES, so that a step's copies have two steps of products to arrive.  The
+// lanes' addresses carry the permutation of the pieces (staged), since the copy puts them down in the order of the lanes.
+// Rows and columns past the arrays' ends are read from the last one inside; what they add up to is not stored.  k past a
+// multiple of BK is staged through registers at the end, with zeros.
+template <typename T, bool AK, bool BK_, int BM, int BN, int BK, int WM, int WN, int STAGES>
+__global__ __launch_bounds__(64 * WM * WN) void k_linear_ring(LinearArgs p) {
+    constexpr int NT = 64 * WM * WN, AW = AK ? BK : BM, BW = BK_ ? BK : BN;
+    constexpr int A8 = BM * BK / 8, B8 = BN * BK / 8, AN = A8 / NT, BN8 = B8 / NT, SLOT = (A8 + B8) * 16;
+    constexpr int TM = BM / WM / 16, TN = BN / WN / 16, COPIES = AN + BN8;
+    static_assert(A8 % NT == 0 && B8 % NT == 0, "whole pieces a thread");
+    extern __shared__ __align__(1024) char s_ring[];
+    const long long rows = rows_of(p.rows_k ? p.k : p.m, p.rows_dev);
+    const long long m_end = p.rows_k ? p.m : rows, k_all = p.rows_k ? rows : p.k;
+    unsigned tile_m, tile_n;
+    tile_at(blockIdx.x, (unsigned)((p.m + BM - 1) / BM), (unsigned)((p.n + BN - 1) / BN), tile_m, tile_n);
+    const long long m0 = (long long)tile_m * BM, n0 = (long long)tile_n * BN;
+    if (m0 >= m_end) return;
+    const long long k_first = (long long)blockIdx.y * p.k_split;
+    const long long k_end = k_first + p.k_split < k_all ? k_first + p.k_split : k_all;
+    const int steps = k_end > k_first ? (int)((k_end - k_first) / BK) : 0;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wm = (wave / WN) * (TM * 16), wn = (wave % WN) * (TN * 16);
+    const unsigned ring = (unsigned)(size_t)(__attribute__((address_space(3))) char*)s_ring;
+
+    // This thread's pieces: byte offsets from the tile's first value at the step's first k.
+    auto offset_of = [&](bool k_contig, int w, int e, long long first, long long end, long long ld) -> unsigned {
+        const int r = e / (w / 8);
+        int c = e % (w / 8);
+        if (k_contig) {
+            c ^= w / 8 >= 8 ? (r & 7) : ((r >> 1) & 3);
+            const long long row = first + r < end ? r : end - 1 - first;
+            return (unsigned)((row * ld + c * 8) * 2);
+        }
+        c ^= (((r & 3) | ((r >> 1) & 4)) & (w / 16 - 1)) << 1;
+        const long long col = first + c * 8 < end ? c * 8 : end - 8 - first;  // (an array's width is a multiple of eight)
+        return (unsigned)((r * ld + col) * 2);
+    };
+    unsigned at_a[AN], at_b[BN8];
+#pragma unroll
+    for (int i = 0; i < AN; ++i) at_a[i] = offset_of(AK, AW, i * NT + tid, m0, AK ? m_end : p.m, AK ? p.k : p.m);
+#pragma unroll
+    for (int i = 0; i < BN8; ++i) at_b[i] = offset_of(BK_, BW, i * NT + tid, n0, p.n, BK_ ? p.k : p.n);
+    const char* base_a = (const char*)p.a + (AK ? m0 * p.k + k_first : k_first * p.m + m0) * 2;
+    const char* base_b = (const char*)p.b + (BK_ ? n0 * p.k + k_first : k_first * p.n + n0) * 2;
+    const long long next_a = (AK ? (long long)BK : BK * p.m) * 2, next_b = (BK_ ? (long long)BK : BK * p.n) * 2;
+    auto copy_step = [&](int slot) {
+        const unsigned to = ring + slot * SLOT + wave * 1024;
+#pragma unroll
+        for (int i = 0; i < AN; ++i) copy_to_lds(base_a, at_a[i], to + i * NT * 16);
+#pragma unroll
+        for (int i = 0; i < BN8; ++i) copy_to_lds(base_b, at_b[i], to + A8 * 16 + i * NT * 16);
+        base_a += next_a;
+        base_b += next_b;
+    };
+
+    f4 acc[TM][TN];
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j) acc[i][j] = f4{0.f, 0.f, 0.f, 0.f};
+    auto multiply = [&](const char* sa, const char* sb) {
+#pragma unroll
+        for (int kk = 0; kk < BK / 32; ++kk) {
+            u32x4 fa[TM], fb[TN];
+#pragma unroll
+            for (int j = 0; j < TN; ++j) fb[j] = fragment<BK_, BW>(sb, wn + j * 16, kk);
+#pragma unroll
+            for (int i = 0; i < TM; ++i) fa[i] = fragment<AK, AW>(sa, wm + i * 16, kk);
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+                for (int j = 0; j < TN; ++j) {
+                    if constexpr (std::is_same<T, __bf16>::value)
+                        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, fb[j]),
+                                                                            __builtin_bit_cast(bf16x8, fa[i]), acc[i][j], 0, 0, 0);
+                    else
+                        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, fb[j]),
+                                                                           __builtin_bit_cast(h8, fa[i]), acc[i][j], 0, 0, 0);
+                }
+        }
+    };
+    // STAGES - 1 steps are on their way before the first product.
+#pragma unroll
+    for (int i = 0; i < STAGES - 1; ++i)
+        if (i < steps) copy_step(i);
+    int slot = 0;
+    for (int step = 0; step < steps; ++step) {
+        // this step's copies have landed; its predecessor has been read by all waves, so that its slot can be filled
+        if (step + STAGES - 1 <= steps) copies_and_barrier<(STAGES - 2) * COPIES>();
+        else copies_and_barrier<0>();
+        if (step + STAGES - 1 < steps) copy_step(slot == 0 ? STAGES - 1 : slot - 1);
+        multiply(s_ring + slot * SLOT, s_ring + slot * SLOT + A8 * 16);
+        slot = slot == STAGES - 1 ? 0 : slot + 1;
+    }
+    const long long k_tail = k_first + (long long)steps * BK;
+    if (k_tail < k_end) {
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < AN; ++i) {
+            const int e = i * NT + tid, r = e / (AW / 8), c = e % (AW / 8);
+            const VecOf<T, 8> v = AK ? load8<T>((const T*)p.a, m0 + r, m_end, k_tail + c * 8, p.k)
+                                     : load8<T>((const T*)p.a, k_tail + r, k_end, m0 + c * 8, p.m);
+            *(u32x4*)(s_ring + staged<AK, AW>(r, c)) = __builtin_bit_cast(u32x4, v);
+        }
+#pragma unroll
+        for (int i = 0; i < BN8; ++i) {
+            const int e = i * NT + tid, r = e / (BW / 8), c = e % (BW / 8);
+            const VecOf<T, 8> v = BK_ ? load8<T>((const T*)p.b, n0 + r, p.n, k_tail + c * 8, p.k)
+                                      : load8<T>((const T*)p.b, k_tail + r, k_end, n0 + c * 8, p.n);
+            *(u32x4*)(s_ring + A8 * 16 + staged<BK_, BW>(r, c)) = __builtin_bit_cast(u32x4, v);
+        }
+        __syncthreads();
+        multiply(s_ring, s_ring + A8 * 16);
+    }
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+        const long long m = m0 + wm + i * 16 + (lane & 15);
+        if (m >= m_end) continue;
+#pragma unroll
+        for (int j = 0; j < TN; ++j) {
+            const long long n = n0 + wn + j * 16 + 4 * (lane >> 4);
+            if (n >= p.n) continue;
+            float z[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
+            if (p.part) __builtin_memcpy(p.part + ((long long)blockIdx.y * p.m + m) * p.n + n, z, 16);
+            else finish4<T>(p, m, n, z);
+        }
+    }
+}
+
 // Joins the partial sums of a split k and ends the call: four neighbouring columns a thread, TS threads a quad, each over
 // every TS-th split, their sums added in order.  (One thread a quad over 205 splits of a 35 x 19 filter: 92 us, each load
 // behind the one before; sixteen: 5.)
@@ -415,29 +570,46 @@ __global__ __launch_bounds__(256) void k_linear_few(LinearArgs p, int row0) {
 }
 
 // ------------------------------------------------------------------ host side
+// Kernel of a product: few rows, tiles staged through registers (any type, width and alignment), or tiles copied to LDS
+// (16-bit types, rows that begin on 16 bytes).
+enum class TileKind { kFew, kStaged, kRing128, kRing64x128, kRing64, kRing32 };
 struct TilePlan {
+    TileKind kind;
+    int bm, bn;
     int splits;
     long long k_split;
-    bool few;
 };
-constexpr int kTileM = 64, kTileN = 64;
 
 // The most k that one chain of 16-bit matrix instructions sums: the instruction cuts its sum off downwards at every step
 // of 32 k, half a last bit on average, so that 65536 k may leave 2^10 last bits of 2^-24, an eighth of a last bit of fp16.
 constexpr long long kChain = 65536;
 
-// k is split where the output has too few tiles to fill the card, and into chains of at most kChain.
-static TilePlan tile_plan(long long m, long long n, long long k, bool forward) {
-    TilePlan t = {1, round_up(k < 1 ? 1 : k, 64), false};
+// bf16, best of several launches, us, of 128 x 128 / 64 x 128 / 64 x 64 / 32 x 64 tiles:
+//   8192 x 4096 x 4096 (m, n, k)   268 / - / - / -          2048 x 2048 x 2048   29 / 24 / 29 / 37
+//   2048 x 2048 x 512             12.3 / 10.7 / 10.9 / 14   1024 x 1024 x 1024   18 / 12.6 / 8.0 / 7.6
+//   64 x 1024 x 12288             14.1 / 13.1 / 12.5 / 11.4   16 x 4096 x 4096   12.2 / 10.5 / 12.9 / 9.6
+//   200000 x 64 x 32                31 / 34 / 16 / 23       100000 x 128 x 128   18.4 / 19.4 / 16.1 / 22
+// Large tiles read their operands least and pay from two (one of 64 x 128) a compute unit on, with k to hide their start and end;
+// short tiles for few rows; else 64 x 64.  k is split where that leaves compute units without a tile: one workgroup a unit was
+// the fastest of 1, 2, 4 and 8 at 12 of 16 shapes, within 15 per cent of it at the others.
+static TilePlan tile_plan(long long m, long long n, long long k, bool forward, bool ring) {
+    TilePlan t = {TileKind::kStaged, 64, 64, 1, round_up(k < 1 ? 1 : k, 64)};
     if (m < 1) return t;
     if (forward && m <= 8) {
-        t.few = true;
+        t.kind = TileKind::kFew;
         return t;
     }
-    const long long tiles = ((m + kTileM - 1) / kTileM) * ((n + kTileN - 1) / kTileN);
-    const long long want = 2LL * device_cu_count();
-    if (tiles < want) {
-        long long s = want / tiles, most = (k + 255) / 256;
+    const long long cus = device_cu_count();
+    auto tiles = [&](long long bm, long long bn) { return ((m + bm - 1) / bm) * ((n + bn - 1) / bn); };
+    if (ring) {
+        if (k >= 512 && n > 64 && tiles(128, 128) >= 2 * cus) t.kind = TileKind::kRing128, t.bm = t.bn = 128;
+        else if (k >= 512 && n > 64 && tiles(64, 128) >= cus) t.kind = TileKind::kRing64x128, t.bn = 128;
+        else if (m <= 32) t.kind = TileKind::kRing32, t.bm = 32;
+        else t.kind = TileKind::kRing64;
+    }
+    const long long all = tiles(t.bm, t.bn), want = ring ? cus : 2 * cus;
+    if (all < want) {
+        long long s = want / all, most = (k + 255) / 256;
         if (s > most) s = most;
         if (s > 1) t.k_split = round_up((k + s - 1) / s, 64);
     }
@@ -447,24 +619,60 @@ static TilePlan tile_plan(long long m, long long n, long long k, bool forward) {
     return t;
 }
 
-static size_t part_bytes(const TilePlan& t, long long m, long long n) {
-    return t.splits > 1 ? (size_t)round_up((long long)t.splits * m * n * 4, 256) : 0;
+// Workspace of a product's partial sums: it must do for either way of staging, which the arrays' addresses decide.
+static size_t part_bytes(int dtype, long long m, long long n, long long k, bool forward) {
+    size_t most = 0;
+    for (int ring = 0; ring <= (dtype == SCNN_F32 ? 0 : 1); ++ring) {
+        const TilePlan t = tile_plan(m, n, k, forward, ring != 0);
+        const size_t b = t.splits > 1 ? (size_t)round_up((long long)t.splits * m * n * 4, 256) : 0;
+        if (b > most) most = b;
+    }
+    return most;
+}
+
+template <typename T, bool AK, bool BK_, int BM, int BN, int WM, int WN, int STAGES>
+static hipError_t ring(const LinearArgs& p, const TilePlan& t, hipStream_t s) {
+    constexpr int BK = 64, lds = (BM + BN) * BK * 2 * STAGES;
+    auto kernel = k_linear_ring<T, AK, BK_, BM, BN, BK, WM, WN, STAGES>;
+    if (lds >= 65536) {
+        const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+        if (e != hipSuccess) return e;
+    }
+    const dim3 grid((unsigned)(((p.m + BM - 1) / BM) * ((p.n + BN - 1) / BN)), (unsigned)t.splits);
+    hipLaunchKernelGGL(kernel, grid, dim3(64 * WM * WN), lds, s, p);
+    return hipGetLastError();
 }
 
 template <typename T, bool AK, bool BK_>
-static hipError_t product(LinearArgs p, const TilePlan& t, hipStream_t s) {
-    constexpr int BK = std::is_same<T, float>::value ? 32 : 64;
+static hipError_t product(LinearArgs p, bool forward, hipStream_t s) {
+    bool copies = false;
+    if constexpr (sizeof(T) == 2) {
+        // rows of both operands begin on 16 bytes, and a tile's rows lie within 32-bit offsets
+        const long long wa = AK ? p.k : p.m, wb = BK_ ? p.k : p.n;
+        copies = wa % 8 == 0 && wb % 8 == 0 && wa < (1 << 22) && wb < (1 << 22) && ((uintptr_t)p.a & 15) == 0 &&
+                 ((uintptr_t)p.b & 15) == 0 && p.n % 8 == 0;
+    }
+    const TilePlan t = tile_plan(p.m, p.n, p.k, forward, copies);
     p.k_split = t.k_split;
     if (t.splits <= 1) p.part = nullptr;
-    const dim3 grid((unsigned)(((p.n + kTileN - 1) / kTileN) * ((p.m + kTileM - 1) / kTileM)), (unsigned)t.splits);
-    hipLaunchKernelGGL((k_linear_tile<T, AK, BK_, kTileM, kTileN, BK, 2, 2>), grid, dim3(256), 0, s, p);
-    if (t.splits > 1) {
-        const long long quads = p.m * ((p.n + 3) / 4);
-        if (t.splits >= 8)
-            hipLaunchKernelGGL((k_linear_join<T, 16>), dim3((unsigned)((quads + 15) / 16)), dim3(256), 0, s, p, t.splits);
-        else
-            hipLaunchKernelGGL((k_linear_join<T, 4>), dim3((unsigned)((quads + 63) / 64)), dim3(256), 0, s, p, t.splits);
+    hipError_t e = hipSuccess;
+    if (t.kind == TileKind::kStaged) {
+        constexpr int BK = std::is_same<T, float>::value ? 32 : 64;
+        const dim3 grid((unsigned)(((p.n + 63) / 64) * ((p.m + 63) / 64)), (unsigned)t.splits);
+        hipLaunchKernelGGL((k_linear_tile<T, AK, BK_, 64, 64, BK, 2, 2>), grid, dim3(256), 0, s, p);
+        e = hipGetLastError();
+    } else if constexpr (sizeof(T) == 2) {
+        if (t.kind == TileKind::kRing128) e = ring<T, AK, BK_, 128, 128, 2, 2, 2>(p, t, s);
+        else if (t.kind == TileKind::kRing64x128) e = ring<T, AK, BK_, 64, 128, 2, 2, 3>(p, t, s);
+        else if (t.kind == TileKind::kRing64) e = ring<T, AK, BK_, 64, 64, 2, 2, 2>(p, t, s);
+        else e = ring<T, AK, BK_, 32, 64, 1, 4, 4>(p, t, s);
     }
+    if (e != hipSuccess || t.splits <= 1) return e;
+    const long long quads = p.m * ((p.n + 3) / 4);
+    if (t.splits >= 8)
+        hipLaunchKernelGGL((k_linear_join<T, 16>), dim3((unsigned)((quads + 15) / 16)), dim3(256), 0, s, p, t.splits);
+    else
+        hipLaunchKernelGGL((k_linear_join<T, 4>), dim3((unsigned)((quads + 63) / 64)), dim3(256), 0, s, p, t.splits);
     return hipGetLastError();
 }
 
@@ -477,8 +685,8 @@ static hipError_t few_rows(const LinearArgs& p, hipStream_t s) {
     return hipGetLastError();
 }
 
-size_t linear_fwd_part_bytes(long long rows, long long c_in, long long c_out) {
-    return part_bytes(tile_plan(rows, c_out, c_in, true), rows, c_out);
+size_t linear_fwd_part_bytes(int dtype, long long rows, long long c_in, long long c_out) {
+    return part_bytes(dtype, rows, c_out, c_in, true);
 }
 
 hipError_t launch_linear_fwd(int dtype, const LinearCall& c, hipStream_t s) {
@@ -490,11 +698,11 @@ hipError_t launch_linear_fwd(int dtype, const LinearCall& c, hipStream_t s) {
     p.bias = c.bias; p.residual = c.residual; p.out = c.out; p.pre = c.pre;
     p.part = (float*)c.workspace;
     p.act = c.act;
-    const TilePlan t = tile_plan(p.m, p.n, p.k, true);
+    const bool few = tile_plan(p.m, p.n, p.k, true, false).kind == TileKind::kFew;
     switch (dtype) {
-        case SCNN_F32: return t.few ? few_rows<float>(p, s) : product<float, true, false>(p, t, s);
-        case SCNN_BF16: return t.few ? few_rows<__bf16>(p, s) : product<__bf16, true, false>(p, t, s);
-        default: return t.few ? few_rows<_Float16>(p, s) : product<_Float16, true, false>(p, t, s);
+        case SCNN_F32: return few ? few_rows<float>(p, s) : product<float, true, false>(p, true, s);
+        case SCNN_BF16: return few ? few_rows<__bf16>(p, s) : product<__bf16, true, false>(p, true, s);
+        default: return few ? few_rows<_Float16>(p, s) : product<_Float16, true, false>(p, true, s);
     }
 }
 
@@ -522,8 +730,7 @@ static BackSpace back_space(int dtype, long long rows, long long c_in, long long
     b.sums = at;
     at += (size_t)round_up((long long)back_plan(rows, c_out, dtype).parts * c_out * 4, 256);
     b.dx = b.dw = at;  // (the two products run one after the other and share their partial sums' place)
-    const size_t dx = part_bytes(tile_plan(rows, c_in, c_out, false), rows, c_in);
-    const size_t dw = part_bytes(tile_plan(c_in, c_out, rows, false), c_in, c_out);
+    const size_t dx = part_bytes(dtype, rows, c_in, c_out, false), dw = part_bytes(dtype, c_in, c_out, rows, false);
     b.total = at + (dx > dw ? dx : dw);
     return b;
 }
@@ -557,7 +764,7 @@ static hipError_t linear_bwd_typed(int dtype, const LinearCall& c, hipStream_t s
         p.a = dz; p.b = c.w; p.out = c.dx;
         p.m = c.rows; p.n = c.c_in; p.k = c.c_out;
         p.part = (float*)(ws + at.dx);
-        const hipError_t e = product<T, true, true>(p, tile_plan(p.m, p.n, p.k, false), s);
+        const hipError_t e = product<T, true, true>(p, false, s);
         if (e != hipSuccess) return e;
     }
     if (c.dw) {
@@ -565,7 +772,7 @@ static hipError_t linear_bwd_typed(int dtype, const LinearCall& c, hipStream_t s
         p.m = c.c_in; p.n = c.c_out; p.k = c.rows;
         p.rows_k = 1;
         p.part = (float*)(ws + at.dw);
-        return product<T, false, false>(p, tile_plan(p.m, p.n, p.k, false), s);
+        return product<T, false, false>(p, false, s);
     }
     return hipGetLastError();
 }

@@ -55,6 +55,31 @@ def test_gradients_match_the_formula(k, size, dtype):
         assert [o is None for o in one] == [i != j for j in range(3)] and torch.equal(one[i], got[i])
 
 
+@pytest.mark.parametrize("dtype", ref.TYPES, ids=str)
+@pytest.mark.parametrize("size", [(16392, 520, 520), (2000, 600, 1032), (1030, 2904, 2904), (30, 2056, 1000), (4100, 130, 1160)], ids=str)
+def test_large_tiles(size, dtype):
+    """Sizes that take every tile of every product, with rows, columns and k that end inside a tile."""
+    d = make(7, *size, dtype)
+    out, pre = scnn.linear_fwd(d["x"], d["w"], d["bias"], act="gelu", residual=d["residual"], keep_pre=True)
+    want, want_pre = ref.linear_fwd(d["x"], d["w"], d["bias"], "gelu", d["residual"], dtype)
+    ref.assert_within(out, want, "out")
+    ref.assert_within(pre, want_pre, "pre")
+    got = scnn.linear_bwd(d["x"], d["w"], d["g"], act="gelu", pre=pre)
+    for what, a, b in zip(("dx", "dw", "dbias"), got, ref.linear_bwd(d["x"], d["w"], d["g"], "gelu", pre, dtype)):
+        ref.assert_within(a, b, what)
+    count = torch.tensor([size[0] - 13], dtype=torch.int64, device=DEV)
+    n = size[0] - 13
+    d["x"][n:] = float("nan")
+    d["g"][n:] = float("nan")
+    part = torch.full_like(out, 3.0)
+    scnn.linear_fwd(d["x"], d["w"], d["bias"], act="gelu", residual=d["residual"], rows_dev=count, out=part)
+    assert torch.equal(part[:n], out[:n]) and bool((part[n:] == 3).all())
+    few = scnn.linear_bwd(d["x"], d["w"], d["g"], act="gelu", pre=pre, rows_dev=count)
+    assert torch.equal(few[0][:n], got[0][:n])
+    for what, a, b in zip(("dw", "dbias"), few[1:], ref.linear_bwd(d["x"][:n], d["w"], d["g"][:n], "gelu", pre[:n], dtype)[1:]):
+        ref.assert_within(a, b, what)
+
+
 @pytest.mark.parametrize("size", [(6, 50, 40), (150, 70, 90), (64, 3000, 20), (1000, 8, 8)], ids=str)
 def test_whole_numbers_come_out_exactly(size):
     """Sums of small whole numbers are exact in fp32, whatever the order: every index is checked to the bit."""
@@ -214,6 +239,20 @@ def test_another_stream_and_two_at_once():
     for i, (a, b) in enumerate(got):
         assert torch.equal(a, want[i % 2])
         assert all(torch.equal(p, q) for p, q in zip(b, back[i % 2]))
+
+
+def test_captured_without_an_eager_run_before():
+    """The large tiles' shared memory is asked for by the call itself, in a capture too."""
+    d = make(43, 1000, 4096, 16640, torch.float16)
+    out = torch.empty((1000, 16640), dtype=torch.float16, device=DEV)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        scnn.linear_fwd(d["x"], d["w"], d["bias"], out=out)
+    for _ in range(3):
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, scnn.linear_fwd(d["x"], d["w"], d["bias"]))
 
 
 def test_captured_and_replayed():

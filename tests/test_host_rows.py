@@ -32,7 +32,9 @@ def test_linear_refusals():
         assert fwd(**{f"_{i}": None}) == -1
     for i in (1, 5, 6, 9, 10, 11):
         assert fwd(**{f"_{i}": P((30 << 20) + 2)}) == -1 and b"aligned" in L.scnn_last_error()
-    assert fwd(_13=8) == -3 and fwd(_12=P((7 << 20) + 8)) == -3 and fwd(_12=None) == -3
+    assert fwd(_13=8) == -3 and fwd(_12=P((7 << 20) + 8)) == -3
+    assert L.linear_fwd_workspace(0, 10, 1 << 14, 8) > 256  # (a split sum: needs its workspace)
+    assert fwd(_4=1 << 14, _5=P(32 << 20), _12=None) == -3
     for i in (1, 5, 6, 11):
         assert fwd(_10=good[i]) == -1 and b"overlap" in L.scnn_last_error()
     assert fwd(_10=P((4 << 20) + 4)) == -1          # beside the residual, not on it
