@@ -115,6 +115,48 @@ __device__ __forceinline__ void finish4(const LinearArgs& p, long long m, long l
     store4(p.out, z);
 }
 
+// The same for all of a wave's blocks, which lie inside the array: everything that is read is on its way before the first
+// value is written.  (A load behind every store, which may be to the same place, was a fifth of a wide layer's time.)
+template <typename T, int TM, int TN>
+__device__ __forceinline__ void finish_tile(const LinearArgs& p, long long m, long long n, const f4 (&acc)[TM][TN]) {
+    typedef VecOf<T, 4> V4;
+    V4 bias[TN], residual[TM][TN];
+#pragma unroll
+    for (int j = 0; j < TN; ++j) {
+        bias[j] = V4{};
+        if (p.bias) __builtin_memcpy(&bias[j], (const T*)p.bias + n + j * 16, sizeof(V4));
+    }
+    if (p.residual)
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int j = 0; j < TN; ++j)
+                __builtin_memcpy(&residual[i][j], (const T*)p.residual + (m + i * 16) * p.n + n + j * 16, sizeof(V4));
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j) {
+            const long long at = (m + i * 16) * p.n + n + j * 16;
+            f4 z = acc[i][j];
+            V4 r;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                if (p.bias) z[c] += (float)bias[j][c];
+                r[c] = (T)z[c];
+            }
+            if (p.pre) __builtin_memcpy((T*)p.pre + at, &r, sizeof(V4));
+            if (p.act != SCNN_ACT_NONE)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) z[c] = activate(z[c], p.act);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                if (p.residual) z[c] += (float)residual[i][j][c];
+                r[c] = (T)z[c];
+            }
+            __builtin_memcpy((T*)p.out + at, &r, sizeof(V4));
+        }
+}
+
 // Eight neighbouring values of a tile's row, 0 past the array's end.
 template <typename T>
 __device__ __forceinline__ VecOf<T, 8> load8(const T* __restrict__ base, long long row, long long rows, long long col, long long cols) {
@@ -379,6 +421,9 @@ __global__ __launch_bounds__(64 * WM * WN) void k_linear_ring(LinearArgs p) {
             for (int j = 0; j < TN; ++j) fb[j] = fragment<BK_, BW>(sb, wn + j * 16, kk);
 #pragma unroll
             for (int i = 0; i < TM; ++i) fa[i] = fragment<AK, AW>(sa, wm + i * 16, kk);
+            // (a wave that multiplies goes before the other workgroup's waves, which then fetch: 1063 -> 1189 TFLOP/s on
+            // 8192 x 4096 x 4096 with 128 x 128 tiles)
+            __builtin_amdgcn_s_setprio(1);
 #pragma unroll
             for (int i = 0; i < TM; ++i)
 #pragma unroll
@@ -390,6 +435,7 @@ __global__ __launch_bounds__(64 * WM * WN) void k_linear_ring(LinearArgs p) {
                         acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, fb[j]),
                                                                            __builtin_bit_cast(h8, fa[i]), acc[i][j], 0, 0, 0);
                 }
+            __builtin_amdgcn_s_setprio(0);
         }
     };
     // STAGES - 1 steps are on their way before the first product.
@@ -424,6 +470,10 @@ __global__ __launch_bounds__(64 * WM * WN) void k_linear_ring(LinearArgs p) {
         }
         __syncthreads();
         multiply(s_ring, s_ring + A8 * 16);
+    }
+    if (!p.part && m0 + BM <= m_end && n0 + BN <= p.n) {
+        finish_tile<T, TM, TN>(p, m0 + wm + (lane & 15), n0 + wn + 4 * (lane >> 4), acc);
+        return;
     }
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
@@ -572,7 +622,7 @@ __global__ __launch_bounds__(256) void k_linear_few(LinearArgs p, int row0) {
 // ------------------------------------------------------------------ host side
 // Kernel of a product: few rows, tiles staged through registers (any type, width and alignment), or tiles copied to LDS
 // (16-bit types, rows that begin on 16 bytes).
-enum class TileKind { kFew, kStaged, kRing128, kRing64x128, kRing64, kRing32 };
+enum class TileKind { kFew, kStaged, kRing256, kRing128, kRing64x128, kRing64, kRing32 };
 struct TilePlan {
     TileKind kind;
     int bm, bn;
@@ -585,10 +635,12 @@ struct TilePlan {
 constexpr long long kChain = 65536;
 
 // bf16, best of several launches, us, of 128 x 128 / 64 x 128 / 64 x 64 / 32 x 64 tiles:
-//   8192 x 4096 x 4096 (m, n, k)   268 / - / - / -          2048 x 2048 x 2048   29 / 24 / 29 / 37
+//   8192 x 4096 x 4096 (m, n, k)   231 / - / - / -          2048 x 2048 x 2048   29 / 24 / 29 / 37
 //   2048 x 2048 x 512             12.3 / 10.7 / 10.9 / 14   1024 x 1024 x 1024   18 / 12.6 / 8.0 / 7.6
 //   64 x 1024 x 12288             14.1 / 13.1 / 12.5 / 11.4   16 x 4096 x 4096   12.2 / 10.5 / 12.9 / 9.6
 //   200000 x 64 x 32                31 / 34 / 16 / 23       100000 x 128 x 128   18.4 / 19.4 / 16.1 / 22
+// and of 256 x 256 tiles: 8192 x 4096 x 4096 with gelu, residual and pre 281 against 313 (231 both without these), 4096 x
+// 4096 x 4096 x^T dz 142 against 124.
 // Large tiles read their operands least and pay from two (one of 64 x 128) a compute unit on, with k to hide their start and end;
 // short tiles for few rows; else 64 x 64.  k is split where that leaves compute units without a tile: one workgroup a unit was
 // the fastest of 1, 2, 4 and 8 at 12 of 16 shapes, within 15 per cent of it at the others.
@@ -602,7 +654,8 @@ static TilePlan tile_plan(long long m, long long n, long long k, bool forward, b
     const long long cus = device_cu_count();
     auto tiles = [&](long long bm, long long bn) { return ((m + bm - 1) / bm) * ((n + bn - 1) / bn); };
     if (ring) {
-        if (k >= 512 && n > 64 && tiles(128, 128) >= 2 * cus) t.kind = TileKind::kRing128, t.bm = t.bn = 128;
+        if (k >= 512 && tiles(256, 256) >= 2 * cus) t.kind = TileKind::kRing256, t.bm = t.bn = 256;
+        else if (k >= 512 && n > 64 && tiles(128, 128) >= 2 * cus) t.kind = TileKind::kRing128, t.bm = t.bn = 128;
         else if (k >= 512 && n > 64 && tiles(64, 128) >= cus) t.kind = TileKind::kRing64x128, t.bn = 128;
         else if (m <= 32) t.kind = TileKind::kRing32, t.bm = 32;
         else t.kind = TileKind::kRing64;
@@ -662,7 +715,8 @@ static hipError_t product(LinearArgs p, bool forward, hipStream_t s) {
         hipLaunchKernelGGL((k_linear_tile<T, AK, BK_, 64, 64, BK, 2, 2>), grid, dim3(256), 0, s, p);
         e = hipGetLastError();
     } else if constexpr (sizeof(T) == 2) {
-        if (t.kind == TileKind::kRing128) e = ring<T, AK, BK_, 128, 128, 2, 2, 2>(p, t, s);
+        if (t.kind == TileKind::kRing256) e = ring<T, AK, BK_, 256, 256, 2, 4, 2>(p, t, s);
+        else if (t.kind == TileKind::kRing128) e = ring<T, AK, BK_, 128, 128, 2, 2, 2>(p, t, s);
         else if (t.kind == TileKind::kRing64x128) e = ring<T, AK, BK_, 64, 128, 2, 2, 3>(p, t, s);
         else if (t.kind == TileKind::kRing64) e = ring<T, AK, BK_, 64, 64, 2, 2, 2>(p, t, s);
         else e = ring<T, AK, BK_, 32, 64, 1, 4, 4>(p, t, s);
