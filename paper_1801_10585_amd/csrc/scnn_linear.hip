@@ -67,6 +67,28 @@ struct LinearArgs {
     int rows_k;
 };
 
+// Eight fp32 values as three bf16 numbers each, to nearest (split8), and what these leave of them, if anything: `lost`
+// gathers the remainders' bits.  Nothing is left of 0 and of magnitudes from 2^-109 on, whose last bit is no smaller than
+// bf16's smallest number; infinities and NaN leave NaN.
+__device__ __forceinline__ void split8(const u32x4 (&x)[2], u32x4 (&part)[3], unsigned& lost) {
+    typedef float f32x2 __attribute__((ext_vector_type(2)));
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        f32x2 v;
+        v.x = __uint_as_float(x[i >> 1][(2 * i) & 3]);
+        v.y = __uint_as_float(x[i >> 1][(2 * i + 1) & 3]);
+#pragma unroll
+        for (int k = 0; k < 3; ++k) {
+            const unsigned p = __builtin_bit_cast(unsigned, __builtin_convertvector(v, bf16x2));
+            part[k][i] = p;
+            v.x -= __uint_as_float(p << 16);
+            v.y -= __uint_as_float(p & 0xffff0000u);
+        }
+        lost |= __float_as_uint(v.x) | __float_as_uint(v.y);
+    }
+}
+
 // Epilogue of four neighbouring columns: bias, activation, residual.
 template <typename T>
 __device__ __forceinline__ void finish4(const LinearArgs& p, long long m, long long n, float (&z)[4]) {
@@ -174,18 +196,20 @@ __device__ __forceinline__ VecOf<T, 8> load8(const T* __restrict__ base, long lo
     return v;
 }
 
-// BM x BN outputs a workgroup of WM x WN waves, BK values of k a step.  The operands swap places at the instruction: its
-// rows are the tile's columns n, so that a lane ends with four neighbouring n of one m (16 or 8 bytes a store).
-template <typename T, bool AK, bool BK_, int BM, int BN, int BK, int WM, int WN>
-__global__ __launch_bounds__(64 * WM * WN) void k_linear_tile(LinearArgs p) {
+// BM x BN outputs a workgroup, BK values of k a step.  KG groups of WM x WN waves take the steps in turn, each with a staging
+// area of its own, and join their sums at the end: waves enough to hide the latencies of short products without as many
+// partial sums in memory.  The operands swap places at the instruction: its rows are the tile's columns n, so that a lane
+// ends with four neighbouring n of one m (16 or 8 bytes a store).
+template <typename T, bool AK, bool BK_, int BM, int BN, int BK, int WM, int WN, int KG>
+__global__ __launch_bounds__(64 * WM * WN * KG) void k_linear_tile(LinearArgs p) {
     constexpr bool SPLIT = std::is_same<T, float>::value;
     constexpr int PARTS = SPLIT ? 3 : 1, NT = 64 * WM * WN;
     constexpr int AW = AK ? BK : BM, BW = BK_ ? BK : BN;          // values of a staged row
     constexpr int A8 = BM * BK / 8, B8 = BN * BK / 8;             // pieces of eight values
-    constexpr int AN = (A8 + NT - 1) / NT, BN8 = (B8 + NT - 1) / NT;
+    constexpr int AN = (A8 + NT - 1) / NT, BN8 = (B8 + NT - 1) / NT, AREA = PARTS * (A8 + B8) * 16;
     constexpr int TM = BM / WM / 16, TN = BN / WN / 16;
-    __shared__ __align__(16) char s_a[PARTS * A8 * 16];
-    __shared__ __align__(16) char s_b[PARTS * B8 * 16];
+    constexpr int JOIN = (KG - 1) * NT * TM * TN * 16;            // bytes in which the groups' sums meet
+    __shared__ __align__(16) char s_stage[KG * AREA > JOIN ? KG * AREA : JOIN];
     const long long rows = rows_of(p.rows_k ? p.k : p.m, p.rows_dev);
     const long long m_end = p.rows_k ? p.m : rows, k_all = p.rows_k ? rows : p.k;
     const unsigned tiles_n = (unsigned)((p.n + BN - 1) / BN);
@@ -193,8 +217,10 @@ __global__ __launch_bounds__(64 * WM * WN) void k_linear_tile(LinearArgs p) {
     if (m0 >= m_end) return;
     const long long k_first = (long long)blockIdx.y * p.k_split;
     const long long k_end = k_first + p.k_split < k_all ? k_first + p.k_split : k_all;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int group = KG == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / NT);
+    const int tid = threadIdx.x - group * NT, lane = tid & 63, wave = tid >> 6;
     const int wm = (wave / WN) * (TM * 16), wn = (wave % WN) * (TN * 16);
+    char *const s_a = s_stage + group * AREA, *const s_b = s_a + PARTS * A8 * 16;
 
     f4 acc[TM][TN];
 #pragma unroll
@@ -202,38 +228,58 @@ __global__ __launch_bounds__(64 * WM * WN) void k_linear_tile(LinearArgs p) {
 #pragma unroll
         for (int j = 0; j < TN; ++j) acc[i][j] = f4{0.f, 0.f, 0.f, 0.f};
 
+    // A tile that lies inside the arrays reads its pieces at 32-bit offsets from its first value, which moves on with k; the
+    // others, and the last step of a k that ends inside it, ask for every piece where it lies.  (A multiplication of 64 bits
+    // and four comparisons a piece cost as much as splitting its eight values.)
     VecOf<T, 8> ra[AN], rb[BN8];
+    const long long wide_a = AK ? p.k : p.m, wide_b = BK_ ? p.k : p.n;
+    const bool inside = m0 + BM <= m_end && n0 + BN <= p.n && A8 % NT == 0 && B8 % NT == 0 && wide_a < (1 << 22) && wide_b < (1 << 22);
+    unsigned at_a[AN], at_b[BN8];
+#pragma unroll
+    for (int i = 0; i < AN; ++i) at_a[i] = (unsigned)((i * NT + tid) / (AW / 8)) * (unsigned)wide_a + (i * NT + tid) % (AW / 8) * 8;
+#pragma unroll
+    for (int i = 0; i < BN8; ++i) at_b[i] = (unsigned)((i * NT + tid) / (BW / 8)) * (unsigned)wide_b + (i * NT + tid) % (BW / 8) * 8;
     auto fetch = [&](long long k) {
+        if (inside && k + BK <= k_end) {
+            const T* __restrict__ pa = (const T*)p.a + (AK ? m0 * p.k + k : k * p.m + m0);
+            const T* __restrict__ pb = (const T*)p.b + (BK_ ? n0 * p.k + k : k * p.n + n0);
+#pragma unroll
+            for (int i = 0; i < AN; ++i) __builtin_memcpy(&ra[i], pa + at_a[i], sizeof(ra[i]));
+#pragma unroll
+            for (int i = 0; i < BN8; ++i) __builtin_memcpy(&rb[i], pb + at_b[i], sizeof(rb[i]));
+            return;
+        }
+        const bool any = k < k_end;  // (a group whose turn does not come stages zeros)
 #pragma unroll
         for (int i = 0; i < AN; ++i) {
             const int e = i * NT + tid, r = e / (AW / 8), c = e % (AW / 8) * 8;
             if (A8 % NT == 0 || e < A8)
-                ra[i] = AK ? load8<T>((const T*)p.a, m0 + r, m_end, k + c, p.k)
+                ra[i] = AK ? load8<T>((const T*)p.a, m0 + r, any ? m_end : 0, k + c, p.k)
                            : load8<T>((const T*)p.a, k + r, k_end, m0 + c, p.m);
         }
 #pragma unroll
         for (int i = 0; i < BN8; ++i) {
             const int e = i * NT + tid, r = e / (BW / 8), c = e % (BW / 8) * 8;
             if (B8 % NT == 0 || e < B8)
-                rb[i] = BK_ ? load8<T>((const T*)p.b, n0 + r, p.n, k + c, p.k)
+                rb[i] = BK_ ? load8<T>((const T*)p.b, n0 + r, any ? p.n : 0, k + c, p.k)
                             : load8<T>((const T*)p.b, k + r, k_end, n0 + c, p.n);
         }
     };
-    int odd = 0;
+    unsigned lost = 0;  // bits of what the three parts of some value leave of it
     auto put = [&](char* tile, int pieces, int at, const VecOf<T, 8>& v) {
         if constexpr (SPLIT) {
             u32x4 x[2], part[3];
             __builtin_memcpy(x, &v, 32);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) odd |= split_exact(x[i >> 2][i & 3]) ? 0 : 1;
-            split8(x, part);
+            split8(x, part, lost);
 #pragma unroll
             for (int q = 0; q < 3; ++q) *(u32x4*)(tile + q * pieces * 16 + at) = part[q];
         } else {
             *(u32x4*)(tile + at) = __builtin_bit_cast(u32x4, v);
         }
     };
-    auto stage = [&]() {
+    fetch(k_first + group * BK);
+    for (long long k0 = k_first; k0 < k_end; k0 += KG * BK) {
+        __syncthreads();
 #pragma unroll
         for (int i = 0; i < AN; ++i) {
             const int e = i * NT + tid;
@@ -244,13 +290,8 @@ __global__ __launch_bounds__(64 * WM * WN) void k_linear_tile(LinearArgs p) {
             const int e = i * NT + tid;
             if (B8 % NT == 0 || e < B8) put(s_b, B8, staged<BK_, BW>(e / (BW / 8), e % (BW / 8)), rb[i]);
         }
-    };
-    fetch(k_first);
-    for (long long k = k_first; k < k_end; k += BK) {
         __syncthreads();
-        stage();
-        __syncthreads();
-        if (k + BK < k_end) fetch(k + BK);
+        if (k0 + KG * BK < k_end) fetch(k0 + (KG + group) * BK);
 #pragma unroll
         for (int kk = 0; kk < BK / 32; ++kk) {
             u32x4 fa[TM][PARTS];
@@ -281,8 +322,16 @@ __global__ __launch_bounds__(64 * WM * WN) void k_linear_tile(LinearArgs p) {
         }
     }
     if constexpr (SPLIT) {
-        // A value that the parts do not hold (infinities, NaN, magnitudes below 2^-109 or from 2^58 up) was among this
-        // workgroup's: its outputs are summed anew with fp32 products.
+        // Values that the parts do not hold: too small ones leave something (lost), infinities and NaN, and magnitudes whose
+        // products overflow though their sums might not, leave no finite sum.  A workgroup that met any sums its outputs
+        // anew with fp32 products, the groups one k in KG of each four.
+        bool odd = lost != 0;
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int j = 0; j < TN; ++j)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) odd |= (__float_as_uint(acc[i][j][c]) & 0x7f800000u) == 0x7f800000u;
         if (__syncthreads_or(odd)) {
             const int q = lane >> 4, i16 = lane & 15;
             auto at_a = [&](long long m, long long k) {
@@ -295,7 +344,7 @@ __global__ __launch_bounds__(64 * WM * WN) void k_linear_tile(LinearArgs p) {
             for (int i = 0; i < TM; ++i)
 #pragma unroll
                 for (int j = 0; j < TN; ++j) acc[i][j] = f4{0.f, 0.f, 0.f, 0.f};
-            for (long long k = k_first; k < k_end; k += 4)
+            for (long long k = k_first + 4 * group; k < k_end; k += 4 * KG)
 #pragma unroll
                 for (int i = 0; i < TM; ++i) {
                     const float va = at_a(m0 + wm + i * 16 + i16, k + q);
@@ -304,6 +353,23 @@ __global__ __launch_bounds__(64 * WM * WN) void k_linear_tile(LinearArgs p) {
                         acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(at_b(n0 + wn + j * 16 + i16, k + q), va, acc[i][j], 0, 0, 0);
                 }
         }
+    }
+    if constexpr (KG > 1) {
+        __syncthreads();
+        f4* const s_join = (f4*)s_stage;
+        if (group > 0)
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+                for (int j = 0; j < TN; ++j) s_join[(((group - 1) * TM + i) * TN + j) * NT + tid] = acc[i][j];
+        __syncthreads();
+        if (group > 0) return;
+#pragma unroll
+        for (int g = 0; g < KG - 1; ++g)
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+                for (int j = 0; j < TN; ++j) acc[i][j] += s_join[((g * TM + i) * TN + j) * NT + tid];
     }
     // lane: row m = lane % 16, columns n = 4 (lane / 16) .. + 3 of each block
 #pragma unroll
@@ -622,7 +688,7 @@ __global__ __launch_bounds__(256) void k_linear_few(LinearArgs p, int row0) {
 // ------------------------------------------------------------------ host side
 // Kernel of a product: few rows, tiles staged through registers (any type, width and alignment), or tiles copied to LDS
 // (16-bit types, rows that begin on 16 bytes).
-enum class TileKind { kFew, kStaged, kRing256, kRing128, kRing64x128, kRing64, kRing32 };
+enum class TileKind { kFew, kStaged, kStagedGroups, kStaged128, kRing256, kRing128, kRing64x128, kRing64, kRing32 };
 struct TilePlan {
     TileKind kind;
     int bm, bn;
@@ -660,7 +726,14 @@ static TilePlan tile_plan(long long m, long long n, long long k, bool forward, b
         else if (m <= 32) t.kind = TileKind::kRing32, t.bm = 32;
         else t.kind = TileKind::kRing64;
     }
-    const long long all = tiles(t.bm, t.bn), want = ring ? cus : 2 * cus;
+    // fp32, us, of 128 x 128 / 64 x 64 / 64 x 64 by four groups of waves, the last with a workgroup a compute unit:
+    //   4096 x 4096 x 4096   756 / 928 / 1080 (the library's product 960)   100000 x 128 x 128   39 / 35 / 79
+    //   1024 x 1024 x 1024    36 / 31 / 22.5    64 x 1024 x 12288    36 / 26 / 24.3    32 x 64 x 200000 (x^T dz)   69 / 32 / 28
+    if (!ring) {
+        if (k >= 512 && m > 64 && n > 64 && tiles(128, 128) >= 2 * cus) t.kind = TileKind::kStaged128, t.bm = t.bn = 128;
+        else if (k >= 256 && tiles(64, 64) < 2 * cus) t.kind = TileKind::kStagedGroups;
+    }
+    const long long all = tiles(t.bm, t.bn), want = cus;
     if (all < want) {
         long long s = want / all, most = (k + 255) / 256;
         if (s > most) s = most;
@@ -684,14 +757,13 @@ static size_t part_bytes(int dtype, long long m, long long n, long long k, bool 
 }
 
 template <typename T, bool AK, bool BK_, int BM, int BN, int WM, int WN, int STAGES>
-static hipError_t ring(const LinearArgs& p, const TilePlan& t, hipStream_t s) {
+static hipError_t ring(const LinearArgs& p, dim3 grid, hipStream_t s) {
     constexpr int BK = 64, lds = (BM + BN) * BK * 2 * STAGES;
     auto kernel = k_linear_ring<T, AK, BK_, BM, BN, BK, WM, WN, STAGES>;
     if (lds >= 65536) {
         const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
         if (e != hipSuccess) return e;
     }
-    const dim3 grid((unsigned)(((p.m + BM - 1) / BM) * ((p.n + BN - 1) / BN)), (unsigned)t.splits);
     hipLaunchKernelGGL(kernel, grid, dim3(64 * WM * WN), lds, s, p);
     return hipGetLastError();
 }
@@ -709,17 +781,23 @@ static hipError_t product(LinearArgs p, bool forward, hipStream_t s) {
     p.k_split = t.k_split;
     if (t.splits <= 1) p.part = nullptr;
     hipError_t e = hipSuccess;
+    constexpr int BK = std::is_same<T, float>::value ? 32 : 64;
+    const dim3 grid((unsigned)(((p.n + t.bn - 1) / t.bn) * ((p.m + t.bm - 1) / t.bm)), (unsigned)t.splits);
     if (t.kind == TileKind::kStaged) {
-        constexpr int BK = std::is_same<T, float>::value ? 32 : 64;
-        const dim3 grid((unsigned)(((p.n + 63) / 64) * ((p.m + 63) / 64)), (unsigned)t.splits);
-        hipLaunchKernelGGL((k_linear_tile<T, AK, BK_, 64, 64, BK, 2, 2>), grid, dim3(256), 0, s, p);
+        hipLaunchKernelGGL((k_linear_tile<T, AK, BK_, 64, 64, BK, 2, 2, 1>), grid, dim3(256), 0, s, p);
+        e = hipGetLastError();
+    } else if (t.kind == TileKind::kStagedGroups) {
+        hipLaunchKernelGGL((k_linear_tile<T, AK, BK_, 64, 64, BK, 2, 2, 4>), grid, dim3(1024), 0, s, p);
+        e = hipGetLastError();
+    } else if (t.kind == TileKind::kStaged128) {
+        hipLaunchKernelGGL((k_linear_tile<T, AK, BK_, 128, 128, BK, 2, 2, 1>), grid, dim3(256), 0, s, p);
         e = hipGetLastError();
     } else if constexpr (sizeof(T) == 2) {
-        if (t.kind == TileKind::kRing256) e = ring<T, AK, BK_, 256, 256, 2, 4, 2>(p, t, s);
-        else if (t.kind == TileKind::kRing128) e = ring<T, AK, BK_, 128, 128, 2, 2, 2>(p, t, s);
-        else if (t.kind == TileKind::kRing64x128) e = ring<T, AK, BK_, 64, 128, 2, 2, 3>(p, t, s);
-        else if (t.kind == TileKind::kRing64) e = ring<T, AK, BK_, 64, 64, 2, 2, 2>(p, t, s);
-        else e = ring<T, AK, BK_, 32, 64, 1, 4, 4>(p, t, s);
+        if (t.kind == TileKind::kRing256) e = ring<T, AK, BK_, 256, 256, 2, 4, 2>(p, grid, s);
+        else if (t.kind == TileKind::kRing128) e = ring<T, AK, BK_, 128, 128, 2, 2, 2>(p, grid, s);
+        else if (t.kind == TileKind::kRing64x128) e = ring<T, AK, BK_, 64, 128, 2, 2, 3>(p, grid, s);
+        else if (t.kind == TileKind::kRing64) e = ring<T, AK, BK_, 64, 64, 2, 2, 2>(p, grid, s);
+        else e = ring<T, AK, BK_, 32, 64, 1, 4, 4>(p, grid, s);
     }
     if (e != hipSuccess || t.splits <= 1) return e;
     const long long quads = p.m * ((p.n + 3) / 4);
