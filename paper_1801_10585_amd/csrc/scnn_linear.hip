@@ -637,6 +637,241 @@ __global__ __launch_bounds__(256) void k_act_back(const T* __restrict__ g, const
     }
 }
 
+// Gradients of a narrow layer in one pass over its rows: bound by reading x, g and pre and writing dx once.  A workgroup
+// keeps w in LDS and takes 64 rows at a time, the next ones on their way to registers meanwhile: dz = g act'(pre) is formed
+// once, staged next to x, and read by both products, dx = dz w^T with its channels contiguous, dw += x^T dz by transposing
+// reads; dw stays in the accumulators and the column sums of dz in registers until the workgroup's rows are done.  part
+// [gridDim.x][c_in * c_out + c_out] then receives both, and one launch adds the workgroups' up.  P: widths up to P.
+template <int P> struct NarrowShape;  // waves of dx (64 x P) and of dw (P x P): rows by columns of waves
+template <> struct NarrowShape<32> { static constexpr int XM = 4, XN = 1, WM = 2, WN = 2; };
+template <> struct NarrowShape<64> { static constexpr int XM = 2, XN = 2, WM = 2, WN = 2; };
+template <> struct NarrowShape<128> { static constexpr int XM = 2, XN = 2, WM = 2, WN = 2; };
+
+struct NarrowArgs {
+    const void *x, *w, *pre, *g;
+    void* dx;
+    float* part;
+    long long rows;
+    const long long* rows_dev;
+    int c_in, c_out, act;
+};
+
+template <typename T, int P>
+__global__ __launch_bounds__(256) void k_linear_bwd_narrow(NarrowArgs p) {
+    constexpr bool SPLIT = std::is_same<T, float>::value;
+    constexpr int PARTS = SPLIT ? 3 : 1, ROWS = 64, CH = P / 8;
+    constexpr int PIECES = ROWS * CH, PN = PIECES / 256, WPIECES = P * CH, WPN = (WPIECES + 255) / 256;
+    typedef NarrowShape<P> S;
+    constexpr int XM = ROWS / S::XM / 16, XN = P / S::XN / 16, WM = P / S::WM / 16, WN = P / S::WN / 16;
+    __shared__ __align__(16) char s_w[PARTS * WPIECES * 16], s_z[2 * PARTS * PIECES * 16];
+    char* const s_x = s_z + PARTS * PIECES * 16;
+    const long long rows = rows_of(p.rows, p.rows_dev);
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const T *const x = (const T*)p.x, *const w = (const T*)p.w, *const pre = (const T*)p.pre, *const g = (const T*)p.g;
+    const int c8 = tid % CH * 8;  // first column of this thread's pieces
+
+    auto put = [&](char* tile, int pieces, int at, const VecOf<T, 8>& v, int& odd) {
+        if constexpr (SPLIT) {
+            u32x4 q[2], part[3];
+            __builtin_memcpy(q, &v, 32);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) odd |= split_exact(q[i >> 2][i & 3]) ? 0 : 1;
+            scnn::split8(q, part);
+#pragma unroll
+            for (int k = 0; k < 3; ++k) *(u32x4*)(tile + k * pieces * 16 + at) = part[k];
+        } else {
+            *(u32x4*)(tile + at) = __builtin_bit_cast(u32x4, v);
+        }
+    };
+    // w [c_in][c_out]: the contraction of dx runs along its rows
+    int odd_w = 0;
+#pragma unroll
+    for (int i = 0; i < WPN; ++i) {
+        const int e = i * 256 + tid;
+        if (WPIECES % 256 == 0 || e < WPIECES)
+            put(s_w, WPIECES, staged<true, P>(e / CH, e % CH), load8<T>(w, e / CH, p.dx ? p.c_in : 0, e % CH * 8, p.c_out), odd_w);
+    }
+    VecOf<T, 8> rx[PN], rg[PN], rp[PN];
+    auto fetch = [&](long long first) {
+#pragma unroll
+        for (int i = 0; i < PN; ++i) {
+            const long long row = first + (i * 256 + tid) / CH;
+            rg[i] = load8<T>(g, row, rows, c8, p.c_out);
+            if (p.act != SCNN_ACT_NONE) rp[i] = load8<T>(pre, row, rows, c8, p.c_out);
+            rx[i] = load8<T>(x, p.part ? row : rows, rows, c8, p.c_in);
+        }
+    };
+    f4 dw[WM][WN];
+#pragma unroll
+    for (int i = 0; i < WM; ++i)
+#pragma unroll
+        for (int j = 0; j < WN; ++j) dw[i][j] = f4{0.f, 0.f, 0.f, 0.f};
+    float db[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) db[i] = 0.0f;
+    auto multiply = [&](const u32x4 (&a)[PARTS], const u32x4 (&b)[PARTS], f4 acc) {  // (b's rows become the lanes' rows)
+        if constexpr (SPLIT) {
+            f4 large, small;
+            split_products(a, b[0], b[1], b[2], large, small);
+            return acc + (large + small);
+        } else if constexpr (std::is_same<T, __bf16>::value) {
+            return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a[0]), __builtin_bit_cast(bf16x8, b[0]), acc, 0, 0, 0);
+        } else {
+            return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, a[0]), __builtin_bit_cast(h8, b[0]), acc, 0, 0, 0);
+        }
+    };
+    const long long step = (long long)gridDim.x * ROWS;
+    const int xm = wave / S::XN * XM * 16, xn = wave % S::XN * XN * 16, wm = wave / S::WN * WM * 16, wn = wave % S::WN * WN * 16;
+    long long first = (long long)blockIdx.x * ROWS;
+    if (first < rows) fetch(first);
+    for (; first < rows; first += step) {
+        int odd = odd_w;
+        if (first != (long long)blockIdx.x * ROWS) __syncthreads();  // (the tiles before these have been read)
+#pragma unroll
+        for (int i = 0; i < PN; ++i) {
+            const int r = (i * 256 + tid) / CH;
+            VecOf<T, 8> z = rg[i];
+#pragma unroll
+            for (int c = 0; c < 8; ++c) {
+                float v = (float)rg[i][c];
+                if (p.act != SCNN_ACT_NONE) {
+                    v = first + r < rows && c8 + c < p.c_out ? activate_back(v, (float)rp[i][c], p.act) : 0.0f;
+                    z[c] = (T)v;
+                }
+                db[c] += v;
+            }
+            put(s_z, PIECES, staged<false, P>(r, tid % CH), z, odd);
+            if (p.part) put(s_x, PIECES, staged<false, P>(r, tid % CH), rx[i], odd);
+        }
+        bool exact = true;
+        if constexpr (SPLIT) exact = !__syncthreads_or(odd);
+        else __syncthreads();
+        if (first + step < rows) fetch(first + step);
+        // dz [64][c_out], rows of dz one way and columns the other
+        auto rows_of_z = [&](int base, int kk, u32x4 (&f)[PARTS]) {
+            const int r = base + (lane & 15);
+#pragma unroll
+            for (int q = 0; q < PARTS; ++q) f[q] = *(const u32x4*)(s_z + q * PIECES * 16 + staged<false, P>(r, kk * 4 + (lane >> 4)));
+        };
+        f4 dx[XM][XN];
+#pragma unroll
+        for (int i = 0; i < XM; ++i)
+#pragma unroll
+            for (int j = 0; j < XN; ++j) dx[i][j] = f4{0.f, 0.f, 0.f, 0.f};
+        if (exact) {
+            if (p.dx)
+#pragma unroll
+                for (int kk = 0; kk < P / 32; ++kk) {
+                    u32x4 fz[XM][PARTS];
+#pragma unroll
+                    for (int i = 0; i < XM; ++i) rows_of_z(xm + i * 16, kk, fz[i]);
+#pragma unroll
+                    for (int j = 0; j < XN; ++j) {
+                        u32x4 fw[PARTS];
+#pragma unroll
+                        for (int q = 0; q < PARTS; ++q) fw[q] = fragment<true, P>(s_w + q * WPIECES * 16, xn + j * 16, kk);
+#pragma unroll
+                        for (int i = 0; i < XM; ++i) dx[i][j] = multiply(fw, fz[i], dx[i][j]);
+                    }
+                }
+            if (p.part)
+#pragma unroll
+                for (int kk = 0; kk < ROWS / 32; ++kk) {
+                    u32x4 fx[WM][PARTS];
+#pragma unroll
+                    for (int i = 0; i < WM; ++i)
+#pragma unroll
+                        for (int q = 0; q < PARTS; ++q) fx[i][q] = fragment<false, P>(s_x + q * PIECES * 16, wm + i * 16, kk);
+#pragma unroll
+                    for (int j = 0; j < WN; ++j) {
+                        u32x4 fz[PARTS];
+#pragma unroll
+                        for (int q = 0; q < PARTS; ++q) fz[q] = fragment<false, P>(s_z + q * PIECES * 16, wn + j * 16, kk);
+#pragma unroll
+                        for (int i = 0; i < WM; ++i) dw[i][j] = multiply(fz, fx[i], dw[i][j]);
+                    }
+                }
+        } else if constexpr (SPLIT) {
+            // a value among these rows or in w that the three parts do not hold: fp32 products, operands from memory
+            const int q = lane >> 4, i16 = lane & 15;
+            auto z_at = [&](long long row, int n) {
+                if (row >= rows || n >= p.c_out) return 0.0f;
+                const float v = (float)g[row * p.c_out + n];
+                return p.act != SCNN_ACT_NONE ? activate_back(v, (float)pre[row * p.c_out + n], p.act) : v;
+            };
+            if (p.dx)
+                for (int k = 0; k < p.c_out; k += 4)
+#pragma unroll
+                    for (int i = 0; i < XM; ++i) {
+                        const float vz = z_at(first + xm + i * 16 + i16, k + q);
+#pragma unroll
+                        for (int j = 0; j < XN; ++j) {
+                            const int n = xn + j * 16 + i16;
+                            const float vw = n < p.c_in && k + q < p.c_out ? (float)w[n * p.c_out + k + q] : 0.0f;
+                            dx[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(vw, vz, dx[i][j], 0, 0, 0);
+                        }
+                    }
+            if (p.part)
+                for (int k = 0; k < ROWS; k += 4)
+#pragma unroll
+                    for (int i = 0; i < WM; ++i) {
+                        const int m = wm + i * 16 + i16;
+                        const float vx = first + k + q < rows && m < p.c_in ? (float)x[(first + k + q) * p.c_in + m] : 0.0f;
+#pragma unroll
+                        for (int j = 0; j < WN; ++j)
+                            dw[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(z_at(first + k + q, wn + j * 16 + i16), vx, dw[i][j], 0, 0, 0);
+                    }
+        }
+        if (p.dx)
+#pragma unroll
+            for (int i = 0; i < XM; ++i) {
+                const long long row = first + xm + i * 16 + (lane & 15);
+                if (row >= rows) continue;
+#pragma unroll
+                for (int j = 0; j < XN; ++j) {
+                    const int n = xn + j * 16 + 4 * (lane >> 4);
+                    T* __restrict__ to = (T*)p.dx + row * p.c_in + n;
+                    if (n + 4 <= p.c_in) {
+                        VecOf<T, 4> v;
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) v[c] = (T)dx[i][j][c];
+                        __builtin_memcpy(to, &v, sizeof(v));
+                    } else {
+#pragma unroll
+                        for (int c = 0; c < 4; ++c)
+                            if (n + c < p.c_in) to[c] = (T)dx[i][j][c];
+                    }
+                }
+            }
+    }
+    if (!p.part) return;
+    float* __restrict__ mine = p.part + (long long)blockIdx.x * ((long long)p.c_in * p.c_out + p.c_out);
+#pragma unroll
+    for (int i = 0; i < WM; ++i) {
+        const int m = wm + i * 16 + (lane & 15);
+        if (m >= p.c_in) continue;
+#pragma unroll
+        for (int j = 0; j < WN; ++j) {
+            const int n = wn + j * 16 + 4 * (lane >> 4);
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+                if (n + c < p.c_out) mine[m * p.c_out + n + c] = dw[i][j][c];
+        }
+    }
+    // column sums: threads with the same columns lie CH apart
+    __syncthreads();
+    float(*s_db)[P] = (float(*)[P])s_z;
+    static_assert(256 / CH * P * 4 <= 2 * PARTS * PIECES * 16, "room for the column sums");
+#pragma unroll
+    for (int c = 0; c < 8; ++c) s_db[tid / CH][c8 + c] = db[c];
+    __syncthreads();
+    if (tid < p.c_out) {
+        float sum = 0.0f;
+        for (int r = 0; r < 256 / CH; ++r) sum += s_db[r][tid];
+        mine[p.c_in * p.c_out + tid] = sum;
+    }
+}
+
 // One to eight rows: bound by reading w once.  A workgroup owns sixteen columns; its threads, four or two side by side on a row of w,
 // share k; fp32 products; the threads' sums meet in LDS.
 template <typename T, int R>
@@ -852,6 +1087,40 @@ static BackPlan back_plan(long long rows, long long cols, int dtype) {
     return b;
 }
 
+// Widths that k_linear_bwd_narrow takes (w and 64 rows of x and dz in LDS): its P, 0 for wider layers.
+static int narrow_width(int dtype, long long c_in, long long c_out) {
+    const long long c = c_in > c_out ? c_in : c_out;
+    if (c <= 32) return 32;
+    if (c <= 64) return 64;
+    return c <= 128 && dtype != SCNN_F32 ? 128 : 0;
+}
+// Two workgroups a compute unit, but at least two tiles of 64 rows each, and no longer chains than kChain rows.
+static int narrow_groups(long long rows) {
+    long long n = (rows + 127) / 128, most = 2LL * device_cu_count();
+    if (most < (rows + kChain - 1) / kChain) most = (rows + kChain - 1) / kChain;
+    if (n > most) n = most;
+    return (int)(n < 1 ? 1 : n);
+}
+
+template <typename T>
+static hipError_t narrow_bwd(int dtype, const LinearCall& c, int width, hipStream_t s) {
+    NarrowArgs p = {};
+    p.x = c.x; p.w = c.w; p.pre = c.pre_in; p.g = c.g; p.dx = c.rows > 0 ? c.dx : nullptr;
+    p.part = c.dw || c.dbias ? (float*)c.workspace : nullptr;
+    p.rows = c.rows;
+    p.rows_dev = c.rows_dev;
+    p.c_in = (int)c.c_in; p.c_out = (int)c.c_out; p.act = c.act;
+    if (!p.part && !p.dx) return hipSuccess;
+    const int groups = narrow_groups(c.rows);
+    if (width == 32) hipLaunchKernelGGL((k_linear_bwd_narrow<T, 32>), dim3(groups), dim3(256), 0, s, p);
+    else if (width == 64) hipLaunchKernelGGL((k_linear_bwd_narrow<T, 64>), dim3(groups), dim3(256), 0, s, p);
+    else if constexpr (sizeof(T) == 2) hipLaunchKernelGGL((k_linear_bwd_narrow<T, 128>), dim3(groups), dim3(256), 0, s, p);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || !p.part) return e;
+    const long long filter = c.c_in * c.c_out;
+    return launch_column_sums(p.part, groups, filter + c.c_out, filter, c.dw, c.dbias, dtype, s);
+}
+
 struct BackSpace { size_t dz, sums, dx, dw, total; };
 static BackSpace back_space(int dtype, long long rows, long long c_in, long long c_out, int act) {
     BackSpace b = {};
@@ -868,11 +1137,14 @@ static BackSpace back_space(int dtype, long long rows, long long c_in, long long
 }
 
 size_t linear_bwd_bytes(int dtype, long long rows, long long c_in, long long c_out, int act) {
+    if (narrow_width(dtype, c_in, c_out) != 0)
+        return (size_t)round_up((long long)narrow_groups(rows) * (c_in * c_out + c_out) * 4, 256);
     return back_space(dtype, rows, c_in, c_out, act).total;
 }
 
 template <typename T>
 static hipError_t linear_bwd_typed(int dtype, const LinearCall& c, hipStream_t s) {
+    if (const int width = narrow_width(dtype, c.c_in, c.c_out)) return narrow_bwd<T>(dtype, c, width, s);
     const BackSpace at = back_space(dtype, c.rows, c.c_in, c.c_out, c.act);
     char* const ws = (char*)c.workspace;
     const void* dz = c.g;
