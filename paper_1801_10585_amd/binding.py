@@ -526,7 +526,7 @@ def _same(t, like: torch.Tensor, shape, name: str, dtype=None):
 def _result(t, like: torch.Tensor, shape, name: str, dtype=None) -> torch.Tensor:
     """An output: the caller's, which must be contiguous, or a new one."""
     if t is None:
-        return torch.empty(shape, dtype=dtype or like.dtype, device=like.device)
+        return like.new_empty(shape) if dtype is None else like.new_empty(shape, dtype=dtype)
     if not _same(t, like, shape, name, dtype).is_contiguous():
         raise ValueError(f"{name} must be contiguous")
     return t
@@ -569,7 +569,7 @@ def _need(query: str, *sizes) -> int:
 def _scratch(workspace, need: int, like: torch.Tensor) -> Optional[torch.Tensor]:
     if workspace is None:
         # (a call that needs the least amount uses none)
-        return None if need <= 256 else torch.empty(need, dtype=torch.uint8, device=like.device)
+        return None if need <= 256 else like.new_empty(need, dtype=torch.uint8)
     if workspace.device != like.device or workspace.dtype != torch.uint8 or not workspace.is_contiguous():
         raise ValueError("workspace must be a contiguous uint8 tensor on the GPU of the rows")
     return workspace
@@ -710,37 +710,40 @@ def _dense(t: torch.Tensor) -> bool:
 
 
 def _grad_clip(grads, max_norm, outs, workspace, stream):
+    """outs: None (the norm alone), the list of gradients itself, or other tensors."""
     L = load_library()
-    grads = list(grads)
-    if outs is not None:
-        outs = list(outs)
-        if len(outs) != len(grads):
-            raise ValueError("outs must hold a tensor for every gradient")
-    if not grads:
+    n = len(grads)
+    if n == 0:
         raise ValueError("no gradients")
     like = grads[0]
-    dev = like.device
-    for t in grads:
-        if not t.is_cuda or t.device != dev:
-            raise ValueError("the gradients must live on one GPU")
-        if t.dtype not in DTYPES:
-            raise ValueError("gradients must be float32, bfloat16 or float16")
-        if not _dense(t):
-            raise ValueError("a gradient must fill one stretch of memory")
+    where = like.get_device()
+    dtypes = [t.dtype for t in grads]
+    types = [DTYPES.get(d, -1) for d in dtypes]
+    if where < 0 or any([t.get_device() != where for t in grads]):
+        raise ValueError("the gradients must live on one GPU")
+    if -1 in types:
+        raise ValueError("gradients must be float32, bfloat16 or float16")
+    plain = all([t.is_contiguous() for t in grads])
+    if not plain and not all([_dense(t) for t in grads]):
+        raise ValueError("a gradient must fill one stretch of memory")
     if outs is not None and outs is not grads:
-        for t, o in zip(grads, outs):
-            if o.device != dev or o.dtype != t.dtype or o.shape != t.shape or o.stride() != t.stride():
-                raise ValueError("an output must be like its gradient (device, type, shape and strides)")
-    n = len(grads)
-    counts = (ctypes.c_int64 * n)(*[t.numel() for t in grads])
-    types = (ctypes.c_int * n)(*[DTYPES[t.dtype] for t in grads])
+        if len(outs) != n:
+            raise ValueError("outs must hold a tensor for every gradient")
+        alike = all([o.get_device() == where for o in outs]) and [o.dtype for o in outs] == dtypes
+        alike = alike and [o.shape for o in outs] == [t.shape for t in grads]
+        if not alike or not (all([o.is_contiguous() for o in outs]) if plain else
+                             [o.stride() for o in outs] == [t.stride() for t in grads]):
+            raise ValueError("an output must be like its gradient (device, type, shape and strides)")
+    sizes = [t.numel() for t in grads]
+    counts = (ctypes.c_int64 * n)(*sizes)
     src = (ctypes.c_void_p * n)(*[t.data_ptr() for t in grads])
-    dst = None if outs is None else (ctypes.c_void_p * n)(*[t.data_ptr() for t in outs])
-    with _on(dev, stream, (*grads, *(outs or ()), workspace)):
-        result = torch.empty(2, dtype=torch.float64, device=dev)
+    dst = src if outs is grads else None if outs is None else (ctypes.c_void_p * n)(*[t.data_ptr() for t in outs])
+    dev = like.device
+    with _on(dev, stream, None if stream is None else (*grads, *(outs or ()), workspace)):
+        result = like.new_empty(2, dtype=torch.float64)
         workspace = _scratch(workspace, int(L.grad_clip_workspace(n, counts)), like)
-        _check(L, L.grad_clip(n, src, dst, counts, types, float(max_norm), _at(result), _at(workspace), _bytes(workspace),
-                              _current()))
+        _check(L, L.grad_clip(n, src, dst, counts, (ctypes.c_int * n)(*types), float(max_norm), _at(result), _at(workspace),
+                              _bytes(workspace), _current()))
     return result
 
 
@@ -748,12 +751,12 @@ def clip_grad_norm(grads, max_norm, *, outs=None, workspace=None, stream=None):
     """Scales all gradients by min(1, max_norm / (norm + 1e-6)), norm = their global 2-norm: in place, or into `outs`.
     Returns double[2] = {norm, scale} on the device."""
     grads = list(grads)
-    return _grad_clip(grads, max_norm, grads if outs is None else outs, workspace, stream)
+    return _grad_clip(grads, max_norm, grads if outs is None else list(outs), workspace, stream)
 
 
 def grad_norm(grads, *, workspace=None, stream=None):
     """Global 2-norm of a list of gradients: a double on the device."""
-    return _grad_clip(grads, float("inf"), None, workspace, stream)[0]
+    return _grad_clip(list(grads), float("inf"), None, workspace, stream)[0]
 
 
 def grad_clip_workspace(counts) -> int:

@@ -3,7 +3,7 @@
 //   norm = sqrt(sum over all entries of g^2),  scale = max_norm / (norm + 1e-6), at most 1,  out = g scale
 //
 // Bound by memory: every entry is read for the norm, then read again and written; nothing can be scaled before the last
-// entry has been squared.  The tensors' addresses travel in the kernels' arguments (a table of up to kClipTensors a launch),
+// entry has been squared.  The tensors' addresses travel in the kernels' arguments (a table of up to 120 a launch),
 // so that a call copies nothing to the device and can be captured in a graph.  A workgroup owns one chunk of one tensor.
 // Squares are summed in fp64, which costs nothing beside the loads, so that no gradient of fp32 overflows its square and the
 // order of addition does not show; the chunks' sums are stored and added in one fixed order by every workgroup of the second
@@ -20,7 +20,7 @@ __device__ __forceinline__ double sum_squares(const T* __restrict__ p, long long
     for (; i + 3 * 256 * V + V <= n; i += 4 * 256 * V) {  // four loads in flight
         float v[4][V];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) load_elems<T>(p + i + k * 256 * V, V, v[k]);
+        for (int k = 0; k < 4; ++k) load_elems<T>(p + i + k * 256 * V, V, true, v[k]);
 #pragma unroll
         for (int k = 0; k < 4; ++k)
 #pragma unroll
@@ -28,7 +28,7 @@ __device__ __forceinline__ double sum_squares(const T* __restrict__ p, long long
     }
     for (; i < n; i += 256 * V) {
         float v[V];
-        load_elems<T>(p + i, (int)(n - i < V ? n - i : V), v);
+        load_elems<T>(p + i, (int)(n - i < V ? n - i : V), n >= V, v);
 #pragma unroll
         for (int j = 0; j < V; ++j) sum += (double)v[j] * (double)v[j];
     }
@@ -42,7 +42,7 @@ __device__ __forceinline__ void scale_chunk(const T* p, T* q, long long n, float
     for (; i + 3 * 256 * V + V <= n; i += 4 * 256 * V) {
         float v[4][V];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) load_elems<T>(p + i + k * 256 * V, V, v[k]);
+        for (int k = 0; k < 4; ++k) load_elems<T>(p + i + k * 256 * V, V, true, v[k]);
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
 #pragma unroll
@@ -53,7 +53,7 @@ __device__ __forceinline__ void scale_chunk(const T* p, T* q, long long n, float
     for (; i < n; i += 256 * V) {
         const int m = (int)(n - i < V ? n - i : V);
         float v[V];
-        load_elems<T>(p + i, m, v);
+        load_elems<T>(p + i, m, false, v);
 #pragma unroll
         for (int j = 0; j < V; ++j) v[j] *= scale;
         store_elems<T>(q + i, m, v);
@@ -70,7 +70,8 @@ __device__ __forceinline__ double block_add(double v, double* s_part /*[4]*/) {
 }
 
 // The tensor that owns workgroup `block` of the launch: first[t] <= block < first[t + 1].
-__device__ __forceinline__ int tensor_of(const ClipTable& tab, unsigned block) {
+template <int N>
+__device__ __forceinline__ int tensor_of(const ClipTable<N>& tab, unsigned block) {
     int lo = 0, hi = tab.n - 1;
     while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
@@ -79,7 +80,8 @@ __device__ __forceinline__ int tensor_of(const ClipTable& tab, unsigned block) {
     return lo;
 }
 
-__global__ __launch_bounds__(256) void k_grad_squares(ClipTable tab, double* __restrict__ part) {
+template <int N>
+__global__ __launch_bounds__(256) void k_grad_squares(ClipTable<N> tab, double* __restrict__ part) {
     __shared__ double s_part[4];
     const ClipTensor& t = tab.t[tensor_of(tab, blockIdx.x)];
     const long long at = (long long)(blockIdx.x - t.first) * tab.chunk;
@@ -93,7 +95,8 @@ __global__ __launch_bounds__(256) void k_grad_squares(ClipTable tab, double* __r
 }
 
 // result = {norm, scale}, by the launch with slot 0.  Without destinations (the norm alone) the grid is one workgroup.
-__global__ __launch_bounds__(256) void k_grad_scale(ClipTable tab, const double* __restrict__ part, int parts, double max_norm,
+template <int N>
+__global__ __launch_bounds__(256) void k_grad_scale(ClipTable<N> tab, const double* __restrict__ part, int parts, double max_norm,
                                                     double* __restrict__ result) {
     __shared__ double s_part[4];
     double sum = 0.0;
@@ -130,14 +133,15 @@ long long grad_norm_parts(int n, const int64_t* counts) {
     return parts;
 }
 
-hipError_t launch_grad_clip(int n, const void* const* src, void* const* dst, const int64_t* counts, const int* dtypes,
+template <int N>
+static hipError_t grad_clip(int n, const void* const* src, void* const* dst, const int64_t* counts, const int* dtypes,
                             double max_norm, double* result, double* part, hipStream_t s) {
     long long total = 0;
     for (int i = 0; i < n; ++i) total += counts[i];
     const long long chunk = chunk_of(total);
     const int parts = (int)grad_norm_parts(n, counts);
     for (int pass = 0; pass < 2; ++pass) {
-        ClipTable tab;
+        ClipTable<N> tab;
         tab.chunk = chunk;
         long long slot = 0;
         int i = 0;
@@ -145,7 +149,7 @@ hipError_t launch_grad_clip(int n, const void* const* src, void* const* dst, con
             tab.n = 0;
             tab.slot = (int)slot;
             unsigned blocks = 0;
-            for (; i < n && tab.n < kClipTensors; ++i) {
+            for (; i < n && tab.n < N; ++i) {
                 if (counts[i] == 0) continue;
                 ClipTensor& t = tab.t[tab.n++];
                 t.src = src[i];
@@ -156,14 +160,14 @@ hipError_t launch_grad_clip(int n, const void* const* src, void* const* dst, con
                 blocks += (unsigned)((counts[i] + chunk - 1) / chunk);
             }
             if (pass == 0) {
-                if (blocks) hipLaunchKernelGGL(k_grad_squares, dim3(blocks), dim3(256), 0, s, tab, part);
+                if (blocks) hipLaunchKernelGGL((k_grad_squares<N>), dim3(blocks), dim3(256), 0, s, tab, part);
             } else {
                 if (!dst) {
                     tab.n = 0;
                     blocks = 1;
                 }
                 if (blocks || slot == 0)
-                    hipLaunchKernelGGL(k_grad_scale, dim3(blocks ? blocks : 1), dim3(256), 0, s, tab, part, parts, max_norm,
+                    hipLaunchKernelGGL((k_grad_scale<N>), dim3(blocks ? blocks : 1), dim3(256), 0, s, tab, part, parts, max_norm,
                                        result);
                 if (!dst) break;
             }
@@ -171,6 +175,12 @@ hipError_t launch_grad_clip(int n, const void* const* src, void* const* dst, con
         } while (i < n);
     }
     return hipGetLastError();
+}
+
+hipError_t launch_grad_clip(int n, const void* const* src, void* const* dst, const int64_t* counts, const int* dtypes,
+                            double max_norm, double* result, double* part, hipStream_t s) {
+    return n <= 24 ? grad_clip<24>(n, src, dst, counts, dtypes, max_norm, result, part, s)
+                   : grad_clip<120>(n, src, dst, counts, dtypes, max_norm, result, part, s);
 }
 
 }  // namespace scnn

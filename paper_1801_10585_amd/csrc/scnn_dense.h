@@ -16,40 +16,88 @@ template <> struct DenseType<SCNN_F16> { using type = _Float16; };
 template <typename T> constexpr int kVec = 16 / (int)sizeof(T);
 template <typename T, int N> using VecOf = T __attribute__((ext_vector_type(N)));
 
+template <typename T> using BitsAs = VecOf<T, kVec<T>>;
+
 // Sixteen bytes from an address aligned to the element only (rows of odd widths start anywhere): the compiler makes one
-// global access of 16 bytes of it, which the hardware takes at any address.  The first `n` elements, the rest 0.
-template <typename T>
-__device__ __forceinline__ VecOf<T, kVec<T>> load_raw(const T* __restrict__ p, int n) {
+// global access of 16 bytes of it, which the hardware takes at any address.  Of a vector that a row ends in, n < kVec elements
+// are there, the others are 0: up to three fp32 one by one; up to seven of 16 bits as the row's last sixteen bytes, shifted,
+// where the row is that long (`whole`), else in pieces of eight, four and two bytes.  (Without TAIL a row ends with a vector.)
+template <typename T, bool TAIL = true>
+__device__ __forceinline__ VecOf<T, kVec<T>> load_raw(const T* __restrict__ p, int n, bool whole) {
     VecOf<T, kVec<T>> r = {};
     if (n >= kVec<T>) {
-        __builtin_memcpy(&r, p, sizeof(r));
-    } else {
+        __builtin_memcpy(&r, p, 16);
+    } else if constexpr (!TAIL) {
+    } else if constexpr (sizeof(T) == 4) {
 #pragma unroll
-        for (int i = 0; i < kVec<T>; ++i)
+        for (int i = 0; i < 3; ++i)
             if (i < n) r[i] = p[i];
+    } else if (n > 0) {
+        typedef unsigned __int128 u128;
+        u128 v = 0;
+        if (whole) {
+            __builtin_memcpy(&v, p + n - 8, 16);
+            v >>= 16 * (8 - n);
+        } else {
+            int at = 0;
+            if (n & 4) {
+                unsigned long long q;
+                __builtin_memcpy(&q, p, 8);
+                v = q;
+                at = 4;
+            }
+            if (n & 2) {
+                unsigned q;
+                __builtin_memcpy(&q, p + at, 4);
+                v |= (u128)q << (16 * at);
+                at += 2;
+            }
+            if (n & 1) {
+                unsigned short q;
+                __builtin_memcpy(&q, p + at, 2);
+                v |= (u128)q << (16 * at);
+            }
+        }
+        r = __builtin_bit_cast(BitsAs<T>, v);
     }
     return r;
 }
-template <typename T>
-__device__ __forceinline__ void load_elems(const T* __restrict__ p, int n, float (&v)[kVec<T>]) {
-    const VecOf<T, kVec<T>> r = load_raw<T>(p, n);
+template <typename T, bool TAIL = true>
+__device__ __forceinline__ void load_elems(const T* __restrict__ p, int n, bool whole, float (&v)[kVec<T>]) {
+    const VecOf<T, kVec<T>> r = load_raw<T, TAIL>(p, n, whole);
 #pragma unroll
     for (int i = 0; i < kVec<T>; ++i) v[i] = (float)r[i];
 }
 
-// Rounded once, to nearest even.
-template <typename T>
-__device__ __forceinline__ void store_elems(T* __restrict__ p, int n, const float (&v)[kVec<T>]) {
+// The first n elements of a vector; those of a row's last one in pieces of eight, four and two bytes.
+template <typename T, bool TAIL = true>
+__device__ __forceinline__ void store_raw(T* __restrict__ p, int n, VecOf<T, kVec<T>> r) {
+    typedef unsigned __int128 u128;
+    u128 v = __builtin_bit_cast(u128, r);
     if (n >= kVec<T>) {
-        VecOf<T, kVec<T>> r;
-#pragma unroll
-        for (int i = 0; i < kVec<T>; ++i) r[i] = (T)v[i];
-        __builtin_memcpy(p, &r, sizeof(r));
-    } else {
-#pragma unroll
-        for (int i = 0; i < kVec<T>; ++i)
-            if (i < n) p[i] = (T)v[i];
+        __builtin_memcpy(p, &v, 16);
+        return;
     }
+    if (!TAIL || n <= 0) return;
+    if (sizeof(T) == 2 && (n & 4)) {
+        __builtin_memcpy(p, &v, 8);
+        v >>= 64;
+        p += 4;
+    }
+    if (n & 2) {
+        __builtin_memcpy(p, &v, 2 * sizeof(T));
+        v >>= 16 * (int)sizeof(T);
+        p += 2;
+    }
+    if (n & 1) __builtin_memcpy(p, &v, sizeof(T));
+}
+// Rounded once, to nearest even.
+template <typename T, bool TAIL = true>
+__device__ __forceinline__ void store_elems(T* __restrict__ p, int n, const float (&v)[kVec<T>]) {
+    VecOf<T, kVec<T>> r;
+#pragma unroll
+    for (int i = 0; i < kVec<T>; ++i) r[i] = (T)v[i];
+    store_raw<T, TAIL>(p, n, r);
 }
 
 // Rows of a call: the host's count, or the device's, held to the arrays' capacity.
@@ -136,8 +184,8 @@ __device__ __forceinline__ F lanes_add(F v) {
 hipError_t launch_column_sums(const float* part, int parts, long long cols, long long split, void* out0, void* out1,
                               int dtype, hipStream_t s);
 
-// Tensors of a gradient list, as the kernels' argument: 120 of them fit the 4096 bytes that a launch may carry.
-constexpr int kClipTensors = 120;
+// Tensors of a gradient list, as the kernels' argument: up to 120 of them fit the 4096 bytes that a launch may carry.  (A
+// launch costs the host more the more it carries: lists of up to 24 take a table of that size.)
 struct ClipTensor {
     const void* src;
     void* dst;
@@ -145,13 +193,14 @@ struct ClipTensor {
     unsigned first;  // first workgroup
     int dtype;
 };
+template <int N>
 struct ClipTable {
-    ClipTensor t[kClipTensors];
+    ClipTensor t[N];
     long long chunk;  // entries a workgroup
     int n;
     int slot;         // the launch's first partial sum
 };
-static_assert(sizeof(ClipTable) + 64 <= 4096, "kernel arguments of one launch");
+static_assert(sizeof(ClipTable<120>) + 64 <= 4096, "kernel arguments of one launch");
 
 long long grad_norm_parts(int n, const int64_t* counts);  // partial sums (double) of a call
 hipError_t launch_grad_clip(int n, const void* const* src, void* const* dst, const int64_t* counts, const int* dtypes,

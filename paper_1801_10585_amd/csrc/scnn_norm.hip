@@ -36,7 +36,7 @@ __device__ __forceinline__ F row_add(F v, F* s_part) {
     }
 }
 
-template <typename T, int P, int VPL>
+template <typename T, int P, int VPL, bool TAIL>
 __global__ __launch_bounds__(kNormBlock<P>) void k_norm_fwd(const T* __restrict__ x, long long rows_cap,
                                                             const long long* __restrict__ rows_dev, int channels,
                                                             const T* __restrict__ gamma, const T* __restrict__ beta,
@@ -46,6 +46,7 @@ __global__ __launch_bounds__(kNormBlock<P>) void k_norm_fwd(const T* __restrict_
     __shared__ float s_part[P <= 64 ? 1 : P / 64];
     __shared__ double s_mean[P <= 64 ? 1 : P / 64];
     const long long rows = rows_of(rows_cap, rows_dev);
+    const bool whole = channels >= kVec<T>;
     const int t = threadIdx.x % P;
     const float inv_c = 1.0f / (float)channels;
     const double inv_c64 = 1.0 / (double)channels;
@@ -56,7 +57,7 @@ __global__ __launch_bounds__(kNormBlock<P>) void k_norm_fwd(const T* __restrict_
 #pragma unroll
         for (int j = 0; j < VPL; ++j) {
             const int c = (j * P + t) * V;
-            load_elems<T>(xr + c, channels - c, v[j]);
+            load_elems<T, TAIL>(xr + c, channels - c, whole, v[j]);
 #pragma unroll
             for (int i = 0; i < V; ++i) sum += (double)v[j][i];
         }
@@ -77,15 +78,15 @@ __global__ __launch_bounds__(kNormBlock<P>) void k_norm_fwd(const T* __restrict_
         for (int j = 0; j < VPL; ++j) {
             const int c = (j * P + t) * V;
             float ga[V], be[V];
-            if (gamma) load_elems<T>(gamma + c, channels - c, ga);
-            if (beta) load_elems<T>(beta + c, channels - c, be);
+            if (gamma) load_elems<T, TAIL>(gamma + c, channels - c, whole, ga);
+            if (beta) load_elems<T, TAIL>(beta + c, channels - c, whole, be);
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 v[j][i] *= rstd;
                 if (gamma) v[j][i] *= ga[i];
                 if (beta) v[j][i] += be[i];
             }
-            store_elems<T>(yr + c, channels - c, v[j]);
+            store_elems<T, TAIL>(yr + c, channels - c, v[j]);
         }
         if (t == 0) {
             if (mean_out) mean_out[row] = mean;
@@ -105,6 +106,7 @@ __global__ __launch_bounds__(1024) void k_norm_fwd_long(const T* __restrict__ x,
     __shared__ float s_part[P / 64];
     __shared__ double s_mean[P / 64];
     const long long rows = rows_of(rows_cap, rows_dev);
+    const bool whole = channels >= kVec<T>;
     const float inv_c = 1.0f / (float)channels;
     const double inv_c64 = 1.0 / (double)channels;
     for (long long row = blockIdx.x; row < rows; row += gridDim.x) {
@@ -114,14 +116,14 @@ __global__ __launch_bounds__(1024) void k_norm_fwd_long(const T* __restrict__ x,
         float sq = 0.0f;
         for (long long c = (long long)threadIdx.x * V; c < channels; c += P * V) {
             float v[V];
-            load_elems<T>(xr + c, channels - (int)c, v);
+            load_elems<T>(xr + c, channels - (int)c, whole, v);
 #pragma unroll
             for (int i = 0; i < V; ++i) sum += (double)v[i];
         }
         const float mean = (float)(row_add<P>(sum, s_mean) * inv_c64);
         for (long long c = (long long)threadIdx.x * V; c < channels; c += P * V) {
             float v[V];
-            load_elems<T>(xr + c, channels - (int)c, v);
+            load_elems<T>(xr + c, channels - (int)c, whole, v);
 #pragma unroll
             for (int i = 0; i < V; ++i) sq += c + i < channels ? (v[i] - mean) * (v[i] - mean) : 0.0f;
         }
@@ -129,9 +131,9 @@ __global__ __launch_bounds__(1024) void k_norm_fwd_long(const T* __restrict__ x,
         for (long long c = (long long)threadIdx.x * V; c < channels; c += P * V) {
             const int n = channels - (int)c;
             float v[V], ga[V], be[V];
-            load_elems<T>(xr + c, n, v);
-            if (gamma) load_elems<T>(gamma + c, n, ga);
-            if (beta) load_elems<T>(beta + c, n, be);
+            load_elems<T>(xr + c, n, whole, v);
+            if (gamma) load_elems<T>(gamma + c, n, whole, ga);
+            if (beta) load_elems<T>(beta + c, n, whole, be);
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 v[i] = (v[i] - mean) * rstd;
@@ -148,7 +150,7 @@ __global__ __launch_bounds__(1024) void k_norm_fwd_long(const T* __restrict__ x,
 }
 
 // part [gridDim.x][2][channels]: this workgroup's sums of g xh and of g (not written where part is null).
-template <typename T, int P, int VPL>
+template <typename T, int P, int VPL, bool TAIL>
 __global__ __launch_bounds__(kBackBlock<P>) void k_norm_bwd(const T* __restrict__ x, const T* __restrict__ g,
                                                             long long rows_cap, const long long* __restrict__ rows_dev,
                                                             int channels, const T* __restrict__ gamma,
@@ -159,6 +161,7 @@ __global__ __launch_bounds__(kBackBlock<P>) void k_norm_bwd(const T* __restrict_
     typedef float f2 __attribute__((ext_vector_type(2)));
     __shared__ f2 s_part[2][P <= 64 ? 1 : B / 64];
     const long long rows = rows_of(rows_cap, rows_dev);
+    const bool whole = channels >= kVec<T>;
     const int t = threadIdx.x % P, group = threadIdx.x / P;
     const float inv_c = 1.0f / (float)channels;
     float d_gamma[VPL][V], d_beta[VPL][V];
@@ -167,7 +170,7 @@ __global__ __launch_bounds__(kBackBlock<P>) void k_norm_bwd(const T* __restrict_
     for (int j = 0; j < VPL; ++j) {
         const int c = (j * P + t) * V;
         ga[j] = VecOf<T, V>{};
-        if (gamma) ga[j] = load_raw<T>(gamma + c, channels - c);
+        if (gamma) ga[j] = load_raw<T, TAIL>(gamma + c, channels - c, whole);
 #pragma unroll
         for (int i = 0; i < V; ++i) d_gamma[j][i] = d_beta[j][i] = 0.0f;
     }
@@ -186,8 +189,8 @@ __global__ __launch_bounds__(kBackBlock<P>) void k_norm_bwd(const T* __restrict_
 #pragma unroll
         for (int j = 0; j < VPL; ++j) {
             const int c = (j * P + t) * V;
-            x_next[j] = load_raw<T>(x + row * channels + c, live ? channels - c : 0);
-            g_next[j] = load_raw<T>(g + row * channels + c, live ? channels - c : 0);
+            x_next[j] = load_raw<T, TAIL>(x + row * channels + c, live ? channels - c : 0, whole);
+            g_next[j] = load_raw<T, TAIL>(g + row * channels + c, live ? channels - c : 0, whole);
         }
     };
     if (AHEAD) fetch((long long)blockIdx.x * G + group);
@@ -234,7 +237,7 @@ __global__ __launch_bounds__(kBackBlock<P>) void k_norm_bwd(const T* __restrict_
                     const float gi = (float)gr[j][i], h = gamma ? gi * (float)ga[j][i] : gi;
                     v[i] = rstd * (h - sums.x - ((float)xr[j][i] - mean) * rstd * sums.y);
                 }
-                store_elems<T>(dx + row * channels + c, channels - c, v);
+                store_elems<T, TAIL>(dx + row * channels + c, channels - c, v);
             }
     }
     if (!part) return;
@@ -278,6 +281,7 @@ __global__ __launch_bounds__(1024) void k_norm_bwd_long(const T* __restrict__ x,
     constexpr int V = kVec<T>, P = 1024;
     __shared__ float s_part[2][P / 64];
     const long long rows = rows_of(rows_cap, rows_dev);
+    const bool whole = channels >= kVec<T>;
     const float inv_c = 1.0f / (float)channels;
     for (long long row = blockIdx.x; row < rows; row += gridDim.x) {
         const float mean = mean_in[row], rstd = rstd_in[row];
@@ -293,9 +297,9 @@ __global__ __launch_bounds__(1024) void k_norm_bwd_long(const T* __restrict__ x,
             for (long long c = (long long)threadIdx.x * V; c < channels; c += P * V) {
                 const int n = channels - (int)c;
                 float v[V], h[V], ga[V];
-                load_elems<T>(xr + c, n, v);
-                load_elems<T>(gr + c, n, h);
-                if (gamma) load_elems<T>(gamma + c, n, ga);
+                load_elems<T>(xr + c, n, whole, v);
+                load_elems<T>(gr + c, n, whole, h);
+                if (gamma) load_elems<T>(gamma + c, n, whole, ga);
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
                     v[i] = i < n ? (v[i] - mean) * rstd : 0.0f;
@@ -321,6 +325,7 @@ __global__ __launch_bounds__(256) void k_norm_cols_long(const T* __restrict__ x,
                                                         const float* __restrict__ rstd_in, float* __restrict__ part) {
     constexpr int V = kVec<T>;
     const long long rows = rows_of(rows_cap, rows_dev);
+    const bool whole = channels >= kVec<T>;
     const long long c = ((long long)blockIdx.x * 256 + threadIdx.x) * V;
     if (c >= channels) return;
     const int n = channels - (int)c;
@@ -330,8 +335,8 @@ __global__ __launch_bounds__(256) void k_norm_cols_long(const T* __restrict__ x,
     for (long long row = blockIdx.y; row < rows; row += gridDim.y) {
         const float mean = mean_in[row], rstd = rstd_in[row];
         float v[V], h[V];
-        load_elems<T>(x + row * channels + c, n, v);
-        load_elems<T>(g + row * channels + c, n, h);
+        load_elems<T>(x + row * channels + c, n, whole, v);
+        load_elems<T>(g + row * channels + c, n, whole, h);
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             d_gamma[i] += i < n ? h[i] * ((v[i] - mean) * rstd) : 0.0f;
@@ -395,20 +400,26 @@ hipError_t launch_column_sums(const float* part, int parts, long long cols, long
 
 static int dtype_vec(int dtype) { return dtype == SCNN_F32 ? 4 : 8; }
 
-// Threads a row and vectors a thread: the fewest threads that hold the row with one vector each up to a wave, then up to
-// four vectors a lane, then a workgroup.  `most` = vectors a thread may hold in a workgroup of 1024 (the backward pass
-// keeps six values an element).
+// Threads a row and vectors a thread: one vector a lane up to a wave; then, where rows are many, more vectors a lane before
+// more waves a row, which meet at a barrier for every sum (forward, 8192 rows of 8192 bf16, 256 threads of four vectors
+// against 1024 of one: 56 / 84 us); where they are few, and in the backward pass, whose sums of columns take the registers,
+// more waves.  p = 0: longer rows than these hold.
 struct NormShape { int p, vpl; };
-static NormShape norm_shape(int channels, int dtype, int most) {
+static NormShape norm_shape(int channels, int dtype, long long rows, bool forward) {
     const int units = (int)(((long long)channels + dtype_vec(dtype) - 1) / dtype_vec(dtype));
     for (int p = 1; p <= 64; p <<= 1)
         if (units <= p) return {p, 1};
     if (units <= 128) return {64, 2};
+    if (forward && rows >= 8LL * device_cu_count()) {
+        if (units <= 256) return {64, 4};
+        if (units <= 512) return {256, 2};
+        if (units <= 1024) return {256, 4};
+    }
     if (units <= 256) return {256, 1};
     if (units <= 512) return {512, 1};
     if (units <= 1024) return {1024, 1};
     if (units <= 2048) return {1024, 2};
-    if (units <= 4096 && most >= 4) return {1024, 4};
+    if (units <= 4096 && forward) return {1024, 4};
     return {0, 0};
 }
 
@@ -416,7 +427,7 @@ static NormShape norm_shape(int channels, int dtype, int most) {
 // of the bytes that the rows take in and out, but enough to fill the card with one workgroup a compute unit, and no more
 // than eight of four waves.
 static int norm_parts(long long rows, int channels, int dtype) {
-    const NormShape n = norm_shape(channels, dtype, 2);
+    const NormShape n = norm_shape(channels, dtype, rows, false);
     const long long cus = device_cu_count();
     if (n.p == 0) return (int)(rows < 1 ? 1 : (rows < cus ? rows : cus));
     const long long per = (n.p <= 64 ? 256 : 1024) / n.p;
@@ -440,7 +451,8 @@ size_t norm_bwd_part_bytes(long long rows, int channels, int dtype) {
 template <typename T>
 static hipError_t norm_fwd(const void* x, long long rows, const long long* rows_dev, int channels, const void* gamma,
                            const void* beta, float eps, void* out, float* mean, float* rstd, int dtype, hipStream_t s) {
-    const NormShape n = norm_shape(channels, dtype, 4);
+    const NormShape n = norm_shape(channels, dtype, rows, true);
+    const bool tail = channels % kVec<T> != 0;  // (code for a row's last elements costs registers)
     const long long per = n.p > 0 && n.p <= 64 ? 256 / n.p : 1;
     const int threads = n.p == 0 ? 1024 : (n.p <= 64 ? 256 : n.p);
     long long blocks = (rows + per - 1) / per;
@@ -448,9 +460,10 @@ static hipError_t norm_fwd(const void* x, long long rows, const long long* rows_
     if (blocks > most) blocks = most;
 #define F(P, VPL)                                                                                                      \
     if (n.p == P && n.vpl == VPL)                                                                                      \
-        hipLaunchKernelGGL((k_norm_fwd<T, P, VPL>), dim3((unsigned)blocks), dim3(kNormBlock<P>), 0, s, (const T*)x, rows,    \
-                           rows_dev, channels, (const T*)gamma, (const T*)beta, eps, (T*)out, mean, rstd);
-    SCNN_NORM_SHAPES(F) F(1024, 4)
+        hipLaunchKernelGGL((tail ? k_norm_fwd<T, P, VPL, true> : k_norm_fwd<T, P, VPL, false>), dim3((unsigned)blocks),   \
+                           dim3(kNormBlock<P>), 0, s, (const T*)x, rows, rows_dev, channels, (const T*)gamma,            \
+                           (const T*)beta, eps, (T*)out, mean, rstd);
+    SCNN_NORM_SHAPES(F) F(64, 4) F(256, 2) F(256, 4) F(1024, 4)
 #undef F
     if (n.p == 0)
         hipLaunchKernelGGL((k_norm_fwd_long<T>), dim3((unsigned)blocks), dim3(1024), 0, s, (const T*)x, rows, rows_dev,
@@ -472,13 +485,15 @@ template <typename T>
 static hipError_t norm_bwd(const void* x, const void* g, long long rows, const long long* rows_dev, int channels,
                            const void* gamma, const float* mean, const float* rstd, void* dx, void* dgamma, void* dbeta,
                            float* part, int dtype, hipStream_t s) {
-    const NormShape n = norm_shape(channels, dtype, 2);
+    const NormShape n = norm_shape(channels, dtype, rows, false);
+    const bool tail = channels % kVec<T> != 0;
     const int parts = norm_parts(rows, channels, dtype);
     float* const sums = dgamma || dbeta ? part : nullptr;
 #define F(P, VPL)                                                                                                      \
     if (n.p == P && n.vpl == VPL)                                                                                      \
-        hipLaunchKernelGGL((k_norm_bwd<T, P, VPL>), dim3((unsigned)parts), dim3(kBackBlock<P>), 0, s, (const T*)x,      \
-                           (const T*)g, rows, rows_dev, channels, (const T*)gamma, mean, rstd, (T*)dx, sums);
+        hipLaunchKernelGGL((tail ? k_norm_bwd<T, P, VPL, true> : k_norm_bwd<T, P, VPL, false>), dim3((unsigned)parts),    \
+                           dim3(kBackBlock<P>), 0, s, (const T*)x, (const T*)g, rows, rows_dev, channels,                \
+                           (const T*)gamma, mean, rstd, (T*)dx, sums);
     SCNN_NORM_SHAPES(F)
 #undef F
     if (n.p == 0) {

@@ -13,7 +13,7 @@ BIG = 1 << 40
 def test_linear_refusals():
     L = scnn.load_library()
     assert L.linear_fwd_workspace(0, 10, 8, 8) >= 256 and L.linear_fwd_workspace(2, 0, 1, 1) >= 256
-    assert L.linear_bwd_workspace(1, 10, 8, 8, 2) > L.linear_bwd_workspace(1, 10, 8, 8, 0) >= 256
+    assert L.linear_bwd_workspace(1, 1000, 200, 200, 2) > L.linear_bwd_workspace(1, 1000, 200, 200, 0) >= 256
     assert L.linear_bwd_workspace(0, 0, 5, 3, 1) >= 256  # (no rows: the filter's gradient is still written)
     for bad in ((3, 10, 8, 8), (0, -1, 8, 8), (0, 10, 0, 8), (0, 10, 8, 0), (0, 1 << 31, 8, 8), (0, 10, (1 << 28) + 1, 8)):
         assert L.linear_fwd_workspace(*bad) == 0 and L.linear_bwd_workspace(*bad, 0) == 0
