@@ -1048,52 +1048,79 @@ __global__ __launch_bounds__(256) void k_linear_fwd_narrow(NarrowFwdArgs p) {
     }
 }
 
-// One to eight rows: bound by reading w once.  A workgroup owns sixteen columns; its threads, four or two side by side on a row of w,
-// share k; fp32 products; the threads' sums meet in LDS.
+// One to four rows: bound by reading w once.  `lanes` threads (a power of two up to 64) hold 16 bytes each of a row of w,
+// every group of them four neighbouring k at a time, against x of the workgroup's k in LDS; fp32 products and sums.  The
+// groups' sums meet by lane exchanges and in LDS, those of a split k in k_linear_join.  (Threads that walked down w in strips
+// of 64 bytes, a load of x beside each of w, took 86 us for 8 x 4096 by 4096 x 4096 bf16, 216 for 8 x 12288 by 12288 x 1024.)
+// (256 threads: 21 us against 11 for 2 x 999 by 999 x 4001 fp32.)
+constexpr int kFewK = 1024;  // the most k of a workgroup
 template <typename T, int R>
-__global__ __launch_bounds__(256) void k_linear_few(LinearArgs p, int row0) {
-    constexpr int V = kVec<T>, TC = 16 / V, TK = 256 / TC;
-    __shared__ float s_sum[4][R][16];
+__global__ __launch_bounds__(1024) void k_linear_few(LinearArgs p, int lanes) {
+    constexpr int V = kVec<T>;
+    __shared__ __align__(16) float s_x[R][kFewK];
+    __shared__ float s_sum[16][64 * V];
     const long long m_end = rows_of(p.m, p.rows_dev);
-    const int tc = threadIdx.x % TC, tk = threadIdx.x / TC, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const long long n = (long long)blockIdx.x * 16 + tc * V;
+    const long long k_first = (long long)blockIdx.y * p.k_split;
+    const int k_count = (int)(p.k - k_first < p.k_split ? p.k - k_first : p.k_split);
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, tc = tid & (lanes - 1), group = tid / lanes, groups = 1024 / lanes;
+    const long long n = ((long long)blockIdx.x * lanes + tc) * V;
     const int w = (int)(p.n - n < V ? p.n - n : V);
+    const T *const x = (const T*)p.a, *const wt = (const T*)p.b + k_first * p.n + n;
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+        for (int k = tid; k < kFewK; k += 1024)
+            s_x[r][k] = r < m_end && k < k_count ? (float)x[r * p.k + k_first + k] : 0.0f;
+    __syncthreads();
     float acc[R][V];
 #pragma unroll
     for (int r = 0; r < R; ++r)
 #pragma unroll
         for (int i = 0; i < V; ++i) acc[r][i] = 0.0f;
-    const T* __restrict__ x = (const T*)p.a;
-    const T* __restrict__ wt = (const T*)p.b;
-#pragma unroll 4
-    for (long long k = tk; k < p.k; k += TK) {
-        float wv[V];
-        load_elems<T>(wt + k * p.n + n, w, p.n >= V, wv);
+#pragma unroll 2
+    for (int k = group * 4; k < k_count; k += groups * 4) {
+        VecOf<T, V> wv[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) wv[j] = load_raw<T>(wt + (long long)(k + j) * p.n, k + j < k_count ? w : 0, p.n >= V);
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            const float xv = row0 + r < m_end ? (float)x[(row0 + r) * p.k + k] : 0.0f;
+            const f4 xv = *(const f4*)&s_x[r][k];
 #pragma unroll
-            for (int i = 0; i < V; ++i) acc[r][i] += xv * wv[i];
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int i = 0; i < V; ++i) acc[r][i] += xv[j] * (float)wv[j][i];
         }
     }
+    for (int d = lanes; d < 64; d <<= 1)  // (all sums a step at a time: an exchange takes a hundred clocks to come back)
 #pragma unroll
-    for (int r = 0; r < R; ++r)
+        for (int r = 0; r < R; ++r)
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-            float v = acc[r][i];
+            for (int i = 0; i < V; ++i) acc[r][i] += __shfl_xor(acc[r][i], d, 64);
 #pragma unroll
-            for (int d = TC; d < 64; d <<= 1) v += __shfl_xor(v, d, 64);
-            if (lane < TC) s_sum[wave][r][tc * V + i] = v;
+    for (int r = 0; r < R; ++r) {
+        if (r >= m_end) break;  // (the same for all threads)
+        if (r > 0) __syncthreads();
+        if (lane < lanes)
+#pragma unroll
+            for (int i = 0; i < V; ++i) s_sum[wave][tc * V + i] = acc[r][i];
+        __syncthreads();
+        const int c = tid * 4;
+        const long long col = (long long)blockIdx.x * lanes * V + c;
+        if (c < lanes * V && col < p.n) {
+            float z[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int q = 0; q < 16; ++q)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) z[j] += s_sum[q][c + j];
+            if (p.part) {
+                float* __restrict__ to = p.part + ((long long)blockIdx.y * p.m + r) * p.n + col;
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (col + j < p.n) to[j] = z[j];
+            } else {
+                finish4<T>(p, r, col, z);
+            }
         }
-    __syncthreads();
-    if (threadIdx.x >= R * 4) return;
-    const int r = threadIdx.x >> 2, c = (threadIdx.x & 3) * 4;
-    const long long col = (long long)blockIdx.x * 16 + c;
-    if (row0 + r >= m_end || col >= p.n) return;
-    float z[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) z[j] = (s_sum[0][r][c + j] + s_sum[1][r][c + j]) + (s_sum[2][r][c + j] + s_sum[3][r][c + j]);
-    finish4<T>(p, row0 + r, col, z);
+    }
 }
 
 // ------------------------------------------------------------------ host side
@@ -1105,6 +1132,7 @@ struct TilePlan {
     int bm, bn;
     int splits;
     long long k_split;
+    int lanes;  // k_linear_few's
 };
 
 // The most k that one chain of 16-bit matrix instructions sums: the instruction cuts its sum off downwards at every step
@@ -1121,11 +1149,24 @@ constexpr long long kChain = 65536;
 // Large tiles read their operands least and pay from two (one of 64 x 128) a compute unit on, with k to hide their start and end;
 // short tiles for few rows; else 64 x 64.  k is split where that leaves compute units without a tile: one workgroup a unit was
 // the fastest of 1, 2, 4 and 8 at 12 of 16 shapes, within 15 per cent of it at the others.
-static TilePlan tile_plan(long long m, long long n, long long k, bool forward, bool ring) {
-    TilePlan t = {TileKind::kStaged, 64, 64, 1, round_up(k < 1 ? 1 : k, 64)};
+static TilePlan tile_plan(int dtype, long long m, long long n, long long k, bool forward, bool ring) {
+    TilePlan t = {TileKind::kStaged, 64, 64, 1, round_up(k < 1 ? 1 : k, 64), 0};
     if (m < 1) return t;
-    if (forward && m <= 8) {
+    // us, few rows against tiles, 4096 x 4096: fp32 1 row 17.8, 4 rows 21.4, 8 rows 32.4 / 30; bf16 10.8, 17.2, 25.9 / 10.8
+    if (forward && m <= (ring ? 1 : 4)) {
+        // Up to kFewK k one launch does, with few lanes a row of w so that there are more workgroups; a longer k is split for
+        // two workgroups a compute unit, 64 lanes a row.
         t.kind = TileKind::kFew;
+        const int v = dtype == SCNN_F32 ? 4 : 8, most = k > kFewK ? 64 : (n * k <= (1 << 20) ? 4 : 16);
+        for (t.lanes = 1; t.lanes < most && (long long)t.lanes * v < n; t.lanes <<= 1) {}
+        const long long strips = (n + (long long)t.lanes * v - 1) / ((long long)t.lanes * v), least = 4 * 1024 / t.lanes;
+        if (k <= kFewK) {
+            t.k_split = kFewK;
+        } else {
+            t.k_split = round_up(k * strips / (2LL * device_cu_count()) + 1, least);
+            if (t.k_split > kFewK) t.k_split = kFewK;
+        }
+        t.splits = (int)((k + t.k_split - 1) / t.k_split);
         return t;
     }
     const long long cus = device_cu_count();
@@ -1160,7 +1201,7 @@ static TilePlan tile_plan(long long m, long long n, long long k, bool forward, b
 static size_t part_bytes(int dtype, long long m, long long n, long long k, bool forward) {
     size_t most = 0;
     for (int ring = 0; ring <= (dtype == SCNN_F32 ? 0 : 1); ++ring) {
-        const TilePlan t = tile_plan(m, n, k, forward, ring != 0);
+        const TilePlan t = tile_plan(dtype, m, n, k, forward, ring != 0);
         const size_t b = t.splits > 1 ? (size_t)round_up((long long)t.splits * m * n * 4, 256) : 0;
         if (b > most) most = b;
     }
@@ -1179,8 +1220,27 @@ static hipError_t ring(const LinearArgs& p, dim3 grid, hipStream_t s) {
     return hipGetLastError();
 }
 
+template <typename T>
+static hipError_t join(const LinearArgs& p, int splits, hipStream_t s) {
+    const long long quads = p.m * ((p.n + 3) / 4);
+    if (splits >= 8)
+        hipLaunchKernelGGL((k_linear_join<T, 16>), dim3((unsigned)((quads + 15) / 16)), dim3(256), 0, s, p, splits);
+    else
+        hipLaunchKernelGGL((k_linear_join<T, 4>), dim3((unsigned)((quads + 63) / 64)), dim3(256), 0, s, p, splits);
+    return hipGetLastError();
+}
+
+template <typename T>
+static hipError_t few_rows(const LinearArgs& p, const TilePlan& t, hipStream_t s) {
+    const long long wide = (long long)t.lanes * kVec<T>;
+    const dim3 grid((unsigned)((p.n + wide - 1) / wide), (unsigned)t.splits);
+    if (p.m == 1) hipLaunchKernelGGL((k_linear_few<T, 1>), grid, dim3(1024), 0, s, p, t.lanes);
+    else hipLaunchKernelGGL((k_linear_few<T, 4>), grid, dim3(1024), 0, s, p, t.lanes);
+    return hipGetLastError();
+}
+
 template <typename T, bool AK, bool BK_>
-static hipError_t product(LinearArgs p, bool forward, hipStream_t s) {
+static hipError_t product(int dtype, LinearArgs p, bool forward, hipStream_t s) {
     bool copies = false;
     if constexpr (sizeof(T) == 2) {
         // rows of both operands begin on 16 bytes, and a tile's rows lie within 32-bit offsets
@@ -1188,13 +1248,15 @@ static hipError_t product(LinearArgs p, bool forward, hipStream_t s) {
         copies = wa % 8 == 0 && wb % 8 == 0 && wa < (1 << 22) && wb < (1 << 22) && ((uintptr_t)p.a & 15) == 0 &&
                  ((uintptr_t)p.b & 15) == 0 && p.n % 8 == 0;
     }
-    const TilePlan t = tile_plan(p.m, p.n, p.k, forward, copies);
+    const TilePlan t = tile_plan(dtype, p.m, p.n, p.k, forward, copies);
     p.k_split = t.k_split;
     if (t.splits <= 1) p.part = nullptr;
     hipError_t e = hipSuccess;
     constexpr int BK = std::is_same<T, float>::value ? 32 : 64;
     const dim3 grid((unsigned)(((p.n + t.bn - 1) / t.bn) * ((p.m + t.bm - 1) / t.bm)), (unsigned)t.splits);
-    if (t.kind == TileKind::kStaged) {
+    if (t.kind == TileKind::kFew) {
+        e = few_rows<T>(p, t, s);  // (only the forward product is planned so)
+    } else if (t.kind == TileKind::kStaged) {
         hipLaunchKernelGGL((k_linear_tile<T, AK, BK_, 64, 64, BK, 2, 2, 1>), grid, dim3(256), 0, s, p);
         e = hipGetLastError();
     } else if (t.kind == TileKind::kStagedGroups) {
@@ -1211,21 +1273,7 @@ static hipError_t product(LinearArgs p, bool forward, hipStream_t s) {
         else e = ring<T, AK, BK_, 32, 64, 1, 4, 4>(p, grid, s);
     }
     if (e != hipSuccess || t.splits <= 1) return e;
-    const long long quads = p.m * ((p.n + 3) / 4);
-    if (t.splits >= 8)
-        hipLaunchKernelGGL((k_linear_join<T, 16>), dim3((unsigned)((quads + 15) / 16)), dim3(256), 0, s, p, t.splits);
-    else
-        hipLaunchKernelGGL((k_linear_join<T, 4>), dim3((unsigned)((quads + 63) / 64)), dim3(256), 0, s, p, t.splits);
-    return hipGetLastError();
-}
-
-template <typename T>
-static hipError_t few_rows(const LinearArgs& p, hipStream_t s) {
-    const dim3 grid((unsigned)((p.n + 15) / 16));
-    if (p.m == 1) hipLaunchKernelGGL((k_linear_few<T, 1>), grid, dim3(256), 0, s, p, 0);
-    else if (p.m <= 4) hipLaunchKernelGGL((k_linear_few<T, 4>), grid, dim3(256), 0, s, p, 0);
-    else hipLaunchKernelGGL((k_linear_few<T, 8>), grid, dim3(256), 0, s, p, 0);
-    return hipGetLastError();
+    return join<T>(p, t.splits, s);
 }
 
 // Widths that k_linear_fwd_narrow takes (w in registers).
@@ -1237,6 +1285,7 @@ static int narrow_width(long long c_in, long long c_out) {
     if (c <= 32) return 32;
     return c <= 64 ? 64 : 0;  // (128, 16-bit types: 69 us against 57 for its three products apart on 100000 rows of 128 -> 128)
 }
+
 template <typename T>
 static hipError_t narrow_fwd(const LinearCall& c, hipStream_t s) {
     NarrowFwdArgs p = {};
@@ -1252,7 +1301,7 @@ static hipError_t narrow_fwd(const LinearCall& c, hipStream_t s) {
 }
 
 size_t linear_fwd_part_bytes(int dtype, long long rows, long long c_in, long long c_out) {
-    if (rows > 8 && narrow_forward(c_in, c_out)) return 0;
+    if (rows > 4 && narrow_forward(c_in, c_out)) return 0;
     return part_bytes(dtype, rows, c_out, c_in, true);
 }
 
@@ -1265,8 +1314,7 @@ hipError_t launch_linear_fwd(int dtype, const LinearCall& c, hipStream_t s) {
     p.bias = c.bias; p.residual = c.residual; p.out = c.out; p.pre = c.pre;
     p.part = (float*)c.workspace;
     p.act = c.act;
-    const bool few = tile_plan(p.m, p.n, p.k, true, false).kind == TileKind::kFew;
-    if (!few && narrow_forward(c.c_in, c.c_out)) {
+    if (p.m > 4 && narrow_forward(c.c_in, c.c_out)) {
         switch (dtype) {
             case SCNN_F32: return narrow_fwd<float>(c, s);
             case SCNN_BF16: return narrow_fwd<__bf16>(c, s);
@@ -1274,9 +1322,9 @@ hipError_t launch_linear_fwd(int dtype, const LinearCall& c, hipStream_t s) {
         }
     }
     switch (dtype) {
-        case SCNN_F32: return few ? few_rows<float>(p, s) : product<float, true, false>(p, true, s);
-        case SCNN_BF16: return few ? few_rows<__bf16>(p, s) : product<__bf16, true, false>(p, true, s);
-        default: return few ? few_rows<_Float16>(p, s) : product<_Float16, true, false>(p, true, s);
+        case SCNN_F32: return product<float, true, false>(dtype, p, true, s);
+        case SCNN_BF16: return product<__bf16, true, false>(dtype, p, true, s);
+        default: return product<_Float16, true, false>(dtype, p, true, s);
     }
 }
 
@@ -1367,7 +1415,7 @@ static hipError_t linear_bwd_typed(int dtype, const LinearCall& c, hipStream_t s
         p.a = dz; p.b = c.w; p.out = c.dx;
         p.m = c.rows; p.n = c.c_in; p.k = c.c_out;
         p.part = (float*)(ws + at.dx);
-        const hipError_t e = product<T, true, true>(p, false, s);
+        const hipError_t e = product<T, true, true>(dtype, p, false, s);
         if (e != hipSuccess) return e;
     }
     if (c.dw) {
@@ -1375,7 +1423,7 @@ static hipError_t linear_bwd_typed(int dtype, const LinearCall& c, hipStream_t s
         p.m = c.c_in; p.n = c.c_out; p.k = c.rows;
         p.rows_k = 1;
         p.part = (float*)(ws + at.dw);
-        return product<T, false, false>(p, false, s);
+        return product<T, false, false>(dtype, p, false, s);
     }
     return hipGetLastError();
 }
