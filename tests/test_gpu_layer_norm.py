@@ -147,6 +147,36 @@ def test_any_start_and_strides(dtype, channels):
     assert all(torch.equal(a, b) for a, b in zip(back, other))
 
 
+def test_offsets_past_32_bits():
+    rows, channels = 140001, 16000
+    x = torch.zeros((rows, channels), dtype=torch.bfloat16, device=DEV)
+    last = make(17, 40, channels, torch.bfloat16)
+    x[-40:] = last["x"]
+    assert x.numel() > 1 << 31
+    out, mean, rstd = scnn.layer_norm_fwd(x, last["gamma"], last["beta"])
+    want = scnn.layer_norm_fwd(last["x"], last["gamma"], last["beta"])
+    for a, b in zip((out, mean, rstd), ref.layer_norm_fwd(last["x"], last["gamma"], last["beta"], 1e-5, torch.bfloat16)):
+        ref.assert_within(a[-40:], b)
+    g = out.zero_()
+    g[-40:] = last["g"]
+    back = scnn.layer_norm_bwd(x, g, last["gamma"], mean, rstd)
+    for i, b in enumerate(ref.layer_norm_bwd(last["x"], last["g"], last["gamma"], want[1], want[2], torch.bfloat16)):
+        ref.assert_within(back[i][-40:] if i == 0 else back[i], b)
+
+
+def test_many_rows_of_every_shape():
+    """Enough rows for the forms that long lists take: several vectors a lane or a thread."""
+    for k, (rows, channels, dtype) in enumerate(((2100, 1500, torch.float32), (2100, 2000, torch.bfloat16), (2050, 3999, torch.float16),
+                                                 (2050, 2047, torch.float32), (2050, 8000, torch.bfloat16), (2050, 4001, torch.float32))):
+        d = make(40 + k, rows, channels, dtype)
+        got = scnn.layer_norm_fwd(d["x"], d["gamma"], d["beta"])
+        for a, b in zip(got, ref.layer_norm_fwd(d["x"], d["gamma"], d["beta"], 1e-5, dtype)):
+            ref.assert_within(a, b)
+        for a, b in zip(scnn.layer_norm_bwd(d["x"], d["g"], d["gamma"], got[1], got[2]),
+                        ref.layer_norm_bwd(d["x"], d["g"], d["gamma"], got[1], got[2], dtype)):
+            ref.assert_within(a, b)
+
+
 def test_captured_and_replayed_and_another_stream():
     d = make(31, 500, 96, torch.float32)
     outs = (torch.empty((500, 96), device=DEV), torch.empty(500, device=DEV), torch.empty(500, device=DEV))

@@ -142,6 +142,41 @@ def test_infinities_nan_and_extremes(dtype, rows):
         assert not scnn.linear_fwd(x, w).any()
 
 
+@pytest.mark.parametrize("size", [(40, 64, 48), (3, 64, 48), (200, 96, 130), (300, 24, 24)], ids=str)
+@pytest.mark.parametrize("power", [-104, -110, -120, -127])
+def test_small_values_keep_their_bits(size, power):
+    """Magnitudes around 2^-109, where three bf16 numbers begin not to hold an fp32 value: products with large ones."""
+    d = make(13, *size, torch.float32)
+    x, w = d["x"] * 2.0 ** power, d["w"] * 2.0 ** 100
+    ref.assert_within(scnn.linear_fwd(x, w), ref.linear_fwd(x, w, None, "none", None, torch.float32)[0], "out")
+    g = d["g"] * 2.0 ** power
+    for a, b in zip(scnn.linear_bwd(x * 2.0 ** 50, w, g), ref.linear_bwd(x * 2.0 ** 50, w, g, "none", None, torch.float32)):
+        ref.assert_within(a, b)
+
+
+def test_offsets_past_32_bits():
+    """More than 2^31 values in an array: the last rows are as a call on them alone gives them."""
+    rows, width = 140001, 16400
+    w = make(15, 4, 16, width, torch.bfloat16)["w"]
+    x = torch.zeros((rows, 16), dtype=torch.bfloat16, device=DEV)
+    last = make(16, 70, 16, width, torch.bfloat16)
+    x[-70:] = last["x"]
+    out = scnn.linear_fwd(x, w, act="relu")
+    assert out.numel() > 1 << 31
+    # (another tile may add another order of sixteen products: one rounding of the result)
+    want = ref.linear_fwd(last["x"], w, None, "relu", None, torch.bfloat16)[0]
+    ref.assert_within(out[-70:], want)
+    assert not out[:1000].any()
+    g = torch.zeros_like(out)
+    g[-70:] = last["g"]
+    del out
+    dx, dw, db = scnn.linear_bwd(x, w, g)
+    del g
+    for a, b in zip((dx[-70:], dw, db), ref.linear_bwd(last["x"], w, last["g"], "none", None, torch.bfloat16)):
+        ref.assert_within(a, b)
+    assert not dx[:-70].any()
+
+
 @pytest.mark.parametrize("name", ["relu", "gelu", "silu"])
 def test_activations_of_far_values(name):
     z = torch.tensor([[0.0, -0.0, 1e-30, -1e-30, 20.0, -20.0, 100.0, -100.0, float("nan"), float("inf")]], device=DEV)
@@ -222,6 +257,23 @@ def test_any_start_and_strides(dtype):
     summed = d["residual"].clone()
     scnn.linear_fwd(d["x"], d["w"], d["bias"], act="gelu", residual=summed, out=summed)
     assert torch.equal(summed, want)
+
+
+def test_refusals_of_tensors():
+    d = make(23, 10, 16, 24, torch.float32)
+    x, w, b, r, g = d["x"], d["w"], d["bias"], d["residual"], d["g"]
+    for bad in (lambda: scnn.linear_fwd(x, w.t()), lambda: scnn.linear_fwd(x, w.half()), lambda: scnn.linear_fwd(x, w, b[:-1]),
+                lambda: scnn.linear_fwd(x, w, residual=r[:-1]), lambda: scnn.linear_fwd(x, w, act="tanh"),
+                lambda: scnn.linear_fwd(x.double(), w.double()), lambda: scnn.linear_fwd(x, w.cpu()),
+                lambda: scnn.linear_fwd(x, w, out=torch.empty((24, 10), device=DEV).t()),
+                lambda: scnn.linear_fwd(x, w, rows_dev=torch.ones(1, device=DEV)), lambda: scnn.linear_fwd(x[0], w),
+                lambda: scnn.linear_bwd(x, w, g, act="relu"), lambda: scnn.linear_bwd(x, w, g[:, :-1])):
+        with pytest.raises(ValueError):
+            bad()
+    with pytest.raises(scnn.ScnnError):   # in place on an input that is still read
+        scnn.linear_fwd(x, torch.eye(16, device=DEV), out=x)
+    with pytest.raises(scnn.ScnnError):
+        scnn.linear_bwd(x, w, g, out=(x, torch.empty_like(w), torch.empty_like(b)))
 
 
 def test_another_stream_and_two_at_once():
