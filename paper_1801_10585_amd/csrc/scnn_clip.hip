@@ -109,9 +109,11 @@ __global__ __launch_bounds__(256) void k_grad_scale(ClipTable<N> tab, const doub
         result[1] = scale;
     }
     if (tab.n == 0) return;
-    const ClipTensor& t = tab.t[tensor_of(tab, blockIdx.x)];
+    // from the last chunk to the first: what the norm read last is what the caches still hold
+    const unsigned block = gridDim.x - 1 - blockIdx.x;
+    const ClipTensor& t = tab.t[tensor_of(tab, block)];
     if (scale == 1.0 && t.dst == t.src) return;  // in place and nothing to change
-    const long long at = (long long)(blockIdx.x - t.first) * tab.chunk;
+    const long long at = (long long)(block - t.first) * tab.chunk;
     const long long n = t.count - at < tab.chunk ? t.count - at : tab.chunk;
     const float by = (float)scale;
     if (t.dtype == SCNN_F32) scale_chunk((const float*)t.src + at, (float*)t.dst + at, n, by);

@@ -371,6 +371,10 @@ __global__ __launch_bounds__(64 * WM * WN * KG) void k_linear_tile(LinearArgs p)
                 for (int j = 0; j < TN; ++j) acc[i][j] += s_join[((g * TM + i) * TN + j) * NT + tid];
     }
     // lane: row m = lane % 16, columns n = 4 (lane / 16) .. + 3 of each block
+    if (!p.part && inside) {
+        finish_tile<T, TM, TN>(p, m0 + wm + (lane & 15), n0 + wn + 4 * (lane >> 4), acc);
+        return;
+    }
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
         const long long m = m0 + wm + i * 16 + (lane & 15);

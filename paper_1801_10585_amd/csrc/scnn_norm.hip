@@ -425,7 +425,7 @@ static NormShape norm_shape(int channels, int dtype, long long rows, bool forwar
 
 // Workgroups of the backward pass.  Each leaves 2 * channels sums, written and read again in fp32: at most about a sixteenth
 // of the bytes that the rows take in and out, but enough to fill the card with one workgroup a compute unit, and no more
-// than eight of four waves.
+// than four of four waves.
 static int norm_parts(long long rows, int channels, int dtype) {
     const NormShape n = norm_shape(channels, dtype, rows, false);
     const long long cus = device_cu_count();
@@ -433,7 +433,7 @@ static int norm_parts(long long rows, int channels, int dtype) {
     const long long per = (n.p <= 64 ? 256 : 1024) / n.p;
     const long long e = dtype == SCNN_F32 ? 4 : 2;
     long long parts = rows * 3 * e / (16 * 16);
-    if (parts > 8 * cus) parts = 8 * cus;
+    if (parts > 4 * cus) parts = 4 * cus;
     if (n.p > 64) parts = cus;
     if (parts < cus) parts = cus;
     const long long need = (rows + per - 1) / per;
