@@ -1147,10 +1147,11 @@ constexpr long long kChain = 65536;
 //   8192 x 4096 x 4096 (m, n, k)   231 / - / - / -          2048 x 2048 x 2048   29 / 24 / 29 / 37
 //   2048 x 2048 x 512             12.3 / 10.7 / 10.9 / 14   1024 x 1024 x 1024   18 / 12.6 / 8.0 / 7.6
 //   64 x 1024 x 12288             14.1 / 13.1 / 12.5 / 11.4   16 x 4096 x 4096   12.2 / 10.5 / 12.9 / 9.6
+//   3000 x 2000 x 2000              39 / 49 / 60 / 84       5000 x 1304 x 1000   23.8 / 30.8 / 33.7 / 44.7
 //   200000 x 64 x 32                31 / 34 / 16 / 23       100000 x 128 x 128   18.4 / 19.4 / 16.1 / 22
 // and of 256 x 256 tiles: 8192 x 4096 x 4096 with gelu, residual and pre 281 against 313 (231 both without these), 4096 x
 // 4096 x 4096 x^T dz 142 against 124.
-// Large tiles read their operands least and pay from two (one of 64 x 128) a compute unit on, with k to hide their start and end;
+// Large tiles read their operands least and pay from five on four compute units (one of 64 x 128 a unit) on, with k to hide their start and end;
 // short tiles for few rows; else 64 x 64.  k is split where that leaves compute units without a tile: one workgroup a unit was
 // the fastest of 1, 2, 4 and 8 at 12 of 16 shapes, within 15 per cent of it at the others.
 static TilePlan tile_plan(int dtype, long long m, long long n, long long k, bool forward, bool ring) {
@@ -1177,16 +1178,17 @@ static TilePlan tile_plan(int dtype, long long m, long long n, long long k, bool
     auto tiles = [&](long long bm, long long bn) { return ((m + bm - 1) / bm) * ((n + bn - 1) / bn); };
     if (ring) {
         if (k >= 512 && tiles(256, 256) >= 2 * cus) t.kind = TileKind::kRing256, t.bm = t.bn = 256;
-        else if (k >= 512 && n > 64 && tiles(128, 128) >= 2 * cus) t.kind = TileKind::kRing128, t.bm = t.bn = 128;
+        else if (k >= 512 && n > 64 && 4 * tiles(128, 128) >= 5 * cus) t.kind = TileKind::kRing128, t.bm = t.bn = 128;
         else if (k >= 512 && n > 64 && tiles(64, 128) >= cus) t.kind = TileKind::kRing64x128, t.bn = 128;
         else if (m <= 32) t.kind = TileKind::kRing32, t.bm = 32;
         else t.kind = TileKind::kRing64;
     }
     // fp32, us, of 128 x 128 / 64 x 64 / 64 x 64 by four groups of waves, the last with a workgroup a compute unit:
     //   4096 x 4096 x 4096   756 / 928 / 1080 (the library's product 960)   100000 x 128 x 128   39 / 35 / 79
+    //   2560 x 2560 x 1024   101 / 111 / 138 (400 tiles of 128 x 128)       3000 x 2000 x 2000   236 / 222 / 249 (384)
     //   1024 x 1024 x 1024    36 / 31 / 22.5    64 x 1024 x 12288    36 / 26 / 24.3    32 x 64 x 200000 (x^T dz)   69 / 32 / 28
     if (!ring) {
-        if (k >= 512 && m > 64 && n > 64 && tiles(128, 128) >= 2 * cus) t.kind = TileKind::kStaged128, t.bm = t.bn = 128;
+        if (k >= 512 && m > 64 && n > 64 && 2 * tiles(128, 128) > 3 * cus) t.kind = TileKind::kStaged128, t.bm = t.bn = 128;
         else if (k >= 256 && tiles(64, 64) < 2 * cus) t.kind = TileKind::kStagedGroups;
     }
     const long long all = tiles(t.bm, t.bn), want = cus;
