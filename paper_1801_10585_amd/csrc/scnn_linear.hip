@@ -51,6 +51,29 @@ __device__ __forceinline__ u32x4 fragment(const char* tile, int base, int kk) {
     }
 }
 
+// The same for columns in pairs of blocks: block b of the pair at `base` takes the columns base + 8 (i / 4) + 4 b + i % 4,
+// i < 16, so that the two blocks' results of a lane are eight neighbouring columns (16 bytes of a 16-bit type; 64 bytes a row
+// a store.  With 8 bytes a lane a wide layer's stores wrote 237 MB to memory for 134 MB of results.)
+template <bool K_CONTIG, int W>
+__device__ __forceinline__ int staged_pair(int r, int c) {  // rows of k: the rows of a read are 0-3, 8-11, 16-19, 24-27 (+ 4 b)
+    if constexpr (K_CONTIG) return (r * (W / 8) + (c ^ (W >= 64 ? (r & 3) | ((r >> 1) & 4) : (r & 3)))) * 16;
+    else return staged<false, W>(r, c);
+}
+template <bool K_CONTIG, int W>
+__device__ __forceinline__ u32x4 fragment_pair(const char* tile, int base, int b, int kk) {
+    const int lane = threadIdx.x & 63, q = lane >> 4, i = lane & 15;
+    if constexpr (K_CONTIG) {
+        return *(const u32x4*)(tile + staged_pair<true, W>(base + 8 * (i >> 2) + 4 * b + (i & 3), kk * 4 + q));
+    } else {
+        typedef __attribute__((address_space(3))) s4 lds_s4;
+        const int k = kk * 32 + 8 * q + (i >> 2), c = (base >> 3) + (i & 3);
+        union { s4 half[2]; u32x4 all; } r;
+        r.half[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4*)(tile + staged<false, W>(k, c) + 8 * b));
+        r.half[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4*)(tile + staged<false, W>(k + 4, c) + 8 * b));
+        return r.all;
+    }
+}
+
 // What a call multiplies.  `rows_k`: the device's row count bounds k (the filter's gradient), else m.
 struct LinearArgs {
     const void* a;
@@ -139,43 +162,46 @@ __device__ __forceinline__ void finish4(const LinearArgs& p, long long m, long l
 
 // The same for all of a wave's blocks, which lie inside the array: everything that is read is on its way before the first
 // value is written.  (A load behind every store, which may be to the same place, was a fifth of a wide layer's time.)
-template <typename T, int TM, int TN>
+// m: the lane's first row; n: its first column, of groups of C that lie GROUP apart (C = 8: pairs of blocks).
+template <typename T, int TM, int TN, int C, int GROUP>
 __device__ __forceinline__ void finish_tile(const LinearArgs& p, long long m, long long n, const f4 (&acc)[TM][TN]) {
-    typedef VecOf<T, 4> V4;
-    V4 bias[TN], residual[TM][TN];
+    typedef VecOf<T, C> V;
+    constexpr int J = TN * 4 / C;
+    V bias[J], residual[TM][J];
 #pragma unroll
-    for (int j = 0; j < TN; ++j) {
-        bias[j] = V4{};
-        if (p.bias) __builtin_memcpy(&bias[j], (const T*)p.bias + n + j * 16, sizeof(V4));
+    for (int j = 0; j < J; ++j) {
+        bias[j] = V{};
+        if (p.bias) __builtin_memcpy(&bias[j], (const T*)p.bias + n + j * GROUP, sizeof(V));
     }
     if (p.residual)
 #pragma unroll
         for (int i = 0; i < TM; ++i)
 #pragma unroll
-            for (int j = 0; j < TN; ++j)
-                __builtin_memcpy(&residual[i][j], (const T*)p.residual + (m + i * 16) * p.n + n + j * 16, sizeof(V4));
+            for (int j = 0; j < J; ++j)
+                __builtin_memcpy(&residual[i][j], (const T*)p.residual + (m + i * 16) * p.n + n + j * GROUP, sizeof(V));
 #pragma unroll
     for (int i = 0; i < TM; ++i)
 #pragma unroll
-        for (int j = 0; j < TN; ++j) {
-            const long long at = (m + i * 16) * p.n + n + j * 16;
-            f4 z = acc[i][j];
-            V4 r;
+        for (int j = 0; j < J; ++j) {
+            const long long at = (m + i * 16) * p.n + n + j * GROUP;
+            float z[C];
+            V r;
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
+            for (int c = 0; c < C; ++c) {
+                z[c] = acc[i][j * (C / 4) + c / 4][c & 3];
                 if (p.bias) z[c] += (float)bias[j][c];
                 r[c] = (T)z[c];
             }
-            if (p.pre) __builtin_memcpy((T*)p.pre + at, &r, sizeof(V4));
+            if (p.pre) __builtin_memcpy((T*)p.pre + at, &r, sizeof(V));
             if (p.act != SCNN_ACT_NONE)
 #pragma unroll
-                for (int c = 0; c < 4; ++c) z[c] = activate(z[c], p.act);
+                for (int c = 0; c < C; ++c) z[c] = activate(z[c], p.act);
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
+            for (int c = 0; c < C; ++c) {
                 if (p.residual) z[c] += (float)residual[i][j][c];
                 r[c] = (T)z[c];
             }
-            __builtin_memcpy((T*)p.out + at, &r, sizeof(V4));
+            __builtin_memcpy((T*)p.out + at, &r, sizeof(V));
         }
 }
 
@@ -372,7 +398,7 @@ __global__ __launch_bounds__(64 * WM * WN * KG) void k_linear_tile(LinearArgs p)
     }
     // lane: row m = lane % 16, columns n = 4 (lane / 16) .. + 3 of each block
     if (!p.part && inside) {
-        finish_tile<T, TM, TN>(p, m0 + wm + (lane & 15), n0 + wn + 4 * (lane >> 4), acc);
+        finish_tile<T, TM, TN, 4, 16>(p, m0 + wm + (lane & 15), n0 + wn + 4 * (lane >> 4), acc);
         return;
     }
 #pragma unroll
@@ -431,6 +457,7 @@ __global__ __launch_bounds__(64 * WM * WN) void k_linear_ring(LinearArgs p) {
     constexpr int NT = 64 * WM * WN, AW = AK ? BK : BM, BW = BK_ ? BK : BN;
     constexpr int A8 = BM * BK / 8, B8 = BN * BK / 8, AN = A8 / NT, BN8 = B8 / NT, SLOT = (A8 + B8) * 16;
     constexpr int TM = BM / WM / 16, TN = BN / WN / 16, COPIES = AN + BN8;
+    constexpr bool PAIR = TN % 2 == 0;  // columns in pairs of blocks (fragment_pair)
     static_assert(A8 % NT == 0 && B8 % NT == 0, "whole pieces a thread");
     extern __shared__ __align__(1024) char s_ring[];
     const long long rows = rows_of(p.rows_k ? p.k : p.m, p.rows_dev);
@@ -447,11 +474,11 @@ __global__ __launch_bounds__(64 * WM * WN) void k_linear_ring(LinearArgs p) {
     const unsigned ring = (unsigned)(size_t)(__attribute__((address_space(3))) char*)s_ring;
 
     // This thread's pieces: byte offsets from the tile's first value at the step's first k.
-    auto offset_of = [&](bool k_contig, int w, int e, long long first, long long end, long long ld) -> unsigned {
+    auto offset_of = [&](bool k_contig, bool pair, int w, int e, long long first, long long end, long long ld) -> unsigned {
         const int r = e / (w / 8);
         int c = e % (w / 8);
         if (k_contig) {
-            c ^= w / 8 >= 8 ? (r & 7) : ((r >> 1) & 3);
+            c ^= pair ? (w >= 64 ? (r & 3) | ((r >> 1) & 4) : (r & 3)) : w / 8 >= 8 ? (r & 7) : ((r >> 1) & 3);
             const long long row = first + r < end ? r : end - 1 - first;
             return (unsigned)((row * ld + c * 8) * 2);
         }
@@ -461,9 +488,9 @@ __global__ __launch_bounds__(64 * WM * WN) void k_linear_ring(LinearArgs p) {
     };
     unsigned at_a[AN], at_b[BN8];
 #pragma unroll
-    for (int i = 0; i < AN; ++i) at_a[i] = offset_of(AK, AW, i * NT + tid, m0, AK ? m_end : p.m, AK ? p.k : p.m);
+    for (int i = 0; i < AN; ++i) at_a[i] = offset_of(AK, false, AW, i * NT + tid, m0, AK ? m_end : p.m, AK ? p.k : p.m);
 #pragma unroll
-    for (int i = 0; i < BN8; ++i) at_b[i] = offset_of(BK_, BW, i * NT + tid, n0, p.n, BK_ ? p.k : p.n);
+    for (int i = 0; i < BN8; ++i) at_b[i] = offset_of(BK_, PAIR, BW, i * NT + tid, n0, p.n, BK_ ? p.k : p.n);
     const char* base_a = (const char*)p.a + (AK ? m0 * p.k + k_first : k_first * p.m + m0) * 2;
     const char* base_b = (const char*)p.b + (BK_ ? n0 * p.k + k_first : k_first * p.n + n0) * 2;
     const long long next_a = (AK ? (long long)BK : BK * p.m) * 2, next_b = (BK_ ? (long long)BK : BK * p.n) * 2;
@@ -487,7 +514,8 @@ __global__ __launch_bounds__(64 * WM * WN) void k_linear_ring(LinearArgs p) {
         for (int kk = 0; kk < BK / 32; ++kk) {
             u32x4 fa[TM], fb[TN];
 #pragma unroll
-            for (int j = 0; j < TN; ++j) fb[j] = fragment<BK_, BW>(sb, wn + j * 16, kk);
+            for (int j = 0; j < TN; ++j)
+                fb[j] = PAIR ? fragment_pair<BK_, BW>(sb, wn + (j & ~1) * 16, j & 1, kk) : fragment<BK_, BW>(sb, wn + j * 16, kk);
 #pragma unroll
             for (int i = 0; i < TM; ++i) fa[i] = fragment<AK, AW>(sa, wm + i * 16, kk);
             // (a wave that multiplies goes before the other workgroup's waves, which then fetch: 1063 -> 1189 TFLOP/s on
@@ -535,13 +563,14 @@ __global__ __launch_bounds__(64 * WM * WN) void k_linear_ring(LinearArgs p) {
             const int e = i * NT + tid, r = e / (BW / 8), c = e % (BW / 8);
             const VecOf<T, 8> v = BK_ ? load8<T>((const T*)p.b, n0 + r, p.n, k_tail + c * 8, p.k)
                                       : load8<T>((const T*)p.b, k_tail + r, k_end, n0 + c * 8, p.n);
-            *(u32x4*)(s_ring + A8 * 16 + staged<BK_, BW>(r, c)) = __builtin_bit_cast(u32x4, v);
+            *(u32x4*)(s_ring + A8 * 16 + (PAIR ? staged_pair<BK_, BW>(r, c) : staged<BK_, BW>(r, c))) = __builtin_bit_cast(u32x4, v);
         }
         __syncthreads();
         multiply(s_ring, s_ring + A8 * 16);
     }
     if (!p.part && m0 + BM <= m_end && n0 + BN <= p.n) {
-        finish_tile<T, TM, TN>(p, m0 + wm + (lane & 15), n0 + wn + 4 * (lane >> 4), acc);
+        if constexpr (PAIR) finish_tile<T, TM, TN, 8, 32>(p, m0 + wm + (lane & 15), n0 + wn + 8 * (lane >> 4), acc);
+        else finish_tile<T, TM, TN, 4, 16>(p, m0 + wm + (lane & 15), n0 + wn + 4 * (lane >> 4), acc);
         return;
     }
 #pragma unroll
@@ -550,7 +579,7 @@ __global__ __launch_bounds__(64 * WM * WN) void k_linear_ring(LinearArgs p) {
         if (m >= m_end) continue;
 #pragma unroll
         for (int j = 0; j < TN; ++j) {
-            const long long n = n0 + wn + j * 16 + 4 * (lane >> 4);
+            const long long n = n0 + wn + (PAIR ? (j & ~1) * 16 + 8 * (lane >> 4) + 4 * (j & 1) : j * 16 + 4 * (lane >> 4));
             if (n >= p.n) continue;
             float z[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
             if (p.part) __builtin_memcpy(p.part + ((long long)blockIdx.y * p.m + m) * p.n + n, z, 16);
