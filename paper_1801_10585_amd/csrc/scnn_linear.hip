@@ -9,7 +9,7 @@
 // (ds_read_b64_tr_b16: sixteen lanes read four rows of sixteen values and each receives one column), so that no operand
 // is laid out anew.  16-bit operands multiply as they are; fp32 operands are split into three bf16 numbers each while they
 // are staged, and six of the nine products are multiplied (split8, split_products: as close to the exact sum as fp32
-// products), at 2.6 times the rate of fp32 instructions.  All sums are fp32.
+// products): 182 TFLOP/s on 4096 x 4096 x 4096 where the library's fp32 product reaches 147.  All sums are fp32.
 #include "scnn_dense.h"
 
 namespace scnn {
@@ -451,7 +451,9 @@ __device__ __forceinline__ void copies_and_barrier() {
 // passing through registers, into a ring of STAGES, so that a step's copies have two steps of products to arrive.  The
 // lanes' addresses carry the permutation of the pieces (staged), since the copy puts them down in the order of the lanes.
 // Rows and columns past the arrays' ends are read from the last one inside; what they add up to is not stored.  k past a
-// multiple of BK is staged through registers at the end, with zeros.
+// multiple of BK is staged through registers at the end, with zeros.  8192 x 4096 x 4096 bf16 (m, n, k): 226 us, 1219 TFLOP/s
+// (the library's product 237), 253 with gelu, residual and pre; the matrix cores are busy 64 per cent of the time in the
+// products of 4096 x 4096 x 4096, LDS a third.
 template <typename T, bool AK, bool BK_, int BM, int BN, int BK, int WM, int WN, int STAGES>
 __global__ __launch_bounds__(64 * WM * WN) void k_linear_ring(LinearArgs p) {
     constexpr int NT = 64 * WM * WN, AW = AK ? BK : BM, BW = BK_ ? BK : BN;
@@ -628,7 +630,8 @@ __global__ __launch_bounds__(256) void k_linear_join(LinearArgs p, int splits) {
 }
 
 // dz = g act'(pre) rounded to the operands' type (what the matrix instructions take), and this workgroup's column sums of
-// the dz before that rounding: part [gridDim.y][cols].  A block is 256 / TR threads wide, each a 16-byte vector of columns.
+// the dz before that rounding: part [gridDim.y][cols].  A block is tn threads wide, each a 16-byte vector of columns.  Bound by
+// memory: 4096 x 4096 bf16 gelu 21.5 us, 4.7 TB/s.
 template <typename T>
 __global__ __launch_bounds__(256) void k_act_back(const T* __restrict__ g, const T* __restrict__ pre, long long rows_cap,
                                                   const long long* __restrict__ rows_dev, long long cols, int act, int tn,
@@ -674,6 +677,8 @@ __global__ __launch_bounds__(256) void k_act_back(const T* __restrict__ g, const
 // once, staged next to x, and read by both products, dx = dz w^T with its channels contiguous, dw += x^T dz by transposing
 // reads; dw stays in the accumulators and the column sums of dz in registers until the workgroup's rows are done.  part
 // [gridDim.x][c_in * c_out + c_out] then receives both, and one launch adds the workgroups' up.  P: widths up to P.
+// 52417 rows of 35 -> 19 fp16, silu: 12 + 4 us, against 30 for the five launches of the general way; 643072 of 64 -> 64 bf16 78
+// us, 4.2 TB/s, fp32 168 us, 3.9 TB/s.
 template <int BYTES, int P> struct NarrowShape;  // threads; waves of dx (64 x P) and of dw (P x P), rows by columns
 template <int BYTES> struct NarrowShape<BYTES, 32> { static constexpr int NT = 256, XM = 4, XN = 1, WM = 2, WN = 2; };
 template <> struct NarrowShape<4, 64> { static constexpr int NT = 256, XM = 2, XN = 2, WM = 2, WN = 2; };
