@@ -557,13 +557,17 @@ def _activation(act: str) -> int:
 
 
 @functools.lru_cache(maxsize=4096)
-def _need(query: str, *sizes) -> int:
-    """Answer of a workspace query, which depends on its arguments alone."""
+def _need(device: int, query: str, *sizes) -> int:
+    """Answer of a workspace query, which depends on its arguments and on the current device (`device`) alone."""
     L = load_library()
     r = int(getattr(L, query)(*sizes))
     if r == 0:
         raise ScnnError(-1, L.scnn_last_error().decode())
     return r
+
+
+def _ask(query: str, *sizes) -> int:
+    return _need.__wrapped__(-1, query, *sizes)
 
 
 def _scratch(workspace, need: int, like: torch.Tensor) -> Optional[torch.Tensor]:
@@ -589,7 +593,7 @@ def _cont(t: Optional[torch.Tensor]) -> Optional[torch.Tensor]:
 
 
 def linear_fwd_workspace(dtype: torch.dtype, rows: int, c_in: int, c_out: int) -> int:
-    return _need("linear_fwd_workspace", DTYPES[dtype], int(rows), int(c_in), int(c_out))
+    return _ask("linear_fwd_workspace", DTYPES[dtype], int(rows), int(c_in), int(c_out))
 
 
 def linear_fwd(x, w, bias=None, *, act="none", residual=None, keep_pre=False, rows_dev=None, out=None, pre=None,
@@ -612,14 +616,14 @@ def linear_fwd(x, w, bias=None, *, act="none", residual=None, keep_pre=False, ro
         out = _result(out, x, (rows, c_out), "out")
         if keep:
             pre = _result(pre, x, (rows, c_out), "pre")
-        workspace = _scratch(workspace, _need("linear_fwd_workspace", dt, rows, c_in, c_out), x)
+        workspace = _scratch(workspace, _need(x.device.index, "linear_fwd_workspace", dt, rows, c_in, c_out), x)
         _check(L, L.linear_fwd(dt, _at(x), rows, _at(rows_dev), c_in, _at(w), _at(bias), c_out, code, _at(residual),
                                _at(out), _at(pre), _at(workspace), _bytes(workspace), _current()))
     return (out, pre) if keep else out
 
 
 def linear_bwd_workspace(dtype: torch.dtype, rows: int, c_in: int, c_out: int, act="none") -> int:
-    return _need("linear_bwd_workspace", DTYPES[dtype], int(rows), int(c_in), int(c_out), _activation(act))
+    return _ask("linear_bwd_workspace", DTYPES[dtype], int(rows), int(c_in), int(c_out), _activation(act))
 
 
 def linear_bwd(x, w, g, *, act="none", pre=None, want=(True, True, True), rows_dev=None, out=None, workspace=None,
@@ -645,7 +649,7 @@ def linear_bwd(x, w, g, *, act="none", pre=None, want=(True, True, True), rows_d
         dx = _result(dx, x, (rows, c_in), "dx") if want[0] else None
         dw = _result(dw, x, (c_in, c_out), "dw") if want[1] else None
         dbias = _result(dbias, x, (c_out,), "dbias") if want[2] else None
-        workspace = _scratch(workspace, _need("linear_bwd_workspace", dt, rows, c_in, c_out, code), x)
+        workspace = _scratch(workspace, _need(x.device.index, "linear_bwd_workspace", dt, rows, c_in, c_out, code), x)
         _check(L, L.linear_bwd(dt, _at(x), rows, _at(rows_dev), c_in, _at(w), c_out, code, _at(pre), _at(g), _at(dx),
                                _at(dw), _at(dbias), _at(workspace), _bytes(workspace), _current()))
     return dx, dw, dbias
@@ -671,7 +675,7 @@ def layer_norm_fwd(x, gamma=None, beta=None, *, eps=1e-5, rows_dev=None, out=Non
 
 
 def layer_norm_bwd_workspace(dtype: torch.dtype, rows: int, channels: int) -> int:
-    return _need("layer_norm_bwd_workspace", DTYPES[dtype], int(rows), int(channels))
+    return _ask("layer_norm_bwd_workspace", DTYPES[dtype], int(rows), int(channels))
 
 
 def layer_norm_bwd(x, g, gamma, mean, rstd, *, want=(True, True, True), rows_dev=None, out=None, workspace=None,
@@ -691,7 +695,7 @@ def layer_norm_bwd(x, g, gamma, mean, rstd, *, want=(True, True, True), rows_dev
         dx = _result(dx, x, (rows, ch), "dx") if want[0] else None
         dgamma = _result(dgamma, x, (ch,), "dgamma") if want[1] else None
         dbeta = _result(dbeta, x, (ch,), "dbeta") if want[2] else None
-        workspace = _scratch(workspace, _need("layer_norm_bwd_workspace", dt, rows, ch), x)
+        workspace = _scratch(workspace, _need(x.device.index, "layer_norm_bwd_workspace", dt, rows, ch), x)
         _check(L, L.layer_norm_bwd(dt, _at(x), _at(g), rows, _at(rows_dev), ch, _at(gamma), _at(mean), _at(rstd),
                                    _at(dx), _at(dgamma), _at(dbeta), _at(workspace), _bytes(workspace), _current()))
     return dx, dgamma, dbeta

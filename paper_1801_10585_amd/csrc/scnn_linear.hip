@@ -735,7 +735,7 @@ __global__ __launch_bounds__((NarrowShape<sizeof(T), P>::NT)) void k_linear_bwd_
             const long long row = first + (i * NT + tid) / CH;
             rg[i] = load8<T>(g, row, rows, c8, p.c_out);
             if (p.act != SCNN_ACT_NONE) rp[i] = load8<T>(pre, row, rows, c8, p.c_out);
-            rx[i] = load8<T>(x, p.part ? row : rows, rows, c8, p.c_in);
+            rx[i] = load8<T>(x, x ? row : rows, rows, c8, p.c_in);  // (null: dw is not asked for)
         }
     };
     f4 dw[WM][WN];
@@ -778,7 +778,7 @@ __global__ __launch_bounds__((NarrowShape<sizeof(T), P>::NT)) void k_linear_bwd_
                 db[c] += v;
             }
             put(s_z, PIECES, staged<false, P>(r, tid % CH), z, odd);
-            if (p.part) put(s_x, PIECES, staged<false, P>(r, tid % CH), rx[i], odd);
+            if (x) put(s_x, PIECES, staged<false, P>(r, tid % CH), rx[i], odd);
         }
         bool exact = true;
         if constexpr (SPLIT) exact = !__syncthreads_or(odd);
@@ -813,7 +813,7 @@ __global__ __launch_bounds__((NarrowShape<sizeof(T), P>::NT)) void k_linear_bwd_
                         for (int i = 0; i < XM; ++i) dx[i][j] = multiply(fw, fz[i], dx[i][j]);
                     }
                 }
-            if (p.part)
+            if (x)
 #pragma unroll
                 for (int kk = 0; kk < ROWS / 32; ++kk) {
                     if (wm >= p.c_in) break;
@@ -852,7 +852,7 @@ __global__ __launch_bounds__((NarrowShape<sizeof(T), P>::NT)) void k_linear_bwd_
                             dx[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(vw, vz, dx[i][j], 0, 0, 0);
                         }
                     }
-            if (p.part)
+            if (x)
                 for (int k = 0; k < ROWS; k += 4)
 #pragma unroll
                     for (int i = 0; i < WM; ++i) {
@@ -1192,7 +1192,7 @@ static TilePlan tile_plan(int dtype, long long m, long long n, long long k, bool
     TilePlan t = {TileKind::kStaged, 64, 64, 1, round_up(k < 1 ? 1 : k, 64), 0};
     if (m < 1) return t;
     // us, few rows against tiles, 4096 x 4096: fp32 1 row 17.8, 4 rows 21.4, 8 rows 32.4 / 30; bf16 10.8, 17.2, 25.9 / 10.8
-    if (forward && m <= (ring ? 1 : 4)) {
+    if (forward && m <= (ring ? 1 : 4) && k <= (1 << 24)) {  // (2^14 workgroups along a split k)
         // Up to kFewK k one launch does, with few lanes a row of w so that there are more workgroups; a longer k is split for
         // two workgroups a compute unit, 64 lanes a row.
         t.kind = TileKind::kFew;
@@ -1393,7 +1393,7 @@ static int narrow_groups(long long rows) {
 template <typename T>
 static hipError_t narrow_bwd(int dtype, const LinearCall& c, int width, hipStream_t s) {
     NarrowArgs p = {};
-    p.x = c.x; p.w = c.w; p.pre = c.pre_in; p.g = c.g; p.dx = c.rows > 0 ? c.dx : nullptr;
+    p.x = c.dw ? c.x : nullptr; p.w = c.w; p.pre = c.pre_in; p.g = c.g; p.dx = c.rows > 0 ? c.dx : nullptr;
     p.part = c.dw || c.dbias ? (float*)c.workspace : nullptr;
     p.rows = c.rows;
     p.rows_dev = c.rows_dev;

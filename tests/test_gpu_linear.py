@@ -10,7 +10,7 @@ DEV = "cuda:0"
 # (rows, c_in, c_out): one of everything, the few-row kernel and its end, tiles and their edges, odd widths, long sums
 SIZES = [(1, 1, 1), (1, 1024, 40), (2, 7, 3), (3, 33, 17), (4, 64, 16), (5, 300, 19), (8, 100, 130), (9, 65, 63), (16, 16, 16),
          (64, 64, 64), (65, 129, 67), (200, 31, 257), (1000, 24, 40), (130, 1001, 505), (70, 4100, 33), (300, 256, 512), (3000, 1, 5),
-         (257, 520, 264)]
+         (257, 520, 264), (300, 8, 72), (40, 72, 8), (300, 56, 200), (5, 24, 16)]
 
 
 def make(seed, rows, c_in, c_out, dtype, scale=1.0):
@@ -219,6 +219,37 @@ def test_row_count_from_the_device(cap, count, dtype):
         for a, b in zip((dx[:n], dw, db), ref.linear_bwd(d["x"][:n], d["w"], d["g"][:n], name,
                                                           None if name == "none" else pre[:n], dtype)):
             ref.assert_within(a, b, name)
+
+
+def test_longest_sums():
+    """More k than the few-row kernel splits over the card."""
+    g = torch.Generator().manual_seed(1)
+    x, w = torch.randn((1, 20000003), generator=g).to(DEV), torch.randn((20000003, 1), generator=g).to(DEV)
+    ref.assert_within(scnn.linear_fwd(x, w), ref.linear_fwd(x, w, None, "none", None, torch.float32)[0])
+    assert torch.equal(scnn.linear_fwd(x, w), scnn.linear_fwd(x, w))
+
+
+@pytest.mark.parametrize("size", [(200, 40, 24), (200, 20, 24), (130, 200, 100)], ids=str)
+@pytest.mark.parametrize("dtype", ref.TYPES, ids=str)
+def test_null_operands_of_what_is_not_asked_for(size, dtype):
+    """Through the C ABI: no x without dw, no w without dx."""
+    L = scnn.load_library()
+    rows, c_in, c_out = size
+    d = make(71, *size, dtype)
+    want = ref.linear_bwd(d["x"], d["w"], d["g"], "none", None, dtype)
+    code = scnn.DTYPES[dtype]
+    ws = torch.empty(scnn.linear_bwd_workspace(dtype, *size), dtype=torch.uint8, device=DEV)
+    stream = torch.cuda.current_stream().cuda_stream
+    outs = [torch.empty_like(d["x"]), torch.empty_like(d["w"]), torch.empty(c_out, dtype=dtype, device=DEV)]
+    for ask in ((True, False, True), (False, True, True), (False, False, True), (True, False, False), (False, True, False)):
+        p = [o.data_ptr() if a else None for o, a in zip(outs, ask)]
+        rc = L.linear_bwd(code, d["x"].data_ptr() if ask[1] else None, rows, None, c_in, d["w"].data_ptr() if ask[0] else None,
+                          c_out, 0, None, d["g"].data_ptr(), *p, ws.data_ptr(), ws.numel(), stream)
+        assert rc == 0
+        for o, a, b in zip(outs, ask, want):
+            if a:
+                ref.assert_within(o, b, str(ask))
+            o.fill_(float("nan"))
 
 
 def test_no_rows():
