@@ -526,7 +526,9 @@ def _same(t, like: torch.Tensor, shape, name: str, dtype=None):
 def _result(t, like: torch.Tensor, shape, name: str, dtype=None) -> torch.Tensor:
     """An output: the caller's, which must be contiguous, or a new one."""
     if t is None:
-        return like.new_empty(shape) if dtype is None else like.new_empty(shape, dtype=dtype)
+        if dtype is not None:
+            return like.new_empty(shape, dtype=dtype)
+        return torch.empty_like(like) if like.shape == shape else like.new_empty(shape)  # (the cheaper call; like is contiguous)
     if not _same(t, like, shape, name, dtype).is_contiguous():
         raise ValueError(f"{name} must be contiguous")
     return t
@@ -668,7 +670,7 @@ def layer_norm_fwd(x, gamma=None, beta=None, *, eps=1e-5, rows_dev=None, out=Non
         x, gamma, beta = x.contiguous(), _cont(gamma), _cont(beta)
         y = _result(y, x, (rows, ch), "out")
         mean = _result(mean, x, (rows,), "mean", torch.float32)
-        rstd = _result(rstd, x, (rows,), "rstd", torch.float32)
+        rstd = _result(rstd, mean, (rows,), "rstd")
         _check(L, L.layer_norm_fwd(dt, _at(x), rows, _at(rows_dev), ch, _at(gamma), _at(beta), float(eps), _at(y),
                                    _at(mean), _at(rstd), _current()))
     return y, mean, rstd

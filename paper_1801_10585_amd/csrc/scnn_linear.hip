@@ -1174,7 +1174,7 @@ struct TilePlan {
 };
 
 // The most k that one chain of 16-bit matrix instructions sums: the instruction cuts its sum off downwards at every step
-// of 32 k, half a last bit on average, so that 65536 k may leave 2^10 last bits of 2^-24, an eighth of a last bit of fp16.
+// of 32 k, half a last bit on average, so that 65536 k may leave 2^10 last bits of 2^-24, an eighth of fp16's rounding.
 constexpr long long kChain = 65536;
 
 // bf16, best of several launches, us, of 128 x 128 / 64 x 128 / 64 x 64 / 32 x 64 tiles:
@@ -1185,8 +1185,8 @@ constexpr long long kChain = 65536;
 //   200000 x 64 x 32                31 / 34 / 16 / 23       100000 x 128 x 128   18.4 / 19.4 / 16.1 / 22
 // and of 256 x 256 tiles: 8192 x 4096 x 4096 with gelu, residual and pre 281 against 313 (231 both without these), 4096 x
 // 4096 x 4096 x^T dz 142 against 124.
-// Large tiles read their operands least and pay from five on four compute units (one of 64 x 128 a unit) on, with k to hide their start and end;
-// short tiles for few rows; else 64 x 64.  k is split where that leaves compute units without a tile: one workgroup a unit was
+// Large tiles read their operands least and pay from five on four compute units (one of 64 x 128 a unit) on, with k to hide
+// their start and end, where both sides fill them; short tiles for few rows; else 64 x 64.  k is split where that leaves compute units without a tile: one workgroup a unit was
 // the fastest of 1, 2, 4 and 8 at 12 of 16 shapes, within 15 per cent of it at the others.
 static TilePlan tile_plan(int dtype, long long m, long long n, long long k, bool forward, bool ring) {
     TilePlan t = {TileKind::kStaged, 64, 64, 1, round_up(k < 1 ? 1 : k, 64), 0};
@@ -1211,9 +1211,9 @@ static TilePlan tile_plan(int dtype, long long m, long long n, long long k, bool
     const long long cus = device_cu_count();
     auto tiles = [&](long long bm, long long bn) { return ((m + bm - 1) / bm) * ((n + bn - 1) / bn); };
     if (ring) {
-        if (k >= 512 && tiles(256, 256) >= 2 * cus) t.kind = TileKind::kRing256, t.bm = t.bn = 256;
-        else if (k >= 512 && n > 64 && 4 * tiles(128, 128) >= 5 * cus) t.kind = TileKind::kRing128, t.bm = t.bn = 128;
-        else if (k >= 512 && n > 64 && tiles(64, 128) >= cus) t.kind = TileKind::kRing64x128, t.bn = 128;
+        if (k >= 512 && m > 128 && n > 128 && tiles(256, 256) >= 2 * cus) t.kind = TileKind::kRing256, t.bm = t.bn = 256;
+        else if (k >= 512 && m > 64 && n > 64 && 4 * tiles(128, 128) >= 5 * cus) t.kind = TileKind::kRing128, t.bm = t.bn = 128;
+        else if (k >= 512 && m > 32 && n > 64 && tiles(64, 128) >= cus) t.kind = TileKind::kRing64x128, t.bn = 128;
         else if (m <= 32) t.kind = TileKind::kRing32, t.bm = 32;
         else t.kind = TileKind::kRing64;
     }
