@@ -1119,9 +1119,9 @@ static int check_workspace(const void* workspace, size_t bytes, size_t need) {
     return SCNN_OK;
 }
 
-// What a call writes may overlap nothing else of the call; `may` is an input that an output may be, as a whole.
+// What a call writes may overlap nothing else of the call.
 struct Span { const void* p; size_t bytes; };
-static int check_apart(std::initializer_list<Span> outs, std::initializer_list<Span> ins, const void* may = nullptr) {
+static int check_apart(std::initializer_list<Span> outs, std::initializer_list<Span> ins) {
     auto meet = [](const Span& a, const Span& b) {
         return a.p && b.p && (uintptr_t)a.p < (uintptr_t)b.p + b.bytes && (uintptr_t)b.p < (uintptr_t)a.p + a.bytes;
     };
@@ -1129,7 +1129,7 @@ static int check_apart(std::initializer_list<Span> outs, std::initializer_list<S
         for (const Span* q = o + 1; q != outs.end(); ++q)
             if (meet(*o, *q)) return fail(SCNN_EINVAL, "two outputs overlap");
         for (const Span& i : ins)
-            if (meet(*o, i) && !(i.p == may && o->p == may)) return fail(SCNN_EINVAL, "an output overlaps an input");
+            if (meet(*o, i)) return fail(SCNN_EINVAL, "an output overlaps an input");
     }
     return SCNN_OK;
 }
@@ -1165,7 +1165,8 @@ int linear_fwd(int dtype, const void* x, int64_t rows, const int64_t* rows_dev, 
     if (rc != SCNN_OK) return rc;
     const size_t in = (size_t)rows * c_in * e, of = (size_t)rows * c_out * e;
     rc = check_apart({{out, of}, {pre, of}, {workspace, need}},
-                     {{x, in}, {w, (size_t)c_in * c_out * e}, {bias, (size_t)c_out * e}, {residual, of}}, out == residual ? out : nullptr);
+                     {{x, in}, {w, (size_t)c_in * c_out * e}, {bias, (size_t)c_out * e},
+                      {residual == out ? nullptr : residual, of}});  // (an element of it is read by the lane that writes it)
     if (rc != SCNN_OK) return rc;
     LinearCall c = {};
     c.x = x; c.w = w; c.bias = bias; c.residual = residual; c.out = out; c.pre = pre;

@@ -132,3 +132,13 @@ def test_python_refusals():
         scnn.clip_grad_norm([x], 1.0)
     with pytest.raises(ValueError):
         scnn.grad_norm([x])
+
+
+def test_linear_in_place_is_for_the_residual_alone():
+    # out on the residual is allowed; the same array as x, w or bias besides is not (other tiles still read those)
+    L = scnn.load_library()
+    for same in ("x", "w", "bias"):
+        a = {"x": P(1 << 20), "w": P(2 << 20), "bias": P(3 << 20), "out": P(5 << 20)}
+        a["out"] = a[same]
+        rc = L.linear_fwd(0, a["x"], 8, None, 8, a["w"], a["bias"], 8, 0, a["out"], a["out"], None, P(7 << 20), 1 << 20, None)
+        assert rc == -1 and b"overlap" in L.scnn_last_error(), same
