@@ -319,9 +319,9 @@ int layer_norm_bwd(int dtype, const void* x, const void* g, int64_t rows, const 
  * scaled entries; outs[i] == grads[i] scales in place, and nothing is written
  * there when scale is 1.  outs null: the norm alone.  Apart from outs[i] ==
  * grads[i] no output may overlap an output or a gradient, which the call checks
- * (a tensor listed twice is refused; with outs null it counts twice); result and
- * workspace overlap no tensor.  The host arrays are read before the call
- * returns.  result (device, double[2]) =
+ * (a tensor listed twice is refused; with outs null it counts twice); nor may
+ * result, workspace and the tensors overlap each other (refused too).  The host
+ * arrays are read before the call returns.  result (device, double[2]) =
  * {norm, scale}; a NaN or infinity among the entries shows there and in what is
  * scaled, as the formulas have it.  Sums in fp64 in a fixed order.  max_norm >= 0
  * (infinity: scale 1). */

@@ -1318,7 +1318,15 @@ int grad_clip(int n, const void* const* grads, void* const* outs, const int64_t*
         if (over < 0) return fail(SCNN_ECAPACITY, "no host memory for the list of tensors");
         if (over > 0) return fail(SCNN_EINVAL, "an output overlaps another tensor of the list");
     }
-    rc = check_workspace(workspace, workspace_bytes, grad_clip_workspace(n, counts));
+    const size_t need = grad_clip_workspace(n, counts);
+    rc = check_workspace(workspace, workspace_bytes, need);
+    if (rc == SCNN_OK) rc = check_apart({{result, 2 * sizeof(double)}, {workspace, need}}, {});
+    for (int i = 0; i < n && rc == SCNN_OK; ++i) {
+        const size_t bytes = (size_t)counts[i] * dtype_size(dtypes[i]);
+        if (bytes != 0)
+            rc = check_apart({{result, 2 * sizeof(double)}, {workspace, need}},
+                             {{grads[i], bytes}, {outs ? outs[i] : nullptr, bytes}});
+    }
     if (rc != SCNN_OK) return rc;
     SCNN_TRY(launch_grad_clip(n, grads, outs, counts, dtypes, max_norm, result, (double*)workspace, (hipStream_t)hip_stream));
     return SCNN_OK;

@@ -142,3 +142,12 @@ def test_linear_in_place_is_for_the_residual_alone():
         a["out"] = a[same]
         rc = L.linear_fwd(0, a["x"], 8, None, 8, a["w"], a["bias"], 8, 0, a["out"], a["out"], None, P(7 << 20), 1 << 20, None)
         assert rc == -1 and b"overlap" in L.scnn_last_error(), same
+
+
+def test_grad_clip_result_apart_from_the_workspace():
+    L = scnn.load_library()
+    g, count, kind = (P * 1)(1 << 20), (ctypes.c_int64 * 1)(10), (ctypes.c_int * 1)(0)
+    for result, ws in ((2 << 30, 2 << 30), ((2 << 30) + 8, 2 << 30), (1 << 20, 2 << 30), ((1 << 20) + 32, 2 << 30),
+                       (1 << 30, 1 << 20)):  # on the workspace, inside it, on a gradient, on its end; the workspace on one
+        rc = L.grad_clip(1, g, None, count, kind, ctypes.c_double(1.0), P(result), P(ws), 1 << 20, None)
+        assert rc == -1 and b"overlap" in L.scnn_last_error(), (result, ws)
