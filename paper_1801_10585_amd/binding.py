@@ -568,8 +568,10 @@ def _need(device: int, query: str, *sizes) -> int:
     return r
 
 
-def _ask(query: str, *sizes) -> int:
-    return _need.__wrapped__(-1, query, *sizes)
+def _ask(query: str, dtype: torch.dtype, *sizes) -> int:
+    if dtype not in DTYPES:
+        raise ValueError("dtype must be float32, bfloat16 or float16")
+    return _need.__wrapped__(-1, query, DTYPES[dtype], *sizes)
 
 
 def _scratch(workspace, need: int, like: torch.Tensor) -> Optional[torch.Tensor]:
@@ -595,7 +597,7 @@ def _cont(t: Optional[torch.Tensor]) -> Optional[torch.Tensor]:
 
 
 def linear_fwd_workspace(dtype: torch.dtype, rows: int, c_in: int, c_out: int) -> int:
-    return _ask("linear_fwd_workspace", DTYPES[dtype], int(rows), int(c_in), int(c_out))
+    return _ask("linear_fwd_workspace", dtype, int(rows), int(c_in), int(c_out))
 
 
 def linear_fwd(x, w, bias=None, *, act="none", residual=None, keep_pre=False, rows_dev=None, out=None, pre=None,
@@ -625,7 +627,7 @@ def linear_fwd(x, w, bias=None, *, act="none", residual=None, keep_pre=False, ro
 
 
 def linear_bwd_workspace(dtype: torch.dtype, rows: int, c_in: int, c_out: int, act="none") -> int:
-    return _ask("linear_bwd_workspace", DTYPES[dtype], int(rows), int(c_in), int(c_out), _activation(act))
+    return _ask("linear_bwd_workspace", dtype, int(rows), int(c_in), int(c_out), _activation(act))
 
 
 def linear_bwd(x, w, g, *, act="none", pre=None, want=(True, True, True), rows_dev=None, out=None, workspace=None,
@@ -677,7 +679,7 @@ def layer_norm_fwd(x, gamma=None, beta=None, *, eps=1e-5, rows_dev=None, out=Non
 
 
 def layer_norm_bwd_workspace(dtype: torch.dtype, rows: int, channels: int) -> int:
-    return _ask("layer_norm_bwd_workspace", DTYPES[dtype], int(rows), int(channels))
+    return _ask("layer_norm_bwd_workspace", dtype, int(rows), int(channels))
 
 
 def layer_norm_bwd(x, g, gamma, mean, rstd, *, want=(True, True, True), rows_dev=None, out=None, workspace=None,

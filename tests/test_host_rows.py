@@ -151,3 +151,11 @@ def test_grad_clip_result_apart_from_the_workspace():
                        (1 << 30, 1 << 20)):  # on the workspace, inside it, on a gradient, on its end; the workspace on one
         rc = L.grad_clip(1, g, None, count, kind, ctypes.c_double(1.0), P(result), P(ws), 1 << 20, None)
         assert rc == -1 and b"overlap" in L.scnn_last_error(), (result, ws)
+
+
+def test_workspace_queries_refuse_other_types():
+    for query, sizes in ((scnn.linear_fwd_workspace, (10, 8, 8)), (scnn.linear_bwd_workspace, (10, 8, 8)),
+                         (scnn.layer_norm_bwd_workspace, (10, 8))):
+        assert query(torch.bfloat16, *sizes) >= 256
+        with pytest.raises(ValueError, match="float32, bfloat16 or float16"):
+            query(torch.float64, *sizes)
