@@ -1186,8 +1186,9 @@ constexpr long long kChain = 65536;
 // and of 256 x 256 tiles: 8192 x 4096 x 4096 with gelu, residual and pre 281 against 313 (231 both without these), 4096 x
 // 4096 x 4096 x^T dz 142 against 124.
 // Large tiles read their operands least and pay from five on four compute units (one of 64 x 128 a unit) on, with k to hide
-// their start and end, where both sides fill them; short tiles for few rows; else 64 x 64.  k is split where that leaves compute units without a tile: one workgroup a unit was
-// the fastest of 1, 2, 4 and 8 at 12 of 16 shapes, within 15 per cent of it at the others.
+// their start and end, where both sides fill them; short tiles for few rows; else 64 x 64.  k is split where that leaves
+// compute units without a tile: one workgroup a unit was the fastest of 1, 2, 4 and 8 at 12 of 16 shapes, within 15 per cent
+// of it at the others.
 static TilePlan tile_plan(int dtype, long long m, long long n, long long k, bool forward, bool ring) {
     TilePlan t = {TileKind::kStaged, 64, 64, 1, round_up(k < 1 ? 1 : k, 64), 0};
     if (m < 1) return t;
