@@ -281,9 +281,10 @@ int linear_fwd(int dtype, const void* x, int64_t rows, const int64_t* rows_dev, 
  *   dz = g act'(z),  dx = dz w^T,  dw = x^T dz,  dbias = sum over rows of dz
  * (the gradient of residual is g itself).  pre: z as linear_fwd gave it; only
  * read where act is not SCNN_ACT_NONE.  dx [rows, c_in], dw [c_in, c_out], dbias
- * [c_out]: each nullable.  With 16-bit types dz is rounded to the type for the
- * two products (not for dbias), which adds an error of the size of the results'
- * own rounding.  With no rows dw and dbias are 0.  x may be null without dw, w
+ * [c_out]: each nullable.  With 16-bit types gelu's and silu's dz keeps 16 bits or
+ * more for the two products where c_in and c_out are at most 64; in wider layers
+ * it is rounded to the type (not for dbias), which adds an error of the size of
+ * the results' own rounding.  With no rows dw and dbias are 0.  x may be null without dw, w
  * without dx. */
 size_t linear_bwd_workspace(int dtype, int64_t rows, int64_t c_in, int64_t c_out, int act);
 int linear_bwd(int dtype, const void* x, int64_t rows, const int64_t* rows_dev, int64_t c_in, const void* w,

@@ -693,20 +693,33 @@ struct NarrowArgs {
     int c_in, c_out, act;
 };
 
-template <typename T, int P>
+// FINE: 16-bit types behind gelu or silu, whose dz has more bits than the type.  dz then enters both products as two bf16
+// numbers (2^-17 of it are left out), bf16 operands as they are and fp16 ones as two bf16 numbers, which hold them exactly; of
+// the products of parts all but low times low.  bf16 has fp32's range, so that no dz overflows or vanishes as it would in fp16.
+// (Rounded to the type, dz cost dw of 52417 x 35 -> 19 fp16 half of its accuracy.  us a call in a graph, this against dz rounded:
+// that layer 18.6 / 16.7; 643072 of 64 -> 64 gelu, bf16 97 / 88, fp16 105 / 89; 209645 of 24 -> 24 silu, bf16 23.0 / 21.5.  To look
+// for infinities in the sums, not in what is staged, saved 2 to 20 us of these.)
+template <typename T, int P, bool FINE>
 __global__ __launch_bounds__((NarrowShape<sizeof(T), P>::NT)) void k_linear_bwd_narrow(NarrowArgs p) {
-    constexpr bool SPLIT = std::is_same<T, float>::value;
-    constexpr int PARTS = SPLIT ? 3 : 1, ROWS = 64, CH = P / 8;
+    constexpr bool SPLIT = std::is_same<T, float>::value, HALF = std::is_same<T, _Float16>::value;
+    constexpr int ZP = SPLIT ? 3 : (FINE ? 2 : 1), XP = SPLIT ? 3 : (FINE && HALF ? 2 : 1);  // parts of dz; of x and w
+    constexpr int ROWS = 64, CH = P / 8;
     typedef NarrowShape<sizeof(T), P> S;
     constexpr int NT = S::NT, PIECES = ROWS * CH, PN = PIECES / NT, WPIECES = P * CH, WPN = (WPIECES + NT - 1) / NT;
     constexpr int XM = ROWS / S::XM / 16, XN = P / S::XN / 16, WM = P / S::WM / 16, WN = P / S::WN / 16;
-    __shared__ __align__(16) char s_w[PARTS * WPIECES * 16], s_z[2 * PARTS * PIECES * 16];
-    char* const s_x = s_z + PARTS * PIECES * 16;
+    __shared__ __align__(16) char s_w[XP * WPIECES * 16], s_z[(ZP + XP) * PIECES * 16];
+    char* const s_x = s_z + ZP * PIECES * 16;
     const long long rows = rows_of(p.rows, p.rows_dev);
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const T *const x = (const T*)p.x, *const w = (const T*)p.w, *const pre = (const T*)p.pre, *const g = (const T*)p.g;
     const int c8 = tid % CH * 8;  // first column of this thread's pieces
 
+    auto put_parts = [&](char* tile, int pieces, int at, const VecOf<float, 8>& v) {
+        const bf16x8 high = __builtin_convertvector(v, bf16x8);
+        const bf16x8 low = __builtin_convertvector(v - __builtin_convertvector(high, VecOf<float, 8>), bf16x8);
+        *(u32x4*)(tile + at) = __builtin_bit_cast(u32x4, high);
+        *(u32x4*)(tile + pieces * 16 + at) = __builtin_bit_cast(u32x4, low);
+    };
     auto put = [&](char* tile, int pieces, int at, const VecOf<T, 8>& v, int& odd) {
         if constexpr (SPLIT) {
             u32x4 q[2], part[3];
@@ -716,6 +729,8 @@ __global__ __launch_bounds__((NarrowShape<sizeof(T), P>::NT)) void k_linear_bwd_
             scnn::split8(q, part);
 #pragma unroll
             for (int k = 0; k < 3; ++k) *(u32x4*)(tile + k * pieces * 16 + at) = part[k];
+        } else if constexpr (FINE && HALF) {
+            put_parts(tile, pieces, at, __builtin_convertvector(v, VecOf<float, 8>));
         } else {
             *(u32x4*)(tile + at) = __builtin_bit_cast(u32x4, v);
         }
@@ -746,11 +761,20 @@ __global__ __launch_bounds__((NarrowShape<sizeof(T), P>::NT)) void k_linear_bwd_
     float db[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) db[i] = 0.0f;
-    auto multiply = [&](const u32x4 (&a)[PARTS], const u32x4 (&b)[PARTS], f4 acc) {  // (b's rows become the lanes' rows)
+    auto multiply = [&](const auto& a, const auto& b, f4 acc) {  // (b's rows become the lanes' rows)
+        constexpr int NA = sizeof(a) / 16, NB = sizeof(b) / 16;
         if constexpr (SPLIT) {
             f4 large, small;
             split_products(a, b[0], b[1], b[2], large, small);
             return acc + (large + small);
+        } else if constexpr (FINE) {
+#pragma unroll
+            for (int i = NA - 1; i >= 0; --i)
+#pragma unroll
+                for (int j = NB - 1; j >= 0; --j)
+                    if (i + j < 2)
+                        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a[i]), __builtin_bit_cast(bf16x8, b[j]), acc, 0, 0, 0);
+            return acc;
         } else if constexpr (std::is_same<T, __bf16>::value) {
             return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a[0]), __builtin_bit_cast(bf16x8, b[0]), acc, 0, 0, 0);
         } else {
@@ -759,6 +783,49 @@ __global__ __launch_bounds__((NarrowShape<sizeof(T), P>::NT)) void k_linear_bwd_
     };
     const long long step = (long long)gridDim.x * ROWS;
     const int xm = wave / S::XN * XM * 16, xn = wave % S::XN * XN * 16, wm = wave / S::WN * WM * 16, wn = wave % S::WN * WN * 16;
+    // The same with fp32 products, operands from memory, for values that the parts do not hold.
+    const int q4 = lane >> 4, i16 = lane & 15;
+    auto z_at = [&](long long row, int n) {
+        if (row >= rows || n >= p.c_out) return 0.0f;
+        const float v = (float)g[row * p.c_out + n];
+        return p.act != SCNN_ACT_NONE ? activate_back(v, (float)pre[row * p.c_out + n], p.act) : v;
+    };
+    auto dx_fp32 = [&](long long at, f4 (&dx)[XM][XN]) {
+        for (int k = 0; k < p.c_out; k += 4)
+#pragma unroll
+            for (int i = 0; i < XM; ++i) {
+                const float vz = z_at(at + xm + i * 16 + i16, k + q4);
+#pragma unroll
+                for (int j = 0; j < XN; ++j) {
+                    const int n = xn + j * 16 + i16;
+                    const float vw = n < p.c_in && k + q4 < p.c_out ? (float)w[n * p.c_out + k + q4] : 0.0f;
+                    dx[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(vw, vz, dx[i][j], 0, 0, 0);
+                }
+            }
+    };
+    auto dw_fp32 = [&](long long at) {
+        for (int k = 0; k < ROWS; k += 4)
+#pragma unroll
+            for (int i = 0; i < WM; ++i) {
+                const int m = wm + i * 16 + i16;
+                const float vx = at + k + q4 < rows && m < p.c_in ? (float)x[(at + k + q4) * p.c_in + m] : 0.0f;
+#pragma unroll
+                for (int j = 0; j < WN; ++j)
+                    dw[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(z_at(at + k + q4, wn + j * 16 + i16), vx, dw[i][j], 0, 0, 0);
+            }
+    };
+    // FINE: low parts beside an infinity make a NaN of what should stay one; either shows in the sums, which the wave then forms
+    // anew.
+    auto odd_sums = [&](const auto& acc) {
+        float none = 0.0f;
+#pragma unroll
+        for (int i = 0; i < (int)(sizeof(acc) / sizeof(acc[0])); ++i)
+#pragma unroll
+            for (int j = 0; j < (int)(sizeof(acc[0]) / 16); ++j)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) none = __builtin_fmaf(acc[i][j][c], 0.0f, none);
+        return __any(none != none) != 0;
+    };
     long long first = (long long)blockIdx.x * ROWS;
     if (first < rows) fetch(first);
     for (; first < rows; first += step) {
@@ -768,16 +835,19 @@ __global__ __launch_bounds__((NarrowShape<sizeof(T), P>::NT)) void k_linear_bwd_
         for (int i = 0; i < PN; ++i) {
             const int r = (i * NT + tid) / CH;
             VecOf<T, 8> z = rg[i];
+            VecOf<float, 8> wide;
 #pragma unroll
             for (int c = 0; c < 8; ++c) {
                 float v = (float)rg[i][c];
                 if (p.act != SCNN_ACT_NONE) {
                     v = first + r < rows && c8 + c < p.c_out ? activate_back(v, (float)rp[i][c], p.act) : 0.0f;
-                    z[c] = (T)v;
+                    z[c] = (T)v;  // (fp32; relu's dz is g or 0)
                 }
+                wide[c] = v;
                 db[c] += v;
             }
-            put(s_z, PIECES, staged<false, P>(r, tid % CH), z, odd);
+            if constexpr (FINE) put_parts(s_z, PIECES, staged<false, P>(r, tid % CH), wide);
+            else put(s_z, PIECES, staged<false, P>(r, tid % CH), z, odd);
             if (x) put(s_x, PIECES, staged<false, P>(r, tid % CH), rx[i], odd);
         }
         bool exact = true;
@@ -785,10 +855,10 @@ __global__ __launch_bounds__((NarrowShape<sizeof(T), P>::NT)) void k_linear_bwd_
         else __syncthreads();
         if (first + step < rows) fetch(first + step);
         // dz [64][c_out], rows of dz one way and columns the other
-        auto rows_of_z = [&](int base, int kk, u32x4 (&f)[PARTS]) {
+        auto rows_of_z = [&](int base, int kk, u32x4 (&f)[ZP]) {
             const int r = base + (lane & 15);
 #pragma unroll
-            for (int q = 0; q < PARTS; ++q) f[q] = *(const u32x4*)(s_z + q * PIECES * 16 + staged<false, P>(r, kk * 4 + (lane >> 4)));
+            for (int q = 0; q < ZP; ++q) f[q] = *(const u32x4*)(s_z + q * PIECES * 16 + staged<false, P>(r, kk * 4 + (lane >> 4)));
         };
         f4 dx[XM][XN];
 #pragma unroll
@@ -800,15 +870,15 @@ __global__ __launch_bounds__((NarrowShape<sizeof(T), P>::NT)) void k_linear_bwd_
 #pragma unroll
                 for (int kk = 0; kk < P / 32; ++kk) {
                     if (kk * 32 >= p.c_out) break;
-                    u32x4 fz[XM][PARTS];
+                    u32x4 fz[XM][ZP];
 #pragma unroll
                     for (int i = 0; i < XM; ++i) rows_of_z(xm + i * 16, kk, fz[i]);
 #pragma unroll
                     for (int j = 0; j < XN; ++j) {
                         if (xn + j * 16 >= p.c_in) break;
-                        u32x4 fw[PARTS];
+                        u32x4 fw[XP];
 #pragma unroll
-                        for (int q = 0; q < PARTS; ++q) fw[q] = fragment<true, P>(s_w + q * WPIECES * 16, xn + j * 16, kk);
+                        for (int q = 0; q < XP; ++q) fw[q] = fragment<true, P>(s_w + q * WPIECES * 16, xn + j * 16, kk);
 #pragma unroll
                         for (int i = 0; i < XM; ++i) dx[i][j] = multiply(fw, fz[i], dx[i][j]);
                     }
@@ -817,52 +887,34 @@ __global__ __launch_bounds__((NarrowShape<sizeof(T), P>::NT)) void k_linear_bwd_
 #pragma unroll
                 for (int kk = 0; kk < ROWS / 32; ++kk) {
                     if (wm >= p.c_in) break;
-                    u32x4 fx[WM][PARTS];
+                    u32x4 fx[WM][XP];
 #pragma unroll
                     for (int i = 0; i < WM; ++i)
 #pragma unroll
-                        for (int q = 0; q < PARTS; ++q) fx[i][q] = fragment<false, P>(s_x + q * PIECES * 16, wm + i * 16, kk);
+                        for (int q = 0; q < XP; ++q) fx[i][q] = fragment<false, P>(s_x + q * PIECES * 16, wm + i * 16, kk);
 #pragma unroll
                     for (int j = 0; j < WN; ++j) {
                         if (wn + j * 16 >= p.c_out) break;
-                        u32x4 fz[PARTS];
+                        u32x4 fz[ZP];
 #pragma unroll
-                        for (int q = 0; q < PARTS; ++q) fz[q] = fragment<false, P>(s_z + q * PIECES * 16, wn + j * 16, kk);
+                        for (int q = 0; q < ZP; ++q) fz[q] = fragment<false, P>(s_z + q * PIECES * 16, wn + j * 16, kk);
 #pragma unroll
                         for (int i = 0; i < WM; ++i) dw[i][j] = multiply(fz, fx[i], dw[i][j]);
                     }
                 }
         } else if constexpr (SPLIT) {
-            // a value among these rows or in w that the three parts do not hold: fp32 products, operands from memory
-            const int q = lane >> 4, i16 = lane & 15;
-            auto z_at = [&](long long row, int n) {
-                if (row >= rows || n >= p.c_out) return 0.0f;
-                const float v = (float)g[row * p.c_out + n];
-                return p.act != SCNN_ACT_NONE ? activate_back(v, (float)pre[row * p.c_out + n], p.act) : v;
-            };
-            if (p.dx)
-                for (int k = 0; k < p.c_out; k += 4)
-#pragma unroll
-                    for (int i = 0; i < XM; ++i) {
-                        const float vz = z_at(first + xm + i * 16 + i16, k + q);
-#pragma unroll
-                        for (int j = 0; j < XN; ++j) {
-                            const int n = xn + j * 16 + i16;
-                            const float vw = n < p.c_in && k + q < p.c_out ? (float)w[n * p.c_out + k + q] : 0.0f;
-                            dx[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(vw, vz, dx[i][j], 0, 0, 0);
-                        }
-                    }
-            if (x)
-                for (int k = 0; k < ROWS; k += 4)
-#pragma unroll
-                    for (int i = 0; i < WM; ++i) {
-                        const int m = wm + i * 16 + i16;
-                        const float vx = first + k + q < rows && m < p.c_in ? (float)x[(first + k + q) * p.c_in + m] : 0.0f;
-#pragma unroll
-                        for (int j = 0; j < WN; ++j)
-                            dw[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(z_at(first + k + q, wn + j * 16 + i16), vx, dw[i][j], 0, 0, 0);
-                    }
+            // a value among these rows or in w that the three parts do not hold
+            if (p.dx) dx_fp32(first, dx);
+            if (x) dw_fp32(first);
         }
+        if constexpr (FINE)
+            if (p.dx && odd_sums(dx)) {
+#pragma unroll
+                for (int i = 0; i < XM; ++i)
+#pragma unroll
+                    for (int j = 0; j < XN; ++j) dx[i][j] = f4{0.f, 0.f, 0.f, 0.f};
+                dx_fp32(first, dx);
+            }
         if (p.dx)
 #pragma unroll
             for (int i = 0; i < XM; ++i) {
@@ -886,6 +938,14 @@ __global__ __launch_bounds__((NarrowShape<sizeof(T), P>::NT)) void k_linear_bwd_
             }
     }
     if (!p.part) return;
+    if constexpr (FINE)
+        if (x && odd_sums(dw)) {
+#pragma unroll
+            for (int i = 0; i < WM; ++i)
+#pragma unroll
+                for (int j = 0; j < WN; ++j) dw[i][j] = f4{0.f, 0.f, 0.f, 0.f};
+            for (long long at = (long long)blockIdx.x * ROWS; at < rows; at += step) dw_fp32(at);
+        }
     float* __restrict__ mine = p.part + (long long)blockIdx.x * ((long long)p.c_in * p.c_out + p.c_out);
 #pragma unroll
     for (int i = 0; i < WM; ++i) {
@@ -902,7 +962,7 @@ __global__ __launch_bounds__((NarrowShape<sizeof(T), P>::NT)) void k_linear_bwd_
     // column sums: threads with the same columns lie CH apart
     __syncthreads();
     float(*s_db)[P] = (float(*)[P])s_z;
-    static_assert(NT / CH * P * 4 <= 2 * PARTS * PIECES * 16, "room for the column sums");
+    static_assert(NT / CH * P * 4 <= (ZP + XP) * PIECES * 16, "room for the column sums");
 #pragma unroll
     for (int c = 0; c < 8; ++c) s_db[tid / CH][c8 + c] = db[c];
     __syncthreads();
@@ -1401,8 +1461,12 @@ static hipError_t narrow_bwd(int dtype, const LinearCall& c, int width, hipStrea
     p.c_in = (int)c.c_in; p.c_out = (int)c.c_out; p.act = c.act;
     if (!p.part && !p.dx) return hipSuccess;
     const int groups = narrow_groups(c.rows);
-    if (width == 32) hipLaunchKernelGGL((k_linear_bwd_narrow<T, 32>), dim3(groups), dim3((NarrowShape<sizeof(T), 32>::NT)), 0, s, p);
-    else hipLaunchKernelGGL((k_linear_bwd_narrow<T, 64>), dim3(groups), dim3((NarrowShape<sizeof(T), 64>::NT)), 0, s, p);
+    constexpr bool PARTS = sizeof(T) == 2;
+    const bool fine = PARTS && (c.act == SCNN_ACT_GELU || c.act == SCNN_ACT_SILU);
+    auto kernel = width == 32 ? (fine ? k_linear_bwd_narrow<T, 32, PARTS> : k_linear_bwd_narrow<T, 32, false>)
+                              : (fine ? k_linear_bwd_narrow<T, 64, PARTS> : k_linear_bwd_narrow<T, 64, false>);
+    const int threads = width == 32 ? NarrowShape<sizeof(T), 32>::NT : NarrowShape<sizeof(T), 64>::NT;
+    hipLaunchKernelGGL(kernel, dim3(groups), dim3(threads), 0, s, p);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || !p.part) return e;
     const long long filter = c.c_in * c.c_out;

@@ -1,0 +1,79 @@
+"""dz = g act'(pre) of 16-bit layers in the products behind dx and dw: its bits and its range."""
+import pytest
+import torch
+
+import paper_1801_10585_amd as scnn
+from . import rows_ref as ref
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+HALVES = (torch.bfloat16, torch.float16)
+# (the larger of c_in and c_out: one pass of up to 32 channels, one of up to 64)
+NARROW = (24, 50)
+
+
+def normal(seed, *shape):
+    return torch.randn(*shape, generator=torch.Generator().manual_seed(seed), dtype=torch.float64)
+
+
+def grads(x, w, g, name, pre):
+    return scnn.linear_bwd(x.to(DEV), w.to(DEV), g.to(DEV), act=name, pre=pre.to(DEV))
+
+
+@pytest.mark.parametrize("name", ["gelu", "silu"])
+@pytest.mark.parametrize("dtype", HALVES, ids=str)
+@pytest.mark.parametrize("wide", NARROW)
+def test_products_of_one_term_are_rounded_once(wide, dtype, name):
+    # one channel out: dx = dz w, one product an element; one row: dw = x dz.  Slopes of pre in 0.5 .. 3 are 0.7 and more, good
+    # to 16 U32 (1 + 3) of 1; dz as two bf16 numbers leaves out 2^-17 of it.
+    slack = 2.0 ** -17 + 16 * 4 / 0.7 * ref.U32 + 8 * ref.U32
+    for rows, c_in, c_out in ((200, wide, 1), (1, wide, wide)):
+        x, w = normal(1, rows, c_in).to(dtype), normal(2, c_in, c_out).to(dtype)
+        g, pre = normal(3, rows, c_out).to(dtype), (0.5 + 2.5 * torch.rand(rows, c_out, generator=torch.Generator().manual_seed(4))).to(dtype)
+        dz = g.double() * ref.act_slope(pre.double(), name)
+        dx, dw, _ = grads(x, w, g, name, pre)
+        for got, want in ((dx, dz @ w.double().t()) if c_out == 1 else (dw, x.double().t() @ dz),):
+            ref.assert_within(got, (want, (ref.half(dtype) + slack) * want.abs() + ref.tiny(dtype)), f"{rows} x {c_in} -> {c_out}")
+
+
+@pytest.mark.parametrize("wide", NARROW)
+def test_fp16_gradients_at_the_ends_of_the_range(wide):
+    dtype = torch.float16
+    # (activation, pre, g, the other operand): |dz| above 65504; |dz| below 2^-25
+    for name, z, v, other in (("gelu", 1.4, 60000.0, 2.0 ** -9), ("silu", 2.4, 60000.0, 2.0 ** -9),
+                              ("gelu", -3.0, 2.0 ** -20, 4096.0), ("silu", -12.0, 2.0 ** -16, 4096.0)):
+        pre = torch.full((70, wide), z, dtype=dtype)
+        g = torch.zeros(70, wide, dtype=dtype)
+        g[::7, 3] = v
+        g[3::7, 3] = -v
+        g[:, 5] = torch.where(torch.arange(70) % 2 == 0, v, -v).to(dtype)
+        x = torch.full((70, wide), other, dtype=dtype)
+        x[::3] = 0
+        w = torch.full((wide, wide), other, dtype=dtype)
+        w[1::2] = -other
+        dz = g.double() * ref.act_slope(pre.double(), name)
+        assert float(dz.abs().max()) > 65504 or float(dz.abs().max()) < 2.0 ** -25
+        got = grads(x, w, g, name, pre)
+        # the slope of silu at -12 is a difference of terms up to 12 times the sigmoid: 16 U32 of their sum each
+        part = g.double().abs() * 16 * ref.U32 * (1 + pre.double().abs()) * torch.sigmoid(pre.double() + 3)
+        for r, have, a, b in (("dx", got[0], dz @ w.double().t(), (dz.abs() * 2.0 ** -16 + part) @ w.double().abs().t()),
+                              ("dw", got[1], x.double().t() @ dz, x.double().t().abs() @ (dz.abs() * 2.0 ** -16 + part))):
+            assert float(a.abs().max()) < 60000
+            ref.assert_within(have, (a, b + ref.half(dtype) * (a.abs() + b) + ref.tiny(dtype)), f"{r}, {name} at {z}")
+
+
+@pytest.mark.parametrize("name", ["gelu", "silu"])
+@pytest.mark.parametrize("dtype", HALVES, ids=str)
+@pytest.mark.parametrize("wide", NARROW)
+def test_infinities_and_nan_stay_where_the_formula_has_them(wide, dtype, name):
+    rows = 300
+    for where in ("g", "x", "w"):
+        for value in (float("inf"), float("nan")):
+            t = {"x": normal(5, rows, wide).to(dtype), "w": normal(6, wide, wide).to(dtype), "g": normal(7, rows, wide).to(dtype)}
+            t[where][11, 4] = value
+            pre = normal(8, rows, wide).abs().add(0.5).to(dtype)
+            got = grads(t["x"], t["w"], t["g"], name, pre)
+            for have, want in zip(got, ref.linear_bwd(t["x"], t["w"], t["g"], name, pre, dtype)):
+                odd = ~torch.isfinite(want[0])
+                want = (want[0], torch.where(odd, torch.zeros_like(want[1]), want[1]))
+                ref.assert_within(have, want, f"{where} {value}")
