@@ -284,7 +284,9 @@ int linear_fwd(int dtype, const void* x, int64_t rows, const int64_t* rows_dev, 
  * [c_out]: each nullable.  With 16-bit types gelu's and silu's dz keeps 16 bits or
  * more for the two products where c_in and c_out are at most 64; in wider layers
  * it is rounded to the type (not for dbias), which adds an error of the size of
- * the results' own rounding.  With no rows dw and dbias are 0.  x may be null without dw, w
+ * the results' own rounding; fp16 holds it scaled by a power of two, so that it
+ * does not overflow and only what is below 2^-39 of the call's largest finite
+ * |g| becomes 0.  With no rows dw and dbias are 0.  x may be null without dw, w
  * without dx. */
 size_t linear_bwd_workspace(int dtype, int64_t rows, int64_t c_in, int64_t c_out, int act);
 int linear_bwd(int dtype, const void* x, int64_t rows, const int64_t* rows_dev, int64_t c_in, const void* w,

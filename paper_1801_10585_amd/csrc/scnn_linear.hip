@@ -88,6 +88,7 @@ struct LinearArgs {
     long long k_split; // k a workgroup sums, a multiple of 64
     int act;
     int rows_k;
+    const float* scale;  // fp16, nullable: what the sums are multiplied by (a power of two)
 };
 
 // Eight fp32 values as three bf16 numbers each, to nearest (split8), and what these leave of them, if anything: `lost`
@@ -143,6 +144,12 @@ __device__ __forceinline__ void finish4(const LinearArgs& p, long long m, long l
         }
     };
     float t[4];
+    if constexpr (std::is_same<T, _Float16>::value)
+        if (p.scale) {
+            const float by = *p.scale;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) z[j] *= by;
+        }
     if (p.bias) {
         load4(p.bias, n, t);
 #pragma unroll
@@ -168,6 +175,9 @@ __device__ __forceinline__ void finish_tile(const LinearArgs& p, long long m, lo
     typedef VecOf<T, C> V;
     constexpr int J = TN * 4 / C;
     V bias[J], residual[TM][J];
+    float by = 1.0f;
+    if constexpr (std::is_same<T, _Float16>::value)
+        if (p.scale) by = *p.scale;
 #pragma unroll
     for (int j = 0; j < J; ++j) {
         bias[j] = V{};
@@ -189,6 +199,7 @@ __device__ __forceinline__ void finish_tile(const LinearArgs& p, long long m, lo
 #pragma unroll
             for (int c = 0; c < C; ++c) {
                 z[c] = acc[i][j * (C / 4) + c / 4][c & 3];
+                if constexpr (std::is_same<T, _Float16>::value) z[c] *= by;
                 if (p.bias) z[c] += (float)bias[j][c];
                 r[c] = (T)z[c];
             }
@@ -629,16 +640,77 @@ __global__ __launch_bounds__(256) void k_linear_join(LinearArgs p, int splits) {
     finish4<T>(p, m, n, out);
 }
 
+// Largest finite magnitude of fp16 g [rows, cols] among this workgroup's values, as its bits: peak [gridDim.x].  A read of g, four
+// loads a thread on their way: it makes a call of 4096 x 4096 -> 4096 longer by 7 us (290 / 284, 5 TB/s), small ones by 4.
+constexpr int kPeaks = 256, kPeakThreads = 1024;
+__global__ __launch_bounds__(kPeakThreads) void k_grad_peak(const _Float16* __restrict__ g, long long rows_cap,
+                                                   const long long* __restrict__ rows_dev, long long cols,
+                                                   unsigned* __restrict__ peak) {
+    __shared__ unsigned s_max[kPeakThreads / 64];
+    const long long n = rows_of(rows_cap, rows_dev) * cols, step = (long long)gridDim.x * kPeakThreads * 8;
+    typedef VecOf<unsigned short, 8> Bits;
+    Bits most = {};
+    auto take = [&](VecOf<_Float16, 8> v) {
+        const Bits bits = __builtin_bit_cast(Bits, v) & (unsigned short)0x7fff;
+        const Bits fine = bits < (unsigned short)0x7c00 ? bits : Bits{};
+        most = fine > most ? fine : most;
+    };
+    long long i = ((long long)blockIdx.x * kPeakThreads + threadIdx.x) * 8;
+    for (; i + 3 * step + 8 <= n; i += 4 * step) {
+        VecOf<_Float16, 8> v[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = load_raw<_Float16>(g + i + k * step, 8, true);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) take(v[k]);
+    }
+    for (; i < n; i += step) take(load_raw<_Float16>(g + i, (int)(n - i < 8 ? n - i : 8), n >= 8));
+    unsigned top = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) top = most[j] > top ? most[j] : top;
+    for (int d = 1; d < 64; d <<= 1) {
+        const unsigned o = __shfl_xor(top, d, 64);
+        top = o > top ? o : top;
+    }
+    if ((threadIdx.x & 63) == 0) s_max[threadIdx.x >> 6] = top;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int k = 1; k < kPeakThreads / 64; ++k) top = s_max[k] > top ? s_max[k] : top;
+        peak[blockIdx.x] = top;
+    }
+}
+
 // dz = g act'(pre) rounded to the operands' type (what the matrix instructions take), and this workgroup's column sums of
 // the dz before that rounding: part [gridDim.y][cols].  A block is tn threads wide, each a 16-byte vector of columns.  Bound by
 // memory: 4096 x 4096 bf16 gelu 21.5 us, 4.7 TB/s.
+// fp16 with peaks: dz is held times the power of two that takes the largest finite |g| to 2^14 .. 2^15, so that none (slopes end
+// at 1.13) passes fp16's end and only what is 2^-39 of that |g| and less is rounded to 0; unscale receives the inverse.
 template <typename T>
 __global__ __launch_bounds__(256) void k_act_back(const T* __restrict__ g, const T* __restrict__ pre, long long rows_cap,
                                                   const long long* __restrict__ rows_dev, long long cols, int act, int tn,
-                                                  T* __restrict__ dz, float* __restrict__ part) {
+                                                  T* __restrict__ dz, float* __restrict__ part,
+                                                  const unsigned* __restrict__ peak, int peaks, float* __restrict__ unscale) {
     constexpr int V = kVec<T>;
     __shared__ float s_sum[256][V];
     const long long rows = rows_of(rows_cap, rows_dev);
+    float scale = 1.0f;
+    if constexpr (std::is_same<T, _Float16>::value)
+        if (peak) {
+            __shared__ unsigned s_max[4];
+            unsigned most = (int)threadIdx.x < peaks ? peak[threadIdx.x] : 0;
+            for (int d = 1; d < 64; d <<= 1) {
+                const unsigned o = __shfl_xor(most, d, 64);
+                most = o > most ? o : most;
+            }
+            if ((threadIdx.x & 63) == 0) s_max[threadIdx.x >> 6] = most;
+            __syncthreads();
+            for (int i = 0; i < 4; ++i) most = s_max[i] > most ? s_max[i] : most;
+            if (most > 0) {
+                const float m = (float)__builtin_bit_cast(_Float16, (unsigned short)most);  // (normal in fp32: its exponent)
+                const int up = 14 - ((int)(__float_as_uint(m) >> 23) - 127);
+                scale = __uint_as_float((unsigned)(127 + up) << 23);
+            }
+            if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *unscale = 1.0f / scale;
+        }
     const int tc = threadIdx.x % tn, tr = threadIdx.x / tn, nr = 256 / tn;
     const long long c = ((long long)blockIdx.x * tn + tc) * V;
     const int n = (int)(cols - c < V ? cols - c : V);
@@ -653,7 +725,14 @@ __global__ __launch_bounds__(256) void k_act_back(const T* __restrict__ g, const
                 load_elems<T>(pre + row * cols + c, n, cols >= V, z);
 #pragma unroll
                 for (int i = 0; i < V; ++i) v[i] = activate_back(v[i], z[i], act);
-                store_elems<T>(dz + row * cols + c, n, v);
+                if constexpr (std::is_same<T, _Float16>::value) {
+                    float held[V];
+#pragma unroll
+                    for (int i = 0; i < V; ++i) held[i] = v[i] * scale;
+                    store_elems<T>(dz + row * cols + c, n, held);
+                } else {
+                    store_elems<T>(dz + row * cols + c, n, v);
+                }
             }
 #pragma unroll
             for (int i = 0; i < V; ++i) sum[i] += v[i];
@@ -1473,13 +1552,18 @@ static hipError_t narrow_bwd(int dtype, const LinearCall& c, int width, hipStrea
     return launch_column_sums(p.part, groups, filter + c.c_out, filter, c.dw, c.dbias, dtype, s);
 }
 
-struct BackSpace { size_t dz, sums, dx, dw, total; };
+// fp16 gradients of gelu and silu hold a scaled dz.
+static bool scaled_dz(int dtype, int act) { return dtype == SCNN_F16 && (act == SCNN_ACT_GELU || act == SCNN_ACT_SILU); }
+
+struct BackSpace { size_t dz, peak, sums, dx, dw, total; };
 static BackSpace back_space(int dtype, long long rows, long long c_in, long long c_out, int act) {
     BackSpace b = {};
     const size_t e = dtype == SCNN_F32 ? 4 : 2;
     size_t at = 0;
     b.dz = at;
     if (act != SCNN_ACT_NONE) at += (size_t)round_up(rows * c_out * (long long)e, 256);
+    b.peak = at;  // (behind the peaks: the inverse of the scale)
+    if (scaled_dz(dtype, act)) at += round_up((kPeaks + 1) * 4, 256);
     b.sums = at;
     at += (size_t)round_up((long long)back_plan(rows, c_out, dtype).parts * c_out * 4, 256);
     b.dx = b.dw = at;  // (the two products run one after the other and share their partial sums' place)
@@ -1502,18 +1586,30 @@ static hipError_t linear_bwd_typed(int dtype, const LinearCall& c, hipStream_t s
     const void* dz = c.g;
     if (c.act != SCNN_ACT_NONE) dz = ws + at.dz;
     const bool products = c.dx || c.dw;
+    LinearArgs p = {};
+    unsigned* peak = nullptr;
+    int peaks = 0;
+    if constexpr (std::is_same<T, _Float16>::value)
+        if (products && scaled_dz(dtype, c.act)) {
+            peak = (unsigned*)(ws + at.peak);
+            p.scale = (const float*)(peak + kPeaks);
+            const long long need = (c.rows * c.c_out + kPeakThreads * 8 - 1) / (kPeakThreads * 8);
+            peaks = (int)(need < 1 ? 1 : (need < kPeaks ? need : kPeaks));
+            hipLaunchKernelGGL(k_grad_peak, dim3((unsigned)peaks), dim3(kPeakThreads), 0, s, (const _Float16*)c.g, c.rows, c.rows_dev,
+                               c.c_out, peak);
+        }
     if (c.dbias || (products && c.act != SCNN_ACT_NONE)) {
         const BackPlan b = back_plan(c.rows, c.c_out, dtype);
         const long long wide = (long long)b.tn * kVec<T>;
         float* const sums = c.dbias ? (float*)(ws + at.sums) : nullptr;
         hipLaunchKernelGGL((k_act_back<T>), dim3((unsigned)((c.c_out + wide - 1) / wide), (unsigned)b.parts), dim3(256), 0, s,
-                           (const T*)c.g, (const T*)c.pre_in, c.rows, c.rows_dev, c.c_out, c.act, b.tn, (T*)(ws + at.dz), sums);
+                           (const T*)c.g, (const T*)c.pre_in, c.rows, c.rows_dev, c.c_out, c.act, b.tn, (T*)(ws + at.dz), sums,
+                           peak, peaks, (float*)p.scale);
         if (c.dbias) {
             const hipError_t e = launch_column_sums(sums, b.parts, c.c_out, c.c_out, c.dbias, nullptr, dtype, s);
             if (e != hipSuccess) return e;
         }
     }
-    LinearArgs p = {};
     p.rows_dev = c.rows_dev;
     p.act = SCNN_ACT_NONE;
     if (c.dx && c.rows > 0) {

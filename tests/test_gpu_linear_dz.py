@@ -77,3 +77,55 @@ def test_infinities_and_nan_stay_where_the_formula_has_them(wide, dtype, name):
                 odd = ~torch.isfinite(want[0])
                 want = (want[0], torch.where(odd, torch.zeros_like(want[1]), want[1]))
                 ref.assert_within(have, want, f"{where} {value}")
+
+
+# (rows, c_in, c_out): tiles staged through registers, tiles copied to LDS, both with a split sum over rows
+WIDE = ((70, 70, 67), (70, 264, 72), (2100, 67, 70), (2100, 136, 72), (70, 64, 2000))
+
+
+@pytest.mark.parametrize("size", WIDE, ids=str)
+def test_fp16_gradients_of_wide_layers_at_the_ends_of_the_range(size):
+    dtype = torch.float16
+    rows, c_in, c_out = size
+    for name, z, v, other in (("gelu", 1.4, 60000.0, 2.0 ** -9), ("silu", 2.4, 60000.0, 2.0 ** -9),
+                              ("gelu", -3.0, 2.0 ** -20, 4096.0), ("silu", -12.0, 2.0 ** -16, 4096.0)):
+        pre = torch.full((rows, c_out), z, dtype=dtype)
+        g = torch.zeros(rows, c_out, dtype=dtype)
+        g[::7, 3] = v
+        g[3::7, 3] = -v
+        g[:, 5] = torch.where(torch.arange(rows) % 2 == 0, v, -v).to(dtype)
+        x = torch.full((rows, c_in), other, dtype=dtype)
+        x[::3] = 0
+        x[100:] *= 0.01
+        w = torch.full((c_in, c_out), other, dtype=dtype)
+        w[1::2] = -other
+        dz = g.double() * ref.act_slope(pre.double(), name)
+        got = grads(x, w, g, name, pre)
+        # dz's own rounding; the rest as in the narrow layers
+        part = dz.abs() * (ref.half(dtype) + 2.0 ** -16) + g.double().abs() * 16 * ref.U32 * (1 + pre.double().abs()) * torch.sigmoid(pre.double() + 3)
+        for r, have, a, b in (("dx", got[0], dz @ w.double().t(), part @ w.double().abs().t()),
+                              ("dw", got[1], x.double().t() @ dz, x.double().t().abs() @ part)):
+            assert float(a.abs().max()) < 60000
+            ref.assert_within(have, (a, b + ref.half(dtype) * (a.abs() + b) + ref.tiny(dtype)), f"{r}, {name} at {z}")
+
+
+@pytest.mark.parametrize("size", WIDE, ids=str)
+def test_fp16_infinities_do_not_move_the_scale(size):
+    rows, c_in, c_out = size
+    for value in (float("inf"), float("nan")):
+        x, w = normal(1, rows, c_in).half(), normal(2, c_in, c_out).half()
+        g, pre = (normal(3, rows, c_out) * 1e-3).half(), normal(4, rows, c_out).abs().add(0.5).half()
+        g[11, 4] = value
+        for have, want in zip(grads(x, w, g, "gelu", pre), ref.linear_bwd(x, w, g, "gelu", pre, torch.float16)):
+            odd = ~torch.isfinite(want[0])
+            ref.assert_within(have, (want[0], torch.where(odd, torch.zeros_like(want[1]), want[1])), str(value))
+    # nothing but zeros; rows past the count hold the largest number, which is not looked at
+    count = torch.tensor([rows // 2], device=DEV)
+    x, w, pre = (normal(5, rows, c_in).half().to(DEV), normal(6, c_in, c_out).half().to(DEV), normal(7, rows, c_out).half().to(DEV))
+    g = torch.zeros(rows, c_out, dtype=torch.float16, device=DEV)
+    assert not any(t.any() for t in scnn.linear_bwd(x, w, g, act="silu", pre=pre))
+    g[:] = (normal(8, rows, c_out) * 1e-6).half()
+    short = scnn.linear_bwd(x, w, g, act="silu", pre=pre, rows_dev=count)
+    g[rows // 2:] = 65504.0
+    again = scnn.linear_bwd(x, w, g, act="silu", pre=pre, rows_dev=count)
+    assert torch.equal(short[0][:rows // 2], again[0][:rows // 2]) and torch.equal(short[1], again[1]) and torch.equal(short[2], again[2])
