@@ -297,7 +297,8 @@ int linear_bwd(int dtype, const void* x, int64_t rows, const int64_t* rows_dev, 
  *   mean = sum x / C,  var = sum (x - mean)^2 / C,  rstd = 1 / sqrt(var + eps),
  *   out = (x - mean) rstd gamma + beta
  * gamma, beta [channels] (nullable: 1 and 0); mean, rstd fp32 [rows] (nullable)
- * are what layer_norm_bwd needs.  eps >= 0; with eps 0 a row of equal values
+ * are what layer_norm_bwd needs.  Deviations are taken from the unrounded mean;
+ * their squares are summed in fp32 (deviations past 1e19 overflow it).  eps >= 0; with eps 0 a row of equal values
  * gives NaN, as the formula does.  channels up to 2^28. */
 int layer_norm_fwd(int dtype, const void* x, int64_t rows, const int64_t* rows_dev, int64_t channels, const void* gamma,
                    const void* beta, double eps, void* out, float* mean, float* rstd, void* hip_stream);
@@ -306,7 +307,8 @@ int layer_norm_fwd(int dtype, const void* x, int64_t rows, const int64_t* rows_d
  * xh = (x - mean) rstd and h = g gamma:
  *   dx = rstd (h - sum(h) / C - xh sum(h xh) / C)   (sums over the row),
  *   dgamma = sum over rows of g xh,  dbeta = sum over rows of g.
- * dx, dgamma, dbeta: each nullable.  Sums over rows are added in a fixed order:
+ * mean is fp32 here: where a row's mean is m times its spread, xh is off by up to
+ * 2^-24 m.  dx, dgamma, dbeta: each nullable.  Sums over rows are added in a fixed order:
  * repeated calls give identical bits.  With no rows dgamma and dbeta are 0. */
 size_t layer_norm_bwd_workspace(int dtype, int64_t rows, int64_t channels);
 int layer_norm_bwd(int dtype, const void* x, const void* g, int64_t rows, const int64_t* rows_dev, int64_t channels,
