@@ -298,8 +298,9 @@ int linear_bwd(int dtype, const void* x, int64_t rows, const int64_t* rows_dev, 
  *   out = (x - mean) rstd gamma + beta
  * gamma, beta [channels] (nullable: 1 and 0); mean, rstd fp32 [rows] (nullable)
  * are what layer_norm_bwd needs.  Deviations are taken from the unrounded mean;
- * their squares are summed in fp32 (deviations past 1e19 overflow it).  eps >= 0; with eps 0 a row of equal values
- * gives NaN, as the formula does.  channels up to 2^28. */
+ * their squares are summed in fp32, which deviations past 1e19 / sqrt(C)
+ * overflow (rstd is 0 then).  eps >= 0, held in fp32; with eps 0 a row of equal
+ * values gives NaN, as the formula does.  channels up to 2^28. */
 int layer_norm_fwd(int dtype, const void* x, int64_t rows, const int64_t* rows_dev, int64_t channels, const void* gamma,
                    const void* beta, double eps, void* out, float* mean, float* rstd, void* hip_stream);
 
