@@ -36,8 +36,9 @@ __device__ __forceinline__ double sum_squares(const T* __restrict__ p, long long
     return sum;
 }
 
-template <typename T>
-__device__ __forceinline__ void scale_chunk(const T* p, T* q, long long n, float scale) {
+// F: the product's type.
+template <typename T, typename F>
+__device__ __forceinline__ void scale_chunk(const T* p, T* q, long long n, F scale) {
     constexpr int V = kVec<T>;
     long long i = (long long)threadIdx.x * V;
     for (; i + 3 * 256 * V + V <= n; i += 4 * 256 * V) {
@@ -47,7 +48,7 @@ __device__ __forceinline__ void scale_chunk(const T* p, T* q, long long n, float
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
 #pragma unroll
-            for (int j = 0; j < V; ++j) v[k][j] *= scale;
+            for (int j = 0; j < V; ++j) v[k][j] = (float)((F)v[k][j] * scale);
             store_elems<T>(q + i + k * 256 * V, V, v[k]);
         }
     }
@@ -56,7 +57,7 @@ __device__ __forceinline__ void scale_chunk(const T* p, T* q, long long n, float
         float v[V];
         load_elems<T>(p + i, m, false, v);
 #pragma unroll
-        for (int j = 0; j < V; ++j) v[j] *= scale;
+        for (int j = 0; j < V; ++j) v[j] = (float)((F)v[j] * scale);
         store_elems<T>(q + i, m, v);
     }
 }
@@ -116,10 +117,14 @@ __global__ __launch_bounds__(256) void k_grad_scale(ClipTable<N> tab, const doub
     if (scale == 1.0 && t.dst == t.src) return;  // in place and nothing to change
     const long long at = (long long)(block - t.first) * tab.chunk;
     const long long n = t.count - at < tab.chunk ? t.count - at : tab.chunk;
-    const float by = (float)scale;
-    if (t.dtype == SCNN_F32) scale_chunk((const float*)t.src + at, (float*)t.dst + at, n, by);
-    else if (t.dtype == SCNN_BF16) scale_chunk((const __bf16*)t.src + at, (__bf16*)t.dst + at, n, by);
-    else scale_chunk((const _Float16*)t.src + at, (_Float16*)t.dst + at, n, by);
+    auto all = [&](auto by) {
+        if (t.dtype == SCNN_F32) scale_chunk((const float*)t.src + at, (float*)t.dst + at, n, by);
+        else if (t.dtype == SCNN_BF16) scale_chunk((const __bf16*)t.src + at, (__bf16*)t.dst + at, n, by);
+        else scale_chunk((const _Float16*)t.src + at, (_Float16*)t.dst + at, n, by);
+    };
+    // a scale that fp32 would hold in few bits or not at all multiplies in fp64: gradients of 10^38 have ordinary results
+    if (scale < 0x1p-100) all(scale);
+    else all((float)scale);
 }
 
 // Entries a workgroup takes: about 2048 workgroups of work where there is enough, never fewer than 4096 entries.
