@@ -449,7 +449,7 @@ __device__ __forceinline__ void tile_at(unsigned block, unsigned tiles_m, unsign
 
 // Sixteen bytes a lane straight from memory to LDS: lane l's to lds + 16 l.
 __device__ __forceinline__ void copy_to_lds(const void* base, unsigned offset, unsigned lds) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(base) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(base) : "memory", "m0");
 }
 // Waits until at most N of this wave's copies are on their way and its LDS reads have arrived, then for the workgroup's
 // other waves.
