@@ -1111,6 +1111,14 @@ static int check_width(int64_t channels, const char* name) {
     return SCNN_OK;
 }
 static size_t dtype_size(int dtype) { return dtype == SCNN_F32 ? 4 : 2; }
+// Arrays of 4 and 8 bytes an element: statistics, a row count, a result.
+static int check_words(std::initializer_list<const void*> fours, std::initializer_list<const void*> eights) {
+    for (const void* p : fours)
+        if ((uintptr_t)p & 3) return fail(SCNN_EINVAL, "an fp32 array is not aligned to its element");
+    for (const void* p : eights)
+        if ((uintptr_t)p & 7) return fail(SCNN_EINVAL, "a 64-bit array is not aligned to its element");
+    return SCNN_OK;
+}
 static bool element_aligned(int dtype, const void* p) { return ((uintptr_t)p & (dtype_size(dtype) - 1)) == 0; }
 static int check_workspace(const void* workspace, size_t bytes, size_t need) {
     if (!workspace && need == 256) return SCNN_OK;  // (the least that a query answers: the call uses none)
@@ -1160,12 +1168,14 @@ int linear_fwd(int dtype, const void* x, int64_t rows, const int64_t* rows_dev, 
     if (!x || !w || !out) return fail(SCNN_EINVAL, "null pointer");
     for (const void* q : {x, w, bias, residual, (const void*)out, (const void*)pre})
         if (!element_aligned(dtype, q)) return fail(SCNN_EINVAL, "an array is not aligned to its element");
+    rc = check_words({}, {rows_dev});
+    if (rc != SCNN_OK) return rc;
     const size_t need = linear_fwd_workspace(dtype, rows, c_in, c_out), e = dtype_size(dtype);
     rc = check_workspace(workspace, workspace_bytes, need);
     if (rc != SCNN_OK) return rc;
     const size_t in = (size_t)rows * c_in * e, of = (size_t)rows * c_out * e;
     rc = check_apart({{out, of}, {pre, of}, {workspace, need}},
-                     {{x, in}, {w, (size_t)c_in * c_out * e}, {bias, (size_t)c_out * e},
+                     {{x, in}, {w, (size_t)c_in * c_out * e}, {bias, (size_t)c_out * e}, {rows_dev, 8},
                       {residual == out ? nullptr : residual, of}});  // (an element of it is read by the lane that writes it)
     if (rc != SCNN_OK) return rc;
     LinearCall c = {};
@@ -1197,12 +1207,14 @@ int linear_bwd(int dtype, const void* x, int64_t rows, const int64_t* rows_dev, 
     }
     for (const void* q : {x, w, pre, g, (const void*)dx, (const void*)dw, (const void*)dbias})
         if (!element_aligned(dtype, q)) return fail(SCNN_EINVAL, "an array is not aligned to its element");
+    rc = check_words({}, {rows_dev});
+    if (rc != SCNN_OK) return rc;
     const size_t need = linear_bwd_workspace(dtype, rows, c_in, c_out, act), e = dtype_size(dtype);
     rc = check_workspace(workspace, workspace_bytes, need);
     if (rc != SCNN_OK) return rc;
     const size_t in = (size_t)rows * c_in * e, of = (size_t)rows * c_out * e, filter = (size_t)c_in * c_out * e;
     rc = check_apart({{dx, in}, {dw, filter}, {dbias, (size_t)c_out * e}, {workspace, need}},
-                     {{x, in}, {w, filter}, {act == SCNN_ACT_NONE ? nullptr : pre, of}, {g, of}});
+                     {{x, in}, {w, filter}, {act == SCNN_ACT_NONE ? nullptr : pre, of}, {g, of}, {rows_dev, 8}});
     if (rc != SCNN_OK) return rc;
     LinearCall c = {};
     c.x = x; c.w = w; c.pre_in = pre; c.g = g; c.dx = dx; c.dw = dw; c.dbias = dbias;
@@ -1224,9 +1236,11 @@ int layer_norm_fwd(int dtype, const void* x, int64_t rows, const int64_t* rows_d
     if (!x || !out) return fail(SCNN_EINVAL, "null pointer");
     for (const void* q : {x, gamma, beta, (const void*)out})
         if (!element_aligned(dtype, q)) return fail(SCNN_EINVAL, "an array is not aligned to its element");
+    rc = check_words({mean, rstd}, {rows_dev});
+    if (rc != SCNN_OK) return rc;
     const size_t e = dtype_size(dtype), all = (size_t)rows * channels * e;
     rc = check_apart({{out, all}, {mean, (size_t)rows * 4}, {rstd, (size_t)rows * 4}},
-                     {{x, all}, {gamma, (size_t)channels * e}, {beta, (size_t)channels * e}});
+                     {{x, all}, {gamma, (size_t)channels * e}, {beta, (size_t)channels * e}, {rows_dev, 8}});
     if (rc != SCNN_OK) return rc;
     SCNN_TRY(launch_norm_fwd(x, rows, (const long long*)rows_dev, (int)channels, gamma, beta, (float)eps, out, mean, rstd,
                              dtype, (hipStream_t)hip_stream));
@@ -1247,11 +1261,14 @@ int layer_norm_bwd(int dtype, const void* x, const void* g, int64_t rows, const 
     if (rows > 0 && (!x || !g || !mean || !rstd)) return fail(SCNN_EINVAL, "null pointer");
     for (const void* q : {x, g, gamma, (const void*)dx, (const void*)dgamma, (const void*)dbeta})
         if (!element_aligned(dtype, q)) return fail(SCNN_EINVAL, "an array is not aligned to its element");
+    rc = check_words({mean, rstd}, {rows_dev});
+    if (rc != SCNN_OK) return rc;
     const size_t need = layer_norm_bwd_workspace(dtype, rows, channels), e = dtype_size(dtype), row = (size_t)channels * e;
     rc = check_workspace(workspace, workspace_bytes, need);
     if (rc != SCNN_OK) return rc;
     rc = check_apart({{dx, rows * row}, {dgamma, row}, {dbeta, row}, {workspace, need}},
-                     {{x, rows * row}, {g, rows * row}, {gamma, row}, {mean, (size_t)rows * 4}, {rstd, (size_t)rows * 4}});
+                     {{x, rows * row}, {g, rows * row}, {gamma, row}, {mean, (size_t)rows * 4}, {rstd, (size_t)rows * 4},
+                      {rows_dev, 8}});
     if (rc != SCNN_OK) return rc;
     SCNN_TRY(launch_norm_bwd(x, g, rows, (const long long*)rows_dev, (int)channels, gamma, mean, rstd, dx, dgamma, dbeta,
                              (float*)workspace, dtype, (hipStream_t)hip_stream));
@@ -1305,6 +1322,8 @@ int grad_clip(int n, const void* const* grads, void* const* outs, const int64_t*
     if (rc != SCNN_OK) return rc;
     if (!(max_norm >= 0.0)) return fail(SCNN_EINVAL, "max_norm = %g must be >= 0", max_norm);
     if (!result || (n > 0 && (!grads || !dtypes))) return fail(SCNN_EINVAL, "null pointer");
+    rc = check_words({}, {result});
+    if (rc != SCNN_OK) return rc;
     for (int i = 0; i < n; ++i) {
         if (dtypes[i] != SCNN_F32 && dtypes[i] != SCNN_BF16 && dtypes[i] != SCNN_F16)
             return fail(SCNN_EINVAL, "dtypes[%d] = %d", i, dtypes[i]);
