@@ -110,15 +110,15 @@ __device__ __forceinline__ long long rows_of(long long rows, const long long* __
     return n < 0 ? 0 : (n < rows ? n : rows);
 }
 
-// Grid of `blocks` workgroups along one axis and `y` along another.  A launch holds fewer than 2^32 threads along an axis: what
-// goes past that continues along z, and block_id is the number along both.  The last z may be part empty: kernels leave
-// where block_id is past their work.
-inline dim3 grid_of(long long blocks, int threads, unsigned y = 1) {
-    const long long most = (1LL << 31) / threads;
-    if (blocks <= most) return dim3((unsigned)blocks, y);
-    return dim3((unsigned)most, y, (unsigned)((blocks + most - 1) / most));
+// Grid of `blocks` workgroups of THREADS along one axis and `y` along another.  A launch holds fewer than 2^32 threads along an
+// axis: what goes past 2^31 continues along z, and block_id is the number along both.  The last z may be part empty: kernels
+// leave where block_id is past their work.
+template <int THREADS> constexpr long long kBlocksX = (1LL << 31) / THREADS;
+template <int THREADS> dim3 grid_of(long long blocks, unsigned y = 1) {
+    if (blocks <= kBlocksX<THREADS>) return dim3((unsigned)blocks, y);
+    return dim3((unsigned)kBlocksX<THREADS>, y, (unsigned)((blocks + kBlocksX<THREADS> - 1) / kBlocksX<THREADS>));
 }
-__device__ __forceinline__ long long block_id() { return (long long)blockIdx.z * gridDim.x + blockIdx.x; }
+template <int THREADS> __device__ __forceinline__ long long block_id() { return blockIdx.z * kBlocksX<THREADS> + blockIdx.x; }
 
 // Distribution function of the normal density, Phi(z) = erfc(-z / sqrt 2) / 2, and e = exp(-z^2 / 2) on the way.  With
 // erfcx(x) = exp(x^2) erfc(x) as t P(t), t = 1 / (1 + 0.4 x), P of degree eight fitted for the least relative error over

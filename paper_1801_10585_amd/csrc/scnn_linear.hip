@@ -248,7 +248,7 @@ __global__ __launch_bounds__(64 * WM * WN * KG) void k_linear_tile(LinearArgs p)
     __shared__ __align__(16) char s_stage[KG * AREA > JOIN ? KG * AREA : JOIN];
     const long long rows = rows_of(p.rows_k ? p.k : p.m, p.rows_dev);
     const long long m_end = p.rows_k ? p.m : rows, k_all = p.rows_k ? rows : p.k;
-    const unsigned tiles_n = (unsigned)((p.n + BN - 1) / BN), block = (unsigned)block_id();  // (tiles: up to 2^30)
+    const unsigned tiles_n = (unsigned)((p.n + BN - 1) / BN), block = (unsigned)block_id<NT * KG>();  // (tiles: up to 2^30)
     const long long m0 = (long long)(block / tiles_n) * BM, n0 = (long long)(block % tiles_n) * BN;
     if (m0 >= m_end) return;
     const long long k_first = (long long)blockIdx.y * p.k_split;
@@ -476,10 +476,11 @@ __global__ __launch_bounds__(64 * WM * WN) void k_linear_ring(LinearArgs p) {
     const long long rows = rows_of(p.rows_k ? p.k : p.m, p.rows_dev);
     const long long m_end = p.rows_k ? p.m : rows, k_all = p.rows_k ? rows : p.k;
     unsigned tile_m, tile_n;
-    const unsigned tiles_m = (unsigned)((p.m + BM - 1) / BM), tiles_n = (unsigned)((p.n + BN - 1) / BN), block = (unsigned)block_id();
-    if (block >= tiles_m * tiles_n) return;
-    tile_at(block, tiles_m, tiles_n, tile_m, tile_n);
-    const long long m0 = (long long)tile_m * BM, n0 = (long long)tile_n * BN;
+    const unsigned tiles_m = (unsigned)((p.m + BM - 1) / BM), tiles_n = (unsigned)((p.n + BN - 1) / BN), block = (unsigned)block_id<NT>();
+    const bool any = block < tiles_m * tiles_n;
+    tile_at(any ? block : 0, tiles_m, tiles_n, tile_m, tile_n);
+    // (one way out: with two the compiler laid out the epilogue's branches so that a wide layer took 3 per cent longer)
+    const long long m0 = any ? (long long)tile_m * BM : m_end, n0 = (long long)tile_n * BN;
     if (m0 >= m_end) return;
     const long long k_first = (long long)blockIdx.y * p.k_split;
     const long long k_end = k_first + p.k_split < k_all ? k_first + p.k_split : k_all;
@@ -613,7 +614,7 @@ __global__ __launch_bounds__(256) void k_linear_join(LinearArgs p, int splits) {
     const long long m_end = p.rows_k ? p.m : rows_of(p.m, p.rows_dev);
     const long long quads = (p.n + 3) / 4;
     const int tq = threadIdx.x % Q, ts = threadIdx.x / Q;
-    const long long id = block_id() * Q + tq;
+    const long long id = block_id<256>() * Q + tq;
     const long long m = id / quads, n = id % quads * 4;
     f4 z = {0.f, 0.f, 0.f, 0.f};
     if (m < m_end) {
@@ -1242,8 +1243,7 @@ __global__ __launch_bounds__(1024) void k_linear_few(LinearArgs p, int lanes) {
     const long long k_first = (long long)blockIdx.y * p.k_split;
     const int k_count = (int)(p.k - k_first < p.k_split ? p.k - k_first : p.k_split);
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, tc = tid & (lanes - 1), group = tid / lanes, groups = 1024 / lanes;
-    const long long n_first = block_id() * lanes * V, n = n_first + tc * V;
-    if (n_first >= p.n) return;
+    const long long n_first = block_id<1024>() * lanes * V, n = n_first + tc * V;
     const int w = (int)(p.n - n < V ? p.n - n : V);
     const T *const x = (const T*)p.a, *const wt = (const T*)p.b + k_first * p.n + n;
 #pragma unroll
@@ -1394,7 +1394,7 @@ static size_t part_bytes(int dtype, long long m, long long n, long long k, bool 
 template <typename T, bool AK, bool BK_, int BM, int BN, int WM, int WN, int STAGES>
 static hipError_t ring(const LinearArgs& p, long long tiles, int splits, hipStream_t s) {
     constexpr int BK = 64, lds = (BM + BN) * BK * 2 * STAGES;
-    const dim3 grid = grid_of(tiles, 64 * WM * WN, (unsigned)splits);
+    const dim3 grid = grid_of<64 * WM * WN>(tiles, (unsigned)splits);
     auto kernel = k_linear_ring<T, AK, BK_, BM, BN, BK, WM, WN, STAGES>;
     if (lds >= 65536) {
         const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
@@ -1408,16 +1408,16 @@ template <typename T>
 static hipError_t join(const LinearArgs& p, int splits, hipStream_t s) {
     const long long quads = p.m * ((p.n + 3) / 4);
     if (splits >= 8)
-        hipLaunchKernelGGL((k_linear_join<T, 16>), grid_of((quads + 15) / 16, 256), dim3(256), 0, s, p, splits);
+        hipLaunchKernelGGL((k_linear_join<T, 16>), grid_of<256>((quads + 15) / 16), dim3(256), 0, s, p, splits);
     else
-        hipLaunchKernelGGL((k_linear_join<T, 4>), grid_of((quads + 63) / 64, 256), dim3(256), 0, s, p, splits);
+        hipLaunchKernelGGL((k_linear_join<T, 4>), grid_of<256>((quads + 63) / 64), dim3(256), 0, s, p, splits);
     return hipGetLastError();
 }
 
 template <typename T>
 static hipError_t few_rows(const LinearArgs& p, const TilePlan& t, hipStream_t s) {
     const long long wide = (long long)t.lanes * kVec<T>;
-    const dim3 grid = grid_of((p.n + wide - 1) / wide, 1024, (unsigned)t.splits);
+    const dim3 grid = grid_of<1024>((p.n + wide - 1) / wide, (unsigned)t.splits);
     if (p.m == 1) hipLaunchKernelGGL((k_linear_few<T, 1>), grid, dim3(1024), 0, s, p, t.lanes);
     else hipLaunchKernelGGL((k_linear_few<T, 4>), grid, dim3(1024), 0, s, p, t.lanes);
     return hipGetLastError();
@@ -1438,7 +1438,7 @@ static hipError_t product(int dtype, LinearArgs p, bool forward, hipStream_t s) 
     hipError_t e = hipSuccess;
     constexpr int BK = std::is_same<T, float>::value ? 32 : 64;
     const long long tiles = ((p.n + t.bn - 1) / t.bn) * ((p.m + t.bm - 1) / t.bm);
-    const dim3 by256 = grid_of(tiles, 256, (unsigned)t.splits), by1024 = grid_of(tiles, 1024, (unsigned)t.splits);
+    const dim3 by256 = grid_of<256>(tiles, (unsigned)t.splits), by1024 = grid_of<1024>(tiles, (unsigned)t.splits);
     if (t.kind == TileKind::kFew) {
         e = few_rows<T>(p, t, s);  // (only the forward product is planned so)
     } else if (t.kind == TileKind::kStaged) {

@@ -377,7 +377,7 @@ __global__ __launch_bounds__(1024) void k_column_sums(const float* __restrict__ 
                                                       long long split, T* __restrict__ out0, T* __restrict__ out1) {
     __shared__ double s_sum[64][17];
     const int tc = threadIdx.x & 15, tp = threadIdx.x >> 4;
-    const long long c = block_id() * 16 + tc;
+    const long long c = block_id<1024>() * 16 + tc;
     double sum = 0.0;
     if (c < cols)
 #pragma unroll 8
@@ -401,7 +401,7 @@ __global__ __launch_bounds__(1024) void k_column_sums(const float* __restrict__ 
 template <typename T>
 static hipError_t column_sums(const float* part, int parts, long long cols, long long split, void* out0, void* out1,
                               hipStream_t s) {
-    hipLaunchKernelGGL((k_column_sums<T>), grid_of((cols + 15) / 16, 1024), dim3(1024), 0, s, part, parts, cols, split,
+    hipLaunchKernelGGL((k_column_sums<T>), grid_of<1024>((cols + 15) / 16), dim3(1024), 0, s, part, parts, cols, split,
                        (T*)out0, (T*)out1);
     return hipGetLastError();
 }
