@@ -1325,8 +1325,13 @@ constexpr long long kChain = 65536;
 //   64 x 1024 x 12288             14.1 / 13.1 / 12.5 / 11.4   16 x 4096 x 4096   12.2 / 10.5 / 12.9 / 9.6
 //   3000 x 2000 x 2000              39 / 49 / 60 / 84       5000 x 1304 x 1000   23.8 / 30.8 / 33.7 / 44.7
 //   200000 x 64 x 32                31 / 34 / 16 / 23       100000 x 128 x 128   18.4 / 19.4 / 16.1 / 22
-// and of 256 x 256 tiles: 8192 x 4096 x 4096 with gelu, residual and pre 281 against 313 (231 both without these), 4096 x
-// 4096 x 4096 x^T dz 142 against 124.
+// 256 x 256 tiles run one a unit, 128 x 128 two; where the last round of the larger ones is part empty they lose more than they
+// save.  us of 256 x 256 / 128 x 128, bf16, 4096 columns, k 4096, by rows (rounds of 256 x 256 tiles on 256 units), without and
+// with gelu, residual and pre:
+//   7936 (1.94)  224 / 231  272 / 270      8192 (2)     232 / 238  274 / 282      8448 (2.06)  299 / 253  345 / 287
+//   10240 (2.5)  314 / 284  377 / 331      11264 (2.75) 329 / 319  386 / 366      11776 (2.88) 334 / 340  393 / 388
+//   12288 (3)    342 / 352  405 / 406      14336 (3.5)  441 / 407  510 / 475      16384 (4)    463 / 468  509 / 614
+// They are taken from two rounds on, at least 95 per cent full.
 // Large tiles read their operands least and pay from five on four compute units (one of 64 x 128 a unit) on, with k to hide
 // their start and end, where both sides fill them; short tiles for few rows; else 64 x 64.  k is split where that leaves
 // compute units without a tile: one workgroup a unit was the fastest of 1, 2, 4 and 8 at 12 of 16 shapes, within 15 per cent
@@ -1354,7 +1359,8 @@ static TilePlan tile_plan(int dtype, long long m, long long n, long long k, bool
     const long long cus = device_cu_count();
     auto tiles = [&](long long bm, long long bn) { return ((m + bm - 1) / bm) * ((n + bn - 1) / bn); };
     if (ring) {
-        if (k >= 512 && m > 128 && n > 128 && tiles(256, 256) >= 2 * cus) t.kind = TileKind::kRing256, t.bm = t.bn = 256;
+        const long long largest = tiles(256, 256), rounds = (largest + cus - 1) / cus;
+        if (k >= 512 && m > 128 && n > 128 && rounds >= 2 && 20 * largest >= 19 * rounds * cus) t.kind = TileKind::kRing256, t.bm = t.bn = 256;
         else if (k >= 512 && m > 64 && n > 64 && 4 * tiles(128, 128) >= 5 * cus) t.kind = TileKind::kRing128, t.bm = t.bn = 128;
         else if (k >= 512 && m > 32 && n > 64 && tiles(64, 128) >= cus) t.kind = TileKind::kRing64x128, t.bn = 128;
         else if (m <= 32) t.kind = TileKind::kRing32, t.bm = 32;

@@ -82,14 +82,17 @@ def whole(seed, *shape, dtype):
 
 
 def largest_tiles(m, n):
-    return -(-m // 256) * -(-n // 256) >= 2 * torch.cuda.get_device_properties(0).multi_processor_count
+    """Whether 256 x 256 tiles are taken: two rounds of them or more, the rounds at least 95 per cent full."""
+    tiles, units = -(-m // 256) * -(-n // 256), torch.cuda.get_device_properties(0).multi_processor_count
+    rounds = -(-tiles // units)
+    return rounds >= 2 and 20 * tiles >= 19 * rounds * units
 
 
 HALVES = (torch.bfloat16, torch.float16)
 
 
 @pytest.mark.parametrize("dtype", HALVES, ids=str)
-@pytest.mark.parametrize("size", [(8200, 520, 4104), (8450, 1000, 4352), (4352, 576, 8192), (16640, 512, 2056)], ids=str)
+@pytest.mark.parametrize("size", [(8100, 520, 4008), (8100, 1000, 6000), (4300, 576, 7640), (16300, 512, 2040)], ids=str)
 def test_forward_by_tiles_of_256(size, dtype):
     """Edges on both sides, k that ends inside a step, a count on the device; sums below 2^24: exact before the one rounding."""
     rows, c_in, c_out = size
@@ -110,12 +113,13 @@ def test_forward_by_tiles_of_256(size, dtype):
 
 @pytest.mark.parametrize("dtype", HALVES, ids=str)
 def test_epilogue_of_tiles_of_256(dtype):
-    rows, c_in, c_out = 8200, 520, 4104
+    rows, c_in, c_out = 8100, 520, 4008
+    assert largest_tiles(rows, c_out)
     g = torch.Generator(device=DEV).manual_seed(1)
     x = torch.randn(rows, c_in, generator=g, device=DEV).to(dtype)
     w = (torch.randn(c_in, c_out, generator=g, device=DEV) * 0.06).to(dtype)
     bias, residual = torch.randn(c_out, generator=g, device=DEV).to(dtype), torch.randn(rows, c_out, generator=g, device=DEV).to(dtype)
-    some = torch.cat([torch.arange(0, 40), torch.arange(4085, 4125), torch.arange(8160, 8200)]).to(DEV)
+    some = torch.cat([torch.arange(0, 40), torch.arange(4085, 4125), torch.arange(8060, 8100)]).to(DEV)
     for name in ("gelu", "silu"):
         out, pre = scnn.linear_fwd(x, w, bias, act=name, residual=residual, keep_pre=True)
         want, want_pre = ref.linear_fwd(x[some], w, bias, name, residual[some], dtype)
@@ -125,8 +129,8 @@ def test_epilogue_of_tiles_of_256(dtype):
 
 @pytest.mark.parametrize("dtype", HALVES, ids=str)
 def test_gradients_by_tiles_of_256(dtype):
-    # dx: 8200 x 4104 over 520 channels; dw: 8200 x 4104 over 520 rows, with a count over 450
-    rows, c_in, c_out = 8200, 4104, 520
+    # dx: 8100 x 4008 over 520 channels; dw: 8100 x 4008 over 520 rows and fewer
+    rows, c_in, c_out = 8100, 4008, 520
     assert largest_tiles(rows, c_in)
     x, w, g = whole(1, rows, c_in, dtype=dtype), whole(2, c_in, c_out, dtype=dtype), whole(3, rows, c_out, dtype=dtype)
     want = (g.double() @ w.double().t().contiguous()).to(dtype)
@@ -137,7 +141,7 @@ def test_gradients_by_tiles_of_256(dtype):
     dx = torch.full_like(dx, 5.0)
     scnn.linear_bwd(x, w, g, want=(True, False, False), rows_dev=count, out=(dx, None, None))
     assert torch.equal(dx[:8000], want[:8000]) and (dx[8000:] == 5).all()
-    rows, c_in, c_out = 520, 8200, 4104
+    rows, c_in, c_out = 520, 8100, 4008
     assert largest_tiles(c_in, c_out)
     x, w, g = whole(4, rows, c_in, dtype=dtype), whole(5, c_in, c_out, dtype=dtype), whole(6, rows, c_out, dtype=dtype)
     for count in (520, 512, 450, 3, 0):
