@@ -129,3 +129,34 @@ def test_fp16_infinities_do_not_move_the_scale(size):
     g[rows // 2:] = 65504.0
     again = scnn.linear_bwd(x, w, g, act="silu", pre=pre, rows_dev=count)
     assert torch.equal(short[0][:rows // 2], again[0][:rows // 2]) and torch.equal(short[1], again[1]) and torch.equal(short[2], again[2])
+
+
+@pytest.mark.parametrize("size", [(70, 264, 72), (2100, 67, 70), (300, 50, 40)], ids=str)
+def test_fp16_gradients_captured_and_replayed(size):
+    """The scale follows the gradients of every replay."""
+    rows, c_in, c_out = size
+    x, w = normal(1, rows, c_in).half().to(DEV), normal(2, c_in, c_out).half().to(DEV)
+    g, pre = normal(3, rows, c_out).half().to(DEV), normal(4, rows, c_out).half().to(DEV)
+    count = torch.tensor([rows], device=DEV)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        scnn.linear_bwd(x, w, g, act="gelu", pre=pre, rows_dev=count)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = scnn.linear_bwd(x, w, g, act="gelu", pre=pre, rows_dev=count)
+    for k, (scale, n) in enumerate(((1e-6, rows), (1.0, rows // 2), (5e3, rows), (1e-3, 1))):
+        g.copy_((normal(10 + k, rows, c_out) * scale).half())
+        count.fill_(n)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in held]
+        got[0] = got[0][:n]
+        want = ref.linear_bwd(x[:n], w, g[:n], "gelu", pre[:n], torch.float16)
+        for have, (value, bound) in zip(got, want):
+            big = value.abs() > 65000  # (past fp16's end where the formula is)
+            ref.assert_within(torch.where(big.to(DEV), torch.zeros_like(have), have), (torch.where(big, torch.zeros_like(value), value), bound))
+        other = scnn.linear_bwd(x, w, g, act="gelu", pre=pre, rows_dev=count, stream=side)
+        torch.cuda.synchronize()
+        assert torch.equal(other[0][:n], got[0]) and torch.equal(other[1], got[1]) and torch.equal(other[2], got[2])
