@@ -268,8 +268,10 @@ int prune_weights(float* w, unsigned char* warned, int64_t n_w, float eps, int64
  * where act is not SCNN_ACT_NONE.  out and residual may be the same array.
  * fp32 products are formed by splitting both operands into three bf16 numbers
  * (as sparse_conv_fwd's split kernels do); a tile of outputs that meets a value
- * these do not hold - infinities, NaN, non-zero magnitudes below 2^-109 or from
- * 2^58 up - is summed with fp32 products instead, several times as slowly.  The
+ * of which these leave something - non-zero magnitudes below 2^-109 - or whose
+ * sums are not finite is summed with fp32 products instead, several times as
+ * slowly (layers of up to 32 channels, gradients of up to 64: from magnitudes of
+ * 2^58 on too).  The
  * error of an fp32 result is a few 2^-24 of the sum of |x w| behind it, as with
  * fp32 products.  Repeated calls give identical bits. */
 size_t linear_fwd_workspace(int dtype, int64_t rows, int64_t c_in, int64_t c_out);

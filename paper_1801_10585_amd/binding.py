@@ -478,7 +478,9 @@ def prune_weights(w, warned, eps, *, stream=None):
 
 
 # Layers on rows of values.  All tensors of a call live on one device, which need not be the current one.  With `stream`
-# the call runs there and its new tensors belong to that stream: the caller orders other streams behind it.
+# the call runs there and its new tensors belong to that stream: the caller orders other streams behind it.  No call records
+# an autograd graph, whatever its tensors require: gradients come from the _bwd calls.  What a call writes in place does not
+# move autograd's version counters.
 
 class _Here:
     """The current device and stream: nothing to change."""

@@ -463,8 +463,9 @@ __device__ __forceinline__ void copies_and_barrier() {
 // lanes' addresses carry the permutation of the pieces (staged), since the copy puts them down in the order of the lanes.
 // Rows and columns past the arrays' ends are read from the last one inside; what they add up to is not stored.  k past a
 // multiple of BK is staged through registers at the end, with zeros.  8192 x 4096 x 4096 bf16 (m, n, k): 226 us, 1219 TFLOP/s
-// (the library's product 237), 253 with gelu, residual and pre; the matrix cores are busy 64 per cent of the time in the
-// products of 4096 x 4096 x 4096, LDS a third.
+// (the library's product 237), 253 with gelu, residual and pre, of whose time the matrix cores are busy 47 per cent (256 x 256
+// tiles, one workgroup a unit: nothing multiplies while they end); 62 per cent in the products of 4096 x 4096 x 4096 (128 x 128
+// tiles), LDS a third.
 template <typename T, bool AK, bool BK_, int BM, int BN, int BK, int WM, int WN, int STAGES>
 __global__ __launch_bounds__(64 * WM * WN) void k_linear_ring(LinearArgs p) {
     constexpr int NT = 64 * WM * WN, AW = AK ? BK : BM, BW = BK_ ? BK : BN;
@@ -759,8 +760,8 @@ __global__ __launch_bounds__(256) void k_act_back(const T* __restrict__ g, const
 // once, staged next to x, and read by both products, dx = dz w^T with its channels contiguous, dw += x^T dz by transposing
 // reads; dw stays in the accumulators and the column sums of dz in registers until the workgroup's rows are done.  part
 // [gridDim.x][c_in * c_out + c_out] then receives both, and one launch adds the workgroups' up.  P: widths up to P.
-// 52417 rows of 35 -> 19 fp16, silu: 12 + 4 us, against 30 for the five launches of the general way; 643072 of 64 -> 64 bf16 78
-// us, 4.2 TB/s, fp32 168 us, 3.9 TB/s.
+// 52417 rows of 35 -> 19 fp16, silu: 13.7 + 4 us, against 30 for the five launches of the general way; 643072 of 64 -> 64 with
+// relu bf16 75 us, 4.4 TB/s, fp32 165 us, 4.0 TB/s.
 template <int BYTES, int P> struct NarrowShape;  // threads; waves of dx (64 x P) and of dw (P x P), rows by columns
 template <int BYTES> struct NarrowShape<BYTES, 32> { static constexpr int NT = 256, XM = 4, XN = 1, WM = 2, WN = 2; };
 template <> struct NarrowShape<4, 64> { static constexpr int NT = 256, XM = 2, XN = 2, WM = 2, WN = 2; };

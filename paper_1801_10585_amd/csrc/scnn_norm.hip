@@ -10,7 +10,7 @@
 // 6e-4 without); a row of equal values, however large, has deviations of exactly 0.  The other sums are fp32.  The sums over rows
 // behind dgamma and dbeta are formed a column a lane in registers while the rows go by, joined within the workgroup, and
 // the workgroups' sums are added by a second launch in a fixed order: no atomics, the same bits every time.
-// Forward: 643072 x 64 fp32 62 us (5.3 TB/s; a large copy 5.2), 8192 x 4096 fp32 51 (5.2 TB/s).  Backward: 643072 x 64 fp32 104
+// Forward: 643072 x 64 fp32 64 us (5.2 TB/s, as a large copy), 8192 x 4096 fp32 51 (5.2 TB/s).  Backward: 643072 x 64 fp32 104
 // (4.8), 8192 x 4096 bf16 37 + 4 for the second launch (4.6), 209645 x 25 fp32 14.5 + 4 (3.5: vectors of rows of 100 bytes).
 #include "scnn_dense.h"
 
