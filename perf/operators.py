@@ -13,7 +13,7 @@ own = False
 
 DTYPES = {"fp32": torch.float32, "bf16": torch.bfloat16, "fp16": torch.float16}
 ACTS = ("none", "relu", "gelu", "silu")
-# the costliest listed passes: no drawn case is above them
+# no drawn case is above these: the costliest listed product; four fifths of the bytes of the largest listed list of gradients
 MOST_FLOPS = 4.0 * 4096 * 4096 * 4096
 MOST_BYTES = 400e6
 # layers (taps, channels in, channels out) of the nine-layer network of the paper's appendix
@@ -61,7 +61,7 @@ def listed():
         _norm("norm_bwd_8192x4096", 8192, 4096, "bf16", back=True),
         # all gradients of the nine-layer network: 18 small tensors, latency
         _clip("clip_nine_layers", "fp32", True, 0, 0, 0.5),
-        # gradients of a model of 60 tensors, 95 M entries in all
+        # gradients of a model of 60 tensors, 127 M entries in all
         _clip("clip_60_tensors", "bf16", False, 60, 12000000, 1.0),
     ]
 
