@@ -318,6 +318,99 @@ int layer_norm_bwd(int dtype, const void* x, const void* g, int64_t rows, const 
                    const void* gamma, const float* mean, const float* rstd, void* dx, void* dgamma, void* dbeta,
                    void* workspace, size_t workspace_bytes, void* hip_stream);
 
+/* First rows of the samples of a coordinate list: offsets[b] (device, int64
+ * [batch + 1]) = number of rows whose sample index is below b, so that sample b
+ * has the rows offsets[b] .. offsets[b + 1] - 1.  The rows ascend by sample (if
+ * not, the results are some numbers from 0 to the row count).  rows_dev as above. */
+int sample_offsets(int ndim, int batch, const int32_t* coords, int64_t rows, const int64_t* rows_dev, int64_t* offsets,
+                   void* hip_stream);
+
+/* Group norm over the samples of rows [rows, channels], and an activation.  The
+ * channels are cut into `groups` equal groups of neighbours; for each sample and
+ * group, over its n = (rows of the sample) * channels / groups values:
+ *   mean = sum x / n,  var = sum (x - mean)^2 / n,  rstd = 1 / sqrt(var + eps),
+ *   out = act((x - mean) rstd gamma + beta)
+ * offsets (nullable, device, int64 [batch + 1], ascending): sample b has the rows
+ * offsets[b] .. offsets[b + 1] - 1, as sample_offsets gives them; a sample may be
+ * empty; rows before the first sample and behind the last are neither read nor
+ * written.  Numbers outside 0 .. rows count as the nearer end; where they do not
+ * ascend the results are undefined, every access stays inside the arrays.  Null:
+ * every sample has rows / batch rows (`rows` a multiple of batch), as dense maps
+ * with their channels last.  gamma, beta [channels] (nullable: 1 and 0); mean,
+ * rstd fp32 [batch, groups] (nullable) are what group_norm_bwd needs, 0 for an
+ * empty sample.  Sums are fp64; deviations are taken from the unrounded mean.  A
+ * NaN or infinity reaches its sample's group and nothing else.  eps >= 0, held in
+ * fp32; with eps 0 a group of equal values gives NaN, as the formula does.
+ * channels up to 2^24.  Repeated calls give identical bits. */
+size_t group_norm_fwd_workspace(int dtype, int64_t rows, int64_t batch, int64_t channels, int64_t groups);
+int group_norm_fwd(int dtype, const void* x, int64_t rows, const int64_t* offsets, int64_t batch, int64_t channels,
+                   int64_t groups, const void* gamma, const void* beta, double eps, int act, void* out, float* mean,
+                   float* rstd, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Gradients of group norm from g [rows, channels], the gradient of out; with
+ * xh = (x - mean) rstd, z = xh gamma + beta, dz = g act'(z) and h = dz gamma:
+ *   dx = rstd (h - sum(h) / n - xh sum(h xh) / n)   (sums over the sample's group),
+ *   dgamma = sum over rows of dz xh,  dbeta = sum over rows of dz.
+ * mean, rstd as group_norm_fwd gave them (mean is fp32 here: where a group's mean
+ * is m times its spread, xh is off by up to 2^-24 m); offsets, batch, gamma, beta
+ * as there.  dx, dgamma, dbeta: each nullable.  Rows outside the samples are
+ * neither read nor written in dx; without any dgamma and dbeta are 0.  Repeated
+ * calls give identical bits. */
+size_t group_norm_bwd_workspace(int dtype, int64_t rows, int64_t batch, int64_t channels, int64_t groups);
+int group_norm_bwd(int dtype, const void* x, const void* g, int64_t rows, const int64_t* offsets, int64_t batch,
+                   int64_t channels, int64_t groups, const void* gamma, const void* beta, const float* mean,
+                   const float* rstd, int act, void* dx, void* dgamma, void* dbeta, void* workspace,
+                   size_t workspace_bytes, void* hip_stream);
+
+/* Dropout: out = x / (1 - p') where a value is kept, 0 where it is dropped (NaN
+ * and infinities too), plus residual (nullable).  p in [0, 1] is held in steps
+ * of 2^-16: p' = t 2^-16, t = p * 2^16 rounded; with t = 2^16 everything is
+ * dropped.  Which values are kept is a function of seed, offset and the value's
+ * number e = row * channels + column alone, not of the type or the row count, and
+ * is stored nowhere: dropout_bwd with the same numbers gives dx = g / (1 - p') where
+ * the value was kept, else 0.  Value e is dropped where its word is below t: of
+ * the four 32-bit results of Philox 4x32 in ten rounds (key = seed, low half
+ * first; counter = e / 8 and offset, 64 bits each, low halves first) it is the
+ * (e mod 8)-th half, lower halves first.  Layers and steps take an offset (or a
+ * seed) of their own.  rng (nullable, device, uint64[2]) = {seed, offset}, read
+ * when the call runs, in place of the host's: a captured call draws another
+ * mask at every replay if the caller moves the offset on.  out may be x or
+ * residual. */
+int dropout_fwd(int dtype, const void* x, int64_t rows, const int64_t* rows_dev, int64_t channels, double p, uint64_t seed,
+                uint64_t offset, const uint64_t* rng, const void* residual, void* out, void* hip_stream);
+int dropout_bwd(int dtype, const void* g, int64_t rows, const int64_t* rows_dev, int64_t channels, double p, uint64_t seed,
+                uint64_t offset, const uint64_t* rng, void* dx, void* hip_stream);
+
+/* Linear layers in 8-bit integers, for serving.  Rows of values and the columns
+ * of a weight are each held as int8 times one fp32 step:
+ *   most = the row's largest magnitude, at least 2^-100,
+ *   scale = most / 127,  q = x * (127 / most) rounded to the nearest integer, ties
+ *   to even (the quotients and the product are fp32, each rounded once).
+ * A row (column) with a NaN or an infinity has scale NaN and q 0.  A row of 8-bit
+ * values takes int8_row_bytes(channels) = channels rounded up to a multiple of 64
+ * bytes, the end filled with zeros; its array starts on 16 bytes.  channels up to
+ * 2^17 - 64: 32-bit sums do not overflow, whatever the int8 values are.
+ * quantize_rows: x [rows, channels] to q [rows, row bytes] and scale [rows].
+ * quantize_weight, once for a layer: w [c_in, c_out] to q [c_out, row bytes of
+ * c_in], one row for each column of w, and scale [c_out]. */
+int64_t int8_row_bytes(int64_t channels);
+int quantize_rows(int dtype, const void* x, int64_t rows, const int64_t* rows_dev, int64_t channels, int8_t* q, float* scale,
+                  void* hip_stream);
+int quantize_weight(int dtype, const void* w, int64_t c_in, int64_t c_out, int8_t* q, float* scale, void* hip_stream);
+
+/* The layer:  z = (sum over k of q[r, k] w[n, k]) x_scale[r] w_scale[n] + bias,
+ * out = act(z) + residual, the sums exact.  w, w_scale as quantize_weight gave
+ * them; bias [c_out], residual [rows, c_out] (nullable) and out [rows, c_out] of
+ * `dtype`; out and residual may be the same array.  With x_scale x holds 8-bit
+ * rows and their steps, as quantize_rows gave them; with x_scale null x is
+ * [rows, c_in] of `dtype` and is brought to 8 bits within the call, with the same
+ * result.  `given` of the query: 1 with x_scale, else 0.  Repeated calls give
+ * identical bits. */
+size_t linear_int8_fwd_workspace(int dtype, int given, int64_t rows, int64_t c_in, int64_t c_out);
+int linear_int8_fwd(int dtype, const void* x, const float* x_scale, int64_t rows, const int64_t* rows_dev, int64_t c_in,
+                    const int8_t* w, const float* w_scale, const void* bias, int64_t c_out, int act, const void* residual,
+                    void* out, void* workspace, size_t workspace_bytes, void* hip_stream);
+
 /* Global norm of the gradients of a network, and clipping by it:
  *   norm = sqrt(sum of squares of all entries of all tensors),
  *   scale = max_norm / (norm + 1e-6), at most 1;  every entry times scale.

@@ -29,6 +29,9 @@ EXPORTED_SYMBOLS = [
     "sparse_relu_static_max_rows", "sparse_relu_static", "scnn_last_conv_kernel",
     "linear_fwd_workspace", "linear_fwd", "linear_bwd_workspace", "linear_bwd", "layer_norm_fwd",
     "layer_norm_bwd_workspace", "layer_norm_bwd", "grad_clip_workspace", "grad_clip",
+    "sample_offsets", "group_norm_fwd_workspace", "group_norm_fwd", "group_norm_bwd_workspace", "group_norm_bwd",
+    "dropout_fwd", "dropout_bwd", "int8_row_bytes", "quantize_rows", "quantize_weight", "linear_int8_fwd_workspace",
+    "linear_int8_fwd",
 ]
 
 
@@ -115,6 +118,31 @@ def load_library():
     L.grad_clip.restype = ci
     L.grad_clip.argtypes = [ci, ctypes.POINTER(vp), ctypes.POINTER(vp), ctypes.POINTER(i64), ctypes.POINTER(ci), dbl, vp, vp,
                             sz, vp]
+    u64 = ctypes.c_uint64
+    L.sample_offsets.restype = ci
+    L.sample_offsets.argtypes = [ci, ci, vp, i64, vp, vp, vp]
+    L.group_norm_fwd_workspace.restype = sz
+    L.group_norm_fwd_workspace.argtypes = [ci, i64, i64, i64, i64]
+    L.group_norm_fwd.restype = ci
+    L.group_norm_fwd.argtypes = [ci, vp, i64, vp, i64, i64, i64, vp, vp, dbl, ci, vp, vp, vp, vp, sz, vp]
+    L.group_norm_bwd_workspace.restype = sz
+    L.group_norm_bwd_workspace.argtypes = [ci, i64, i64, i64, i64]
+    L.group_norm_bwd.restype = ci
+    L.group_norm_bwd.argtypes = [ci, vp, vp, i64, vp, i64, i64, i64, vp, vp, vp, vp, ci, vp, vp, vp, vp, sz, vp]
+    L.dropout_fwd.restype = ci
+    L.dropout_fwd.argtypes = [ci, vp, i64, vp, i64, dbl, u64, u64, vp, vp, vp, vp]
+    L.dropout_bwd.restype = ci
+    L.dropout_bwd.argtypes = [ci, vp, i64, vp, i64, dbl, u64, u64, vp, vp, vp]
+    L.int8_row_bytes.restype = i64
+    L.int8_row_bytes.argtypes = [i64]
+    L.quantize_rows.restype = ci
+    L.quantize_rows.argtypes = [ci, vp, i64, vp, i64, vp, vp, vp]
+    L.quantize_weight.restype = ci
+    L.quantize_weight.argtypes = [ci, vp, i64, i64, vp, vp, vp]
+    L.linear_int8_fwd_workspace.restype = sz
+    L.linear_int8_fwd_workspace.argtypes = [ci, ci, i64, i64, i64]
+    L.linear_int8_fwd.restype = ci
+    L.linear_int8_fwd.argtypes = [ci, vp, vp, i64, vp, i64, vp, vp, vp, i64, ci, vp, vp, vp, sz, vp]
     L.scnn_validate_rows.restype = ci
     L.scnn_validate_rows.argtypes = [ci, i32p, ci, vp, i64, vp, sz, vp]
     L.scnn_calibration_copy.restype = ci
@@ -705,6 +733,221 @@ def layer_norm_bwd(x, g, gamma, mean, rstd, *, want=(True, True, True), rows_dev
         _check(L, L.layer_norm_bwd(dt, _at(x), _at(g), rows, _at(rows_dev), ch, _at(gamma), _at(mean), _at(rstd),
                                    _at(dx), _at(dgamma), _at(dbeta), _at(workspace), _bytes(workspace), _current()))
     return dx, dgamma, dbeta
+
+
+def sample_offsets(coords, batch, *, rows_dev=None, out=None, stream=None):
+    """First row of every sample of coords int32 [rows, 1 + ndim], rows ascending by sample: int64 [batch + 1] on the
+    device, sample b being the rows offsets[b] .. offsets[b + 1] - 1; what group_norm_fwd takes."""
+    L = load_library()
+    if not coords.is_cuda or coords.dtype != torch.int32 or coords.dim() != 2:
+        raise ValueError("coords must be an int32 [rows, 1 + ndim] tensor on the GPU")
+    batch = int(batch)
+    if batch < 1:
+        raise ValueError("batch must be positive")
+    rows_dev = _rows_dev(rows_dev, coords)
+    with _on(coords.device, stream, (coords, rows_dev, out)):
+        coords = coords.contiguous()
+        out = _result(out, coords, (batch + 1,), "out", torch.int64)
+        _check(L, L.sample_offsets(coords.shape[1] - 1, batch, _at(coords), coords.shape[0], _at(rows_dev), _at(out),
+                                   _current()))
+    return out
+
+
+def _samples(offsets, batch, like: torch.Tensor) -> int:
+    """Number of samples of a group norm."""
+    if offsets is None:
+        return 1 if batch is None else int(batch)
+    if offsets.device != like.device or offsets.dtype != torch.int64 or offsets.dim() != 1 or offsets.shape[0] < 2:
+        raise ValueError("offsets must be an int64 [batch + 1] tensor on the GPU of the rows")
+    if batch is not None and batch != offsets.shape[0] - 1:
+        raise ValueError("offsets must hold batch + 1 numbers")
+    return offsets.shape[0] - 1
+
+
+def group_norm_fwd_workspace(dtype: torch.dtype, rows: int, batch: int, channels: int, groups: int) -> int:
+    return _ask("group_norm_fwd_workspace", dtype, int(rows), int(batch), int(channels), int(groups))
+
+
+def group_norm_fwd(x, groups, gamma=None, beta=None, *, offsets=None, batch=None, eps=1e-5, act="none", out=None,
+                   workspace=None, stream=None):
+    """act(group norm) of rows x [rows, channels] over the samples that `offsets` (int64 [batch + 1], of sample_offsets)
+    names or, without it, over `batch` (1) samples of equal size.  Returns (out, mean, rstd), the statistics fp32
+    [batch, groups], which group_norm_bwd needs; `out`: three tensors to put them in.  Rows outside the samples stay as they
+    are in `out`."""
+    L = load_library()
+    dt, rows, ch = _rows_of(x, "x")
+    batch, groups = _samples(offsets, batch, x), int(groups)
+    _same(gamma, x, (ch,), "gamma")
+    _same(beta, x, (ch,), "beta")
+    code = _activation(act)
+    need = _need(x.device.index, "group_norm_fwd_workspace", dt, rows, batch, ch, groups)
+    y, mean, rstd = out if out is not None else (None, None, None)
+    with _on(x.device, stream, (x, gamma, beta, offsets, y, mean, rstd, workspace)):
+        x, gamma, beta, offsets = x.contiguous(), _cont(gamma), _cont(beta), _cont(offsets)
+        y = _result(y, x, (rows, ch), "out")
+        mean = _result(mean, x, (batch, groups), "mean", torch.float32)
+        rstd = _result(rstd, mean, (batch, groups), "rstd")
+        workspace = _scratch(workspace, need, x)
+        _check(L, L.group_norm_fwd(dt, _at(x), rows, _at(offsets), batch, ch, groups, _at(gamma), _at(beta), float(eps), code,
+                                   _at(y), _at(mean), _at(rstd), _at(workspace), _bytes(workspace), _current()))
+    return y, mean, rstd
+
+
+def group_norm_bwd_workspace(dtype: torch.dtype, rows: int, batch: int, channels: int, groups: int) -> int:
+    return _ask("group_norm_bwd_workspace", dtype, int(rows), int(batch), int(channels), int(groups))
+
+
+def group_norm_bwd(x, g, groups, gamma, beta, mean, rstd, *, offsets=None, act="none", want=(True, True, True), out=None,
+                   workspace=None, stream=None):
+    """Gradients of group_norm_fwd from g [rows, channels], the gradient of its result; gamma and beta may be None, mean and
+    rstd as group_norm_fwd gave them.  Returns (dx, dgamma, dbeta), None where `want` is False; `out`: tensors to put them
+    in.  Rows outside the samples stay as they are in dx."""
+    L = load_library()
+    dt, rows, ch = _rows_of(x, "x")
+    batch, groups = _samples(offsets, mean.shape[0], x), int(groups)
+    _same(g, x, (rows, ch), "g")
+    _same(gamma, x, (ch,), "gamma")
+    _same(beta, x, (ch,), "beta")
+    _same(mean, x, (batch, groups), "mean", torch.float32)
+    _same(rstd, x, (batch, groups), "rstd", torch.float32)
+    code = _activation(act)
+    need = _need(x.device.index, "group_norm_bwd_workspace", dt, rows, batch, ch, groups)
+    dx, dgamma, dbeta = out if out is not None else (None, None, None)
+    with _on(x.device, stream, (x, g, gamma, beta, mean, rstd, offsets, dx, dgamma, dbeta, workspace)):
+        x, g, gamma, beta, mean, rstd, offsets = (x.contiguous(), g.contiguous(), _cont(gamma), _cont(beta), mean.contiguous(),
+                                                  rstd.contiguous(), _cont(offsets))
+        dx = _result(dx, x, (rows, ch), "dx") if want[0] else None
+        dgamma = _result(dgamma, x, (ch,), "dgamma") if want[1] else None
+        dbeta = _result(dbeta, x, (ch,), "dbeta") if want[2] else None
+        workspace = _scratch(workspace, need, x)
+        _check(L, L.group_norm_bwd(dt, _at(x), _at(g), rows, _at(offsets), batch, ch, groups, _at(gamma), _at(beta), _at(mean),
+                                   _at(rstd), code, _at(dx), _at(dgamma), _at(dbeta), _at(workspace), _bytes(workspace),
+                                   _current()))
+    return dx, dgamma, dbeta
+
+
+def _word(v, name: str) -> int:
+    v = int(v)
+    if not 0 <= v < 1 << 64:
+        raise ValueError(f"{name} must be from 0 to 2^64 - 1")
+    return v
+
+
+def _rng(rng, like: torch.Tensor):
+    if rng is not None and (rng.device != like.device or rng.dtype not in (torch.int64, torch.uint64) or rng.shape != (2,)
+                            or not rng.is_contiguous()):
+        raise ValueError("rng must be a contiguous int64 or uint64 [2] tensor on the GPU of the rows")
+    return rng
+
+
+def dropout_fwd(x, p, *, seed=0, offset=0, rng=None, residual=None, rows_dev=None, out=None, stream=None):
+    """x / (1 - p) where a value of x [rows, channels] is kept, 0 where it is dropped, + residual.  What is dropped follows
+    from seed, offset (each 0 .. 2^64 - 1) and the value's place; with rng, a device tensor {seed, offset}, they are read
+    when the call runs, so that replays of a captured call differ where the caller moves the offset on.  p is held in steps of
+    2^-16.  out may be x or residual."""
+    L = load_library()
+    dt, rows, ch = _rows_of(x, "x")
+    _same(residual, x, (rows, ch), "residual")
+    seed, offset, rng, rows_dev = _word(seed, "seed"), _word(offset, "offset"), _rng(rng, x), _rows_dev(rows_dev, x)
+    with _on(x.device, stream, (x, rng, residual, rows_dev, out)):
+        x, residual = x.contiguous(), _cont(residual)
+        out = _result(out, x, (rows, ch), "out")
+        _check(L, L.dropout_fwd(dt, _at(x), rows, _at(rows_dev), ch, float(p), seed, offset, _at(rng), _at(residual), _at(out),
+                                _current()))
+    return out
+
+
+def dropout_bwd(g, p, *, seed=0, offset=0, rng=None, rows_dev=None, out=None, stream=None):
+    """Gradient of dropout_fwd's x from g [rows, channels], the gradient of its result (which is the residual's gradient
+    too), with the seed and offset of the forward call.  out may be g."""
+    L = load_library()
+    dt, rows, ch = _rows_of(g, "g")
+    seed, offset, rng, rows_dev = _word(seed, "seed"), _word(offset, "offset"), _rng(rng, g), _rows_dev(rows_dev, g)
+    with _on(g.device, stream, (g, rng, rows_dev, out)):
+        g = g.contiguous()
+        out = _result(out, g, (rows, ch), "out")
+        _check(L, L.dropout_bwd(dt, _at(g), rows, _at(rows_dev), ch, float(p), seed, offset, _at(rng), _at(out), _current()))
+    return out
+
+
+def int8_row_bytes(channels: int) -> int:
+    """Bytes of a row of 8-bit values: channels rounded up to a multiple of 64."""
+    L = load_library()
+    r = int(L.int8_row_bytes(int(channels)))
+    if r < 0:
+        _check(L, r)
+    return r
+
+
+def quantize_rows(x, *, rows_dev=None, out=None, stream=None):
+    """Rows x [rows, channels] in 8 bits: (q int8 [rows, int8_row_bytes(channels)], scale fp32 [rows]), x about q times its
+    row's scale; `out`: two tensors to put them in."""
+    L = load_library()
+    dt, rows, ch = _rows_of(x, "x")
+    rows_dev, width = _rows_dev(rows_dev, x), int8_row_bytes(ch)
+    q, scale = out if out is not None else (None, None)
+    with _on(x.device, stream, (x, rows_dev, q, scale)):
+        x = x.contiguous()
+        q = _result(q, x, (rows, width), "q", torch.int8)
+        scale = _result(scale, x, (rows,), "scale", torch.float32)
+        _check(L, L.quantize_rows(dt, _at(x), rows, _at(rows_dev), ch, _at(q), _at(scale), _current()))
+    return q, scale
+
+
+def quantize_weight(w, *, out=None, stream=None):
+    """A layer's weight w [c_in, c_out] in 8 bits, once for linear_int8_fwd: (q int8 [c_out, int8_row_bytes(c_in)], scale fp32
+    [c_out]), a row for each column of w; `out`: two tensors to put them in."""
+    L = load_library()
+    dt, c_in, c_out = _rows_of(w, "w")
+    width = int8_row_bytes(c_in)
+    q, scale = out if out is not None else (None, None)
+    with _on(w.device, stream, (w, q, scale)):
+        w = w.contiguous()
+        q = _result(q, w, (c_out, width), "q", torch.int8)
+        scale = _result(scale, w, (c_out,), "scale", torch.float32)
+        _check(L, L.quantize_weight(dt, _at(w), c_in, c_out, _at(q), _at(scale), _current()))
+    return q, scale
+
+
+def linear_int8_fwd_workspace(dtype: torch.dtype, rows: int, c_in: int, c_out: int, given: bool = False) -> int:
+    """given: x comes in 8 bits (with x_scale)."""
+    return _ask("linear_int8_fwd_workspace", dtype, int(bool(given)), int(rows), int(c_in), int(c_out))
+
+
+def linear_int8_fwd(x, w, w_scale, bias=None, *, x_scale=None, act="none", residual=None, dtype=None, rows_dev=None, out=None,
+                    workspace=None, stream=None):
+    """out = act(x w + bias) + residual in 8-bit integers; w, w_scale as quantize_weight gave them.  x: rows [rows, c_in] of
+    fp32, bf16 or fp16, brought to 8 bits within the call, or with x_scale the 8-bit rows that quantize_rows gave.  bias,
+    residual and out are of `dtype`: x's type, or where x is in 8 bits that of bias, residual or out, whichever is there."""
+    L = load_library()
+    given = x_scale is not None
+    if not x.is_cuda or x.dim() != 2:
+        raise ValueError("x must be [rows, channels] on the GPU")
+    if dtype is None:
+        dtype = next((t.dtype for t in (bias, residual, out) if t is not None), None) if given else x.dtype
+    if dtype not in DTYPES:
+        raise ValueError("dtype must be float32, bfloat16 or float16")
+    if x.dtype != (torch.int8 if given else dtype):
+        raise ValueError("x must be int8 where x_scale is given" if given else f"x must be {dtype}, or int8 with x_scale")
+    dt, (rows, c_in), c_out = DTYPES[dtype], x.shape, w.shape[0]
+    _same(w, x, (c_out, int8_row_bytes(c_in)), "w", torch.int8)
+    if given and c_in != w.shape[1]:
+        raise ValueError("x must be rows of int8_row_bytes(c_in) values")
+    _same(w_scale, x, (c_out,), "w_scale", torch.float32)
+    _same(x_scale, x, (rows,), "x_scale", torch.float32)
+    _same(bias, x, (c_out,), "bias", dtype)
+    _same(residual, x, (rows, c_out), "residual", dtype)
+    code = _activation(act)
+    rows_dev = _rows_dev(rows_dev, x)
+    need = _need(x.device.index, "linear_int8_fwd_workspace", dt, int(given), rows, c_in, c_out)
+    with _on(x.device, stream, (x, x_scale, w, w_scale, bias, residual, rows_dev, out, workspace)):
+        x, w, w_scale, x_scale, bias, residual = (x.contiguous(), w.contiguous(), w_scale.contiguous(), _cont(x_scale),
+                                                  _cont(bias), _cont(residual))
+        out = _result(out, x, (rows, c_out), "out", dtype)
+        workspace = _scratch(workspace, need, x)
+        _check(L, L.linear_int8_fwd(dt, _at(x), _at(x_scale), rows, _at(rows_dev), c_in, _at(w), _at(w_scale), _at(bias), c_out,
+                                    code, _at(residual), _at(out), _at(workspace), _bytes(workspace), _current()))
+    return out
 
 
 def _dense(t: torch.Tensor) -> bool:

@@ -1275,6 +1275,235 @@ int layer_norm_bwd(int dtype, const void* x, const void* g, int64_t rows, const 
     return SCNN_OK;
 }
 
+// ---------------------------------------------------------------- group norm
+int sample_offsets(int ndim, int batch, const int32_t* coords, int64_t rows, const int64_t* rows_dev, int64_t* offsets,
+                   void* hip_stream) {
+    if (ndim != 2 && ndim != 3) return fail(SCNN_EINVAL, "ndim = %d", ndim);
+    if (batch < 1) return fail(SCNN_EINVAL, "batch = %d", batch);
+    if (rows < 0) return fail(SCNN_EINVAL, "rows = %lld", (long long)rows);
+    if (rows > kMaxIndex) return fail(SCNN_ECAPACITY, "more than 2^31-1 rows");
+    if (!offsets || (rows > 0 && !coords)) return fail(SCNN_EINVAL, "null pointer");
+    int rc = check_words({coords}, {rows_dev, offsets});
+    if (rc == SCNN_OK)
+        rc = check_apart({{offsets, ((size_t)batch + 1) * 8}}, {{coords, (size_t)rows * (1 + ndim) * 4}, {rows_dev, 8}});
+    if (rc != SCNN_OK) return rc;
+    SCNN_TRY(launch_sample_offsets(coords, 1 + ndim, rows, (const long long*)rows_dev, batch, (long long*)offsets,
+                                   (hipStream_t)hip_stream));
+    return SCNN_OK;
+}
+
+static constexpr long long kMaxGroupWidth = 1LL << 24;  // channels of a group norm: slabs of them lie along a launch's second axis
+
+static int check_group(int dtype, int64_t rows, int64_t batch, int64_t channels, int64_t groups) {
+    int rc = check_rows(dtype, rows);
+    if (rc == SCNN_OK) rc = check_width(channels, "channels");
+    if (rc != SCNN_OK) return rc;
+    if (channels > kMaxGroupWidth) return fail(SCNN_ECAPACITY, "channels = %lld exceeds 2^24", (long long)channels);
+    if (groups < 1 || channels % groups != 0)
+        return fail(SCNN_EINVAL, "%lld channels are no whole number of %lld groups", (long long)channels, (long long)groups);
+    if (batch < 1) return fail(SCNN_EINVAL, "batch = %lld", (long long)batch);
+    if (batch > (1LL << 30)) return fail(SCNN_ECAPACITY, "more than 2^30 samples");
+    if ((double)rows * (double)channels > 0x1p42 || (double)batch * (double)channels > 0x1p42)
+        return fail(SCNN_ECAPACITY, "more than 2^42 values in an array");
+    return SCNN_OK;
+}
+static int check_samples(int64_t rows, int64_t batch, const int64_t* offsets) {
+    if (!offsets && rows % batch != 0)
+        return fail(SCNN_EINVAL, "%lld rows are no whole number for each of %lld samples", (long long)rows, (long long)batch);
+    return SCNN_OK;
+}
+
+size_t group_norm_fwd_workspace(int dtype, int64_t rows, int64_t batch, int64_t channels, int64_t groups) {
+    if (check_group(dtype, rows, batch, channels, groups) != SCNN_OK) return 0;
+    return 256 + group_norm_bytes(dtype, rows, batch, (int)channels, (int)groups, false);
+}
+
+int group_norm_fwd(int dtype, const void* x, int64_t rows, const int64_t* offsets, int64_t batch, int64_t channels,
+                   int64_t groups, const void* gamma, const void* beta, double eps, int act, void* out, float* mean,
+                   float* rstd, void* workspace, size_t workspace_bytes, void* hip_stream) {
+    int rc = check_group(dtype, rows, batch, channels, groups);
+    if (rc == SCNN_OK) rc = check_samples(rows, batch, offsets);
+    if (rc != SCNN_OK) return rc;
+    if (!(eps >= 0.0) || std::isinf((float)eps)) return fail(SCNN_EINVAL, "eps = %g", eps);
+    if (act < SCNN_ACT_NONE || act > SCNN_ACT_SILU) return fail(SCNN_EINVAL, "unknown activation %d", act);
+    if (rows > 0 && (!x || !out)) return fail(SCNN_EINVAL, "null pointer");
+    for (const void* q : {x, gamma, beta, (const void*)out})
+        if (!element_aligned(dtype, q)) return fail(SCNN_EINVAL, "an array is not aligned to its element");
+    rc = check_words({mean, rstd}, {offsets});
+    if (rc != SCNN_OK) return rc;
+    const size_t need = group_norm_fwd_workspace(dtype, rows, batch, channels, groups), e = dtype_size(dtype);
+    rc = check_workspace(workspace, workspace_bytes, need);
+    if (rc != SCNN_OK) return rc;
+    const size_t all = (size_t)rows * channels * e, wide = (size_t)channels * e, stats = (size_t)batch * groups * 4;
+    rc = check_apart({{out, all}, {mean, stats}, {rstd, stats}, {workspace, need}},
+                     {{x, all}, {gamma, wide}, {beta, wide}, {offsets, ((size_t)batch + 1) * 8}});
+    if (rc != SCNN_OK) return rc;
+    GroupCall c = {};
+    c.x = x; c.gamma = gamma; c.beta = beta; c.out = out; c.mean = mean; c.rstd = rstd;
+    c.offsets = (const long long*)offsets;
+    c.rows = rows; c.batch = batch;
+    c.channels = (int)channels; c.groups = (int)groups; c.act = act; c.eps = (float)eps;
+    c.workspace = workspace;
+    SCNN_TRY(launch_group_fwd(dtype, c, (hipStream_t)hip_stream));
+    return SCNN_OK;
+}
+
+size_t group_norm_bwd_workspace(int dtype, int64_t rows, int64_t batch, int64_t channels, int64_t groups) {
+    if (check_group(dtype, rows, batch, channels, groups) != SCNN_OK) return 0;
+    return 256 + group_norm_bytes(dtype, rows, batch, (int)channels, (int)groups, true);
+}
+
+int group_norm_bwd(int dtype, const void* x, const void* g, int64_t rows, const int64_t* offsets, int64_t batch,
+                   int64_t channels, int64_t groups, const void* gamma, const void* beta, const float* mean,
+                   const float* rstd, int act, void* dx, void* dgamma, void* dbeta, void* workspace,
+                   size_t workspace_bytes, void* hip_stream) {
+    int rc = check_group(dtype, rows, batch, channels, groups);
+    if (rc == SCNN_OK) rc = check_samples(rows, batch, offsets);
+    if (rc != SCNN_OK) return rc;
+    if (act < SCNN_ACT_NONE || act > SCNN_ACT_SILU) return fail(SCNN_EINVAL, "unknown activation %d", act);
+    if (rows > 0 && (!x || !g || !mean || !rstd)) return fail(SCNN_EINVAL, "null pointer");
+    for (const void* q : {x, g, gamma, beta, (const void*)dx, (const void*)dgamma, (const void*)dbeta})
+        if (!element_aligned(dtype, q)) return fail(SCNN_EINVAL, "an array is not aligned to its element");
+    rc = check_words({mean, rstd}, {offsets});
+    if (rc != SCNN_OK) return rc;
+    const size_t need = group_norm_bwd_workspace(dtype, rows, batch, channels, groups), e = dtype_size(dtype);
+    rc = check_workspace(workspace, workspace_bytes, need);
+    if (rc != SCNN_OK) return rc;
+    const size_t all = (size_t)rows * channels * e, wide = (size_t)channels * e, stats = (size_t)batch * groups * 4;
+    rc = check_apart({{dx, all}, {dgamma, wide}, {dbeta, wide}, {workspace, need}},
+                     {{x, all}, {g, all}, {gamma, wide}, {beta, wide}, {mean, stats}, {rstd, stats},
+                      {offsets, ((size_t)batch + 1) * 8}});
+    if (rc != SCNN_OK) return rc;
+    GroupCall c = {};
+    c.x = x; c.g = g; c.gamma = gamma; c.beta = beta; c.dx = dx; c.dgamma = dgamma; c.dbeta = dbeta;
+    c.mean = const_cast<float*>(mean); c.rstd = const_cast<float*>(rstd);
+    c.offsets = (const long long*)offsets;
+    c.rows = rows; c.batch = batch;
+    c.channels = (int)channels; c.groups = (int)groups; c.act = act;
+    c.workspace = workspace;
+    SCNN_TRY(launch_group_bwd(dtype, c, (hipStream_t)hip_stream));
+    return SCNN_OK;
+}
+
+// ---------------------------------------------------------------- dropout
+static int dropout(int dtype, const void* x, int64_t rows, const int64_t* rows_dev, int64_t channels, double p, uint64_t seed,
+                   uint64_t offset, const uint64_t* rng, const void* residual, void* out, void* hip_stream) {
+    int rc = check_rows(dtype, rows);
+    if (rc == SCNN_OK) rc = check_width(channels, "channels");
+    if (rc != SCNN_OK) return rc;
+    if ((double)rows * (double)channels > 0x1p42) return fail(SCNN_ECAPACITY, "more than 2^42 values in an array");
+    if (!(p >= 0.0 && p <= 1.0)) return fail(SCNN_EINVAL, "p = %g must be in [0, 1]", p);
+    if (rows == 0) return SCNN_OK;
+    if (!x || !out) return fail(SCNN_EINVAL, "null pointer");
+    for (const void* q : {x, residual, (const void*)out})
+        if (!element_aligned(dtype, q)) return fail(SCNN_EINVAL, "an array is not aligned to its element");
+    rc = check_words({}, {rows_dev, rng});
+    if (rc != SCNN_OK) return rc;
+    const size_t all = (size_t)rows * channels * dtype_size(dtype);
+    rc = check_apart({{out, all}}, {{x == out ? nullptr : x, all}, {residual == out ? nullptr : residual, all}, {rows_dev, 8}, {rng, 16}});
+    if (rc != SCNN_OK) return rc;
+    SCNN_TRY(launch_dropout(dtype, x, residual, out, rows, (const long long*)rows_dev, channels, p, seed, offset,
+                            (const unsigned long long*)rng, (hipStream_t)hip_stream));
+    return SCNN_OK;
+}
+
+int dropout_fwd(int dtype, const void* x, int64_t rows, const int64_t* rows_dev, int64_t channels, double p, uint64_t seed,
+                uint64_t offset, const uint64_t* rng, const void* residual, void* out, void* hip_stream) {
+    return dropout(dtype, x, rows, rows_dev, channels, p, seed, offset, rng, residual, out, hip_stream);
+}
+
+int dropout_bwd(int dtype, const void* g, int64_t rows, const int64_t* rows_dev, int64_t channels, double p, uint64_t seed,
+                uint64_t offset, const uint64_t* rng, void* dx, void* hip_stream) {
+    return dropout(dtype, g, rows, rows_dev, channels, p, seed, offset, rng, nullptr, dx, hip_stream);
+}
+
+// ---------------------------------------------------------------- linear layers in 8-bit integers
+static constexpr long long kMaxInt8Width = (1LL << 17) - 64;  // products of 2^14 whose sum stays below 2^31
+
+static int check_int8(int dtype, int64_t rows, int64_t c_in, int64_t c_out) {
+    const int rc = check_linear(dtype, rows, c_in, c_out);
+    if (rc != SCNN_OK) return rc;
+    if (c_in > kMaxInt8Width) return fail(SCNN_ECAPACITY, "c_in = %lld exceeds 2^17 - 64", (long long)c_in);
+    return SCNN_OK;
+}
+static bool on16(const void* p) { return ((uintptr_t)p & 15) == 0; }
+
+int64_t int8_row_bytes(int64_t channels) {
+    const int rc = check_int8(SCNN_F32, 0, channels, 1);
+    return rc != SCNN_OK ? rc : int8_width(channels);
+}
+
+int quantize_rows(int dtype, const void* x, int64_t rows, const int64_t* rows_dev, int64_t channels, int8_t* q, float* scale,
+                  void* hip_stream) {
+    int rc = check_int8(dtype, rows, channels, 1);
+    if (rc != SCNN_OK) return rc;
+    if (rows == 0) return SCNN_OK;
+    if (!x || !q || !scale) return fail(SCNN_EINVAL, "null pointer");
+    if (!element_aligned(dtype, x)) return fail(SCNN_EINVAL, "an array is not aligned to its element");
+    if (!on16(q)) return fail(SCNN_EINVAL, "rows of 8-bit values must begin on 16 bytes");
+    rc = check_words({scale}, {rows_dev});
+    if (rc != SCNN_OK) return rc;
+    rc = check_apart({{q, (size_t)rows * int8_width(channels)}, {scale, (size_t)rows * 4}},
+                     {{x, (size_t)rows * channels * dtype_size(dtype)}, {rows_dev, 8}});
+    if (rc != SCNN_OK) return rc;
+    SCNN_TRY(launch_quantize_rows(dtype, x, rows, (const long long*)rows_dev, channels, (signed char*)q, scale, (hipStream_t)hip_stream));
+    return SCNN_OK;
+}
+
+int quantize_weight(int dtype, const void* w, int64_t c_in, int64_t c_out, int8_t* q, float* scale, void* hip_stream) {
+    int rc = check_int8(dtype, 0, c_in, c_out);
+    if (rc != SCNN_OK) return rc;
+    if (!w || !q || !scale) return fail(SCNN_EINVAL, "null pointer");
+    if (!element_aligned(dtype, w)) return fail(SCNN_EINVAL, "an array is not aligned to its element");
+    if (!on16(q)) return fail(SCNN_EINVAL, "rows of 8-bit values must begin on 16 bytes");
+    rc = check_words({scale}, {});
+    if (rc != SCNN_OK) return rc;
+    rc = check_apart({{q, (size_t)c_out * int8_width(c_in)}, {scale, (size_t)c_out * 4}},
+                     {{w, (size_t)c_in * c_out * dtype_size(dtype)}});
+    if (rc != SCNN_OK) return rc;
+    SCNN_TRY(launch_quantize_weight(dtype, w, c_in, c_out, (signed char*)q, scale, (hipStream_t)hip_stream));
+    return SCNN_OK;
+}
+
+size_t linear_int8_fwd_workspace(int dtype, int given, int64_t rows, int64_t c_in, int64_t c_out) {
+    if (check_int8(dtype, rows, c_in, c_out) != SCNN_OK) return 0;
+    return 256 + linear_int8_bytes(dtype, given != 0, rows, c_in, c_out);
+}
+
+int linear_int8_fwd(int dtype, const void* x, const float* x_scale, int64_t rows, const int64_t* rows_dev, int64_t c_in,
+                    const int8_t* w, const float* w_scale, const void* bias, int64_t c_out, int act, const void* residual,
+                    void* out, void* workspace, size_t workspace_bytes, void* hip_stream) {
+    int rc = check_int8(dtype, rows, c_in, c_out);
+    if (rc != SCNN_OK) return rc;
+    if (act < SCNN_ACT_NONE || act > SCNN_ACT_SILU) return fail(SCNN_EINVAL, "unknown activation %d", act);
+    if (rows == 0) return SCNN_OK;
+    if (!x || !w || !w_scale || !out) return fail(SCNN_EINVAL, "null pointer");
+    const bool given = x_scale != nullptr;
+    for (const void* q : {given ? nullptr : x, bias, residual, (const void*)out})
+        if (!element_aligned(dtype, q)) return fail(SCNN_EINVAL, "an array is not aligned to its element");
+    if (!on16(w) || (given && !on16(x))) return fail(SCNN_EINVAL, "rows of 8-bit values must begin on 16 bytes");
+    rc = check_words({x_scale, w_scale}, {rows_dev});
+    if (rc != SCNN_OK) return rc;
+    const size_t need = linear_int8_fwd_workspace(dtype, given, rows, c_in, c_out), e = dtype_size(dtype);
+    rc = check_workspace(workspace, workspace_bytes, need);
+    if (rc != SCNN_OK) return rc;
+    const size_t width = (size_t)int8_width(c_in), in = (size_t)rows * (given ? width : c_in * e), of = (size_t)rows * c_out * e;
+    rc = check_apart({{out, of}, {workspace, need}},
+                     {{x, in}, {x_scale, (size_t)rows * 4}, {w, (size_t)c_out * width}, {w_scale, (size_t)c_out * 4},
+                      {bias, (size_t)c_out * e}, {rows_dev, 8},
+                      {residual == out ? nullptr : residual, of}});  // (an element of it is read by the lane that writes it)
+    if (rc != SCNN_OK) return rc;
+    Int8Call c = {};
+    c.x = x; c.x_scale = x_scale; c.w = (const signed char*)w; c.w_scale = w_scale; c.bias = bias; c.residual = residual;
+    c.out = out;
+    c.rows = rows; c.c_in = c_in; c.c_out = c_out;
+    c.rows_dev = (const long long*)rows_dev;
+    c.act = act;
+    c.workspace = workspace;
+    SCNN_TRY(launch_linear_int8(dtype, c, (hipStream_t)hip_stream));
+    return SCNN_OK;
+}
+
 // ---------------------------------------------------------------- gradient clipping
 static int check_counts(int n, const int64_t* counts) {
     if (n < 0 || (n > 0 && !counts)) return fail(SCNN_EINVAL, "bad tensor list");

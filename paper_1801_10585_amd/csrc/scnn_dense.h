@@ -225,6 +225,48 @@ hipError_t launch_norm_bwd(const void* x, const void* g, long long rows, const l
                            const void* gamma, const float* mean, const float* rstd, void* dx, void* dgamma, void* dbeta,
                            float* part, int dtype, hipStream_t s);
 
+// A group norm's call, forward (x, gamma, beta, out, mean, rstd) or backward (x, g, gamma, beta, mean, rstd, dx, dgamma, dbeta).
+struct GroupCall {
+    const void *x, *g, *gamma, *beta;
+    void *out, *dx, *dgamma, *dbeta;
+    float *mean, *rstd;  // (read, not written, backward)
+    const long long* offsets;
+    long long rows, batch;
+    int channels, groups, act;
+    float eps;
+    void* workspace;
+};
+size_t group_norm_bytes(int dtype, long long rows, long long batch, int channels, int groups, bool back);
+hipError_t launch_group_fwd(int dtype, const GroupCall& c, hipStream_t s);
+hipError_t launch_group_bwd(int dtype, const GroupCall& c, hipStream_t s);
+hipError_t launch_sample_offsets(const int* coords, int stride, long long rows, const long long* rows_dev, long long batch,
+                                 long long* offsets, hipStream_t s);
+
+hipError_t launch_dropout(int dtype, const void* x, const void* residual, void* out, long long rows, const long long* rows_dev,
+                          long long channels, double p, unsigned long long seed, unsigned long long offset,
+                          const unsigned long long* rng, hipStream_t s);
+
+// Values of a row of 8-bit operands in memory.
+constexpr long long int8_width(long long channels) { return (channels + 63) / 64 * 64; }
+struct Int8Call {
+    const void* x;          // rows of `dtype`, or with x_scale of 8-bit values
+    const float* x_scale;
+    const signed char* w;
+    const float* w_scale;
+    const void *bias, *residual;
+    void* out;
+    long long rows, c_in, c_out;
+    const long long* rows_dev;
+    int act;
+    void* workspace;
+};
+size_t linear_int8_bytes(int dtype, bool given, long long rows, long long c_in, long long c_out);
+hipError_t launch_linear_int8(int dtype, const Int8Call& c, hipStream_t s);
+hipError_t launch_quantize_rows(int dtype, const void* x, long long rows, const long long* rows_dev, long long channels,
+                                signed char* q, float* scale, hipStream_t s);
+hipError_t launch_quantize_weight(int dtype, const void* w, long long c_in, long long c_out, signed char* q, float* scale,
+                                  hipStream_t s);
+
 // A linear layer's call, forward (x, w, bias, residual, out, pre) or backward (x, w, pre, g, dx, dw, dbias).
 struct LinearCall {
     const void *x, *w, *bias, *residual, *g;
