@@ -36,7 +36,7 @@ def is_stale() -> bool:
 def _compile(src: str, force: bool) -> str:
     obj = os.path.join(BUILD, src.replace(".hip", ".o"))
     src_path = os.path.join(CSRC, src)
-    hdr_m = max(os.path.getmtime(p) for p in [os.path.join(CSRC, "scnn_internal.h"), os.path.join(CSRC, "scnn_dense.h"),
+    hdr_m = max(os.path.getmtime(p) for p in [os.path.join(CSRC, "scnn_internal.h"), os.path.join(CSRC, "scnn_dense.h"), os.path.join(CSRC, "scnn_tiles.h"),
                                               os.path.join(HERE, "..", "include", "scnn.h")])
     if not force and os.path.exists(obj) and os.path.getmtime(obj) >= max(os.path.getmtime(src_path), hdr_m):
         return obj

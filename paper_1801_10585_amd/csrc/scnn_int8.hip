@@ -6,7 +6,7 @@
 //
 // The sums are exact: 32-bit integers, |q w| <= 2^14 and fewer than 2^17 of them.  Rows of 8-bit values are filled up with zeros to
 // a multiple of 64, so that every row begins on 64 bytes and k needs no ends.
-#include "scnn_dense.h"
+#include "scnn_tiles.h"
 
 namespace scnn {
 
@@ -43,23 +43,25 @@ __device__ __forceinline__ int quantized(float v, const Quantizer& q) {
     return q.inverse == 0.0f ? 0 : (int)__builtin_rintf(v * q.inverse);
 }
 
-// A workgroup of P threads a row, H vectors of the row in a thread's registers; what a longer row has more is read again.
+// P threads a row (a group of lanes of a wave, or a workgroup of whole waves), H vectors of the row in a thread's registers; what a
+// longer row has more is read again.
 template <typename T, int P, int H>
-__global__ __launch_bounds__(P) void k_quantize_rows(const T* __restrict__ x, long long rows_cap, const long long* __restrict__ rows_dev,
-                                                     long long channels, long long width, signed char* __restrict__ out,
-                                                     float* __restrict__ scale) {
-    constexpr int V = kVec<T>;
+__global__ __launch_bounds__(P < 256 ? 256 : P) void k_quantize_rows(const T* __restrict__ x, long long rows_cap,
+                                                                     const long long* __restrict__ rows_dev, long long channels,
+                                                                     long long width, signed char* __restrict__ out,
+                                                                     float* __restrict__ scale) {
+    constexpr int V = kVec<T>, B = P < 256 ? 256 : P, G = B / P;
     typedef signed char Q __attribute__((ext_vector_type(V)));
-    __shared__ unsigned s_most[P / 64];
-    const long long rows = rows_of(rows_cap, rows_dev), row = block_id<P>();
-    if (row >= rows) return;
-    const bool whole = channels >= V;
+    __shared__ unsigned s_most[B / 64];
+    const int t = threadIdx.x % P;
+    const long long rows = rows_of(rows_cap, rows_dev), row = block_id<B>() * G + threadIdx.x / P;
+    const bool live = row < rows, whole = channels >= V;
     const T* __restrict__ xr = x + row * channels;
     VecOf<T, V> held[H];
     unsigned most = 0;
-    auto at = [&](long long j) { return (j * P + threadIdx.x) * V; };
+    auto at = [&](long long j) { return (j * P + t) * V; };
     auto take = [&](long long c) {
-        const long long n = channels - c;
+        const long long n = live ? channels - c : 0;
         return load_raw<T>(xr + c, (int)(n < V ? (n > 0 ? n : 0) : V), whole);
     };
     auto look = [&](const VecOf<T, V>& v) {
@@ -74,11 +76,18 @@ __global__ __launch_bounds__(P) void k_quantize_rows(const T* __restrict__ x, lo
 #pragma unroll
     for (int j = 0; j < H; ++j) look(held[j]);
     for (long long j = H; at(j) < channels; ++j) look(take(at(j)));
-    most = wave_most(most);
-    if ((threadIdx.x & 63) == 0) s_most[threadIdx.x >> 6] = most;
-    __syncthreads();
 #pragma unroll
-    for (int k = 0; k < P / 64; ++k) most = s_most[k] > most ? s_most[k] : most;
+    for (int d = 1; d < (P < 64 ? P : 64); d <<= 1) {
+        const unsigned o = __shfl_xor(most, d, 64);
+        most = o > most ? o : most;
+    }
+    if constexpr (P > 64) {
+        if ((threadIdx.x & 63) == 0) s_most[threadIdx.x >> 6] = most;
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < P / 64; ++k) most = s_most[k] > most ? s_most[k] : most;
+    }
+    if (!live) return;
     const Quantizer q = quantizer(most);
     signed char* __restrict__ to = out + row * width;
     auto put = [&](long long c, const VecOf<T, V>& v) {
@@ -90,7 +99,7 @@ __global__ __launch_bounds__(P) void k_quantize_rows(const T* __restrict__ x, lo
 #pragma unroll
     for (int j = 0; j < H; ++j) put(at(j), held[j]);
     for (long long j = H; at(j) < width; ++j) put(at(j), take(at(j)));
-    if (threadIdx.x == 0) scale[row] = q.scale;
+    if (t == 0) scale[row] = q.scale;
 }
 
 // 32 columns of w [c_in, c_out] a workgroup: their largest magnitudes, then their values as rows of q by way of LDS.
@@ -136,71 +145,351 @@ struct Int8Args {
     long long m, n, width;
     const long long* rows_dev;
     int act;
+    int* part;          // [splits][m][n], joined by k_int8_join; null: the tile ends the call itself
+    long long k_split;  // bytes of a row that a workgroup sums, a multiple of 64
 };
 
-// Epilogue of four neighbouring columns.
-template <typename T>
-__device__ __forceinline__ void finish4(const Int8Args& p, long long m, long long n, const i4& sum) {
-    const float xs = p.x_scale[m];
-    const int w = (int)(p.n - n < 4 ? p.n - n : 4);
+// Epilogue of C neighbouring columns of which w are there; everything is read before the first is written (out may be residual).
+template <typename T, int C>
+__device__ __forceinline__ void finish(const Int8Args& p, long long m, long long n, int w, float xs, const int (&sum)[C]) {
+    typedef VecOf<T, C> V;
+    float ws[C];
+    V bias = {}, residual = {}, y;
+    const long long at = m * p.n + n;
+    if (w >= C) {
+        __builtin_memcpy(ws, p.w_scale + n, sizeof(ws));
+        if (p.bias) __builtin_memcpy(&bias, (const T*)p.bias + n, sizeof(V));
+        if (p.residual) __builtin_memcpy(&residual, (const T*)p.residual + at, sizeof(V));
+    } else {
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-        if (j < w) {
-            float z = (float)sum[j] * xs * p.w_scale[n + j];
-            if (p.bias) z += (float)((const T*)p.bias)[n + j];
-            z = activate(z, p.act);
-            if (p.residual) z += (float)((const T*)p.residual)[m * p.n + n + j];
-            ((T*)p.out)[m * p.n + n + j] = (T)z;
+        for (int j = 0; j < C; ++j) {
+            ws[j] = j < w ? p.w_scale[n + j] : 0.0f;
+            if (p.bias && j < w) bias[j] = ((const T*)p.bias)[n + j];
+            if (p.residual && j < w) residual[j] = ((const T*)p.residual)[at + j];
         }
+    }
+#pragma unroll
+    for (int j = 0; j < C; ++j) {
+        float z = (float)sum[j] * xs * ws[j];
+        if (p.bias) z += (float)bias[j];
+        z = activate(z, p.act);
+        if (p.residual) z += (float)residual[j];
+        y[j] = (T)z;
+    }
+    if (w >= C) {
+        __builtin_memcpy((T*)p.out + at, &y, sizeof(V));
+    } else {
+#pragma unroll
+        for (int j = 0; j < C; ++j)
+            if (j < w) ((T*)p.out)[at + j] = y[j];
+    }
 }
 
-// 64 x 64 outputs a workgroup of four waves, 64 k a step through registers into LDS.
-template <typename T>
-__global__ __launch_bounds__(256) void k_int8_tile(Int8Args p) {
-    __shared__ i4 s_x[64][4], s_w[64][4];
+// BM x BN outputs a workgroup; a step is 128 bytes of every row, copied from memory to LDS in a ring of STAGES without passing
+// through registers.  Rows of a step are eight pieces of 16 bytes; piece c of row r lies at place c ^ (r % 8), so that the lanes of a
+// read meet different banks (the copy puts pieces down in the order of the lanes, whose addresses carry the permutation).  Rows past
+// the arrays' ends are read from the last one, what they add up to is not stored; a row that ends in the middle of a step has
+// its first half copied twice and multiplied once.  The operands swap places at the instruction: its rows are the tile's
+// columns n, in pairs of blocks (block b of a pair takes columns 8 (i / 4) + 4 b + i % 4, i < 16), so that a lane ends with
+// eight neighbouring columns of one row.
+template <typename T, int BM, int BN, int WM, int WN, int STAGES>
+__global__ __launch_bounds__(64 * WM * WN) void k_int8_ring(Int8Args p) {
+    constexpr int NT = 64 * WM * WN, A8 = BM * 8, B8 = BN * 8, AN = A8 / NT, BN8 = B8 / NT, SLOT = (A8 + B8) * 16, COPIES = AN + BN8;
+    constexpr int TM = BM / WM / 16, TN = BN / WN / 16;
+    static_assert(A8 % NT == 0 && B8 % NT == 0 && TN % 2 == 0, "whole pieces a thread, pairs of blocks");
+    extern __shared__ __align__(1024) char s_ring[];
     const long long m_end = rows_of(p.m, p.rows_dev);
-    const unsigned tiles_n = (unsigned)((p.n + 63) / 64), block = (unsigned)block_id<256>();
-    const long long m0 = (long long)(block / tiles_n) * 64, n0 = (long long)(block % tiles_n) * 64;
+    unsigned tile_m, tile_n;
+    const unsigned tiles_m = (unsigned)((p.m + BM - 1) / BM), tiles_n = (unsigned)((p.n + BN - 1) / BN), block = (unsigned)block_id<NT>();
+    const bool any = block < tiles_m * tiles_n;
+    tile_at(any ? block : 0, tiles_m, tiles_n, tile_m, tile_n);
+    const long long m0 = any ? (long long)tile_m * BM : m_end, n0 = (long long)tile_n * BN;
     if (m0 >= m_end) return;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, i16 = lane & 15, q = lane >> 4;
-    const int wm = (wave >> 1) * 32, wn = (wave & 1) * 32;
-    const int r = tid >> 2, c = tid & 3;
-    // (rows past the end are read from the last one, what they add up to is not stored)
-    const signed char* __restrict__ xr = p.x + (m0 + r < m_end ? m0 + r : m_end - 1) * p.width + c * 16;
-    const signed char* __restrict__ wr = p.w + (n0 + r < p.n ? n0 + r : p.n - 1) * p.width + c * 16;
-    i4 acc[2][2] = {};
-    i4 nx = *(const i4*)xr, nw = *(const i4*)wr;
-    for (long long k = 0; k < p.width; k += 64) {
-        __syncthreads();
-        s_x[r][c ^ ((r >> 1) & 3)] = nx;
-        s_w[r][c ^ ((r >> 1) & 3)] = nw;
-        __syncthreads();
-        if (k + 64 < p.width) {
-            nx = *(const i4*)(xr + k + 64);
-            nw = *(const i4*)(wr + k + 64);
+    const long long k_first = (long long)blockIdx.y * p.k_split;
+    const int bytes = (int)(p.width - k_first < p.k_split ? p.width - k_first : p.k_split);  // (of every row: a multiple of 64)
+    const int steps = (bytes + 127) / 128;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wm = (wave / WN) * (TM * 16), wn = (wave % WN) * (TN * 16), q = lane >> 4, i16 = lane & 15;
+    const unsigned ring = (unsigned)(size_t)(__attribute__((address_space(3))) char*)s_ring;
+
+    // this thread's pieces: byte offsets from the tile's first value at the step's first k
+    auto offset_of = [&](int e, long long first, long long end) -> unsigned {
+        const int r = e >> 3, c = (e & 7) ^ (r & 7);
+        const long long row = first + r < end ? r : end - 1 - first;
+        return (unsigned)(row * p.width + c * 16);
+    };
+    unsigned at_a[AN], at_b[BN8];
+#pragma unroll
+    for (int i = 0; i < AN; ++i) at_a[i] = offset_of(i * NT + tid, m0, m_end);
+#pragma unroll
+    for (int i = 0; i < BN8; ++i) at_b[i] = offset_of(i * NT + tid, n0, p.n);
+    const signed char *base_a = p.x + m0 * p.width + k_first, *base_b = p.w + n0 * p.width + k_first;
+    // (piece 4 to 7 of the last step, where the row has none: 64 bytes back)
+    auto copy_step = [&](int slot, bool half) {
+        const unsigned to = ring + slot * SLOT + wave * 1024;
+#pragma unroll
+        for (int i = 0; i < AN; ++i) {
+            const int e = i * NT + tid, c = (e & 7) ^ ((e >> 3) & 7);
+            copy_to_lds(base_a, at_a[i] - (half && c >= 4 ? 64u : 0u), to + i * NT * 16);
         }
-        i4 fx[2], fw[2];
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int a = wm + i * 16 + i16, b = wn + i * 16 + i16;
-            fx[i] = s_x[a][q ^ ((a >> 1) & 3)];
-            fw[i] = s_w[b][q ^ ((b >> 1) & 3)];
+        for (int i = 0; i < BN8; ++i) {
+            const int e = i * NT + tid, c = (e & 7) ^ ((e >> 3) & 7);
+            copy_to_lds(base_b, at_b[i] - (half && c >= 4 ? 64u : 0u), to + A8 * 16 + i * NT * 16);
+        }
+        base_a += 128;
+        base_b += 128;
+    };
+    i4 acc[TM][TN];
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j) acc[i][j] = i4{0, 0, 0, 0};
+    auto multiply = [&](const char* sa, const char* sb, int kk) {
+        i4 fa[TM], fb[TN];
+#pragma unroll
+        for (int j = 0; j < TN; ++j) {
+            const int r = wn + (j & ~1) * 16 + 8 * (i16 >> 2) + 4 * (j & 1) + (i16 & 3);
+            fb[j] = *(const i4*)(sb + (r * 8 + ((kk * 4 + q) ^ (r & 7))) * 16);
         }
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int i = 0; i < TM; ++i) {
+            const int r = wm + i * 16 + i16;
+            fa[i] = *(const i4*)(sa + (r * 8 + ((kk * 4 + q) ^ (r & 7))) * 16);
+        }
+        __builtin_amdgcn_s_setprio(1);  // (a wave that multiplies goes before those that fetch)
 #pragma unroll
-            for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fw[j], fx[i], acc[i][j], 0, 0, 0);
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int j = 0; j < TN; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fb[j], fa[i], acc[i][j], 0, 0, 0);
+        __builtin_amdgcn_s_setprio(0);
+    };
+    const bool odd = (bytes & 127) != 0;
+#pragma unroll
+    for (int i = 0; i < STAGES - 1; ++i)
+        if (i < steps) copy_step(i, odd && i == steps - 1);
+    int slot = 0;
+    for (int step = 0; step < steps; ++step) {
+        // this step's copies have landed; its predecessor has been read by all waves, so that its slot can be filled
+        if (step + STAGES - 1 <= steps) copies_and_barrier<(STAGES - 2) * COPIES>();
+        else copies_and_barrier<0>();
+        if (step + STAGES - 1 < steps) copy_step(slot == 0 ? STAGES - 1 : slot - 1, odd && step + STAGES == steps);
+        const char* const s = s_ring + slot * SLOT;
+        multiply(s, s + A8 * 16, 0);
+        if (!odd || step + 1 < steps) multiply(s, s + A8 * 16, 1);
+        slot = slot == STAGES - 1 ? 0 : slot + 1;
     }
-    // lane: row m = lane % 16, columns n = 4 (lane / 16) .. + 3 of each block
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < TM; ++i) {
         const long long m = m0 + wm + i * 16 + i16;
         if (m >= m_end) continue;
+        const float xs = p.part ? 0.0f : p.x_scale[m];
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const long long n = n0 + wn + j * 16 + 4 * q;
-            if (n < p.n) finish4<T>(p, m, n, acc[i][j]);
+        for (int j = 0; j < TN; j += 2) {
+            const long long n = n0 + wn + j * 16 + 8 * q;
+            if (n >= p.n) continue;
+            const int sum[8] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3],
+                                acc[i][j + 1][0], acc[i][j + 1][1], acc[i][j + 1][2], acc[i][j + 1][3]};
+            const int w = (int)(p.n - n < 8 ? p.n - n : 8);
+            if (p.part) {
+                int* to = p.part + ((long long)blockIdx.y * p.m + m) * p.n + n;
+                if (w == 8) {
+                    __builtin_memcpy(to, sum, sizeof(sum));
+                } else {
+#pragma unroll
+                    for (int c = 0; c < 8; ++c)
+                        if (c < w) to[c] = sum[c];
+                }
+            } else {
+                finish<T, 8>(p, m, n, w, xs, sum);
+            }
         }
+    }
+}
+
+// Up to 16 MB rows: bound by reading w once.  Eight waves share the k of 16 NB columns, operands straight from memory to the
+// registers that the instruction wants, a lane 16 bytes of one row; their sums meet in LDS.
+template <typename T, int MB, int NB>
+__global__ __launch_bounds__(512) void k_int8_skinny(Int8Args p) {
+    constexpr int W = 8, U = 4;
+    __shared__ int s_sum[W][MB * NB][4][64];
+    const long long m_end = rows_of(p.m, p.rows_dev);
+    const long long n0 = block_id<512>() * (16 * NB);
+    if (n0 >= p.n || m_end < 1) return;
+    const long long k_first = (long long)blockIdx.y * p.k_split;
+    const int bytes = (int)(p.width - k_first < p.k_split ? p.width - k_first : p.k_split);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = lane >> 4, i16 = lane & 15;
+    const signed char *x[MB], *w[NB];
+#pragma unroll
+    for (int i = 0; i < MB; ++i) x[i] = p.x + (16 * i + i16 < m_end ? 16 * i + i16 : m_end - 1) * p.width + k_first + q * 16;
+#pragma unroll
+    for (int j = 0; j < NB; ++j) w[j] = p.w + (n0 + 16 * j + i16 < p.n ? n0 + 16 * j + i16 : p.n - 1) * p.width + k_first + q * 16;
+    i4 acc[MB][NB];
+#pragma unroll
+    for (int i = 0; i < MB; ++i)
+#pragma unroll
+        for (int j = 0; j < NB; ++j) acc[i][j] = i4{0, 0, 0, 0};
+    // a wave's steps of 64 bytes lie next to each other
+    const int steps = bytes / 64, each = (steps + W - 1) / W;
+    const int from = wave * each, to = from + each < steps ? from + each : steps;
+    for (int s = from; s < to; s += U) {
+        i4 fx[U][MB], fw[U][NB];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const bool live = s + u < to;
+            const long long at = (long long)(live ? s + u : s) * 64;
+#pragma unroll
+            for (int j = 0; j < NB; ++j) fw[u][j] = *(const i4*)(w[j] + at);
+#pragma unroll
+            for (int i = 0; i < MB; ++i) fx[u][i] = *(const i4*)(x[i] + at);
+            if (!live)
+#pragma unroll
+                for (int j = 0; j < NB; ++j) fw[u][j] = i4{0, 0, 0, 0};
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int i = 0; i < MB; ++i)
+#pragma unroll
+                for (int j = 0; j < NB; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fw[u][j], fx[u][i], acc[i][j], 0, 0, 0);
+    }
+#pragma unroll
+    for (int i = 0; i < MB; ++i)
+#pragma unroll
+        for (int j = 0; j < NB; ++j)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) s_sum[wave][i * NB + j][c][lane] = acc[i][j][c];
+    __syncthreads();
+    // four neighbouring columns a thread: lane (m, q) of block (i, j) as the instruction left them
+    for (int e = threadIdx.x; e < MB * NB * 64; e += 512) {
+        const int l = e & 63, b = e >> 6, i = b / NB, j = b % NB;
+        const long long m = 16 * i + (l & 15), n = n0 + 16 * j + 4 * (l >> 4);
+        if (m >= m_end || n >= p.n) continue;
+        int sum[4] = {0, 0, 0, 0};
+#pragma unroll
+        for (int v = 0; v < W; ++v)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) sum[c] += s_sum[v][b][c][l];
+        const int width = (int)(p.n - n < 4 ? p.n - n : 4);
+        if (p.part) {
+            int* to4 = p.part + ((long long)blockIdx.y * p.m + m) * p.n + n;
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+                if (c < width) to4[c] = sum[c];
+        } else {
+            finish<T, 4>(p, m, n, width, p.x_scale[m], sum);
+        }
+    }
+}
+
+// Joins the sums of a split k and ends the call: four neighbouring columns a thread.
+template <typename T>
+__global__ __launch_bounds__(256) void k_int8_join(Int8Args p, int splits) {
+    const long long m_end = rows_of(p.m, p.rows_dev), quads = (p.n + 3) / 4;
+    const long long id = block_id<256>() * 256 + threadIdx.x, m = id / quads, n = id % quads * 4;
+    if (m >= m_end) return;
+    const int w = (int)(p.n - n < 4 ? p.n - n : 4);
+    const int* __restrict__ f = p.part + m * p.n + n;
+    const long long step = p.m * p.n;
+    int sum[4] = {0, 0, 0, 0};
+#pragma unroll 8
+    for (int s = 0; s < splits; ++s) {
+        i4 v = {0, 0, 0, 0};
+        if (w == 4) {
+            __builtin_memcpy(&v, f + s * step, sizeof(v));
+        } else {
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+                if (c < w) v[c] = f[s * step + c];
+        }
+#pragma unroll
+        for (int c = 0; c < 4; ++c) sum[c] += v[c];
+    }
+    finish<T, 4>(p, m, n, w, p.x_scale[m], sum);
+}
+
+// One row, brought to 8 bits by every workgroup for itself: bound by reading w once.  A wave takes R columns (rows of w), its first
+// pieces of them on their way while the row is quantised; a lane multiplies 16 bytes at a time, four products an instruction.
+// GIVEN: the row is there in 8 bits.
+constexpr int kRowThreads = 256, kRowLds = 16384;  // bytes of the row in LDS at a time
+template <typename T, int R, bool GIVEN>
+__global__ __launch_bounds__(kRowThreads) void k_int8_row(Int8Args p, const T* __restrict__ x, int c_in) {
+    constexpr int V = kVec<T>, P = kRowThreads, U = 4;
+    __shared__ __align__(16) signed char s_x[kRowLds];
+    __shared__ unsigned s_most[P / 64];
+    if (rows_of(p.m, p.rows_dev) < 1) return;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const long long n0 = (block_id<P>() * (P / 64) + wave) * R;
+    const int width = (int)p.width;
+    const signed char* w[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) w[r] = p.w + (n0 + r < p.n ? n0 + r : p.n - 1) * p.width;
+    i4 held[U][R];
+    auto fetch = [&](int u, int k) {  // (past the row's end: its first bytes, times 0)
+#pragma unroll
+        for (int r = 0; r < R; ++r) held[u][r] = *(const i4*)(w[r] + (k < width ? k : 0));
+    };
+#pragma unroll
+    for (int u = 0; u < U; ++u) fetch(u, (u * 64 + lane) * 16);
+    Quantizer z = {0.0f, 0.0f};
+    if constexpr (!GIVEN) {
+        unsigned most = 0;
+        for (int c = threadIdx.x * V; c < c_in; c += P * V) {
+            const VecOf<T, V> v = load_raw<T>(x + c, c_in - c, c_in >= V);
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const unsigned a = magnitude((float)v[i]);
+                most = a > most ? a : most;
+            }
+        }
+        most = wave_most(most);
+        if (lane == 0) s_most[wave] = most;
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < P / 64; ++k) most = s_most[k] > most ? s_most[k] : most;
+        z = quantizer(most);
+    } else {
+        z.scale = p.x_scale[0];
+    }
+    int acc[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) acc[r] = 0;
+    for (int k0 = 0; k0 < width; k0 += kRowLds) {
+        const int part = width - k0 < kRowLds ? width - k0 : kRowLds;
+        __syncthreads();
+        if constexpr (GIVEN) {
+            for (int c = threadIdx.x * 16; c < part; c += P * 16) *(i4*)(s_x + c) = *(const i4*)(p.x + k0 + c);
+        } else {
+            typedef signed char Q __attribute__((ext_vector_type(V)));
+            for (int c = threadIdx.x * V; c < part; c += P * V) {
+                const int n = c_in - k0 - c;
+                const VecOf<T, V> v = load_raw<T>(x + k0 + c, n > 0 ? n : 0, c_in >= V);
+                Q b;
+#pragma unroll
+                for (int i = 0; i < V; ++i) b[i] = (signed char)quantized((float)v[i], z);
+                *(Q*)(s_x + c) = b;
+            }
+        }
+        __syncthreads();
+        for (int k = lane * 16; k < part; k += U * 1024) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int at = k + u * 1024;
+                const i4 v = at < part ? *(const i4*)(s_x + at) : i4{0, 0, 0, 0};
+#pragma unroll
+                for (int r = 0; r < R; ++r)
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) acc[r] = __builtin_amdgcn_sdot4(v[c], held[u][r][c], acc[r], false);
+                fetch(u, k0 + at + U * 1024);
+            }
+        }
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        int sum[1] = {acc[r]};
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) sum[0] += __shfl_xor(sum[0], d, 64);
+        if (lane == r && n0 + r < p.n) finish<T, 1>(p, 0, n0 + r, 1, z.scale, sum);
     }
 }
 
@@ -208,9 +497,15 @@ __global__ __launch_bounds__(256) void k_int8_tile(Int8Args p) {
 template <typename T>
 static hipError_t quantize(const void* x, long long rows, const long long* rows_dev, long long channels, signed char* q, float* scale,
                            hipStream_t s) {
-    const long long width = int8_width(channels);
-    hipLaunchKernelGGL((k_quantize_rows<T, 256, 4>), grid_of<256>(rows), dim3(256), 0, s, (const T*)x, rows, rows_dev, channels, width,
-                       q, scale);
+    const long long width = int8_width(channels), units = width / kVec<T>;
+#define F(P, H)                                                                                                           \
+    hipLaunchKernelGGL((k_quantize_rows<T, P, H>), (grid_of<P < 256 ? 256 : P>((rows + (P < 256 ? 256 / P : 1) - 1) / (P < 256 ? 256 / P : 1))), \
+                       dim3(P < 256 ? 256 : P), 0, s, (const T*)x, rows, rows_dev, channels, width, q, scale)
+    if (units <= 32) F(16, 2);
+    else if (units <= 128) F(64, 2);
+    else if (units <= 512 || rows >= 4LL * device_cu_count()) F(256, 2);
+    else F(1024, 2);
+#undef F
     return hipGetLastError();
 }
 
@@ -239,24 +534,94 @@ hipError_t launch_quantize_weight(int dtype, const void* w, long long c_in, long
     }
 }
 
-struct Int8Space { size_t q, scale, total; };
-static Int8Space int8_space(bool given, long long rows, long long c_in) {
+enum class Int8Kind { kRow, kSkinny, kRing256, kRing128, kRing64x128, kRing64 };
+struct Int8Plan {
+    Int8Kind kind;
+    int bm, bn, splits;
+    long long k_split;
+};
+static Int8Plan int8_plan(long long m, long long n, long long width) {
+    Int8Plan t = {Int8Kind::kRow, 1, 1, 1, width};
+    if (m <= 1) return t;
+    const long long cus = device_cu_count();
+    auto tiles = [&](long long bm, long long bn) { return ((m + bm - 1) / bm) * ((n + bn - 1) / bn); };
+    long long least = 512;  // bytes of k that a workgroup of a split has at least
+    if (m <= 64) {
+        t.kind = Int8Kind::kSkinny;
+        t.bm = m <= 16 ? 16 : (m <= 32 ? 32 : 64);
+        t.bn = m <= 32 ? 16 : 32;
+        least = 1024;
+    } else {
+        const long long largest = tiles(256, 256), rounds = (largest + cus - 1) / cus;
+        if (m > 128 && n > 128 && rounds >= 2 && 20 * largest >= 19 * rounds * cus) t.kind = Int8Kind::kRing256, t.bm = t.bn = 256;
+        else if (n > 64 && 4 * tiles(128, 128) >= 5 * cus) t.kind = Int8Kind::kRing128, t.bm = t.bn = 128;
+        else if (n > 64 && tiles(64, 128) >= cus) t.kind = Int8Kind::kRing64x128, t.bm = 64, t.bn = 128;
+        else t.kind = Int8Kind::kRing64, t.bm = t.bn = 64;
+    }
+    const long long all = tiles(t.bm, t.bn);
+    if (all < cus) {
+        long long s = cus / all, most = width / least;
+        if (s > most) s = most;
+        if (s > 1) t.k_split = round_up((width + s - 1) / s, t.kind == Int8Kind::kSkinny ? 512 : 128);
+    }
+    t.splits = (int)((width + t.k_split - 1) / t.k_split);
+    return t;
+}
+
+struct Int8Space { size_t q, scale, part, total; };
+static Int8Space int8_space(bool given, long long rows, long long c_in, long long c_out) {
     Int8Space a = {};
-    if (given) return a;
-    a.scale = (size_t)round_up(rows * int8_width(c_in), 256);
-    a.total = a.scale + (size_t)round_up(rows * 4, 256);
+    const Int8Plan t = int8_plan(rows, c_out, int8_width(c_in));
+    if (t.kind == Int8Kind::kRow) return a;
+    if (!given) {
+        a.scale = (size_t)round_up(rows * int8_width(c_in), 256);
+        a.part = a.scale + (size_t)round_up(rows * 4, 256);
+    }
+    a.total = a.part + (t.splits > 1 ? (size_t)round_up(t.splits * rows * c_out * 4, 256) : 0);
     return a;
 }
 size_t linear_int8_bytes(int dtype, bool given, long long rows, long long c_in, long long c_out) {
-    return int8_space(given, rows, c_in).total;
+    return int8_space(given, rows, c_in, c_out).total;
+}
+
+template <typename T, int BM, int BN, int WM, int WN, int STAGES>
+static hipError_t ring(const Int8Args& p, long long tiles, int splits, hipStream_t s) {
+    constexpr int lds = (BM + BN) * 128 * STAGES;
+    auto kernel = k_int8_ring<T, BM, BN, WM, WN, STAGES>;
+    if (lds >= 65536) {
+        const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+        if (e != hipSuccess) return e;
+    }
+    hipLaunchKernelGGL(kernel, grid_of<64 * WM * WN>(tiles, (unsigned)splits), dim3(64 * WM * WN), lds, s, p);
+    return hipGetLastError();
+}
+
+template <typename T, bool GIVEN>
+static void one_row(const Int8Args& p, const void* x, int c_in, hipStream_t s) {
+    const long long cus = device_cu_count(), waves = kRowThreads / 64;
+#define F(R) hipLaunchKernelGGL((k_int8_row<T, R, GIVEN>), grid_of<kRowThreads>((p.n + waves * R - 1) / (waves * R)), dim3(kRowThreads), 0, s, p, (const T*)x, c_in)
+    if (p.n >= 4 * waves * cus) F(4);
+    else if (p.n >= 2 * waves * cus) F(2);
+    else F(1);
+#undef F
 }
 
 template <typename T>
 static hipError_t linear_int8(int dtype, const Int8Call& c, hipStream_t s) {
     Int8Args p = {};
-    const Int8Space at = int8_space(c.x_scale != nullptr, c.rows, c.c_in);
     p.x = (const signed char*)c.x;
     p.x_scale = c.x_scale;
+    p.w = c.w; p.w_scale = c.w_scale; p.bias = c.bias; p.residual = c.residual; p.out = c.out;
+    p.m = c.rows; p.n = c.c_out; p.width = int8_width(c.c_in);
+    p.rows_dev = c.rows_dev;
+    p.act = c.act;
+    const Int8Plan t = int8_plan(p.m, p.n, p.width);
+    if (t.kind == Int8Kind::kRow) {
+        if (c.x_scale) one_row<T, true>(p, c.x, (int)c.c_in, s);
+        else one_row<T, false>(p, c.x, (int)c.c_in, s);
+        return hipGetLastError();
+    }
+    const Int8Space at = int8_space(c.x_scale != nullptr, c.rows, c.c_in, c.c_out);
     if (!c.x_scale) {
         signed char* const q = (signed char*)c.workspace + at.q;
         float* const scale = (float*)((char*)c.workspace + at.scale);
@@ -265,12 +630,26 @@ static hipError_t linear_int8(int dtype, const Int8Call& c, hipStream_t s) {
         p.x = q;
         p.x_scale = scale;
     }
-    p.w = c.w; p.w_scale = c.w_scale; p.bias = c.bias; p.residual = c.residual; p.out = c.out;
-    p.m = c.rows; p.n = c.c_out; p.width = int8_width(c.c_in);
-    p.rows_dev = c.rows_dev;
-    p.act = c.act;
-    const long long tiles = ((p.m + 63) / 64) * ((p.n + 63) / 64);
-    hipLaunchKernelGGL((k_int8_tile<T>), grid_of<256>(tiles), dim3(256), 0, s, p);
+    p.k_split = t.k_split;
+    if (t.splits > 1) p.part = (int*)((char*)c.workspace + at.part);
+    const long long tiles = ((p.m + t.bm - 1) / t.bm) * ((p.n + t.bn - 1) / t.bn);
+    hipError_t e = hipSuccess;
+    switch (t.kind) {
+        case Int8Kind::kSkinny: {
+            const dim3 grid = grid_of<512>(tiles, (unsigned)t.splits);
+            if (t.bm == 16) hipLaunchKernelGGL((k_int8_skinny<T, 1, 1>), grid, dim3(512), 0, s, p);
+            else if (t.bm == 32) hipLaunchKernelGGL((k_int8_skinny<T, 2, 1>), grid, dim3(512), 0, s, p);
+            else hipLaunchKernelGGL((k_int8_skinny<T, 4, 2>), grid, dim3(512), 0, s, p);
+            e = hipGetLastError();
+            break;
+        }
+        case Int8Kind::kRing256: e = ring<T, 256, 256, 2, 4, 2>(p, tiles, t.splits, s); break;
+        case Int8Kind::kRing128: e = ring<T, 128, 128, 2, 2, 2>(p, tiles, t.splits, s); break;
+        case Int8Kind::kRing64x128: e = ring<T, 64, 128, 2, 2, 3>(p, tiles, t.splits, s); break;
+        default: e = ring<T, 64, 64, 2, 2, 2>(p, tiles, t.splits, s);
+    }
+    if (e != hipSuccess || t.splits <= 1) return e;
+    hipLaunchKernelGGL((k_int8_join<T>), grid_of<256>((p.m * ((p.n + 3) / 4) + 255) / 256), dim3(256), 0, s, p, t.splits);
     return hipGetLastError();
 }
 

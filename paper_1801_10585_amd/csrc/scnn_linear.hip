@@ -10,7 +10,7 @@
 // is laid out anew.  16-bit operands multiply as they are; fp32 operands are split into three bf16 numbers each while they
 // are staged, and six of the nine products are multiplied (split8, split_products: as close to the exact sum as fp32
 // products): 182 TFLOP/s on 4096 x 4096 x 4096 where the library's fp32 product reaches 147.  All sums are fp32.
-#include "scnn_dense.h"
+#include "scnn_tiles.h"
 
 namespace scnn {
 
@@ -431,31 +431,6 @@ __global__ __launch_bounds__(64 * WM * WN * KG) void k_linear_tile(LinearArgs p)
             }
         }
     }
-}
-
-// Tiles of a launch in the order of its workgroups.  Workgroup i runs on XCD i % 8: each XCD takes one run of neighbouring
-// tiles, and within a run eight rows of tiles go side by side, so that the tiles that an L2 works on share their operands.
-__device__ __forceinline__ void tile_at(unsigned block, unsigned tiles_m, unsigned tiles_n, unsigned& tm, unsigned& tn) {
-    const unsigned all = tiles_m * tiles_n, each = all / kXcds, more = all % kXcds;
-    const unsigned xcd = block % kXcds, i = block / kXcds;
-    const unsigned at = xcd * each + (xcd < more ? xcd : more) + i;
-    constexpr unsigned kSide = 8;
-    const unsigned group = at / (kSide * tiles_n), in = at % (kSide * tiles_n);
-    const unsigned side = tiles_m - group * kSide < kSide ? tiles_m - group * kSide : kSide;
-    // (divisions leave the vector unit: the addresses that follow from these are to be scalar)
-    tm = (unsigned)__builtin_amdgcn_readfirstlane((int)(group * kSide + in % side));
-    tn = (unsigned)__builtin_amdgcn_readfirstlane((int)(in / side));
-}
-
-// Sixteen bytes a lane straight from memory to LDS: lane l's to lds + 16 l.
-__device__ __forceinline__ void copy_to_lds(const void* base, unsigned offset, unsigned lds) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(base) : "memory", "m0");
-}
-// Waits until at most N of this wave's copies are on their way and its LDS reads have arrived, then for the workgroup's
-// other waves.
-template <int N>
-__device__ __forceinline__ void copies_and_barrier() {
-    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
 }
 
 // The same product for 16-bit operands whose rows begin on 16 bytes: tiles of BM x BN x BK go from memory to LDS without
