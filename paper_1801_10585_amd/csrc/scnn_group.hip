@@ -22,7 +22,7 @@
 
 namespace scnn {
 
-constexpr int kGroupThreads = 512;  // most threads of a workgroup that takes a block of rows
+constexpr int kGroupThreads = 256;  // most threads of a workgroup that takes a block of rows
 constexpr int kHereGroups = 64;     // most groups of a slab whose sums a workgroup joins by itself
 
 // How threads lie over columns.  A workgroup takes `wide` columns from c0 on: tv threads a row, a vector each, `reps` rows at
@@ -33,7 +33,9 @@ struct GroupLayout {
     int tv, reps, active, pitch, flat;
     int wide, slabs, pieces;  // a slab is whole groups (pieces 1), or one of `pieces` pieces of a group
     int merged;               // a vector's columns are of one group
+    int sub;                  // neighbouring values of a vector that are of one group, whatever the vector (a power of two)
     float inv_tv, inv_per, inv_c;
+    double inv_reps;
 };
 
 struct GroupArgs {
@@ -44,6 +46,7 @@ struct GroupArgs {
     long long each;              // rows of a sample where offsets is null
     long long rows, chunk;       // chunk: rows of a block
     long long batch, blocks, places;
+    double inv_each, inv_chunk;
     int channels, groups, per, act;
     float eps;
     float* cols;                 // backward: [places][2][channels], sums of dz xh and dz over a place's rows; null: not wanted
@@ -54,15 +57,18 @@ struct GroupArgs {
 
 // a / d for whole numbers a < 2^21 by way of 1 / d in fp32: (a + 1/2) / d is no nearer to a whole number than 1 / (2 d).
 __device__ __forceinline__ int quotient(int a, float inverse) { return (int)(((float)a + 0.5f) * inverse); }
+// The same for a < 2^31.  (A division of 64 bits is a hundred instructions.)
+__device__ __forceinline__ long long quotient(long long a, double inverse) { return (long long)(unsigned)(((double)(unsigned)a + 0.5) * inverse); }
 
 // The samples' bounds.  Up to 63 samples a wave holds them all, a lane each.
 struct Bounds {
     const long long* offsets;
     long long each, rows, batch, lane_row;
+    double inv_each;
     bool here;
 };
 __device__ __forceinline__ Bounds bounds_of(const GroupArgs& p) {
-    Bounds s = {p.offsets, p.each, p.rows, p.batch, 0, p.offsets != nullptr && p.batch < 64};
+    Bounds s = {p.offsets, p.each, p.rows, p.batch, 0, p.inv_each, p.offsets != nullptr && p.batch < 64};
     const int lane = threadIdx.x & 63;
     if (s.here) {
         const long long r = p.offsets[lane <= p.batch ? lane : p.batch];
@@ -76,11 +82,8 @@ __device__ __forceinline__ long long uniform(long long v) {
 }
 __device__ __forceinline__ long long first_row(const Bounds& s, long long b) {
     if (!s.offsets) return b * s.each;
-    if (s.here) {
-        const int lane = __builtin_amdgcn_readfirstlane((int)b);
-        return (long long)((unsigned long long)(unsigned)__builtin_amdgcn_readlane((int)((unsigned long long)s.lane_row >> 32), lane) << 32 |
-                           (unsigned)__builtin_amdgcn_readlane((int)s.lane_row, lane));
-    }
+    if (s.here)  // (rows: fewer than 2^31)
+        return (unsigned)__builtin_amdgcn_readlane((int)s.lane_row, __builtin_amdgcn_readfirstlane((int)b));
     const long long r = s.offsets[b];
     return r < 0 ? 0 : (r < s.rows ? r : s.rows);
 }
@@ -113,7 +116,7 @@ __device__ __forceinline__ long long count_up_to(long long n, long long limit, F
 __device__ __forceinline__ long long sample_at(const Bounds& s, long long r) {
     long long b;
     if (!s.offsets) {
-        b = s.each > 0 ? r / s.each : 0;
+        b = s.each > 0 ? quotient(r, s.inv_each) : 0;
     } else if (s.here) {
         const int lane = threadIdx.x & 63;
         b = __popcll(__ballot(lane > 0 && lane <= s.batch && s.lane_row <= r));
@@ -138,6 +141,7 @@ __device__ __forceinline__ Block block_of(const GroupArgs& p, const Bounds& s, l
 struct Slab { int c0, c1, j0, ng, w; };
 __device__ __forceinline__ Slab slab_of(const GroupArgs& p) {
     const int s = blockIdx.y;
+    if (p.l.slabs == 1) return {0, p.channels, 0, p.groups, p.per};
     Slab a;
     if (p.l.pieces > 1) {
         a.j0 = s / p.l.pieces;
@@ -148,8 +152,8 @@ __device__ __forceinline__ Slab slab_of(const GroupArgs& p) {
     } else {
         a.c0 = s * p.l.wide;
         a.c1 = a.c0 + p.l.wide < p.channels ? a.c0 + p.l.wide : p.channels;
-        a.j0 = p.l.slabs > 1 ? a.c0 / p.per : 0;
-        a.ng = p.l.slabs > 1 ? (a.c1 - a.c0) / p.per : p.groups;
+        a.j0 = a.c0 / p.per;
+        a.ng = (a.c1 - a.c0) / p.per;
         a.w = p.per;
     }
     return a;
@@ -182,10 +186,9 @@ template <int V>
 __device__ __forceinline__ Walk walk_of(const GroupArgs& p, const Slab& a, const Place& t, long long lo, long long hi) {
     Walk w = {0, 0, 0, 0, 0};
     if ((int)threadIdx.x >= p.l.active || hi <= lo) return w;
-    const unsigned rows = (unsigned)(hi - lo), steps = rows / (unsigned)p.l.reps;  // (rows: fewer than 2^31)
-    const int left = (int)(rows - steps * (unsigned)p.l.reps);
+    const int steps = (int)quotient(hi - lo, p.l.inv_reps), left = (int)(hi - lo - (long long)steps * p.l.reps);
     w.step = (long long)p.l.reps * p.channels;
-    w.full = (int)steps;
+    w.full = steps;
     if (p.l.flat) {
         w.at = lo * p.channels + t.col;
         const int n = left * p.channels - t.col;  // (fewer than a step's values)
@@ -209,67 +212,6 @@ template <typename T> __device__ __forceinline__ VecOf<T, kVec<T>> take(const T*
 // Results are not read again soon: they leave the L2 to the rows.
 template <typename T> __device__ __forceinline__ void put(T* p, VecOf<T, kVec<T>> v) { __builtin_nontemporal_store(v, (Loose<T>*)p); }
 
-__device__ __forceinline__ float finite_or_zero(float v) { return __builtin_fabsf(v) < __builtin_huge_valf() ? v : 0.0f; }
-
-// Power of two of lanes that add n values: at most a wave.
-__device__ __forceinline__ int lanes_for(int n) {
-    int q = 1;
-    while (q < n && q < 64) q <<= 1;
-    return q;
-}
-
-// Accumulators of a thread: one a column, or two for all of a vector's columns where these are of one group.
-template <typename T, bool M> constexpr int kSums = M ? 2 : kVec<T>;
-
-// Sums over the slab's groups of the threads' numbers, then done(group, sum) by one lane a group.  All threads of the workgroup call it.
-// s_all: a number a thread (merged), or a vector of them.
-template <typename T, bool M, typename F>
-__device__ __forceinline__ void add_groups(const GroupArgs& p, const Slab& a, const double (&v)[kSums<T, M>], double* s_all, F done) {
-    constexpr int V = kVec<T>;
-    __syncthreads();
-    if ((int)threadIdx.x < p.l.active) {
-        if constexpr (M) {
-            s_all[threadIdx.x] = v[0] + v[1];
-        } else {
-#pragma unroll
-            for (int i = 0; i < V; ++i) s_all[threadIdx.x * V + i] = v[i];
-        }
-    }
-    __syncthreads();
-    const int w = M ? (a.w + V - 1) / V : a.w, pitch = M ? p.l.tv : p.l.pitch, n = w * p.l.reps, q = lanes_for(n);
-    const float inv = 1.0f / (float)w;
-    const int set = threadIdx.x / q, sets = blockDim.x / q, in = threadIdx.x & (q - 1);
-    for (int j0 = 0; j0 < a.ng; j0 += sets) {
-        const int j = j0 + set;
-        double sum = 0.0;
-        if (j < a.ng)
-            for (int e = in; e < n; e += q) {
-                const int k = quotient(e, inv);
-                sum += s_all[k * pitch + j * w + (e - k * w)];
-            }
-        for (int d = 1; d < q; d <<= 1) sum += __shfl_xor(sum, d, 64);
-        if (in == 0 && j < a.ng) done(j, sum);
-    }
-}
-
-// The first value of each accumulator's group in row `origin`.
-template <typename T, bool M>
-__device__ __forceinline__ void first_values(const GroupArgs& p, const Slab& a, const Place& t, long long origin, float (&s)[kSums<T, M>]) {
-    const T* __restrict__ x = (const T*)p.x + origin * p.channels + (long long)a.j0 * p.per;
-#pragma unroll
-    for (int i = 0; i < kSums<T, M>; ++i)
-        s[i] = M && i ? s[0] : (float)x[(long long)group_of(p, column_of(p, a, t, i)) * p.per];
-#pragma unroll
-    for (int i = 0; i < kSums<T, M>; ++i) s[i] = finite_or_zero(s[i]);
-}
-template <typename T, bool M>
-__device__ __forceinline__ void add_value(float x, int i, const double (&s)[kSums<T, M>], double (&s1)[kSums<T, M>], double (&s2)[kSums<T, M>]) {
-    const int k = M ? i & 1 : i;
-    const double d = (double)x - s[k];
-    s1[k] += d;
-    s2[k] = __builtin_fma(d, d, s2[k]);
-}
-
 // U vectors of a thread on their way: number k, k + 1, ... upwards, or k - 1, k - 2, ... downwards (the last ones of a block are
 // what the L2 still has when its rows are read again).
 template <typename T, int U, bool DOWN>
@@ -280,20 +222,65 @@ __device__ __forceinline__ void fetch(const T* __restrict__ x, const Walk& w, in
     for (int u = 0; u < U; ++u)
         if (u < n) r[u] = take(at + (DOWN ? -u : u) * w.step);
 }
+
+__device__ __forceinline__ float finite_or_zero(float v) { return __builtin_fabsf(v) < __builtin_huge_valf() ? v : 0.0f; }
+
+// Power of two of lanes that add n values: at most a wave.
+__device__ __forceinline__ int lanes_for(int n) {
+    int q = 1;
+    while (q < n && q < 64) q <<= 1;
+    return q;
+}
+
+struct Two { double a, b; };
+__device__ __forceinline__ Two lanes_two(Two v, int q) {
+    for (int d = 1; d < q; d <<= 1) {
+        v.a += __shfl_xor(v.a, d, 64);
+        v.b += __shfl_xor(v.b, d, 64);
+    }
+    return v;
+}
+
+// ------------------------------------------------------------------ forward
+// Accumulators of a thread: one a column, or two for all of a vector's columns where these are of one group.
+template <typename T, bool M> constexpr int kSums = M ? 2 : kVec<T>;
+template <typename T, bool M>
+struct Sums { double s[kSums<T, M>], one[kSums<T, M>], two[kSums<T, M>]; };
+
+// The first value of each accumulator's group in row `origin`.
+template <typename T, bool M>
+__device__ __forceinline__ void first_values(const GroupArgs& p, const Slab& a, const Place& t, long long origin, float (&s)[kSums<T, M>]) {
+    const T* __restrict__ x = (const T*)p.x + origin * p.channels + (long long)a.j0 * p.per;
+#pragma unroll
+    for (int i = 0; i < kSums<T, M>; ++i)
+        s[i] = M && i ? s[0] : (float)x[(long long)group_of(p, column_of(p, a, t, i)) * p.per];
+}
+template <typename T, bool M>
+__device__ __forceinline__ void begin_sums(const float (&near)[kSums<T, M>], Sums<T, M>& v) {
+#pragma unroll
+    for (int i = 0; i < kSums<T, M>; ++i) {
+        v.s[i] = (double)finite_or_zero(near[i]);
+        v.one[i] = v.two[i] = 0.0;
+    }
+}
+template <typename T, bool M>
+__device__ __forceinline__ void add_value(float x, int i, Sums<T, M>& v) {
+    const int k = M ? i & 1 : i;
+    const double d = (double)x - v.s[k];
+    v.one[k] += d;
+    v.two[k] = __builtin_fma(d, d, v.two[k]);
+}
 // Sums over a thread's vectors from number k on, of which the first U are there, and over its odd values.
 template <typename T, bool M, int U>
-__device__ __forceinline__ void sum_from(const T* __restrict__ x, const Walk& w, int k, VecOf<T, kVec<T>> (&r)[U], const double (&s)[kSums<T, M>],
-                                         double (&s1)[kSums<T, M>], double (&s2)[kSums<T, M>]) {
+__device__ __forceinline__ void sum_from(const T* __restrict__ x, const Walk& w, int k, VecOf<T, kVec<T>> (&r)[U], Sums<T, M>& v) {
     constexpr int V = kVec<T>;
     while (k < w.full) {
 #pragma unroll
         for (int u = 0; u < U; ++u)
             if (u < w.full - k) {
 #pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    add_value<T, M>((float)r[u][i], i, s, s1, s2);
-                    if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);  // (the compiler would take all of them apart at once, in twice the registers)
-                }
+                for (int i = 0; i < V; ++i) add_value<T, M>((float)r[u][i], i, v);
+                __builtin_amdgcn_sched_barrier(0);  // (the compiler would take all of them apart at once, in twice the registers)
             }
         k += U;
         fetch<T, U, false>(x, w, k, r);
@@ -302,84 +289,146 @@ __device__ __forceinline__ void sum_from(const T* __restrict__ x, const Walk& w,
     for (k = 0; k < w.part; ++k, at += w.step)
 #pragma unroll
         for (int i = 0; i < V - 1; ++i)
-            if (i < w.n) add_value<T, M>((float)x[at + i], i, s, s1, s2);
+            if (i < w.n) add_value<T, M>((float)x[at + i], i, v);
+}
+
+// Sums over the slab's groups of the threads' pairs, then done(group, sums) by one lane a group.  All threads of the workgroup call
+// it.  s_all: a row of a step after the other, the sums of `sub` neighbouring values as one pair, a pair between two rows so that
+// neighbouring rows' are in different banks.
+template <typename T, bool M, typename F>
+__device__ __forceinline__ void add_groups(const GroupArgs& p, const Slab& a, const Place& t, const Sums<T, M>& v, Two* s_all, F done) {
+    constexpr int V = kVec<T>;
+    const int sub = M ? V : p.l.sub, w = M ? (a.w + V - 1) / V : a.w / sub, pitch = p.l.flat ? p.l.pitch : p.l.pitch / sub + 1;
+    Two* const mine = s_all + (p.l.flat ? t.col : t.row * pitch + t.col / sub);
+    if ((int)threadIdx.x < p.l.active) {
+        if constexpr (M) {
+            mine[0] = {v.one[0] + v.one[1], v.two[0] + v.two[1]};
+        } else if (sub == 1) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) mine[i] = {v.one[i], v.two[i]};
+        } else if (sub == 2) {
+#pragma unroll
+            for (int i = 0; i < V; i += 2) mine[i / 2] = {v.one[i] + v.one[i + 1], v.two[i] + v.two[i + 1]};
+        } else if constexpr (V == 8) {
+#pragma unroll
+            for (int i = 0; i < V; i += 4)
+                mine[i / 4] = {(v.one[i] + v.one[i + 1]) + (v.one[i + 2] + v.one[i + 3]), (v.two[i] + v.two[i + 1]) + (v.two[i + 2] + v.two[i + 3])};
+        }
+    }
+    __syncthreads();
+    const int n = w * p.l.reps, q = lanes_for(n);
+    const float inv = 1.0f / (float)w;
+    const int set = threadIdx.x / q, sets = blockDim.x / q, in = threadIdx.x & (q - 1);
+    for (int j0 = 0; j0 < a.ng; j0 += sets) {
+        const int j = j0 + set;
+        Two sum = {0.0, 0.0};
+        if (j < a.ng)
+            for (int e = in; e < n; e += q) {
+                const int k = quotient(e, inv);
+                const Two o = s_all[k * pitch + j * w + (e - k * w)];
+                sum.a += o.a;
+                sum.b += o.b;
+            }
+        sum = lanes_two(sum, q);
+        if (in == 0 && j < a.ng) done(j, sum);
+    }
 }
 
 struct GroupStat { float mean, rest, rstd, none; };
 // Statistics of n values from their sums about s.
-__device__ __forceinline__ GroupStat stat_of(double s, double s1, double s2, double n, float eps) {
-    const double off = s1 / n, mean = s + off;
-    double var = (s2 - s1 * off) / n;
+__device__ __forceinline__ GroupStat stat_of(float near, Two sum, double n, float eps) {
+    const double s = (double)finite_or_zero(near), inv = 1.0 / n, off = sum.a * inv, mean = s + off;
+    double var = (sum.b - sum.a * off) * inv;
     if (var < 0.0) var = 0.0;  // (a NaN stays one)
+    // 1 / sqrt by one step of Newton's from the instruction's estimate (2^-23 or better): far past fp32's rounding
+    const double v = var + (double)eps, y = __builtin_amdgcn_rsq(v), half = __builtin_fma(-0.5 * v * y, y, 0.5);
     GroupStat r;
     r.mean = (float)mean;
     r.rest = (float)(mean - (double)r.mean);
-    r.rstd = (float)(1.0 / sqrt(var + (double)eps));
+    r.rstd = half == half ? (float)__builtin_fma(y, half, y) : (float)y;  // (no step from 0, infinity and NaN)
     r.none = 0.0f;
     return r;
 }
 
-// What the forward pass knows of a thread's columns.
-template <int V>
-struct Columns { float mean[V], rest[V], scale[V], beta[V]; };
+// gamma and beta of a thread's columns, 1 and 0 where there are none.
 template <typename T>
-__device__ __forceinline__ Columns<kVec<T>> columns_of(const GroupArgs& p, const Slab& a, const Place& t, const GroupStat* stat) {
+struct Affine { VecOf<T, kVec<T>> gamma, beta; };
+template <typename T>
+__device__ __forceinline__ VecOf<T, kVec<T>> column_values(const GroupArgs& p, const Slab& a, const Place& t, const void* from, float none) {
     constexpr int V = kVec<T>;
-    Columns<V> k;
+    VecOf<T, V> v;
+    if (from && !p.l.flat && t.col + V <= a.c1 - a.c0) {
+        v = take((const T*)from + a.c0 + t.col);
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[i] = from ? ((const T*)from)[a.c0 + column_of(p, a, t, i)] : (T)none;
+    }
+    return v;
+}
+template <typename T>
+__device__ __forceinline__ Affine<T> affine_of(const GroupArgs& p, const Slab& a, const Place& t) {
+    return {column_values<T>(p, a, t, p.gamma, 1.0f), column_values<T>(p, a, t, p.beta, 0.0f)};
+}
+
+// What the forward pass knows of a thread's columns (mean and what its rounding leaves once, where they are of one group).
+template <int V, int A>
+struct Columns { float mean[A], rest[A], scale[V], beta[V]; };
+template <typename T, bool M>
+__device__ __forceinline__ Columns<kVec<T>, M ? 1 : kVec<T>> columns_of(const GroupArgs& p, const Slab& a, const Place& t, const Affine<T>& f,
+                                                                       const GroupStat* stat) {
+    constexpr int V = kVec<T>, A = M ? 1 : V;
+    Columns<V, A> k;
+    GroupStat s = {};
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-        const int c = column_of(p, a, t, i);
-        const GroupStat s = stat[group_of(p, c)];
-        k.mean[i] = s.mean;
-        k.rest[i] = s.rest;
-        k.scale[i] = p.gamma ? s.rstd * (float)((const T*)p.gamma)[a.c0 + c] : s.rstd;
-        k.beta[i] = p.beta ? (float)((const T*)p.beta)[a.c0 + c] : 0.0f;
+        if (i < A) {
+            s = stat[group_of(p, column_of(p, a, t, i))];
+            k.mean[i] = s.mean;
+            k.rest[i] = s.rest;
+        }
+        k.scale[i] = s.rstd * (float)f.gamma[i];
+        k.beta[i] = (float)f.beta[i];
     }
     return k;
 }
-template <int V>
-__device__ __forceinline__ float forward_value(const Columns<V>& k, int i, float x, int act) {
-    return activate(__builtin_fmaf((x - k.mean[i]) - k.rest[i], k.scale[i], k.beta[i]), act);
+template <int V, int A>
+__device__ __forceinline__ float forward_value(const Columns<V, A>& k, int i, float x, int act) {
+    const int j = A == 1 ? 0 : i;
+    return activate(__builtin_fmaf((x - k.mean[j]) - k.rest[j], k.scale[i], k.beta[i]), act);
 }
-template <typename T>
-__device__ __forceinline__ void forward_vector(const GroupArgs& p, const Columns<kVec<T>>& k, long long at, VecOf<T, kVec<T>> r) {
+template <typename T, int A>
+__device__ __forceinline__ void forward_vector(const GroupArgs& p, const Columns<kVec<T>, A>& k, long long at, VecOf<T, kVec<T>> r) {
     VecOf<T, kVec<T>> y;
 #pragma unroll
-    for (int i = 0; i < kVec<T>; ++i) {
-        y[i] = (T)forward_value<kVec<T>>(k, i, (float)r[i], p.act);
-        if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);
-    }
+    for (int i = 0; i < kVec<T>; ++i) y[i] = (T)forward_value<kVec<T>, A>(k, i, (float)r[i], p.act);
     put((T*)p.out + at, y);
+    __builtin_amdgcn_sched_barrier(0);
 }
-// A thread's vectors from number k - 1 down to `from`, of which the first U are there.
-template <typename T, int U>
-__device__ __forceinline__ void forward_down(const GroupArgs& p, const Columns<kVec<T>>& c, const Walk& w, int from, int k,
+// A thread's vectors from number k - 1 down to `from`, of which the first U are there, and its odd values.
+template <typename T, int A, int U>
+__device__ __forceinline__ void forward_down(const GroupArgs& p, const Columns<kVec<T>, A>& c, const Walk& w, int from, int k,
                                              VecOf<T, kVec<T>> (&r)[U]) {
     while (k > from) {
         const long long at = w.at + (long long)(k - 1) * w.step;
 #pragma unroll
         for (int u = 0; u < U; ++u)
-            if (u < k - from) {
-                forward_vector<T>(p, c, at - u * w.step, r[u]);
-                __builtin_amdgcn_sched_barrier(0);
-            }
+            if (u < k - from) forward_vector<T, A>(p, c, at - u * w.step, r[u]);
         k -= U;
         fetch<T, U, true>((const T*)p.x, w, k, r);
     }
-}
-template <typename T>
-__device__ __forceinline__ void forward_part(const GroupArgs& p, const Columns<kVec<T>>& c, const Walk& w) {
     long long at = w.at + (long long)w.full * w.step;
-    for (int k = 0; k < w.part; ++k, at += w.step)
+    for (k = 0; k < w.part; ++k, at += w.step)
 #pragma unroll
         for (int i = 0; i < kVec<T> - 1; ++i)
-            if (i < w.n) ((T*)p.out)[at + i] = (T)forward_value<kVec<T>>(c, i, (float)((const T*)p.x)[at + i], p.act);
+            if (i < w.n) ((T*)p.out)[at + i] = (T)forward_value<kVec<T>, A>(c, i, (float)((const T*)p.x)[at + i], p.act);
 }
 
+constexpr int kAhead = 8;  // vectors of x that a thread of the blocks' kernels has on their way
+
 template <typename T, bool M>
-__global__ __launch_bounds__(kGroupThreads, 4) void k_group_sums(GroupArgs p) {
-    constexpr int V = kVec<T>, A = kSums<T, M>;
-    __shared__ double s_all[kGroupThreads * (M ? 1 : V)];
+__global__ __launch_bounds__(kGroupThreads, 2) void k_group_sums(GroupArgs p) {
+    constexpr int V = kVec<T>;
+    extern __shared__ __align__(16) char s_step[];
     const long long i = block_id<kGroupThreads>();
     if (i >= p.blocks) return;
     const Bounds s = bounds_of(p);
@@ -390,92 +439,87 @@ __global__ __launch_bounds__(kGroupThreads, 4) void k_group_sums(GroupArgs p) {
     for (long long b = k.b0; b <= k.b1; ++b) {
         const Rows r = rows_of_sample(s, b);
         const long long lo = r.first > k.r0 ? r.first : k.r0, hi = r.end < k.r1 ? r.end : k.r1;
-        double* const part = (double*)p.part + ((i + b) * p.groups * p.l.pieces + to) * 2;
+        Two* const part = (Two*)p.part + (i + b) * p.groups * p.l.pieces + to;
         if (hi <= lo) {
-            for (int j = threadIdx.x; j < 2 * a.ng; j += blockDim.x) part[j] = 0.0;
+            for (int j = threadIdx.x; j < a.ng; j += blockDim.x) part[j] = {0.0, 0.0};
             continue;
         }
-        float near[A];
-        double from[A], s1[A], s2[A];
-        first_values<T, M>(p, a, t, r.first, near);
-        const Walk w = walk_of<V>(p, a, t, lo, hi);
         // (the first vectors are on their way with the values that they are taken about)
-        VecOf<T, V> x[4];
-        fetch<T, 4, false>((const T*)p.x, w, 0, x);
-#pragma unroll
-        for (int c = 0; c < A; ++c) {
-            from[c] = (double)near[c];
-            s1[c] = s2[c] = 0.0;
-        }
-        sum_from<T, M, 4>((const T*)p.x, w, 0, x, from, s1, s2);
-        add_groups<T, M>(p, a, s1, s_all, [&](int j, double sum) { part[2 * j] = sum; });
-        add_groups<T, M>(p, a, s2, s_all, [&](int j, double sum) { part[2 * j + 1] = sum; });
+        float near[kSums<T, M>];
+        const Walk w = walk_of<V>(p, a, t, lo, hi);
+        VecOf<T, V> x[kAhead];
+        first_values<T, M>(p, a, t, r.first, near);
+        fetch<T, kAhead, false>((const T*)p.x, w, 0, x);
+        Sums<T, M> v;
+        begin_sums<T, M>(near, v);
+        sum_from<T, M, kAhead>((const T*)p.x, w, 0, x, v);
+        add_groups<T, M>(p, a, t, v, (Two*)s_step, [&](int j, Two sum) { part[j] = sum; });
+        if (b < k.b1) __syncthreads();
     }
 }
 
 // Sum over the Q threads (a power of two up to 256) of each of a workgroup's sets; all 256 threads call it.
-__device__ __forceinline__ double set_add(double v, int q, double* s_wave) {
-    for (int d = 1; d < q && d < 64; d <<= 1) v += __shfl_xor(v, d, 64);
+__device__ __forceinline__ Two set_add(Two v, int q, Two* s_wave) {
+    v = lanes_two(v, q < 64 ? q : 64);
     if (q <= 64) return v;
-    __syncthreads();
     if ((threadIdx.x & 63) == 0) s_wave[threadIdx.x >> 6] = v;
     __syncthreads();
     const int w = threadIdx.x / q * (q / 64);
-    v = 0.0;
-    for (int k = 0; k < q / 64; ++k) v += s_wave[w + k];
+    v = {0.0, 0.0};
+    for (int k = 0; k < q / 64; ++k) {
+        v.a += s_wave[w + k].a;
+        v.b += s_wave[w + k].b;
+    }
     return v;
 }
 
-template <typename T>
-__device__ __forceinline__ GroupStat joined_stat(const GroupArgs& p, const Rows& r, int j, double s1, double s2) {
-    const float s = finite_or_zero((float)((const T*)p.x)[r.first * p.channels + (long long)j * p.per]);
-    return stat_of((double)s, s1, s2, (double)(r.end - r.first) * p.per, p.eps);
-}
-
 // The places that hold the sums of a sample: from, and how many.
-__device__ __forceinline__ long long places_of(const GroupArgs& p, long long b, const Rows& r, long long& count) {
-    const long long i0 = (long long)((unsigned)r.first / (unsigned)p.chunk), i1 = (long long)((unsigned)(r.end - 1) / (unsigned)p.chunk);
-    count = i1 - i0 + 1;
+__device__ __forceinline__ long long places_of(const GroupArgs& p, long long b, const Rows& r, int& count) {
+    const long long i0 = quotient(r.first, p.inv_chunk), i1 = quotient(r.end - 1, p.inv_chunk);
+    count = (int)(i1 - i0) + 1;
     return i0 + b;
+}
+template <typename T>
+__device__ __forceinline__ float near_value(const GroupArgs& p, const Rows& r, int j) {
+    return (float)((const T*)p.x)[r.first * p.channels + (long long)j * p.per];
 }
 
 // Q threads for each sample and group.  BACK: means of h and h xh, else the statistics.
 template <typename T, bool BACK>
 __global__ __launch_bounds__(256) void k_group_join(GroupArgs p, int q) {
     typedef typename std::conditional<BACK, float, double>::type F;
-    __shared__ double s_wave[4];
+    __shared__ Two s_wave[4];
     const long long id = block_id<256>() * (256 / q) + threadIdx.x / q;
     const int in = threadIdx.x & (q - 1);
     const bool live = id < p.batch * p.groups;
     const long long b = live ? id / p.groups : 0;
     const int j = (int)(live ? id - b * p.groups : 0);
-    Bounds s = {p.offsets, p.each, p.rows, p.batch, 0, false};  // (b differs from lane to lane)
+    const Bounds s = {p.offsets, p.each, p.rows, p.batch, 0, p.inv_each, false};  // (b differs from lane to lane)
     Rows r = {first_row(s, b), first_row(s, b + 1)};
     if (r.end < r.first) r.end = r.first;
-    double s1 = 0.0, s2 = 0.0;
+    Two sum = {0.0, 0.0};
     if (live && r.end > r.first) {
-        long long count;
+        int count;
         const long long from = places_of(p, b, r, count);
         const F* __restrict__ part = (const F*)p.part;
-        const unsigned pieces = (unsigned)p.l.pieces;
-        const long long n = count * pieces;
+        const int pieces = p.l.pieces;
+        const long long n = (long long)count * pieces;
 #pragma unroll 4
         for (long long e = in; e < n; e += q) {
             const long long i = pieces > 1 ? e / pieces : e;
             const F* at = part + (((from + i) * p.groups + j) * pieces + (e - i * pieces)) * 2;
-            s1 += (double)at[0];
-            s2 += (double)at[1];
+            sum.a += (double)at[0];
+            sum.b += (double)at[1];
         }
     }
-    s1 = set_add(s1, q, s_wave);
-    s2 = set_add(s2, q, s_wave);
+    sum = set_add(sum, q, s_wave);
     if (!live || in != 0) return;
     if constexpr (BACK) {
         const double n = r.end > r.first ? (double)(r.end - r.first) * p.per : 1.0;
-        ((float2*)p.stat)[id] = make_float2((float)(s1 / n), (float)(s2 / n));
+        ((float2*)p.stat)[id] = make_float2((float)(sum.a / n), (float)(sum.b / n));
     } else {
         GroupStat v = {0.0f, 0.0f, 0.0f, 0.0f};
-        if (r.end > r.first) v = joined_stat<T>(p, r, j, s1, s2);
+        if (r.end > r.first) v = stat_of(near_value<T>(p, r, j), sum, (double)(r.end - r.first) * p.per, p.eps);
         ((GroupStat*)p.stat)[id] = v;
         if (p.mean) p.mean[id] = v.mean;
         if (p.rstd) p.rstd[id] = v.rstd;
@@ -483,52 +527,58 @@ __global__ __launch_bounds__(256) void k_group_join(GroupArgs p, int q) {
 }
 
 // The sums of a sample's groups by one workgroup: threads side by side take neighbouring groups of a place, their sums meet in
-// s_two, then done(group of the slab, sums) by one lane a group.  (Reads the places' lines whole: a lane a place took four times as
-// long.)  All threads call it; up to kHereGroups groups.
-template <typename F, typename D>
-__device__ __forceinline__ void join_here(const GroupArgs& p, const Slab& a, long long b, const Rows& r, double2* s_two, D done) {
-    const int ng = a.ng, sets = (int)blockDim.x / ng, set = threadIdx.x / ng, j = threadIdx.x - set * ng;
-    long long count;
+// s_two, then one lane a group ends with them (group k < ng, lane 0 of its q).  All threads call it; up to kHereGroups groups.
+struct Joiner { int sets, set, j, q, k, in; };
+__device__ __forceinline__ Joiner joiner_of(const Slab& a) {
+    Joiner o;
+    const float inv = 1.0f / (float)a.ng;
+    o.sets = quotient((int)blockDim.x, inv);
+    o.set = quotient((int)threadIdx.x, inv);
+    o.j = threadIdx.x - o.set * a.ng;
+    o.q = 1;
+    while (2 * o.q * a.ng <= (int)blockDim.x && o.q < 64 && o.q < o.sets) o.q <<= 1;
+    o.k = threadIdx.x / o.q;
+    o.in = threadIdx.x & (o.q - 1);
+    return o;
+}
+template <typename F>
+__device__ __forceinline__ Two join_here(const GroupArgs& p, const Slab& a, const Joiner& o, long long b, const Rows& r, Two* s_two) {
+    int count;
     const long long from = places_of(p, b, r, count);
-    double2 sum = make_double2(0.0, 0.0);
-    if (set < sets) {
-        const F* __restrict__ part = (const F*)p.part + ((from + set) * p.groups + a.j0 + j) * 2;
-        const long long step = (long long)sets * p.groups * 2;
+    Two sum = {0.0, 0.0};
+    if (o.set < o.sets) {
+        const F* __restrict__ part = (const F*)p.part + ((from + o.set) * p.groups + a.j0 + o.j) * 2;
+        const long long step = (long long)o.sets * p.groups * 2;
 #pragma unroll 8
-        for (long long i = set; i < count; i += sets, part += step) {
-            sum.x += (double)part[0];
-            sum.y += (double)part[1];
+        for (int i = o.set; i < count; i += o.sets, part += step) {
+            sum.a += (double)part[0];
+            sum.b += (double)part[1];
         }
     }
     __syncthreads();
     s_two[threadIdx.x] = sum;
     __syncthreads();
-    int q = 1;
-    while (2 * q * ng <= (int)blockDim.x && q < 64 && q < sets) q <<= 1;
-    const int k = threadIdx.x / q, in = threadIdx.x & (q - 1);
-    sum = make_double2(0.0, 0.0);
-    if (k < ng)
-        for (int e = in; e < sets; e += q) {
-            sum.x += s_two[e * ng + k].x;
-            sum.y += s_two[e * ng + k].y;
+    sum = {0.0, 0.0};
+    if (o.k < a.ng)
+        for (int e = o.in; e < o.sets; e += o.q) {
+            sum.a += s_two[e * a.ng + o.k].a;
+            sum.b += s_two[e * a.ng + o.k].b;
         }
-    for (int d = 1; d < q; d <<= 1) {
-        sum.x += __shfl_xor(sum.x, d, 64);
-        sum.y += __shfl_xor(sum.y, d, 64);
-    }
-    if (k < ng && in == 0) done(k, sum);
+    return lanes_two(sum, o.q);
 }
 
-template <typename T>
-__global__ __launch_bounds__(kGroupThreads, 4) void k_group_apply(GroupArgs p) {
-    constexpr int V = kVec<T>, U = 16 / V;
-    __shared__ double2 s_two[kGroupThreads];
+template <typename T, bool M>
+__global__ __launch_bounds__(kGroupThreads, 2) void k_group_apply(GroupArgs p) {
+    constexpr int V = kVec<T>, A = M ? 1 : V;
+    __shared__ Two s_two[kGroupThreads];
     __shared__ GroupStat s_stat[kHereGroups];
     const long long i = block_id<kGroupThreads>();
     if (i >= p.blocks) return;
     const Bounds s = bounds_of(p);
     const Slab a = slab_of(p);
     const Place t = place_of<V>(p);
+    const Affine<T> f = affine_of<T>(p, a, t);
+    const Joiner o = joiner_of(a);
     const Block k = block_of(p, s, i);
     for (long long b = k.b0; b <= k.b1; ++b) {
         const Rows r = rows_of_sample(s, b);
@@ -541,111 +591,104 @@ __global__ __launch_bounds__(kGroupThreads, 4) void k_group_apply(GroupArgs p) {
         if (hi <= lo) continue;
         const Walk w = walk_of<V>(p, a, t, lo, hi);
         // (the last vectors are on their way while the sums are joined)
-        VecOf<T, V> x[U];
-        fetch<T, U, true>((const T*)p.x, w, w.full, x);
+        VecOf<T, V> x[kAhead];
+        fetch<T, kAhead, true>((const T*)p.x, w, w.full, x);
         const GroupStat* stat = (const GroupStat*)p.stat + id;
         if (!p.stat) {
-            join_here<double>(p, a, b, r, s_two, [&](int j, double2 sum) {
-                const GroupStat v = joined_stat<T>(p, r, a.j0 + j, sum.x, sum.y);
-                s_stat[j] = v;
+            const bool ends = o.k < a.ng && o.in == 0;
+            const float near = ends ? near_value<T>(p, r, a.j0 + o.k) : 0.0f;
+            const Two sum = join_here<double>(p, a, o, b, r, s_two);
+            if (ends) {
+                const GroupStat v = stat_of(near, sum, (double)(r.end - r.first) * p.per, p.eps);
+                s_stat[o.k] = v;
                 if (r.first >= k.r0) {
-                    if (p.mean) p.mean[id + j] = v.mean;
-                    if (p.rstd) p.rstd[id + j] = v.rstd;
+                    if (p.mean) p.mean[id + o.k] = v.mean;
+                    if (p.rstd) p.rstd[id + o.k] = v.rstd;
                 }
-            });
+            }
             __syncthreads();
             stat = s_stat;
         }
-        const Columns<V> c = columns_of<T>(p, a, t, stat);
-        forward_down<T, U>(p, c, w, 0, w.full, x);
-        forward_part<T>(p, c, w);
+        const Columns<V, A> c = columns_of<T, M>(p, a, t, f, stat);
+        forward_down<T, A, kAhead>(p, c, w, 0, w.full, x);
     }
 }
 
 // A sample's slab of whole groups by one workgroup of up to B threads, H vectors a thread in registers; what a larger sample has
 // more is read again.
 template <typename T, bool M, int B, int H>
-__global__ __launch_bounds__(B) void k_group_one(GroupArgs p) {
-    constexpr int V = kVec<T>, A = kSums<T, M>;
-    __shared__ double s_all[B * (M ? 1 : V)];
-    __shared__ union { double sum; GroupStat stat; } s_group[M ? B : B * V / 4];
+__global__ __launch_bounds__(B, 2) void k_group_one(GroupArgs p) {
+    constexpr int V = kVec<T>, A = M ? 1 : V;
+    extern __shared__ __align__(16) char s_step[];
+    GroupStat* const s_stat = (GroupStat*)s_step;
+    Two* const s_all = (Two*)(s_stat + p.l.wide / p.per);
     const long long b = block_id<B>();
     if (b >= p.batch) return;
-    const Bounds s = {p.offsets, p.each, p.rows, p.batch, 0, false};
+    const Bounds s = {p.offsets, p.each, p.rows, p.batch, 0, p.inv_each, false};
     const Slab a = slab_of(p);
     const Place t = place_of<V>(p);
     const Rows r = rows_of_sample(s, b);
     const long long id = b * p.groups + a.j0;
-    if (r.end > r.first) {
-        const T* __restrict__ x = (const T*)p.x;
-        const Walk w = walk_of<V>(p, a, t, r.first, r.end);
-        float near[A];
-        double from[A], s1[A], s2[A];
-        first_values<T, M>(p, a, t, r.first, near);
-        VecOf<T, V> held[H];
-#pragma unroll
-        for (int h = 0; h < H; ++h)
-            if (h < w.full) held[h] = take(x + w.at + h * w.step);
-#pragma unroll
-        for (int c = 0; c < A; ++c) {
-            from[c] = (double)near[c];
-            s1[c] = s2[c] = 0.0;
-        }
-#pragma unroll
-        for (int h = 0; h < H; ++h)
-            if (h < w.full) {
-#pragma unroll
-                for (int i = 0; i < V; ++i) add_value<T, M>((float)held[h][i], i, from, s1, s2);
-                __builtin_amdgcn_sched_barrier(0);
-            }
-        VecOf<T, V> more[4];
-        fetch<T, 4, false>(x, w, H, more);
-        sum_from<T, M, 4>(x, w, H, more, from, s1, s2);
-        add_groups<T, M>(p, a, s1, s_all, [&](int j, double sum) { s_group[j].sum = sum; });
-        add_groups<T, M>(p, a, s2, s_all, [&](int j, double sum) {
-            const GroupStat v = joined_stat<T>(p, r, a.j0 + j, s_group[j].sum, sum);
-            s_group[j].stat = v;
-            if (p.mean) p.mean[id + j] = v.mean;
-            if (p.rstd) p.rstd[id + j] = v.rstd;
-        });
-        __syncthreads();
-        const Columns<V> c = columns_of<T>(p, a, t, &s_group[0].stat);
-#pragma unroll
-        for (int h = 0; h < H; ++h)
-            if (h < w.full) {
-                forward_vector<T>(p, c, w.at + h * w.step, held[h]);
-                __builtin_amdgcn_sched_barrier(0);
-            }
-        if (w.full > H) {
-            fetch<T, 4, true>(x, w, w.full, more);
-            forward_down<T, 4>(p, c, w, H, w.full, more);
-        }
-        forward_part<T>(p, c, w);
-    } else {
+    if (r.end == r.first) {
         for (int j = threadIdx.x; j < a.ng; j += blockDim.x) {
             if (p.mean) p.mean[id + j] = 0.0f;
             if (p.rstd) p.rstd[id + j] = 0.0f;
         }
+        return;
     }
+    const T* __restrict__ x = (const T*)p.x;
+    const Walk w = walk_of<V>(p, a, t, r.first, r.end);
+    float near[kSums<T, M>];
+    first_values<T, M>(p, a, t, r.first, near);
+    VecOf<T, V> held[H];
+    fetch<T, H, false>(x, w, 0, held);
+    const Affine<T> f = affine_of<T>(p, a, t);
+    Sums<T, M> v;
+    begin_sums<T, M>(near, v);
+#pragma unroll
+    for (int h = 0; h < H; ++h)
+        if (h < w.full) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) add_value<T, M>((float)held[h][i], i, v);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    VecOf<T, V> more[4];
+    fetch<T, 4, false>(x, w, H, more);
+    sum_from<T, M, 4>(x, w, H, more, v);
+    add_groups<T, M>(p, a, t, v, s_all, [&](int j, Two sum) {
+        const GroupStat g = stat_of(near_value<T>(p, r, a.j0 + j), sum, (double)(r.end - r.first) * p.per, p.eps);
+        s_stat[j] = g;
+        if (p.mean) p.mean[id + j] = g.mean;
+        if (p.rstd) p.rstd[id + j] = g.rstd;
+    });
+    __syncthreads();
+    const Columns<V, A> c = columns_of<T, M>(p, a, t, f, s_stat);
+#pragma unroll
+    for (int h = 0; h < H; ++h)
+        if (h < w.full) forward_vector<T, A>(p, c, w.at + h * w.step, held[h]);
+    if (w.full > H) fetch<T, 4, true>(x, w, w.full, more);
+    forward_down<T, A, 4>(p, c, w, H, w.full, more);
 }
 
+// ------------------------------------------------------------------ backward
 // What the backward pass knows of a thread's columns (mean and rstd once where they are of one group).
 template <int V, int A>
 struct BackColumns { float mean[A], rstd[A], gamma[V], beta[V]; };
 template <typename T, bool M>
-__device__ __forceinline__ BackColumns<kVec<T>, M ? 1 : kVec<T>> back_columns(const GroupArgs& p, const Slab& a, const Place& t, long long b) {
-    constexpr int V = kVec<T>;
-    BackColumns<V, M ? 1 : V> k;
+__device__ __forceinline__ BackColumns<kVec<T>, M ? 1 : kVec<T>> back_columns(const GroupArgs& p, const Slab& a, const Place& t, const Affine<T>& f,
+                                                                             long long b) {
+    constexpr int V = kVec<T>, A = M ? 1 : V;
+    BackColumns<V, A> k;
+#pragma unroll
+    for (int i = 0; i < A; ++i) {
+        const long long s = b * p.groups + a.j0 + group_of(p, column_of(p, a, t, i));
+        k.mean[i] = p.mean[s];
+        k.rstd[i] = p.rstd[s];
+    }
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-        const int c = column_of(p, a, t, i);
-        if (!M || i == 0) {
-            const long long s = b * p.groups + a.j0 + group_of(p, c);
-            k.mean[i] = p.mean[s];
-            k.rstd[i] = p.rstd[s];
-        }
-        k.gamma[i] = p.gamma ? (float)((const T*)p.gamma)[a.c0 + c] : 1.0f;
-        k.beta[i] = p.beta ? (float)((const T*)p.beta)[a.c0 + c] : 0.0f;
+        k.gamma[i] = (float)f.gamma[i];
+        k.beta[i] = (float)f.beta[i];
     }
     return k;
 }
@@ -666,29 +709,29 @@ __device__ __forceinline__ void back_value(const BackColumns<V, A>& k, int i, fl
     }
     dz = activate_back(g, z, act);
 }
+template <int V>
+struct BackSums { float a[V], b[V]; };  // of dz xh and dz
 template <int V, int A>
-__device__ __forceinline__ void back_add(const BackColumns<V, A>& k, int i, float x, float g, int act, float (&da)[V], float (&db)[V], float& dz) {
-    float xh;
+__device__ __forceinline__ float back_add(const BackColumns<V, A>& k, int i, float x, float g, int act, BackSums<V>& v) {
+    float xh, dz;
     back_value<V, A>(k, i, x, g, act, xh, dz);
-    da[i] = __builtin_fmaf(dz, xh, da[i]);
-    db[i] += dz;
+    v.a[i] = __builtin_fmaf(dz, xh, v.a[i]);
+    v.b[i] += dz;
+    return dz;
 }
 
-template <typename T, bool M, int U>
-__device__ __forceinline__ void back_sum_from(const GroupArgs& p, const BackColumns<kVec<T>, M ? 1 : kVec<T>>& c, const Walk& w, int k,
-                                              VecOf<T, kVec<T>> (&r)[U], VecOf<T, kVec<T>> (&q)[U], float (&da)[kVec<T>], float (&db)[kVec<T>]) {
-    constexpr int V = kVec<T>, A = M ? 1 : V;
+template <typename T, int A, int U>
+__device__ __forceinline__ void back_sum_from(const GroupArgs& p, const BackColumns<kVec<T>, A>& c, const Walk& w, int k,
+                                              VecOf<T, kVec<T>> (&r)[U], VecOf<T, kVec<T>> (&q)[U], BackSums<kVec<T>>& v) {
+    constexpr int V = kVec<T>;
     const T *__restrict__ x = (const T*)p.x, *__restrict__ g = (const T*)p.g;
-    float dz;
     while (k < w.full) {
 #pragma unroll
         for (int u = 0; u < U; ++u)
             if (u < w.full - k) {
 #pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    back_add<V, A>(c, i, (float)r[u][i], (float)q[u][i], p.act, da, db, dz);
-                    if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);
-                }
+                for (int i = 0; i < V; ++i) back_add<V, A>(c, i, (float)r[u][i], (float)q[u][i], p.act, v);
+                __builtin_amdgcn_sched_barrier(0);
             }
         k += U;
         fetch<T, U, false>(x, w, k, r);
@@ -698,60 +741,69 @@ __device__ __forceinline__ void back_sum_from(const GroupArgs& p, const BackColu
     for (k = 0; k < w.part; ++k, at += w.step)
 #pragma unroll
         for (int i = 0; i < V - 1; ++i)
-            if (i < w.n) back_add<V, A>(c, i, (float)x[at + i], (float)g[at + i], p.act, da, db, dz);
+            if (i < w.n) back_add<V, A>(c, i, (float)x[at + i], (float)g[at + i], p.act, v);
 }
 
-// Sums over a step's rows: done(column of the slab, sum) by one lane a column.  All threads call it; s_all: a vector a thread.
-template <int V, typename F>
-__device__ __forceinline__ void add_columns(const GroupArgs& p, const Slab& a, const float (&v)[V], float* s_all, F done) {
-    __syncthreads();
+// Sums over a step's rows, given to s_col [2][wide].  All threads call it and meet at its end; s_all: a step's rows, as in add_groups.
+// (Rows without a number between them: 36.9 us in place of 26.6 for 64 samples of 512 x 256 bf16, all lanes of a sum in one bank.)
+template <int V>
+__device__ __forceinline__ void add_columns(const GroupArgs& p, const Slab& a, const Place& t, const BackSums<V>& v, float2* s_all, float* s_col) {
+    const int wide = a.c1 - a.c0, pitch = p.l.flat ? p.l.pitch : p.l.pitch + 1;
+    float2* const mine = s_all + (p.l.flat ? t.col : t.row * pitch + t.col);
     if ((int)threadIdx.x < p.l.active)
 #pragma unroll
-        for (int i = 0; i < V; ++i) s_all[threadIdx.x * V + i] = v[i];
+        for (int i = 0; i < V; ++i) mine[i] = make_float2(v.a[i], v.b[i]);
     __syncthreads();
-    const int wide = a.c1 - a.c0;
     int q = 1;
     while (2 * q * wide <= (int)blockDim.x && q < p.l.reps && q < 64) q <<= 1;
     const int sets = blockDim.x / q, in = threadIdx.x & (q - 1);
     for (int c0 = 0; c0 < wide; c0 += sets) {
         const int c = c0 + threadIdx.x / q;
-        float sum = 0.0f;
+        float2 sum = make_float2(0.0f, 0.0f);
         if (c < wide)
-            for (int k = in; k < p.l.reps; k += q) sum += s_all[k * p.l.pitch + c];
-        for (int d = 1; d < q; d <<= 1) sum += __shfl_xor(sum, d, 64);
-        if (c < wide && in == 0) done(c, sum);
+            for (int k = in; k < p.l.reps; k += q) {
+                const float2 o = s_all[k * pitch + c];
+                sum.x += o.x;
+                sum.y += o.y;
+            }
+        for (int d = 1; d < q; d <<= 1) {
+            sum.x += __shfl_xor(sum.x, d, 64);
+            sum.y += __shfl_xor(sum.y, d, 64);
+        }
+        if (c < wide && in == 0) {
+            s_col[c] = sum.x;
+            s_col[wide + c] = sum.y;
+        }
     }
+    __syncthreads();
 }
 
-// Sums of h and h xh over the slab's groups from the columns' sums of dz xh and dz: done(group, sum h, sum h xh).
+// Sums of h and h xh over the slab's groups from the columns' sums of dz xh and dz: done(group, {sum h, sum h xh}) by one lane a group.
 template <typename T, typename F>
-__device__ __forceinline__ void back_groups(const GroupArgs& p, const Slab& a, const float* s_a, const float* s_b, F done) {
+__device__ __forceinline__ void back_groups(const GroupArgs& p, const Slab& a, const float* s_col, F done) {
     const T* __restrict__ gamma = p.gamma ? (const T*)p.gamma + a.c0 : nullptr;
-    const int q = lanes_for(a.w), set = threadIdx.x / q, sets = blockDim.x / q, in = threadIdx.x & (q - 1);
+    const int wide = a.c1 - a.c0, q = lanes_for(a.w), set = threadIdx.x / q, sets = blockDim.x / q, in = threadIdx.x & (q - 1);
     for (int j0 = 0; j0 < a.ng; j0 += sets) {
         const int j = j0 + set;
-        double h = 0.0, hx = 0.0;
+        Two sum = {0.0, 0.0};
         if (j < a.ng)
             for (int e = in; e < a.w; e += q) {
                 const int c = j * a.w + e;
                 const double by = gamma ? (double)(float)gamma[c] : 1.0;
-                hx += by * (double)s_a[c];
-                h += by * (double)s_b[c];
+                sum.a += by * (double)s_col[wide + c];
+                sum.b += by * (double)s_col[c];
             }
-        for (int d = 1; d < q; d <<= 1) {
-            h += __shfl_xor(h, d, 64);
-            hx += __shfl_xor(hx, d, 64);
-        }
-        if (in == 0 && j < a.ng) done(j, h, hx);
+        sum = lanes_two(sum, q);
+        if (in == 0 && j < a.ng) done(j, sum);
     }
 }
 
-template <int V, int A>
+template <int A>
 struct Means { float h[A], hx[A]; };
 template <typename T, bool M>
-__device__ __forceinline__ Means<kVec<T>, M ? 1 : kVec<T>> means_of(const GroupArgs& p, const Slab& a, const Place& t, const float2* stat) {
-    constexpr int V = kVec<T>, A = M ? 1 : V;
-    Means<V, A> m;
+__device__ __forceinline__ Means<M ? 1 : kVec<T>> means_of(const GroupArgs& p, const Slab& a, const Place& t, const float2* stat) {
+    constexpr int A = M ? 1 : kVec<T>;
+    Means<A> m;
 #pragma unroll
     for (int i = 0; i < A; ++i) {
         const float2 s = stat[group_of(p, column_of(p, a, t, i))];
@@ -761,37 +813,29 @@ __device__ __forceinline__ Means<kVec<T>, M ? 1 : kVec<T>> means_of(const GroupA
     return m;
 }
 template <int V, int A>
-__device__ __forceinline__ float back_result(const BackColumns<V, A>& k, const Means<V, A>& m, int i, float xh, float dz) {
+__device__ __forceinline__ float back_result(const BackColumns<V, A>& k, const Means<A>& m, int i, float xh, float dz) {
     const int j = A == 1 ? 0 : i;
     return k.rstd[j] * (dz * k.gamma[i] - m.h[j] - xh * m.hx[j]);
 }
-template <typename T, bool M>
-__device__ __forceinline__ void back_vector(const GroupArgs& p, const BackColumns<kVec<T>, M ? 1 : kVec<T>>& k,
-                                            const Means<kVec<T>, M ? 1 : kVec<T>>& m, long long at, VecOf<T, kVec<T>> r, VecOf<T, kVec<T>> q) {
-    constexpr int V = kVec<T>, A = M ? 1 : V;
-    VecOf<T, V> y;
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-        float xh, dz;
-        back_value<V, A>(k, i, (float)r[i], (float)q[i], p.act, xh, dz);
-        y[i] = (T)back_result<V, A>(k, m, i, xh, dz);
-        if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);
-    }
-    put((T*)p.out + at, y);
-}
 // A thread's vectors from number k - 1 down to `from`, of which the first U are there, and its odd values.
-template <typename T, bool M, int U>
-__device__ __forceinline__ void back_down(const GroupArgs& p, const BackColumns<kVec<T>, M ? 1 : kVec<T>>& c,
-                                          const Means<kVec<T>, M ? 1 : kVec<T>>& m, const Walk& w, int from, int k,
+template <typename T, int A, int U>
+__device__ __forceinline__ void back_down(const GroupArgs& p, const BackColumns<kVec<T>, A>& c, const Means<A>& m, const Walk& w, int from, int k,
                                           VecOf<T, kVec<T>> (&r)[U], VecOf<T, kVec<T>> (&q)[U]) {
-    constexpr int V = kVec<T>, A = M ? 1 : V;
+    constexpr int V = kVec<T>;
     const T *__restrict__ x = (const T*)p.x, *__restrict__ g = (const T*)p.g;
     while (k > from) {
         const long long at = w.at + (long long)(k - 1) * w.step;
 #pragma unroll
         for (int u = 0; u < U; ++u)
             if (u < k - from) {
-                back_vector<T, M>(p, c, m, at - u * w.step, r[u], q[u]);
+                VecOf<T, V> y;
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    float xh, dz;
+                    back_value<V, A>(c, i, (float)r[u][i], (float)q[u][i], p.act, xh, dz);
+                    y[i] = (T)back_result<V, A>(c, m, i, xh, dz);
+                }
+                put((T*)p.out + at - u * w.step, y);
                 __builtin_amdgcn_sched_barrier(0);
             }
         k -= U;
@@ -799,7 +843,7 @@ __device__ __forceinline__ void back_down(const GroupArgs& p, const BackColumns<
         fetch<T, U, true>(g, w, k, q);
     }
     long long at = w.at + (long long)w.full * w.step;
-    for (int n = 0; n < w.part; ++n, at += w.step)
+    for (k = 0; k < w.part; ++k, at += w.step)
 #pragma unroll
         for (int i = 0; i < V - 1; ++i)
             if (i < w.n) {
@@ -809,59 +853,56 @@ __device__ __forceinline__ void back_down(const GroupArgs& p, const BackColumns<
             }
 }
 
+constexpr int kBackAhead = 4;  // vectors of x and of g
+
+// LDS: a step's rows, then the columns' sums.
+__host__ __device__ __forceinline__ int step_values(const GroupLayout& l) { return l.reps * (l.pitch + 1); }
+
 template <typename T, bool M>
-__global__ __launch_bounds__(kGroupThreads, 4) void k_group_back_sums(GroupArgs p) {
-    constexpr int V = kVec<T>, U = 8 / V;
-    __shared__ float s_all[kGroupThreads * V];
-    __shared__ float s_col[2][kGroupThreads * V];
+__global__ __launch_bounds__(kGroupThreads, 2) void k_group_back_sums(GroupArgs p) {
+    constexpr int V = kVec<T>, A = M ? 1 : V, U = kBackAhead;
+    extern __shared__ __align__(16) char s_step[];
+    float2* const s_all = (float2*)s_step;
+    float* const s_col = (float*)(s_all + step_values(p.l));
     const long long i = block_id<kGroupThreads>();
     if (i >= p.blocks) return;
     const Bounds s = bounds_of(p);
     const Slab a = slab_of(p);
     const Place t = place_of<V>(p);
+    const Affine<T> f = affine_of<T>(p, a, t);
     const Block k = block_of(p, s, i);
     const int wide = a.c1 - a.c0, to = p.l.pieces > 1 ? (int)blockIdx.y : a.j0;
     for (long long b = k.b0; b <= k.b1; ++b) {
         const Rows r = rows_of_sample(s, b);
         const long long lo = r.first > k.r0 ? r.first : k.r0, hi = r.end < k.r1 ? r.end : k.r1;
         float* const cols = p.cols + (i + b) * 2 * p.channels + a.c0;
-        float* const part = (float*)p.part + ((i + b) * p.groups * p.l.pieces + to) * 2;
+        float2* const part = (float2*)p.part + (i + b) * p.groups * p.l.pieces + to;
         if (hi <= lo) {
             if (p.cols)
                 for (int c = threadIdx.x; c < wide; c += blockDim.x) cols[c] = cols[p.channels + c] = 0.0f;
-            for (int j = threadIdx.x; j < 2 * a.ng; j += blockDim.x) part[j] = 0.0f;
+            for (int j = threadIdx.x; j < a.ng; j += blockDim.x) part[j] = make_float2(0.0f, 0.0f);
             continue;
         }
-        float da[V], db[V];
-#pragma unroll
-        for (int c = 0; c < V; ++c) da[c] = db[c] = 0.0f;
         const Walk w = walk_of<V>(p, a, t, lo, hi);
         VecOf<T, V> x[U], g[U];
         fetch<T, U, false>((const T*)p.x, w, 0, x);
         fetch<T, U, false>((const T*)p.g, w, 0, g);
-        back_sum_from<T, M, U>(p, back_columns<T, M>(p, a, t, b), w, 0, x, g, da, db);
-        add_columns<V>(p, a, da, s_all, [&](int c, float sum) {
-            s_col[0][c] = sum;
-            if (p.cols) cols[c] = sum;
-        });
-        add_columns<V>(p, a, db, s_all, [&](int c, float sum) {
-            s_col[1][c] = sum;
-            if (p.cols) cols[p.channels + c] = sum;
-        });
-        if (!p.out) continue;
-        __syncthreads();
-        back_groups<T>(p, a, s_col[0], s_col[1], [&](int j, double h, double hx) {
-            part[2 * j] = (float)h;
-            part[2 * j + 1] = (float)hx;
-        });
-        __syncthreads();
+        BackSums<V> v = {};
+        back_sum_from<T, A, U>(p, back_columns<T, M>(p, a, t, f, b), w, 0, x, g, v);
+        add_columns<V>(p, a, t, v, s_all, s_col);
+        if (p.cols)
+            for (int c = threadIdx.x; c < wide; c += blockDim.x) {
+                cols[c] = s_col[c];
+                cols[p.channels + c] = s_col[wide + c];
+            }
+        if (p.out) back_groups<T>(p, a, s_col, [&](int j, Two sum) { part[j] = make_float2((float)sum.a, (float)sum.b); });
+        if (b < k.b1) __syncthreads();
     }
 }
 
 // Four columns of the places' sums of dz xh and dz by one workgroup.
 template <typename T>
-__device__ __forceinline__ void back_columns_sum(const GroupArgs& p, long long at, double2* s_two) {
-    double* const s_sum = (double*)s_two;
+__device__ __forceinline__ void back_columns_sum(const GroupArgs& p, long long at, double* s_sum) {
     const int c4 = threadIdx.x & 3, threads = blockDim.x / 4;
     const long long cols = 2LL * p.channels, c = at * 4 + c4;
     double sum = 0.0;
@@ -881,18 +922,20 @@ __device__ __forceinline__ void back_columns_sum(const GroupArgs& p, long long a
 
 // Workgroups past the blocks add the columns' sums.
 template <typename T, bool M>
-__global__ __launch_bounds__(kGroupThreads, 4) void k_group_back(GroupArgs p) {
-    constexpr int V = kVec<T>, U = 8 / V;
-    __shared__ double2 s_two[kGroupThreads];
+__global__ __launch_bounds__(kGroupThreads, 2) void k_group_back(GroupArgs p) {
+    constexpr int V = kVec<T>, A = M ? 1 : V, U = kBackAhead;
+    __shared__ Two s_two[kGroupThreads];
     __shared__ float2 s_stat[kHereGroups];
     const long long i = block_id<kGroupThreads>();
     if (i >= p.blocks) {
-        if (blockIdx.y == 0 && p.cols && (i - p.blocks) * 4 < 2LL * p.channels) back_columns_sum<T>(p, i - p.blocks, s_two);
+        if (blockIdx.y == 0 && p.cols && (i - p.blocks) * 4 < 2LL * p.channels) back_columns_sum<T>(p, i - p.blocks, (double*)s_two);
         return;
     }
     const Bounds s = bounds_of(p);
     const Slab a = slab_of(p);
     const Place t = place_of<V>(p);
+    const Affine<T> f = affine_of<T>(p, a, t);
+    const Joiner o = joiner_of(a);
     const Block k = block_of(p, s, i);
     for (long long b = k.b0; b <= k.b1; ++b) {
         const Rows r = rows_of_sample(s, b);
@@ -902,29 +945,32 @@ __global__ __launch_bounds__(kGroupThreads, 4) void k_group_back(GroupArgs p) {
         VecOf<T, V> x[U], g[U];
         fetch<T, U, true>((const T*)p.x, w, w.full, x);
         fetch<T, U, true>((const T*)p.g, w, w.full, g);
+        const BackColumns<V, A> c = back_columns<T, M>(p, a, t, f, b);
         const float2* stat = (const float2*)p.stat + b * p.groups + a.j0;
         if (!p.stat) {
-            const double n = (double)(r.end - r.first) * p.per;
-            join_here<float>(p, a, b, r, s_two, [&](int j, double2 sum) { s_stat[j] = make_float2((float)(sum.x / n), (float)(sum.y / n)); });
+            const Two sum = join_here<float>(p, a, o, b, r, s_two);
+            if (o.k < a.ng && o.in == 0) {
+                const double inv = 1.0 / ((double)(r.end - r.first) * p.per);
+                s_stat[o.k] = make_float2((float)(sum.a * inv), (float)(sum.b * inv));
+            }
             __syncthreads();
             stat = s_stat;
         }
-        const auto c = back_columns<T, M>(p, a, t, b);
-        const auto m = means_of<T, M>(p, a, t, stat);
-        back_down<T, M, U>(p, c, m, w, 0, w.full, x, g);
+        back_down<T, A, U>(p, c, means_of<T, M>(p, a, t, stat), w, 0, w.full, x, g);
     }
 }
 
 // cols [batch][2][channels]; with one sample dgamma and dbeta themselves.
 template <typename T, bool M, int B, int H>
-__global__ __launch_bounds__(B) void k_group_back_one(GroupArgs p) {
+__global__ __launch_bounds__(B, 2) void k_group_back_one(GroupArgs p) {
     constexpr int V = kVec<T>, A = M ? 1 : V;
-    __shared__ float s_all[B * V];
-    __shared__ float s_col[2][B * V / 4];
-    __shared__ float2 s_stat[M ? B : B * V / 4];
+    extern __shared__ __align__(16) char s_step[];
+    float2* const s_all = (float2*)s_step;
+    float* const s_col = (float*)(s_all + step_values(p.l));
+    float2* const s_stat = s_all;  // (when the columns' sums are done)
     const long long b = block_id<B>();
     if (b >= p.batch) return;
-    const Bounds s = {p.offsets, p.each, p.rows, p.batch, 0, false};
+    const Bounds s = {p.offsets, p.each, p.rows, p.batch, 0, p.inv_each, false};
     const Slab a = slab_of(p);
     const Place t = place_of<V>(p);
     const Rows r = rows_of_sample(s, b);
@@ -945,37 +991,30 @@ __global__ __launch_bounds__(B) void k_group_back_one(GroupArgs p) {
     const T *__restrict__ x = (const T*)p.x, *__restrict__ g = (const T*)p.g;
     const Walk w = walk_of<V>(p, a, t, r.first, r.end);
     VecOf<T, V> held[H], grad[H];
+    const Affine<T> f = affine_of<T>(p, a, t);
+    const BackColumns<V, A> k = back_columns<T, M>(p, a, t, f, b);
+    fetch<T, H, false>(x, w, 0, held);
+    fetch<T, H, false>(g, w, 0, grad);
+    BackSums<V> v = {};
+    float dz[H][V];
 #pragma unroll
     for (int h = 0; h < H; ++h)
         if (h < w.full) {
-            held[h] = take(x + w.at + h * w.step);
-            grad[h] = take(g + w.at + h * w.step);
-        }
-    const BackColumns<V, A> k = back_columns<T, M>(p, a, t, b);
-    float da[V], db[V], dz[H][V];
 #pragma unroll
-    for (int c = 0; c < V; ++c) da[c] = db[c] = 0.0f;
-#pragma unroll
-    for (int h = 0; h < H; ++h)
-        if (h < w.full)
-        {
-#pragma unroll
-            for (int i = 0; i < V; ++i) back_add<V, A>(k, i, (float)held[h][i], (float)grad[h][i], p.act, da, db, dz[h][i]);
+            for (int i = 0; i < V; ++i) dz[h][i] = back_add<V, A>(k, i, (float)held[h][i], (float)grad[h][i], p.act, v);
             __builtin_amdgcn_sched_barrier(0);
         }
     VecOf<T, V> more[2], more_g[2];
     fetch<T, 2, false>(x, w, H, more);
     fetch<T, 2, false>(g, w, H, more_g);
-    back_sum_from<T, M, 2>(p, k, w, H, more, more_g, da, db);
-    add_columns<V>(p, a, da, s_all, [&](int c, float sum) { s_col[0][c] = sum; });
-    add_columns<V>(p, a, db, s_all, [&](int c, float sum) { s_col[1][c] = sum; });
-    __syncthreads();
-    for (int c = threadIdx.x; c < wide; c += blockDim.x) give(c, s_col[0][c], s_col[1][c]);
+    back_sum_from<T, A, 2>(p, k, w, H, more, more_g, v);
+    add_columns<V>(p, a, t, v, s_all, s_col);
+    for (int c = threadIdx.x; c < wide; c += blockDim.x) give(c, s_col[c], s_col[wide + c]);
     if (!p.out) return;
-    const double n = (double)(r.end - r.first) * p.per;
-    back_groups<T>(p, a, s_col[0], s_col[1], [&](int j, double h, double hx) { s_stat[j] = make_float2((float)(h / n), (float)(hx / n)); });
+    const double inv = 1.0 / ((double)(r.end - r.first) * p.per);
+    back_groups<T>(p, a, s_col, [&](int j, Two sum) { s_stat[j] = make_float2((float)(sum.a * inv), (float)(sum.b * inv)); });
     __syncthreads();
-    const Means<V, A> m = means_of<T, M>(p, a, t, s_stat);
+    const Means<A> m = means_of<T, M>(p, a, t, s_stat);
 #pragma unroll
     for (int h = 0; h < H; ++h)
         if (h < w.full) {
@@ -992,7 +1031,7 @@ __global__ __launch_bounds__(B) void k_group_back_one(GroupArgs p) {
         fetch<T, 2, true>(x, w, w.full, more);
         fetch<T, 2, true>(g, w, w.full, more_g);
     }
-    back_down<T, M, 2>(p, k, m, w, H, w.full, more, more_g);
+    back_down<T, A, 2>(p, k, m, w, H, w.full, more, more_g);
 }
 
 // offsets[b]: the rows whose sample index is below b, a wave a sample.
@@ -1013,14 +1052,14 @@ static int group_vec(int dtype) { return dtype == SCNN_F32 ? 4 : 8; }
 static GroupLayout group_layout(int channels, int per, int dtype, int threads, int most) {
     const int v = group_vec(dtype);
     GroupLayout l = {};
-    l.slabs = l.pieces = 1;
+    l.slabs = l.pieces = l.sub = 1;
     l.wide = channels;
     int even = 1;  // the largest power of two that both the vector and a row are a multiple of
     while (even < v && channels % (2 * even) == 0) even *= 2;
-    const long long period = channels / even;  // vectors after which a run of rows meets the same columns
-    if (even < v && period <= threads && (long long)channels <= most) {
+    const int period = channels / even;  // vectors after which a run of rows meets the same columns
+    if (even < v && period <= threads && channels <= most) {
         l.flat = 1;
-        l.active = (int)(threads / period * period);
+        l.active = threads / period * period;
         l.reps = (int)((long long)l.active * v / channels);
         l.tv = l.active;
         l.pitch = channels;
@@ -1041,37 +1080,45 @@ static GroupLayout group_layout(int channels, int per, int dtype, int threads, i
         l.active = l.tv * l.reps;
         l.pitch = l.tv * v;
         l.merged = l.pieces > 1 || per % v == 0;
+        while (l.sub < v && per % (2 * l.sub) == 0) l.sub *= 2;
     }
     l.inv_tv = 1.0f / (float)l.tv;
     l.inv_per = 1.0f / (float)per;
     l.inv_c = 1.0f / (float)channels;
+    l.inv_reps = 1.0 / (double)l.reps;
     return l;
 }
 static unsigned group_threads(const GroupLayout& l) { return (unsigned)((l.active + 63) / 64 * 64); }
+// Bytes of LDS: pairs in fp64 for `sub` neighbours (and a group's statistics), pairs in fp32 and the columns' sums.
+static unsigned sums_lds(const GroupLayout& l, int v) {
+    return (unsigned)(l.reps * ((l.flat ? l.pitch : l.pitch / (l.merged ? v : l.sub)) + 1) * 16);
+}
+static unsigned one_lds(const GroupLayout& l, int v, int per) { return sums_lds(l, v) + (unsigned)(l.wide / per) * 16; }
+static unsigned back_lds(const GroupLayout& l) { return (unsigned)(step_values(l) + l.wide) * 8; }
 
-// Rows of a block: four workgroups of 256 threads a compute unit, but no fewer than two vectors a thread.
+// Rows of a block: two workgroups of 256 threads a compute unit (what a workgroup does before and after its rows costs all its waves
+// as much as some vectors each), but no fewer than two vectors a thread.
 static long long group_chunk(const GroupLayout& l, long long rows) {
-    long long want = 4LL * 256 * device_cu_count() / group_threads(l) / l.slabs;
+    long long want = 2LL * device_cu_count() / l.slabs;
     if (want < 1) want = 1;
     long long chunk = (rows + want - 1) / want;
     if (chunk < 2LL * l.reps) chunk = 2LL * l.reps;
     return round_up(chunk, l.reps);
 }
 
-// A workgroup a sample and slab, its values in registers: up to kOneHeld (backward half as many) on the average.
-constexpr long long kOneHeld = 32768;
-constexpr int kOneThreads = 1024, kOneOdd = 512;  // threads where vectors are of one group, and where they are not
-static bool group_one(long long rows, long long batch, int channels, int per, int dtype, bool back, GroupLayout& l) {
+// A workgroup a sample and slab, its values in registers: 16384 of them, in 256 threads, or in 512 where workgroups are few; samples of
+// up to twice that on the average.
+constexpr int kOneFew = 512, kOneMany = 256;
+constexpr long long kOneHeld = 16384;
+static bool group_one(long long rows, long long batch, int channels, int per, int dtype, GroupLayout& l, int& threads) {
     const int v = group_vec(dtype), least = 64 / (16 / v);  // (64 bytes of a row)
-    const long long held = back ? kOneHeld / 2 : kOneHeld, values = rows * channels / batch;
-    const bool merged = per % v == 0;
-    const int threads = merged ? kOneThreads : kOneOdd;
-    int most = threads * v / 4;
+    const long long values = rows * channels / batch, cus = device_cu_count();
+    int most = kOneMany * v / 2;
     if (per > most) return false;
-    if (merged) {
+    if (per % v == 0) {
         // narrower slabs where a sample has more values than that, or compute units would idle
-        long long want = (values + held - 1) / held;
-        if (want * batch < device_cu_count() && values > 4096) want = device_cu_count() / batch;
+        long long want = (values + kOneHeld - 1) / kOneHeld;
+        if (want * batch < cus && values > 4096) want = cus / batch;
         if (want > 1) {
             long long wide = (channels + want - 1) / want;
             if (wide < least) wide = least;
@@ -1079,22 +1126,27 @@ static bool group_one(long long rows, long long batch, int channels, int per, in
             if (wide < most) most = (int)wide;
         }
     }
-    if (rows * (channels < most ? channels : most) > held * batch) return false;
+    if (rows * (channels < most ? channels : most) > 2 * kOneHeld * batch) return false;
+    threads = kOneFew;
     l = group_layout(channels, per, dtype, threads, most);
+    if (batch * l.slabs >= cus || one_lds(l, v, per) > 60000) {
+        threads = kOneMany;
+        l = group_layout(channels, per, dtype, threads, most);
+    }
     return l.pieces == 1;
 }
 
-struct GroupSpace { GroupLayout l; long long blocks, chunk, places; size_t part, cols, stat, total; bool one, joined; };
+struct GroupSpace { GroupLayout l; long long blocks, chunk, places; size_t part, cols, stat, total; bool one, joined; int threads; };
 static GroupSpace group_space(long long rows, long long batch, int channels, int groups, int dtype, bool back) {
     GroupSpace s = {};
     const int per = channels / groups;
-    s.one = group_one(rows, batch, channels, per, dtype, back, s.l);
+    s.one = group_one(rows, batch, channels, per, dtype, s.l, s.threads);
     if (s.one) {
         s.places = batch;
         if (back && batch > 1) s.total = (size_t)round_up(batch * channels * 8, 256);
         return s;
     }
-    s.l = group_layout(channels, per, dtype, 256, kGroupThreads * group_vec(dtype));
+    s.l = group_layout(channels, per, dtype, kGroupThreads, kGroupThreads * group_vec(dtype));
     s.chunk = group_chunk(s.l, rows);
     s.blocks = rows < 1 ? 1 : (rows + s.chunk - 1) / s.chunk;
     s.places = s.blocks + batch - 1;
@@ -1124,6 +1176,8 @@ static GroupArgs group_args(int dtype, const GroupCall& c, bool back, GroupSpace
     s = group_space(c.rows, c.batch, c.channels, c.groups, dtype, back);
     p.l = s.l;
     p.chunk = s.chunk; p.blocks = s.blocks; p.places = s.places;
+    p.inv_each = p.each > 0 ? 1.0 / (double)p.each : 0.0;
+    p.inv_chunk = s.one ? 0.0 : 1.0 / (double)s.chunk;
     p.part = (char*)c.workspace + s.part;
     if (c.dgamma || c.dbeta) p.cols = (float*)((char*)c.workspace + s.cols);
     if (s.joined) p.stat = (char*)c.workspace + s.stat;
@@ -1139,42 +1193,40 @@ static void group_join(const GroupArgs& p, hipStream_t s) {
     hipLaunchKernelGGL((k_group_join<T, BACK>), grid_of<256>((p.batch * p.groups + 256 / q - 1) / (256 / q)), dim3(256), 0, s, p, q);
 }
 
-template <typename T>
-static hipError_t group_fwd(int dtype, const GroupCall& c, hipStream_t s) {
-    GroupSpace at;
-    const GroupArgs p = group_args(dtype, c, false, at);
+template <typename T, bool M>
+static hipError_t group_fwd(int dtype, const GroupCall& c, const GroupArgs& p, const GroupSpace& at, hipStream_t s) {
+    constexpr int V = kVec<T>;
     const dim3 threads(group_threads(p.l));
     if (at.one) {
-        if (p.l.merged) hipLaunchKernelGGL((k_group_one<T, true, kOneThreads, 32 / kVec<T>>), grid_of<kOneThreads>(c.batch, p.l.slabs), threads, 0, s, p);
-        else hipLaunchKernelGGL((k_group_one<T, false, kOneOdd, 8>), grid_of<kOneOdd>(c.batch, p.l.slabs), threads, 0, s, p);
+        const unsigned lds = one_lds(p.l, V, p.per);
+        if (at.threads == kOneFew) hipLaunchKernelGGL((k_group_one<T, M, kOneFew, 32 / V>), grid_of<kOneFew>(c.batch, p.l.slabs), threads, lds, s, p);
+        else hipLaunchKernelGGL((k_group_one<T, M, kOneMany, 64 / V>), grid_of<kOneMany>(c.batch, p.l.slabs), threads, lds, s, p);
         return hipGetLastError();
     }
     const dim3 grid = grid_of<kGroupThreads>(p.blocks, p.l.slabs);
-    hipLaunchKernelGGL((p.l.merged ? k_group_sums<T, true> : k_group_sums<T, false>), grid, threads, 0, s, p);
+    hipLaunchKernelGGL((k_group_sums<T, M>), grid, threads, sums_lds(p.l, V), s, p);
     if (p.stat) group_join<T, false>(p, s);
-    hipLaunchKernelGGL((k_group_apply<T>), grid, threads, 0, s, p);
+    hipLaunchKernelGGL((k_group_apply<T, M>), grid, threads, 0, s, p);
     return hipGetLastError();
 }
 
-template <typename T>
-static hipError_t group_bwd(int dtype, const GroupCall& c, hipStream_t s) {
-    GroupSpace at;
-    const GroupArgs p = group_args(dtype, c, true, at);
+template <typename T, bool M>
+static hipError_t group_bwd(int dtype, const GroupCall& c, const GroupArgs& p, const GroupSpace& at, hipStream_t s) {
+    constexpr int V = kVec<T>;
     const dim3 threads(group_threads(p.l));
+    const unsigned lds = back_lds(p.l);
     hipError_t e;
     if (at.one) {
-        if (p.l.merged) hipLaunchKernelGGL((k_group_back_one<T, true, kOneThreads, 16 / kVec<T>>), grid_of<kOneThreads>(c.batch, p.l.slabs), threads, 0, s, p);
-        else hipLaunchKernelGGL((k_group_back_one<T, false, kOneOdd, 4>), grid_of<kOneOdd>(c.batch, p.l.slabs), threads, 0, s, p);
+        if (at.threads == kOneFew) hipLaunchKernelGGL((k_group_back_one<T, M, kOneFew, 32 / V>), grid_of<kOneFew>(c.batch, p.l.slabs), threads, lds, s, p);
+        else hipLaunchKernelGGL((k_group_back_one<T, M, kOneMany, 64 / V>), grid_of<kOneMany>(c.batch, p.l.slabs), threads, lds, s, p);
         e = hipGetLastError();
         if (c.batch == 1) return e;
     } else {
-        hipLaunchKernelGGL((p.l.merged ? k_group_back_sums<T, true> : k_group_back_sums<T, false>),
-                           grid_of<kGroupThreads>(p.blocks, p.l.slabs), threads, 0, s, p);
+        hipLaunchKernelGGL((k_group_back_sums<T, M>), grid_of<kGroupThreads>(p.blocks, p.l.slabs), threads, lds, s, p);
         if (p.out) {
             if (p.stat) group_join<T, true>(p, s);
             const long long more = p.cols ? (2LL * p.channels + 3) / 4 : 0;
-            hipLaunchKernelGGL((p.l.merged ? k_group_back<T, true> : k_group_back<T, false>),
-                               grid_of<kGroupThreads>(p.blocks + more, p.l.slabs), threads, 0, s, p);
+            hipLaunchKernelGGL((k_group_back<T, M>), grid_of<kGroupThreads>(p.blocks + more, p.l.slabs), threads, 0, s, p);
             return hipGetLastError();
         }
         e = hipGetLastError();
@@ -1183,21 +1235,22 @@ static hipError_t group_bwd(int dtype, const GroupCall& c, hipStream_t s) {
     return launch_column_sums(p.cols, (int)p.places, 2LL * p.channels, p.channels, c.dgamma, c.dbeta, dtype, s);
 }
 
-hipError_t launch_group_fwd(int dtype, const GroupCall& c, hipStream_t s) {
+template <typename T>
+static hipError_t group_norm(int dtype, const GroupCall& c, bool back, hipStream_t s) {
+    GroupSpace at;
+    const GroupArgs p = group_args(dtype, c, back, at);
+    if (back) return p.l.merged ? group_bwd<T, true>(dtype, c, p, at, s) : group_bwd<T, false>(dtype, c, p, at, s);
+    return p.l.merged ? group_fwd<T, true>(dtype, c, p, at, s) : group_fwd<T, false>(dtype, c, p, at, s);
+}
+static hipError_t group_norm(int dtype, const GroupCall& c, bool back, hipStream_t s) {
     switch (dtype) {
-        case SCNN_F32: return group_fwd<float>(dtype, c, s);
-        case SCNN_BF16: return group_fwd<__bf16>(dtype, c, s);
-        default: return group_fwd<_Float16>(dtype, c, s);
+        case SCNN_F32: return group_norm<float>(dtype, c, back, s);
+        case SCNN_BF16: return group_norm<__bf16>(dtype, c, back, s);
+        default: return group_norm<_Float16>(dtype, c, back, s);
     }
 }
-
-hipError_t launch_group_bwd(int dtype, const GroupCall& c, hipStream_t s) {
-    switch (dtype) {
-        case SCNN_F32: return group_bwd<float>(dtype, c, s);
-        case SCNN_BF16: return group_bwd<__bf16>(dtype, c, s);
-        default: return group_bwd<_Float16>(dtype, c, s);
-    }
-}
+hipError_t launch_group_fwd(int dtype, const GroupCall& c, hipStream_t s) { return group_norm(dtype, c, false, s); }
+hipError_t launch_group_bwd(int dtype, const GroupCall& c, hipStream_t s) { return group_norm(dtype, c, true, s); }
 
 hipError_t launch_sample_offsets(const int* coords, int stride, long long rows, const long long* rows_dev, long long batch,
                                  long long* offsets, hipStream_t s) {
