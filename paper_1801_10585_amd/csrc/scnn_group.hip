@@ -27,13 +27,13 @@ constexpr int kHereGroups = 64;     // most groups of a slab whose sums a workgr
 
 // How threads lie over columns.  A workgroup takes `wide` columns from c0 on: tv threads a row, a vector each, `reps` rows at
 // a time.  Rows of all C columns that are no whole number of vectors run on without a gap (flat): `active` vectors are `reps`
-// whole rows, so that a thread meets the same columns at every step.  Either way value (thread, i) is number thread V + i of a
-// step, and row k's column c number k pitch + c.
+// whole rows, so that a thread meets the same columns at every step; value i of thread t is then number t V + i of a step, and row k's
+// column c number k C + c.
 struct GroupLayout {
-    int tv, reps, active, pitch, flat;
+    int tv, reps, active, flat;
     int wide, slabs, pieces;  // a slab is whole groups (pieces 1), or one of `pieces` pieces of a group
     int merged;               // a vector's columns are of one group
-    int sub;                  // neighbouring values of a vector that are of one group, whatever the vector (a power of two)
+    int sub;                  // 2^sub neighbouring values of a vector are of one group, whatever the vector
     float inv_tv, inv_per, inv_c;
     double inv_reps;
 };
@@ -45,7 +45,7 @@ struct GroupArgs {
     const long long* offsets;
     long long each;              // rows of a sample where offsets is null
     long long rows, chunk;       // chunk: rows of a block
-    long long batch, blocks, places;
+    long long batch, blocks, places, sum_blocks;
     double inv_each, inv_chunk;
     int channels, groups, per, act;
     float eps;
@@ -177,16 +177,20 @@ __device__ __forceinline__ int column_of(const GroupArgs& p, const Slab& a, cons
 // Group in the slab of a column of it.
 __device__ __forceinline__ int group_of(const GroupArgs& p, int column) { return p.l.pieces > 1 ? 0 : quotient(column, p.l.inv_per); }
 
-// A thread's vectors among the rows lo .. hi - 1: `full` whole ones, then `part` of n values.
+// A thread's vectors among the rows lo .. hi - 1: `full` whole ones, then `part` of n values.  All threads that have any whole one have
+// `common` of them (the same in every lane).
 struct Walk {
     long long at, step;
-    int full, part, n;
+    int full, part, n, common;
 };
 template <int V>
 __device__ __forceinline__ Walk walk_of(const GroupArgs& p, const Slab& a, const Place& t, long long lo, long long hi) {
-    Walk w = {0, 0, 0, 0, 0};
-    if ((int)threadIdx.x >= p.l.active || hi <= lo) return w;
-    const int steps = (int)quotient(hi - lo, p.l.inv_reps), left = (int)(hi - lo - (long long)steps * p.l.reps);
+    Walk w = {0, 0, 0, 0, 0, 0};
+    if (hi <= lo) return w;
+    const int steps = __builtin_amdgcn_readfirstlane((int)quotient(hi - lo, p.l.inv_reps));
+    w.common = steps;
+    if ((int)threadIdx.x >= p.l.active) return w;
+    const int left = (int)(hi - lo - (long long)steps * p.l.reps);
     w.step = (long long)p.l.reps * p.channels;
     w.full = steps;
     if (p.l.flat) {
@@ -212,25 +216,39 @@ template <typename T> __device__ __forceinline__ VecOf<T, kVec<T>> take(const T*
 // Results are not read again soon: they leave the L2 to the rows.
 template <typename T> __device__ __forceinline__ void put(T* p, VecOf<T, kVec<T>> v) { __builtin_nontemporal_store(v, (Loose<T>*)p); }
 
-// U vectors of a thread on their way: number k, k + 1, ... upwards, or k - 1, k - 2, ... downwards (the last ones of a block are
-// what the L2 still has when its rows are read again).
+// Vector number k of a thread, counted from its first one or, DOWN, from its last one (the last ones of a block are what the L2 still
+// has when its rows are read again).
+template <bool DOWN> __device__ __forceinline__ long long position(const Walk& w, int k) { return w.at + (long long)(DOWN ? w.full - 1 - k : k) * w.step; }
+// U vectors of a thread on their way, from number k on.
 template <typename T, int U, bool DOWN>
 __device__ __forceinline__ void fetch(const T* __restrict__ x, const Walk& w, int k, VecOf<T, kVec<T>> (&r)[U]) {
-    const T* at = x + w.at + (long long)(DOWN ? k - 1 : k) * w.step;
-    const int n = DOWN ? k : w.full - k;
 #pragma unroll
     for (int u = 0; u < U; ++u)
-        if (u < n) r[u] = take(at + (DOWN ? -u : u) * w.step);
+        if (k + u < w.full) r[u] = take(x + position<DOWN>(w, k + u));
+}
+// Calls use(slot, k) for a thread's vectors from number k up to `end`; the first U are there, and each slot is loaded again as soon as it
+// was used: load(slot, k).  (Loaded all at once behind the last use, sums of 643072 x 64 bf16 in 64 groups took 27 us.)
+template <int U, typename Use, typename Load>
+__device__ __forceinline__ void walk(const Walk& w, int k, int end, Use use, Load load) {
+    if (k >= end) return;
+    for (const int common = w.common - (w.full - end); k + 2 * U <= common; k += U)
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            use(u, k + u);
+            load(u, k + U + u);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    for (; k < end; k += U)
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (k + u < end) {
+                use(u, k + u);
+                if (k + U + u < end) load(u, k + U + u);
+                __builtin_amdgcn_sched_barrier(0);
+            }
 }
 
 __device__ __forceinline__ float finite_or_zero(float v) { return __builtin_fabsf(v) < __builtin_huge_valf() ? v : 0.0f; }
-
-// Power of two of lanes that add n values: at most a wave.
-__device__ __forceinline__ int lanes_for(int n) {
-    int q = 1;
-    while (q < n && q < 64) q <<= 1;
-    return q;
-}
 
 struct Two { double a, b; };
 __device__ __forceinline__ Two lanes_two(Two v, int q) {
@@ -274,17 +292,12 @@ __device__ __forceinline__ void add_value(float x, int i, Sums<T, M>& v) {
 template <typename T, bool M, int U>
 __device__ __forceinline__ void sum_from(const T* __restrict__ x, const Walk& w, int k, VecOf<T, kVec<T>> (&r)[U], Sums<T, M>& v) {
     constexpr int V = kVec<T>;
-    while (k < w.full) {
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (u < w.full - k) {
+    walk<U>(w, k, w.full,
+            [&](int u, int) {
 #pragma unroll
                 for (int i = 0; i < V; ++i) add_value<T, M>((float)r[u][i], i, v);
-                __builtin_amdgcn_sched_barrier(0);  // (the compiler would take all of them apart at once, in twice the registers)
-            }
-        k += U;
-        fetch<T, U, false>(x, w, k, r);
-    }
+            },
+            [&](int u, int n) { r[u] = take(x + position<false>(w, n)); });
     long long at = w.at + (long long)w.full * w.step;
     for (k = 0; k < w.part; ++k, at += w.step)
 #pragma unroll
@@ -292,40 +305,53 @@ __device__ __forceinline__ void sum_from(const T* __restrict__ x, const Walk& w,
             if (i < w.n) add_value<T, M>((float)x[at + i], i, v);
 }
 
-// Sums over the slab's groups of the threads' pairs, then done(group, sums) by one lane a group.  All threads of the workgroup call
-// it.  s_all: a row of a step after the other, the sums of `sub` neighbouring values as one pair, a pair between two rows so that
-// neighbouring rows' are in different banks.
+// Lanes that add the n values of each of `groups` sums, as a power of two: no more than there are values, threads for them all, or lanes
+// of a wave.
+__device__ __forceinline__ int lane_bits(int n, int groups) {
+    int q = 0;
+    while (1 << q < n && q < 6 && 2 * groups << q <= (int)blockDim.x) ++q;
+    return q;
+}
+// Where the numbers of a step lie in LDS: number i of each thread beside that of the others (lanes that write meet different banks), the
+// arrays of two i one number apart from being so many banks apart.  2^sub neighbouring values are one number, 2^v a vector.
+__device__ __forceinline__ int step_at(const GroupArgs& p, int v, int sub, int row, int column) {
+    const int e = p.l.flat ? row * p.channels + column : column >> sub, each = v - sub;
+    return (e & ((1 << each) - 1)) * (p.l.active + 1) + (p.l.flat ? e >> each : row * p.l.tv + (e >> each));
+}
+
+// Sums over the slab's groups of the threads' pairs, then done(group, sums) by one lane a group.  All threads of the workgroup call it.
 template <typename T, bool M, typename F>
-__device__ __forceinline__ void add_groups(const GroupArgs& p, const Slab& a, const Place& t, const Sums<T, M>& v, Two* s_all, F done) {
+__device__ __forceinline__ void add_groups(const GroupArgs& p, const Slab& a, const Sums<T, M>& v, Two* s_all, F done) {
     constexpr int V = kVec<T>;
-    const int sub = M ? V : p.l.sub, w = M ? (a.w + V - 1) / V : a.w / sub, pitch = p.l.flat ? p.l.pitch : p.l.pitch / sub + 1;
-    Two* const mine = s_all + (p.l.flat ? t.col : t.row * pitch + t.col / sub);
+    constexpr int VB = V == 8 ? 3 : 2;
+    const int sub = M ? VB : p.l.sub, w = (a.w + (1 << sub) - 1) >> sub, next = p.l.active + 1;
+    Two* const mine = s_all + threadIdx.x;
     if ((int)threadIdx.x < p.l.active) {
         if constexpr (M) {
             mine[0] = {v.one[0] + v.one[1], v.two[0] + v.two[1]};
+        } else if (sub == 0) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) mine[i * next] = {v.one[i], v.two[i]};
         } else if (sub == 1) {
 #pragma unroll
-            for (int i = 0; i < V; ++i) mine[i] = {v.one[i], v.two[i]};
-        } else if (sub == 2) {
-#pragma unroll
-            for (int i = 0; i < V; i += 2) mine[i / 2] = {v.one[i] + v.one[i + 1], v.two[i] + v.two[i + 1]};
+            for (int i = 0; i < V; i += 2) mine[i / 2 * next] = {v.one[i] + v.one[i + 1], v.two[i] + v.two[i + 1]};
         } else if constexpr (V == 8) {
 #pragma unroll
             for (int i = 0; i < V; i += 4)
-                mine[i / 4] = {(v.one[i] + v.one[i + 1]) + (v.one[i + 2] + v.one[i + 3]), (v.two[i] + v.two[i + 1]) + (v.two[i + 2] + v.two[i + 3])};
+                mine[i / 4 * next] = {(v.one[i] + v.one[i + 1]) + (v.one[i + 2] + v.one[i + 3]), (v.two[i] + v.two[i + 1]) + (v.two[i + 2] + v.two[i + 3])};
         }
     }
     __syncthreads();
-    const int n = w * p.l.reps, q = lanes_for(n);
+    const int n = w * p.l.reps, bits = lane_bits(n, a.ng), q = 1 << bits;
     const float inv = 1.0f / (float)w;
-    const int set = threadIdx.x / q, sets = blockDim.x / q, in = threadIdx.x & (q - 1);
+    const int set = threadIdx.x >> bits, sets = blockDim.x >> bits, in = threadIdx.x & (q - 1);
     for (int j0 = 0; j0 < a.ng; j0 += sets) {
         const int j = j0 + set;
         Two sum = {0.0, 0.0};
         if (j < a.ng)
             for (int e = in; e < n; e += q) {
                 const int k = quotient(e, inv);
-                const Two o = s_all[k * pitch + j * w + (e - k * w)];
+                const Two o = s_all[step_at(p, VB, sub, k, (j * w + (e - k * w)) << sub)];
                 sum.a += o.a;
                 sum.b += o.b;
             }
@@ -402,28 +428,21 @@ __device__ __forceinline__ void forward_vector(const GroupArgs& p, const Columns
 #pragma unroll
     for (int i = 0; i < kVec<T>; ++i) y[i] = (T)forward_value<kVec<T>, A>(k, i, (float)r[i], p.act);
     put((T*)p.out + at, y);
-    __builtin_amdgcn_sched_barrier(0);
 }
-// A thread's vectors from number k - 1 down to `from`, of which the first U are there, and its odd values.
+// A thread's vectors from its last down to number `from`, of which the first U are there, and its odd values.
 template <typename T, int A, int U>
-__device__ __forceinline__ void forward_down(const GroupArgs& p, const Columns<kVec<T>, A>& c, const Walk& w, int from, int k,
+__device__ __forceinline__ void forward_down(const GroupArgs& p, const Columns<kVec<T>, A>& c, const Walk& w, int from,
                                              VecOf<T, kVec<T>> (&r)[U]) {
-    while (k > from) {
-        const long long at = w.at + (long long)(k - 1) * w.step;
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (u < k - from) forward_vector<T, A>(p, c, at - u * w.step, r[u]);
-        k -= U;
-        fetch<T, U, true>((const T*)p.x, w, k, r);
-    }
+    walk<U>(w, 0, w.full - from, [&](int u, int n) { forward_vector<T, A>(p, c, position<true>(w, n), r[u]); },
+            [&](int u, int n) { r[u] = take((const T*)p.x + position<true>(w, n)); });
     long long at = w.at + (long long)w.full * w.step;
-    for (k = 0; k < w.part; ++k, at += w.step)
+    for (int k = 0; k < w.part; ++k, at += w.step)
 #pragma unroll
         for (int i = 0; i < kVec<T> - 1; ++i)
             if (i < w.n) ((T*)p.out)[at + i] = (T)forward_value<kVec<T>, A>(c, i, (float)((const T*)p.x)[at + i], p.act);
 }
 
-constexpr int kAhead = 8;  // vectors of x that a thread of the blocks' kernels has on their way
+constexpr int kAhead = 4;  // vectors of x that a thread of the blocks' kernels has on their way
 
 template <typename T, bool M>
 __global__ __launch_bounds__(kGroupThreads, 2) void k_group_sums(GroupArgs p) {
@@ -453,7 +472,7 @@ __global__ __launch_bounds__(kGroupThreads, 2) void k_group_sums(GroupArgs p) {
         Sums<T, M> v;
         begin_sums<T, M>(near, v);
         sum_from<T, M, kAhead>((const T*)p.x, w, 0, x, v);
-        add_groups<T, M>(p, a, t, v, (Two*)s_step, [&](int j, Two sum) { part[j] = sum; });
+        add_groups<T, M>(p, a, v, (Two*)s_step, [&](int j, Two sum) { part[j] = sum; });
         if (b < k.b1) __syncthreads();
     }
 }
@@ -504,12 +523,20 @@ __global__ __launch_bounds__(256) void k_group_join(GroupArgs p, int q) {
         const F* __restrict__ part = (const F*)p.part;
         const int pieces = p.l.pieces;
         const long long n = (long long)count * pieces;
-#pragma unroll 4
-        for (long long e = in; e < n; e += q) {
-            const long long i = pieces > 1 ? e / pieces : e;
-            const F* at = part + (((from + i) * p.groups + j) * pieces + (e - i * pieces)) * 2;
-            sum.a += (double)at[0];
-            sum.b += (double)at[1];
+        // (four at a time: a load behind the other takes a microsecond each)
+        for (long long e0 = in; e0 < n; e0 += 4LL * q) {
+            F two[4][2];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const long long e = e0 + u * q < n ? e0 + u * q : n - 1, i = pieces > 1 ? e / pieces : e;
+                __builtin_memcpy(two[u], part + (((from + i) * p.groups + j) * pieces + (e - i * pieces)) * 2, sizeof(two[u]));
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                if (e0 + u * q < n) {
+                    sum.a += (double)two[u][0];
+                    sum.b += (double)two[u][1];
+                }
         }
     }
     sum = set_add(sum, q, s_wave);
@@ -535,9 +562,9 @@ __device__ __forceinline__ Joiner joiner_of(const Slab& a) {
     o.sets = quotient((int)blockDim.x, inv);
     o.set = quotient((int)threadIdx.x, inv);
     o.j = threadIdx.x - o.set * a.ng;
-    o.q = 1;
-    while (2 * o.q * a.ng <= (int)blockDim.x && o.q < 64 && o.q < o.sets) o.q <<= 1;
-    o.k = threadIdx.x / o.q;
+    const int bits = lane_bits(o.sets, a.ng);
+    o.q = 1 << bits;
+    o.k = threadIdx.x >> bits;
     o.in = threadIdx.x & (o.q - 1);
     return o;
 }
@@ -547,12 +574,18 @@ __device__ __forceinline__ Two join_here(const GroupArgs& p, const Slab& a, cons
     const long long from = places_of(p, b, r, count);
     Two sum = {0.0, 0.0};
     if (o.set < o.sets) {
-        const F* __restrict__ part = (const F*)p.part + ((from + o.set) * p.groups + a.j0 + o.j) * 2;
-        const long long step = (long long)o.sets * p.groups * 2;
-#pragma unroll 8
-        for (int i = o.set; i < count; i += o.sets, part += step) {
-            sum.a += (double)part[0];
-            sum.b += (double)part[1];
+        const F* __restrict__ part = (const F*)p.part + (from * p.groups + a.j0 + o.j) * 2;
+        for (int i = o.set; i < count; i += 4 * o.sets) {  // (four at a time, as in k_group_join)
+            F two[4][2];
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                __builtin_memcpy(two[u], part + (long long)(i + u * o.sets < count ? i + u * o.sets : count - 1) * p.groups * 2, sizeof(two[u]));
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                if (i + u * o.sets < count) {
+                    sum.a += (double)two[u][0];
+                    sum.b += (double)two[u][1];
+                }
         }
     }
     __syncthreads();
@@ -592,7 +625,7 @@ __global__ __launch_bounds__(kGroupThreads, 2) void k_group_apply(GroupArgs p) {
         const Walk w = walk_of<V>(p, a, t, lo, hi);
         // (the last vectors are on their way while the sums are joined)
         VecOf<T, V> x[kAhead];
-        fetch<T, kAhead, true>((const T*)p.x, w, w.full, x);
+        fetch<T, kAhead, true>((const T*)p.x, w, 0, x);
         const GroupStat* stat = (const GroupStat*)p.stat + id;
         if (!p.stat) {
             const bool ends = o.k < a.ng && o.in == 0;
@@ -610,7 +643,7 @@ __global__ __launch_bounds__(kGroupThreads, 2) void k_group_apply(GroupArgs p) {
             stat = s_stat;
         }
         const Columns<V, A> c = columns_of<T, M>(p, a, t, f, stat);
-        forward_down<T, A, kAhead>(p, c, w, 0, w.full, x);
+        forward_down<T, A, kAhead>(p, c, w, 0, x);
     }
 }
 
@@ -652,10 +685,10 @@ __global__ __launch_bounds__(B, 2) void k_group_one(GroupArgs p) {
             for (int i = 0; i < V; ++i) add_value<T, M>((float)held[h][i], i, v);
             __builtin_amdgcn_sched_barrier(0);
         }
-    VecOf<T, V> more[4];
-    fetch<T, 4, false>(x, w, H, more);
-    sum_from<T, M, 4>(x, w, H, more, v);
-    add_groups<T, M>(p, a, t, v, s_all, [&](int j, Two sum) {
+    VecOf<T, V> more[2];
+    fetch<T, 2, false>(x, w, H, more);
+    sum_from<T, M, 2>(x, w, H, more, v);
+    add_groups<T, M>(p, a, v, s_all, [&](int j, Two sum) {
         const GroupStat g = stat_of(near_value<T>(p, r, a.j0 + j), sum, (double)(r.end - r.first) * p.per, p.eps);
         s_stat[j] = g;
         if (p.mean) p.mean[id + j] = g.mean;
@@ -665,9 +698,12 @@ __global__ __launch_bounds__(B, 2) void k_group_one(GroupArgs p) {
     const Columns<V, A> c = columns_of<T, M>(p, a, t, f, s_stat);
 #pragma unroll
     for (int h = 0; h < H; ++h)
-        if (h < w.full) forward_vector<T, A>(p, c, w.at + h * w.step, held[h]);
-    if (w.full > H) fetch<T, 4, true>(x, w, w.full, more);
-    forward_down<T, A, 4>(p, c, w, H, w.full, more);
+        if (h < w.full) {
+            forward_vector<T, A>(p, c, position<false>(w, h), held[h]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    if (w.full > H) fetch<T, 2, true>(x, w, 0, more);
+    forward_down<T, A, 2>(p, c, w, H, more);
 }
 
 // ------------------------------------------------------------------ backward
@@ -692,32 +728,53 @@ __device__ __forceinline__ BackColumns<kVec<T>, M ? 1 : kVec<T>> back_columns(co
     }
     return k;
 }
-// xh and dz of a value.  relu's slope hangs on the sign of z alone, and in fp32 one z in some ten million lies on the wrong side of
-// 0 and takes a whole gradient with it: what is nearer to 0 than 8 roundings of its parts (three are made) is formed anew in fp64.
-template <int V, int A>
-__device__ __forceinline__ void back_value(const BackColumns<V, A>& k, int i, float x, float g, int act, float& xh, float& dz) {
-    const float mean = k.mean[A == 1 ? 0 : i], rstd = k.rstd[A == 1 ? 0 : i];
-    xh = (x - mean) * rstd;
-    float z = __builtin_fmaf(xh, k.gamma[i], k.beta[i]);
-    if (act == SCNN_ACT_RELU) {
-        if (__builtin_fabsf(z) <= 0x1p-21f * (__builtin_fabsf(xh * k.gamma[i]) + __builtin_fabsf(k.beta[i]))) {
-            float m = mean, r = rstd, c = k.gamma[i], o = k.beta[i];
-            asm volatile("" : "+v"(m), "+v"(r), "+v"(c), "+v"(o));  // (else all columns' values are held in fp64 besides)
-            const double far = __builtin_fma(((double)x - (double)m) * (double)r, (double)c, (double)o);
-            z = far <= 0.0 ? 0.0f : 1.0f;
-        }
+// xh and dz of N values of a thread, whose columns are those from i0 on.  relu's slope hangs on the sign of z alone, and in fp32 one z
+// in some ten million lies on the wrong side of 0 and takes a whole gradient with it: what is nearer to 0 than 8 roundings of its
+// parts (three are made) is formed anew in fp64.
+template <int V, int A, int N>
+__device__ __forceinline__ void back_values(const BackColumns<V, A>& k, int i0, const float (&x)[N], const float (&g)[N], int act, float (&xh)[N],
+                                            float (&dz)[N]) {
+    float z[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const int j = A == 1 ? 0 : i0 + i;
+        xh[i] = (x[i] - k.mean[j]) * k.rstd[j];
+        z[i] = __builtin_fmaf(xh[i], k.gamma[i0 + i], k.beta[i0 + i]);
     }
-    dz = activate_back(g, z, act);
+    if (act == SCNN_ACT_RELU) {
+        bool near = false;
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            near |= __builtin_fabsf(z[i]) <= 0x1p-21f * (__builtin_fabsf(xh[i] * k.gamma[i0 + i]) + __builtin_fabsf(k.beta[i0 + i]));
+        if (near)
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                float m = k.mean[A == 1 ? 0 : i0 + i], r = k.rstd[A == 1 ? 0 : i0 + i], c = k.gamma[i0 + i], o = k.beta[i0 + i];
+                asm volatile("" : "+v"(m), "+v"(r), "+v"(c), "+v"(o));  // (else all columns' values are held in fp64 besides)
+                const double far = __builtin_fma(((double)x[i] - (double)m) * (double)r, (double)c, (double)o);
+                z[i] = far <= 0.0 ? 0.0f : 1.0f;  // (a NaN's slope is 1, as with activate_back)
+            }
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) dz[i] = activate_back(g[i], z[i], act);
 }
 template <int V>
 struct BackSums { float a[V], b[V]; };  // of dz xh and dz
-template <int V, int A>
-__device__ __forceinline__ float back_add(const BackColumns<V, A>& k, int i, float x, float g, int act, BackSums<V>& v) {
-    float xh, dz;
-    back_value<V, A>(k, i, x, g, act, xh, dz);
-    v.a[i] = __builtin_fmaf(dz, xh, v.a[i]);
-    v.b[i] += dz;
-    return dz;
+template <int V, int A, int N>
+__device__ __forceinline__ void back_add(const BackColumns<V, A>& k, int i0, const float (&x)[N], const float (&g)[N], int act, BackSums<V>& v,
+                                         float (&dz)[N]) {
+    float xh[N];
+    back_values<V, A, N>(k, i0, x, g, act, xh, dz);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        v.a[i0 + i] = __builtin_fmaf(dz[i], xh[i], v.a[i0 + i]);
+        v.b[i0 + i] += dz[i];
+    }
+}
+template <typename T>
+__device__ __forceinline__ void apart(VecOf<T, kVec<T>> r, float (&v)[kVec<T>]) {
+#pragma unroll
+    for (int i = 0; i < kVec<T>; ++i) v[i] = (float)r[i];
 }
 
 template <typename T, int A, int U>
@@ -725,44 +782,44 @@ __device__ __forceinline__ void back_sum_from(const GroupArgs& p, const BackColu
                                               VecOf<T, kVec<T>> (&r)[U], VecOf<T, kVec<T>> (&q)[U], BackSums<kVec<T>>& v) {
     constexpr int V = kVec<T>;
     const T *__restrict__ x = (const T*)p.x, *__restrict__ g = (const T*)p.g;
-    while (k < w.full) {
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (u < w.full - k) {
-#pragma unroll
-                for (int i = 0; i < V; ++i) back_add<V, A>(c, i, (float)r[u][i], (float)q[u][i], p.act, v);
-                __builtin_amdgcn_sched_barrier(0);
-            }
-        k += U;
-        fetch<T, U, false>(x, w, k, r);
-        fetch<T, U, false>(g, w, k, q);
-    }
+    walk<U>(w, k, w.full,
+            [&](int u, int) {
+                float xs[V], gs[V], dz[V];
+                apart<T>(r[u], xs);
+                apart<T>(q[u], gs);
+                back_add<V, A, V>(c, 0, xs, gs, p.act, v, dz);
+            },
+            [&](int u, int n) {
+                r[u] = take(x + position<false>(w, n));
+                q[u] = take(g + position<false>(w, n));
+            });
     long long at = w.at + (long long)w.full * w.step;
     for (k = 0; k < w.part; ++k, at += w.step)
 #pragma unroll
         for (int i = 0; i < V - 1; ++i)
-            if (i < w.n) back_add<V, A>(c, i, (float)x[at + i], (float)g[at + i], p.act, v);
+            if (i < w.n) {
+                const float xs[1] = {(float)x[at + i]}, gs[1] = {(float)g[at + i]};
+                float dz[1];
+                back_add<V, A, 1>(c, i, xs, gs, p.act, v, dz);
+            }
 }
 
-// Sums over a step's rows, given to s_col [2][wide].  All threads call it and meet at its end; s_all: a step's rows, as in add_groups.
-// (Rows without a number between them: 36.9 us in place of 26.6 for 64 samples of 512 x 256 bf16, all lanes of a sum in one bank.)
+// Sums over a step's rows, given to s_col [2][wide].  All threads call it and meet at its end; s_all: a step's numbers, as in add_groups.
+// (Rows one behind the other, all lanes of a sum in one bank: 64 samples of 512 x 256 bf16 10 us longer.)
 template <int V>
-__device__ __forceinline__ void add_columns(const GroupArgs& p, const Slab& a, const Place& t, const BackSums<V>& v, float2* s_all, float* s_col) {
-    const int wide = a.c1 - a.c0, pitch = p.l.flat ? p.l.pitch : p.l.pitch + 1;
-    float2* const mine = s_all + (p.l.flat ? t.col : t.row * pitch + t.col);
+__device__ __forceinline__ void add_columns(const GroupArgs& p, const Slab& a, const BackSums<V>& v, float2* s_all, float* s_col) {
+    const int wide = a.c1 - a.c0;
     if ((int)threadIdx.x < p.l.active)
 #pragma unroll
-        for (int i = 0; i < V; ++i) mine[i] = make_float2(v.a[i], v.b[i]);
+        for (int i = 0; i < V; ++i) s_all[i * (p.l.active + 1) + threadIdx.x] = make_float2(v.a[i], v.b[i]);
     __syncthreads();
-    int q = 1;
-    while (2 * q * wide <= (int)blockDim.x && q < p.l.reps && q < 64) q <<= 1;
-    const int sets = blockDim.x / q, in = threadIdx.x & (q - 1);
+    const int bits = lane_bits(p.l.reps, wide), q = 1 << bits, sets = blockDim.x >> bits, in = threadIdx.x & (q - 1);
     for (int c0 = 0; c0 < wide; c0 += sets) {
-        const int c = c0 + threadIdx.x / q;
+        const int c = c0 + (threadIdx.x >> bits);
         float2 sum = make_float2(0.0f, 0.0f);
         if (c < wide)
             for (int k = in; k < p.l.reps; k += q) {
-                const float2 o = s_all[k * pitch + c];
+                const float2 o = s_all[step_at(p, V == 8 ? 3 : 2, 0, k, c)];
                 sum.x += o.x;
                 sum.y += o.y;
             }
@@ -782,7 +839,8 @@ __device__ __forceinline__ void add_columns(const GroupArgs& p, const Slab& a, c
 template <typename T, typename F>
 __device__ __forceinline__ void back_groups(const GroupArgs& p, const Slab& a, const float* s_col, F done) {
     const T* __restrict__ gamma = p.gamma ? (const T*)p.gamma + a.c0 : nullptr;
-    const int wide = a.c1 - a.c0, q = lanes_for(a.w), set = threadIdx.x / q, sets = blockDim.x / q, in = threadIdx.x & (q - 1);
+    const int wide = a.c1 - a.c0, bits = lane_bits(a.w, a.ng), q = 1 << bits, set = threadIdx.x >> bits, sets = blockDim.x >> bits,
+              in = threadIdx.x & (q - 1);
     for (int j0 = 0; j0 < a.ng; j0 += sets) {
         const int j = j0 + set;
         Two sum = {0.0, 0.0};
@@ -817,53 +875,50 @@ __device__ __forceinline__ float back_result(const BackColumns<V, A>& k, const M
     const int j = A == 1 ? 0 : i;
     return k.rstd[j] * (dz * k.gamma[i] - m.h[j] - xh * m.hx[j]);
 }
-// A thread's vectors from number k - 1 down to `from`, of which the first U are there, and its odd values.
+// A thread's vectors from its last down to number `from`, of which the first U are there, and its odd values.
 template <typename T, int A, int U>
-__device__ __forceinline__ void back_down(const GroupArgs& p, const BackColumns<kVec<T>, A>& c, const Means<A>& m, const Walk& w, int from, int k,
+__device__ __forceinline__ void back_down(const GroupArgs& p, const BackColumns<kVec<T>, A>& c, const Means<A>& m, const Walk& w, int from,
                                           VecOf<T, kVec<T>> (&r)[U], VecOf<T, kVec<T>> (&q)[U]) {
     constexpr int V = kVec<T>;
     const T *__restrict__ x = (const T*)p.x, *__restrict__ g = (const T*)p.g;
-    while (k > from) {
-        const long long at = w.at + (long long)(k - 1) * w.step;
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (u < k - from) {
+    walk<U>(w, 0, w.full - from,
+            [&](int u, int n) {
                 VecOf<T, V> y;
+                float xs[V], gs[V], xh[V], dz[V];
+                apart<T>(r[u], xs);
+                apart<T>(q[u], gs);
+                back_values<V, A, V>(c, 0, xs, gs, p.act, xh, dz);
 #pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    float xh, dz;
-                    back_value<V, A>(c, i, (float)r[u][i], (float)q[u][i], p.act, xh, dz);
-                    y[i] = (T)back_result<V, A>(c, m, i, xh, dz);
-                }
-                put((T*)p.out + at - u * w.step, y);
-                __builtin_amdgcn_sched_barrier(0);
-            }
-        k -= U;
-        fetch<T, U, true>(x, w, k, r);
-        fetch<T, U, true>(g, w, k, q);
-    }
+                for (int i = 0; i < V; ++i) y[i] = (T)back_result<V, A>(c, m, i, xh[i], dz[i]);
+                put((T*)p.out + position<true>(w, n), y);
+            },
+            [&](int u, int n) {
+                r[u] = take(x + position<true>(w, n));
+                q[u] = take(g + position<true>(w, n));
+            });
     long long at = w.at + (long long)w.full * w.step;
-    for (k = 0; k < w.part; ++k, at += w.step)
+    for (int k = 0; k < w.part; ++k, at += w.step)
 #pragma unroll
         for (int i = 0; i < V - 1; ++i)
             if (i < w.n) {
-                float xh, dz;
-                back_value<V, A>(c, i, (float)x[at + i], (float)g[at + i], p.act, xh, dz);
-                ((T*)p.out)[at + i] = (T)back_result<V, A>(c, m, i, xh, dz);
+                const float xs[1] = {(float)x[at + i]}, gs[1] = {(float)g[at + i]};
+                float xh[1], dz[1];
+                back_values<V, A, 1>(c, i, xs, gs, p.act, xh, dz);
+                ((T*)p.out)[at + i] = (T)back_result<V, A>(c, m, i, xh[0], dz[0]);
             }
 }
 
-constexpr int kBackAhead = 4;  // vectors of x and of g
+constexpr int kBackAhead = 2;  // vectors of x and of g
 
-// LDS: a step's rows, then the columns' sums.
-__host__ __device__ __forceinline__ int step_values(const GroupLayout& l) { return l.reps * (l.pitch + 1); }
+// LDS: a step's numbers, then the columns' sums.
+__host__ __device__ __forceinline__ int step_values(const GroupLayout& l, int v) { return v * (l.active + 1); }
 
 template <typename T, bool M>
 __global__ __launch_bounds__(kGroupThreads, 2) void k_group_back_sums(GroupArgs p) {
     constexpr int V = kVec<T>, A = M ? 1 : V, U = kBackAhead;
     extern __shared__ __align__(16) char s_step[];
     float2* const s_all = (float2*)s_step;
-    float* const s_col = (float*)(s_all + step_values(p.l));
+    float* const s_col = (float*)(s_all + step_values(p.l, V));
     const long long i = block_id<kGroupThreads>();
     if (i >= p.blocks) return;
     const Bounds s = bounds_of(p);
@@ -889,7 +944,7 @@ __global__ __launch_bounds__(kGroupThreads, 2) void k_group_back_sums(GroupArgs 
         fetch<T, U, false>((const T*)p.g, w, 0, g);
         BackSums<V> v = {};
         back_sum_from<T, A, U>(p, back_columns<T, M>(p, a, t, f, b), w, 0, x, g, v);
-        add_columns<V>(p, a, t, v, s_all, s_col);
+        add_columns<V>(p, a, v, s_all, s_col);
         if (p.cols)
             for (int c = threadIdx.x; c < wide; c += blockDim.x) {
                 cols[c] = s_col[c];
@@ -900,25 +955,46 @@ __global__ __launch_bounds__(kGroupThreads, 2) void k_group_back_sums(GroupArgs 
     }
 }
 
-// Four columns of the places' sums of dz xh and dz by one workgroup.
-template <typename T>
+// 4 N columns of the places' sums of dz xh and dz by one workgroup, four neighbours a thread.
+template <typename T, int N>
 __device__ __forceinline__ void back_columns_sum(const GroupArgs& p, long long at, double* s_sum) {
-    const int c4 = threadIdx.x & 3, threads = blockDim.x / 4;
-    const long long cols = 2LL * p.channels, c = at * 4 + c4;
-    double sum = 0.0;
-    if (c < cols)
-#pragma unroll 8
-        for (long long i = threadIdx.x >> 2; i < p.places; i += threads) sum += (double)p.cols[i * cols + c];
+    constexpr int U = 4;
+    const int cn = threadIdx.x & (N - 1), threads = blockDim.x / N;
+    const long long cols = 2LL * p.channels, c = (at * N + cn) * 4;
+    const int n = (int)(cols - c < 4 ? cols - c : 4);
+    double sum[4] = {0.0, 0.0, 0.0, 0.0};
+    if (n > 0)
+        for (long long i = threadIdx.x / N; i < p.places; i += U * threads) {
+            float v[U][4];
 #pragma unroll
-    for (int d = 4; d < 64; d <<= 1) sum += __shfl_xor(sum, d, 64);
-    if ((threadIdx.x & 63) < 4) s_sum[threadIdx.x >> 6 << 2 | c4] = sum;
+            for (int u = 0; u < U; ++u) {
+                const float* from = p.cols + (i + u * threads < p.places ? i + u * threads : p.places - 1) * cols + c;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) v[u][k] = from[k < n ? k : 0];
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (i + u * threads < p.places)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) sum[k] += (double)v[u][k];
+        }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+#pragma unroll
+        for (int d = N; d < 64; d <<= 1) sum[k] += __shfl_xor(sum[k], d, 64);
+        if ((threadIdx.x & 63) < N) s_sum[((threadIdx.x >> 6) * N + cn) * 4 + k] = sum[k];
+    }
     __syncthreads();
-    if (threadIdx.x >= 4 || c >= cols) return;
-    sum = 0.0;
-    for (int w = 0; w < (int)blockDim.x / 64; ++w) sum += s_sum[w << 2 | c4];
-    T* const to = (T*)(c < p.channels ? p.dgamma : p.dbeta);
-    if (to) to[c < p.channels ? c : c - p.channels] = (T)(float)sum;
+    if (threadIdx.x >= N * 4) return;
+    const long long out = at * N * 4 + threadIdx.x;
+    if (out >= cols) return;
+    double all = 0.0;
+    for (int w = 0; w < (int)blockDim.x / 64; ++w) all += s_sum[w * N * 4 + threadIdx.x];
+    T* const to = (T*)(out < p.channels ? p.dgamma : p.dbeta);
+    if (to) to[out < p.channels ? out : out - p.channels] = (T)(float)all;
 }
+
+constexpr int kSumColumns = 16;  // (64 bytes of a place)
 
 // Workgroups past the blocks add the columns' sums.
 template <typename T, bool M>
@@ -928,7 +1004,7 @@ __global__ __launch_bounds__(kGroupThreads, 2) void k_group_back(GroupArgs p) {
     __shared__ float2 s_stat[kHereGroups];
     const long long i = block_id<kGroupThreads>();
     if (i >= p.blocks) {
-        if (blockIdx.y == 0 && p.cols && (i - p.blocks) * 4 < 2LL * p.channels) back_columns_sum<T>(p, i - p.blocks, (double*)s_two);
+        if (blockIdx.y == 0 && i - p.blocks < p.sum_blocks) back_columns_sum<T, kSumColumns / 4>(p, i - p.blocks, (double*)s_two);
         return;
     }
     const Bounds s = bounds_of(p);
@@ -943,8 +1019,8 @@ __global__ __launch_bounds__(kGroupThreads, 2) void k_group_back(GroupArgs p) {
         if (hi <= lo) continue;
         const Walk w = walk_of<V>(p, a, t, lo, hi);
         VecOf<T, V> x[U], g[U];
-        fetch<T, U, true>((const T*)p.x, w, w.full, x);
-        fetch<T, U, true>((const T*)p.g, w, w.full, g);
+        fetch<T, U, true>((const T*)p.x, w, 0, x);
+        fetch<T, U, true>((const T*)p.g, w, 0, g);
         const BackColumns<V, A> c = back_columns<T, M>(p, a, t, f, b);
         const float2* stat = (const float2*)p.stat + b * p.groups + a.j0;
         if (!p.stat) {
@@ -956,7 +1032,7 @@ __global__ __launch_bounds__(kGroupThreads, 2) void k_group_back(GroupArgs p) {
             __syncthreads();
             stat = s_stat;
         }
-        back_down<T, A, U>(p, c, means_of<T, M>(p, a, t, stat), w, 0, w.full, x, g);
+        back_down<T, A, U>(p, c, means_of<T, M>(p, a, t, stat), w, 0, x, g);
     }
 }
 
@@ -966,7 +1042,7 @@ __global__ __launch_bounds__(B, 2) void k_group_back_one(GroupArgs p) {
     constexpr int V = kVec<T>, A = M ? 1 : V;
     extern __shared__ __align__(16) char s_step[];
     float2* const s_all = (float2*)s_step;
-    float* const s_col = (float*)(s_all + step_values(p.l));
+    float* const s_col = (float*)(s_all + step_values(p.l, V));
     float2* const s_stat = s_all;  // (when the columns' sums are done)
     const long long b = block_id<B>();
     if (b >= p.batch) return;
@@ -1000,15 +1076,17 @@ __global__ __launch_bounds__(B, 2) void k_group_back_one(GroupArgs p) {
 #pragma unroll
     for (int h = 0; h < H; ++h)
         if (h < w.full) {
-#pragma unroll
-            for (int i = 0; i < V; ++i) dz[h][i] = back_add<V, A>(k, i, (float)held[h][i], (float)grad[h][i], p.act, v);
+            float xs[V], gs[V];
+            apart<T>(held[h], xs);
+            apart<T>(grad[h], gs);
+            back_add<V, A, V>(k, 0, xs, gs, p.act, v, dz[h]);
             __builtin_amdgcn_sched_barrier(0);
         }
     VecOf<T, V> more[2], more_g[2];
     fetch<T, 2, false>(x, w, H, more);
     fetch<T, 2, false>(g, w, H, more_g);
     back_sum_from<T, A, 2>(p, k, w, H, more, more_g, v);
-    add_columns<V>(p, a, t, v, s_all, s_col);
+    add_columns<V>(p, a, v, s_all, s_col);
     for (int c = threadIdx.x; c < wide; c += blockDim.x) give(c, s_col[c], s_col[wide + c]);
     if (!p.out) return;
     const double inv = 1.0 / ((double)(r.end - r.first) * p.per);
@@ -1028,10 +1106,10 @@ __global__ __launch_bounds__(B, 2) void k_group_back_one(GroupArgs p) {
             __builtin_amdgcn_sched_barrier(0);
         }
     if (w.full > H) {
-        fetch<T, 2, true>(x, w, w.full, more);
-        fetch<T, 2, true>(g, w, w.full, more_g);
+        fetch<T, 2, true>(x, w, 0, more);
+        fetch<T, 2, true>(g, w, 0, more_g);
     }
-    back_down<T, A, 2>(p, k, m, w, H, w.full, more, more_g);
+    back_down<T, A, 2>(p, k, m, w, H, more, more_g);
 }
 
 // offsets[b]: the rows whose sample index is below b, a wave a sample.
@@ -1052,7 +1130,7 @@ static int group_vec(int dtype) { return dtype == SCNN_F32 ? 4 : 8; }
 static GroupLayout group_layout(int channels, int per, int dtype, int threads, int most) {
     const int v = group_vec(dtype);
     GroupLayout l = {};
-    l.slabs = l.pieces = l.sub = 1;
+    l.slabs = l.pieces = 1;
     l.wide = channels;
     int even = 1;  // the largest power of two that both the vector and a row are a multiple of
     while (even < v && channels % (2 * even) == 0) even *= 2;
@@ -1062,7 +1140,6 @@ static GroupLayout group_layout(int channels, int per, int dtype, int threads, i
         l.active = threads / period * period;
         l.reps = (int)((long long)l.active * v / channels);
         l.tv = l.active;
-        l.pitch = channels;
     } else {
         if (channels > most) {
             if (per <= most) {
@@ -1078,9 +1155,8 @@ static GroupLayout group_layout(int channels, int per, int dtype, int threads, i
         l.tv = (l.wide + v - 1) / v;
         l.reps = l.tv >= threads ? 1 : threads / l.tv;
         l.active = l.tv * l.reps;
-        l.pitch = l.tv * v;
         l.merged = l.pieces > 1 || per % v == 0;
-        while (l.sub < v && per % (2 * l.sub) == 0) l.sub *= 2;
+        while (1 << l.sub < v && per % (2 << l.sub) == 0) ++l.sub;
     }
     l.inv_tv = 1.0f / (float)l.tv;
     l.inv_per = 1.0f / (float)per;
@@ -1090,11 +1166,9 @@ static GroupLayout group_layout(int channels, int per, int dtype, int threads, i
 }
 static unsigned group_threads(const GroupLayout& l) { return (unsigned)((l.active + 63) / 64 * 64); }
 // Bytes of LDS: pairs in fp64 for `sub` neighbours (and a group's statistics), pairs in fp32 and the columns' sums.
-static unsigned sums_lds(const GroupLayout& l, int v) {
-    return (unsigned)(l.reps * ((l.flat ? l.pitch : l.pitch / (l.merged ? v : l.sub)) + 1) * 16);
-}
+static unsigned sums_lds(const GroupLayout& l, int v) { return (unsigned)((l.merged ? 1 : v >> l.sub) * (l.active + 1) * 16); }
 static unsigned one_lds(const GroupLayout& l, int v, int per) { return sums_lds(l, v) + (unsigned)(l.wide / per) * 16; }
-static unsigned back_lds(const GroupLayout& l) { return (unsigned)(step_values(l) + l.wide) * 8; }
+static unsigned back_lds(const GroupLayout& l, int v) { return (unsigned)(step_values(l, v) + l.wide) * 8; }
 
 // Rows of a block: two workgroups of 256 threads a compute unit (what a workgroup does before and after its rows costs all its waves
 // as much as some vectors each), but no fewer than two vectors a thread.
@@ -1214,7 +1288,7 @@ template <typename T, bool M>
 static hipError_t group_bwd(int dtype, const GroupCall& c, const GroupArgs& p, const GroupSpace& at, hipStream_t s) {
     constexpr int V = kVec<T>;
     const dim3 threads(group_threads(p.l));
-    const unsigned lds = back_lds(p.l);
+    const unsigned lds = back_lds(p.l, V);
     hipError_t e;
     if (at.one) {
         if (at.threads == kOneFew) hipLaunchKernelGGL((k_group_back_one<T, M, kOneFew, 32 / V>), grid_of<kOneFew>(c.batch, p.l.slabs), threads, lds, s, p);
@@ -1225,8 +1299,9 @@ static hipError_t group_bwd(int dtype, const GroupCall& c, const GroupArgs& p, c
         hipLaunchKernelGGL((k_group_back_sums<T, M>), grid_of<kGroupThreads>(p.blocks, p.l.slabs), threads, lds, s, p);
         if (p.out) {
             if (p.stat) group_join<T, true>(p, s);
-            const long long more = p.cols ? (2LL * p.channels + 3) / 4 : 0;
-            hipLaunchKernelGGL((k_group_back<T, M>), grid_of<kGroupThreads>(p.blocks + more, p.l.slabs), threads, 0, s, p);
+            GroupArgs b = p;
+            b.sum_blocks = p.cols ? (2LL * p.channels + kSumColumns - 1) / kSumColumns : 0;
+            hipLaunchKernelGGL((k_group_back<T, M>), grid_of<kGroupThreads>(p.blocks + b.sum_blocks, p.l.slabs), threads, 0, s, b);
             return hipGetLastError();
         }
         e = hipGetLastError();
