@@ -185,16 +185,19 @@ __device__ __forceinline__ void finish(const Int8Args& p, long long m, long long
     }
 }
 
-// BM x BN outputs a workgroup; a step is 128 bytes of every row, copied from memory to LDS in a ring of STAGES without passing
-// through registers.  Rows of a step are eight pieces of 16 bytes; piece c of row r lies at place c ^ (r % 8), so that the lanes of a
-// read meet different banks (the copy puts pieces down in the order of the lanes, whose addresses carry the permutation).  Rows past
-// the arrays' ends are read from the last one, what they add up to is not stored; a row that ends in the middle of a step has
-// its first half copied twice and multiplied once.  The operands swap places at the instruction: its rows are the tile's
+// BM x BN outputs a workgroup; a step is 128 bytes of every row, copied from memory to LDS without passing through registers, the
+// next step's while this one's is multiplied.  (Steps of 64 bytes in three, four and five places: 3 to 12 per cent longer.)  Rows of a step are pieces of 16 bytes; piece c of row r lies at place c ^ spread(r), so that the lanes of a read
+// meet different banks (the copy puts pieces down in the order of the lanes, whose addresses carry the permutation).  Rows past the
+// arrays' ends are read from the last one, what they add up to is not stored; a row that ends in the middle of a step
+// has its first half copied twice and multiplied once.  The operands swap places at the instruction: its rows are the tile's
 // columns n, in pairs of blocks (block b of a pair takes columns 8 (i / 4) + 4 b + i % 4, i < 16), so that a lane ends with
 // eight neighbouring columns of one row.
-template <typename T, int BM, int BN, int WM, int WN, int STAGES>
+template <bool PAIR>
+__device__ __forceinline__ int spread(int r) { return PAIR ? (r & 3) | ((r >> 1) & 4) : r & 7; }  // (eight lanes read rows 0 to 7, PAIR: 0 to 3 and 8 to 11)
+
+template <typename T, int BM, int BN, int WM, int WN>
 __global__ __launch_bounds__(64 * WM * WN) void k_int8_ring(Int8Args p) {
-    constexpr int NT = 64 * WM * WN, A8 = BM * 8, B8 = BN * 8, AN = A8 / NT, BN8 = B8 / NT, SLOT = (A8 + B8) * 16, COPIES = AN + BN8;
+    constexpr int P = 8, NT = 64 * WM * WN, A8 = BM * P, B8 = BN * P, AN = A8 / NT, BN8 = B8 / NT, SLOT = (A8 + B8) * 16;
     constexpr int TM = BM / WM / 16, TN = BN / WN / 16;
     static_assert(A8 % NT == 0 && B8 % NT == 0 && TN % 2 == 0, "whole pieces a thread, pairs of blocks");
     extern __shared__ __align__(1024) char s_ring[];
@@ -213,30 +216,26 @@ __global__ __launch_bounds__(64 * WM * WN) void k_int8_ring(Int8Args p) {
     const unsigned ring = (unsigned)(size_t)(__attribute__((address_space(3))) char*)s_ring;
 
     // this thread's pieces: byte offsets from the tile's first value at the step's first k
-    auto offset_of = [&](int e, long long first, long long end) -> unsigned {
-        const int r = e >> 3, c = (e & 7) ^ (r & 7);
+    auto piece_a = [&](int e) { return (e % P) ^ spread<false>(e / P); };
+    auto piece_b = [&](int e) { return (e % P) ^ spread<true>(e / P); };
+    auto offset_of = [&](int r, int c, long long first, long long end) -> unsigned {
         const long long row = first + r < end ? r : end - 1 - first;
         return (unsigned)(row * p.width + c * 16);
     };
     unsigned at_a[AN], at_b[BN8];
 #pragma unroll
-    for (int i = 0; i < AN; ++i) at_a[i] = offset_of(i * NT + tid, m0, m_end);
+    for (int i = 0; i < AN; ++i) at_a[i] = offset_of((i * NT + tid) / P, piece_a(i * NT + tid), m0, m_end);
 #pragma unroll
-    for (int i = 0; i < BN8; ++i) at_b[i] = offset_of(i * NT + tid, n0, p.n);
+    for (int i = 0; i < BN8; ++i) at_b[i] = offset_of((i * NT + tid) / P, piece_b(i * NT + tid), n0, p.n);
     const signed char *base_a = p.x + m0 * p.width + k_first, *base_b = p.w + n0 * p.width + k_first;
-    // (piece 4 to 7 of the last step, where the row has none: 64 bytes back)
+    // (half: pieces 4 to 7 of the last step, where the row has none: 64 bytes back)
     auto copy_step = [&](int slot, bool half) {
         const unsigned to = ring + slot * SLOT + wave * 1024;
 #pragma unroll
-        for (int i = 0; i < AN; ++i) {
-            const int e = i * NT + tid, c = (e & 7) ^ ((e >> 3) & 7);
-            copy_to_lds(base_a, at_a[i] - (half && c >= 4 ? 64u : 0u), to + i * NT * 16);
-        }
+        for (int i = 0; i < AN; ++i) copy_to_lds(base_a, at_a[i] - (half && piece_a(i * NT + tid) >= 4 ? 64u : 0u), to + i * NT * 16);
 #pragma unroll
-        for (int i = 0; i < BN8; ++i) {
-            const int e = i * NT + tid, c = (e & 7) ^ ((e >> 3) & 7);
-            copy_to_lds(base_b, at_b[i] - (half && c >= 4 ? 64u : 0u), to + A8 * 16 + i * NT * 16);
-        }
+        for (int i = 0; i < BN8; ++i)
+            copy_to_lds(base_b, at_b[i] - (half && piece_b(i * NT + tid) >= 4 ? 64u : 0u), to + A8 * 16 + i * NT * 16);
         base_a += 128;
         base_b += 128;
     };
@@ -250,12 +249,12 @@ __global__ __launch_bounds__(64 * WM * WN) void k_int8_ring(Int8Args p) {
 #pragma unroll
         for (int j = 0; j < TN; ++j) {
             const int r = wn + (j & ~1) * 16 + 8 * (i16 >> 2) + 4 * (j & 1) + (i16 & 3);
-            fb[j] = *(const i4*)(sb + (r * 8 + ((kk * 4 + q) ^ (r & 7))) * 16);
+            fb[j] = *(const i4*)(sb + (r * P + ((kk * 4 + q) ^ spread<true>(r))) * 16);
         }
 #pragma unroll
         for (int i = 0; i < TM; ++i) {
             const int r = wm + i * 16 + i16;
-            fa[i] = *(const i4*)(sa + (r * 8 + ((kk * 4 + q) ^ (r & 7))) * 16);
+            fa[i] = *(const i4*)(sa + (r * P + ((kk * 4 + q) ^ spread<false>(r))) * 16);
         }
         __builtin_amdgcn_s_setprio(1);  // (a wave that multiplies goes before those that fetch)
 #pragma unroll
@@ -265,19 +264,14 @@ __global__ __launch_bounds__(64 * WM * WN) void k_int8_ring(Int8Args p) {
         __builtin_amdgcn_s_setprio(0);
     };
     const bool odd = (bytes & 127) != 0;
-#pragma unroll
-    for (int i = 0; i < STAGES - 1; ++i)
-        if (i < steps) copy_step(i, odd && i == steps - 1);
-    int slot = 0;
+    copy_step(0, odd && steps == 1);
     for (int step = 0; step < steps; ++step) {
-        // this step's copies have landed; its predecessor has been read by all waves, so that its slot can be filled
-        if (step + STAGES - 1 <= steps) copies_and_barrier<(STAGES - 2) * COPIES>();
-        else copies_and_barrier<0>();
-        if (step + STAGES - 1 < steps) copy_step(slot == 0 ? STAGES - 1 : slot - 1, odd && step + STAGES == steps);
-        const char* const s = s_ring + slot * SLOT;
+        // this step's copies have landed; its predecessor has been read by all waves, so that its place can be filled
+        copies_and_barrier<0>();
+        if (step + 1 < steps) copy_step((step + 1) & 1, odd && step + 2 == steps);
+        const char* const s = s_ring + (step & 1) * SLOT;
         multiply(s, s + A8 * 16, 0);
         if (!odd || step + 1 < steps) multiply(s, s + A8 * 16, 1);
-        slot = slot == STAGES - 1 ? 0 : slot + 1;
     }
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
@@ -432,16 +426,23 @@ __global__ __launch_bounds__(kRowThreads) void k_int8_row(Int8Args p, const T* _
 #pragma unroll
     for (int u = 0; u < U; ++u) fetch(u, (u * 64 + lane) * 16);
     Quantizer z = {0.0f, 0.0f};
+    constexpr int H = 2;  // vectors of the row that a thread keeps between the two looks at them
+    VecOf<T, V> mine[H];
+    auto value = [&](int c) { return load_raw<T>(x + c, c < c_in ? c_in - c : 0, c_in >= V); };
     if constexpr (!GIVEN) {
         unsigned most = 0;
-        for (int c = threadIdx.x * V; c < c_in; c += P * V) {
-            const VecOf<T, V> v = load_raw<T>(x + c, c_in - c, c_in >= V);
+        auto look = [&](const VecOf<T, V>& v) {
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 const unsigned a = magnitude((float)v[i]);
                 most = a > most ? a : most;
             }
-        }
+        };
+#pragma unroll
+        for (int h = 0; h < H; ++h) mine[h] = value((h * P + threadIdx.x) * V);
+#pragma unroll
+        for (int h = 0; h < H; ++h) look(mine[h]);
+        for (int c = (H * P + threadIdx.x) * V; c < c_in; c += P * V) look(value(c));
         most = wave_most(most);
         if (lane == 0) s_most[wave] = most;
         __syncthreads();
@@ -461,14 +462,18 @@ __global__ __launch_bounds__(kRowThreads) void k_int8_row(Int8Args p, const T* _
             for (int c = threadIdx.x * 16; c < part; c += P * 16) *(i4*)(s_x + c) = *(const i4*)(p.x + k0 + c);
         } else {
             typedef signed char Q __attribute__((ext_vector_type(V)));
-            for (int c = threadIdx.x * V; c < part; c += P * V) {
-                const int n = c_in - k0 - c;
-                const VecOf<T, V> v = load_raw<T>(x + k0 + c, n > 0 ? n : 0, c_in >= V);
+            auto keep = [&](int c, const VecOf<T, V>& v) {
                 Q b;
 #pragma unroll
                 for (int i = 0; i < V; ++i) b[i] = (signed char)quantized((float)v[i], z);
                 *(Q*)(s_x + c) = b;
-            }
+            };
+            static_assert(H * P * V <= kRowLds, "the vectors that are kept are of the first part");
+            if (k0 == 0)
+#pragma unroll
+                for (int h = 0; h < H; ++h)
+                    if ((h * P + (int)threadIdx.x) * V < part) keep((h * P + threadIdx.x) * V, mine[h]);
+            for (int c = (k0 == 0 ? H * P + threadIdx.x : threadIdx.x) * V; c < part; c += P * V) keep(c, value(k0 + c));
         }
         __syncthreads();
         for (int k = lane * 16; k < part; k += U * 1024) {
@@ -534,7 +539,16 @@ hipError_t launch_quantize_weight(int dtype, const void* w, long long c_in, long
     }
 }
 
-enum class Int8Kind { kRow, kSkinny, kRing256, kRing128, kRing64x128, kRing64 };
+// Kernel of a product: one row, up to 32 rows straight from memory, or tiles of 256, 128 or 64 squared.  bf16 with silu and residual,
+// us, of 256 / 128 / 64 / (64 x 128, left out) tiles, and of up to 32 rows by k_int8_skinny / tiles of 64:
+//   8192 x 4096 x 4096 (m, k, n)  168 / 184 / 229 / 205     4096 x 4096 x 4096   84 / 98 / 131 / 114
+//   6000 x 4096 x 4096  149 / 130 / 170 / 145 (384 tiles of 256 on 256 units)    2048 x 2048 x 2048   39 / 23.3 / 19.4 / 19.2
+//   8192 x 1024 x 1024   44 / 25.4 / 27.9 / 28.2 (512 of 128)                    5000 x 1000 x 1304   41 / 23.8 / 22.2 / 25.7 (440)
+//   1000 x 12288 x 1000  44 / 37 / 43 / 45 (k split four ways, 64: twice)        1024 x 1024 x 1024   21 / 12.5 / 9.3 / 11.3
+//   200000 x 64 x 64     93 / 51 / 24 / 39      300 x 300 x 3000   27 / 14.7 / 6.6 / 9.4      100 x 4096 x 4096   17.9 / 14.7 / 12.5 / 13.1
+// The largest where their rounds over the units are 95 per cent full, 128 from two a unit on with k to hide their start and end, or where
+// k is long.  k is split where workgroups are few, down to 1024 bytes of it: one a unit (tiles of 64: two).
+enum class Int8Kind { kRow, kSkinny, kRing256, kRing128, kRing64 };
 struct Int8Plan {
     Int8Kind kind;
     int bm, bn, splits;
@@ -545,22 +559,20 @@ static Int8Plan int8_plan(long long m, long long n, long long width) {
     if (m <= 1) return t;
     const long long cus = device_cu_count();
     auto tiles = [&](long long bm, long long bn) { return ((m + bm - 1) / bm) * ((n + bn - 1) / bn); };
-    long long least = 512;  // bytes of k that a workgroup of a split has at least
-    if (m <= 64) {
+    long long want = cus;  // workgroups
+    if (m <= 32) {
         t.kind = Int8Kind::kSkinny;
-        t.bm = m <= 16 ? 16 : (m <= 32 ? 32 : 64);
-        t.bn = m <= 32 ? 16 : 32;
-        least = 1024;
+        t.bm = m <= 16 ? 16 : 32;
+        t.bn = 16;
     } else {
-        const long long largest = tiles(256, 256), rounds = (largest + cus - 1) / cus;
-        if (m > 128 && n > 128 && rounds >= 2 && 20 * largest >= 19 * rounds * cus) t.kind = Int8Kind::kRing256, t.bm = t.bn = 256;
-        else if (n > 64 && 4 * tiles(128, 128) >= 5 * cus) t.kind = Int8Kind::kRing128, t.bm = t.bn = 128;
-        else if (n > 64 && tiles(64, 128) >= cus) t.kind = Int8Kind::kRing64x128, t.bm = 64, t.bn = 128;
-        else t.kind = Int8Kind::kRing64, t.bm = t.bn = 64;
+        const long long largest = tiles(256, 256), rounds = (largest + cus - 1) / cus, large = tiles(128, 128);
+        if (width >= 2048 && 20 * largest >= 19 * rounds * cus) t.kind = Int8Kind::kRing256, t.bm = t.bn = 256;
+        else if ((width >= 1024 && large >= 2 * cus) || (width >= 8192 && 4 * large >= cus && m > 64)) t.kind = Int8Kind::kRing128, t.bm = t.bn = 128;
+        else t.kind = Int8Kind::kRing64, t.bm = t.bn = 64, want = 2 * cus;
     }
     const long long all = tiles(t.bm, t.bn);
-    if (all < cus) {
-        long long s = cus / all, most = width / least;
+    if (all < want) {
+        long long s = want / all, most = width / 1024;
         if (s > most) s = most;
         if (s > 1) t.k_split = round_up((width + s - 1) / s, t.kind == Int8Kind::kSkinny ? 512 : 128);
     }
@@ -584,10 +596,10 @@ size_t linear_int8_bytes(int dtype, bool given, long long rows, long long c_in, 
     return int8_space(given, rows, c_in, c_out).total;
 }
 
-template <typename T, int BM, int BN, int WM, int WN, int STAGES>
+template <typename T, int BM, int BN, int WM, int WN>
 static hipError_t ring(const Int8Args& p, long long tiles, int splits, hipStream_t s) {
-    constexpr int lds = (BM + BN) * 128 * STAGES;
-    auto kernel = k_int8_ring<T, BM, BN, WM, WN, STAGES>;
+    constexpr int lds = (BM + BN) * 256;
+    auto kernel = k_int8_ring<T, BM, BN, WM, WN>;
     if (lds >= 65536) {
         const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
         if (e != hipSuccess) return e;
@@ -638,15 +650,13 @@ static hipError_t linear_int8(int dtype, const Int8Call& c, hipStream_t s) {
         case Int8Kind::kSkinny: {
             const dim3 grid = grid_of<512>(tiles, (unsigned)t.splits);
             if (t.bm == 16) hipLaunchKernelGGL((k_int8_skinny<T, 1, 1>), grid, dim3(512), 0, s, p);
-            else if (t.bm == 32) hipLaunchKernelGGL((k_int8_skinny<T, 2, 1>), grid, dim3(512), 0, s, p);
-            else hipLaunchKernelGGL((k_int8_skinny<T, 4, 2>), grid, dim3(512), 0, s, p);
+            else hipLaunchKernelGGL((k_int8_skinny<T, 2, 1>), grid, dim3(512), 0, s, p);
             e = hipGetLastError();
             break;
         }
-        case Int8Kind::kRing256: e = ring<T, 256, 256, 2, 4, 2>(p, tiles, t.splits, s); break;
-        case Int8Kind::kRing128: e = ring<T, 128, 128, 2, 2, 2>(p, tiles, t.splits, s); break;
-        case Int8Kind::kRing64x128: e = ring<T, 64, 128, 2, 2, 3>(p, tiles, t.splits, s); break;
-        default: e = ring<T, 64, 64, 2, 2, 2>(p, tiles, t.splits, s);
+        case Int8Kind::kRing256: e = ring<T, 256, 256, 2, 4>(p, tiles, t.splits, s); break;
+        case Int8Kind::kRing128: e = ring<T, 128, 128, 2, 2>(p, tiles, t.splits, s); break;
+        default: e = ring<T, 64, 64, 2, 2>(p, tiles, t.splits, s);
     }
     if (e != hipSuccess || t.splits <= 1) return e;
     hipLaunchKernelGGL((k_int8_join<T>), grid_of<256>((p.m * ((p.n + 3) / 4) + 255) / 256), dim3(256), 0, s, p, t.splits);
