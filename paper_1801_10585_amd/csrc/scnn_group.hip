@@ -1171,8 +1171,9 @@ static unsigned one_lds(const GroupLayout& l, int v, int per) { return sums_lds(
 static unsigned back_lds(const GroupLayout& l, int v) { return (unsigned)(step_values(l, v) + l.wide) * 8; }
 
 // Rows of a block: two workgroups of 256 threads a compute unit (what a workgroup does before and after its rows costs all its waves
-// as much as some vectors each), but no fewer than two vectors a thread.
+// as much as some vectors each), but no fewer than two vectors a thread; one where that makes no more than a workgroup a unit.
 static long long group_chunk(const GroupLayout& l, long long rows) {
+    if ((rows + l.reps - 1) / l.reps * l.slabs <= device_cu_count()) return l.reps;
     long long want = 2LL * device_cu_count() / l.slabs;
     if (want < 1) want = 1;
     long long chunk = (rows + want - 1) / want;

@@ -506,7 +506,8 @@ static hipError_t quantize(const void* x, long long rows, const long long* rows_
 #define F(P, H)                                                                                                           \
     hipLaunchKernelGGL((k_quantize_rows<T, P, H>), (grid_of<P < 256 ? 256 : P>((rows + (P < 256 ? 256 / P : 1) - 1) / (P < 256 ? 256 / P : 1))), \
                        dim3(P < 256 ? 256 : P), 0, s, (const T*)x, rows, rows_dev, channels, width, q, scale)
-    if (units <= 32) F(16, 2);
+    if (units <= 8) F(4, 2);
+    else if (units <= 32) F(16, 2);
     else if (units <= 128) F(64, 2);
     else if (units <= 512 || rows >= 4LL * device_cu_count()) F(256, 2);
     else F(1024, 2);
