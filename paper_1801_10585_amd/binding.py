@@ -742,8 +742,8 @@ def sample_offsets(coords, batch, *, rows_dev=None, out=None, stream=None):
     if not coords.is_cuda or coords.dtype != torch.int32 or coords.dim() != 2:
         raise ValueError("coords must be an int32 [rows, 1 + ndim] tensor on the GPU")
     batch = int(batch)
-    if batch < 1:
-        raise ValueError("batch must be positive")
+    if not 1 <= batch < 1 << 31:
+        raise ValueError("batch must be from 1 to 2^31 - 1")
     rows_dev = _rows_dev(rows_dev, coords)
     with _on(coords.device, stream, (coords, rows_dev, out)):
         coords = coords.contiguous()
@@ -780,14 +780,13 @@ def group_norm_fwd(x, groups, gamma=None, beta=None, *, offsets=None, batch=None
     _same(gamma, x, (ch,), "gamma")
     _same(beta, x, (ch,), "beta")
     code = _activation(act)
-    need = _need(x.device.index, "group_norm_fwd_workspace", dt, rows, batch, ch, groups)
     y, mean, rstd = out if out is not None else (None, None, None)
     with _on(x.device, stream, (x, gamma, beta, offsets, y, mean, rstd, workspace)):
         x, gamma, beta, offsets = x.contiguous(), _cont(gamma), _cont(beta), _cont(offsets)
         y = _result(y, x, (rows, ch), "out")
         mean = _result(mean, x, (batch, groups), "mean", torch.float32)
         rstd = _result(rstd, mean, (batch, groups), "rstd")
-        workspace = _scratch(workspace, need, x)
+        workspace = _scratch(workspace, _need(x.device.index, "group_norm_fwd_workspace", dt, rows, batch, ch, groups), x)
         _check(L, L.group_norm_fwd(dt, _at(x), rows, _at(offsets), batch, ch, groups, _at(gamma), _at(beta), float(eps), code,
                                    _at(y), _at(mean), _at(rstd), _at(workspace), _bytes(workspace), _current()))
     return y, mean, rstd
@@ -804,6 +803,8 @@ def group_norm_bwd(x, g, groups, gamma, beta, mean, rstd, *, offsets=None, act="
     in.  Rows outside the samples stay as they are in dx."""
     L = load_library()
     dt, rows, ch = _rows_of(x, "x")
+    if mean.dim() != 2:
+        raise ValueError("mean must be [batch, groups]")
     batch, groups = _samples(offsets, mean.shape[0], x), int(groups)
     _same(g, x, (rows, ch), "g")
     _same(gamma, x, (ch,), "gamma")
@@ -811,7 +812,6 @@ def group_norm_bwd(x, g, groups, gamma, beta, mean, rstd, *, offsets=None, act="
     _same(mean, x, (batch, groups), "mean", torch.float32)
     _same(rstd, x, (batch, groups), "rstd", torch.float32)
     code = _activation(act)
-    need = _need(x.device.index, "group_norm_bwd_workspace", dt, rows, batch, ch, groups)
     dx, dgamma, dbeta = out if out is not None else (None, None, None)
     with _on(x.device, stream, (x, g, gamma, beta, mean, rstd, offsets, dx, dgamma, dbeta, workspace)):
         x, g, gamma, beta, mean, rstd, offsets = (x.contiguous(), g.contiguous(), _cont(gamma), _cont(beta), mean.contiguous(),
@@ -819,7 +819,7 @@ def group_norm_bwd(x, g, groups, gamma, beta, mean, rstd, *, offsets=None, act="
         dx = _result(dx, x, (rows, ch), "dx") if want[0] else None
         dgamma = _result(dgamma, x, (ch,), "dgamma") if want[1] else None
         dbeta = _result(dbeta, x, (ch,), "dbeta") if want[2] else None
-        workspace = _scratch(workspace, need, x)
+        workspace = _scratch(workspace, _need(x.device.index, "group_norm_bwd_workspace", dt, rows, batch, ch, groups), x)
         _check(L, L.group_norm_bwd(dt, _at(x), _at(g), rows, _at(offsets), batch, ch, groups, _at(gamma), _at(beta), _at(mean),
                                    _at(rstd), code, _at(dx), _at(dgamma), _at(dbeta), _at(workspace), _bytes(workspace),
                                    _current()))
@@ -929,6 +929,8 @@ def linear_int8_fwd(x, w, w_scale, bias=None, *, x_scale=None, act="none", resid
         raise ValueError("dtype must be float32, bfloat16 or float16")
     if x.dtype != (torch.int8 if given else dtype):
         raise ValueError("x must be int8 where x_scale is given" if given else f"x must be {dtype}, or int8 with x_scale")
+    if w.dim() != 2:
+        raise ValueError("w must be [c_out, int8_row_bytes(c_in)]")
     dt, (rows, c_in), c_out = DTYPES[dtype], x.shape, w.shape[0]
     _same(w, x, (c_out, int8_row_bytes(c_in)), "w", torch.int8)
     if given and c_in != w.shape[1]:
@@ -939,12 +941,11 @@ def linear_int8_fwd(x, w, w_scale, bias=None, *, x_scale=None, act="none", resid
     _same(residual, x, (rows, c_out), "residual", dtype)
     code = _activation(act)
     rows_dev = _rows_dev(rows_dev, x)
-    need = _need(x.device.index, "linear_int8_fwd_workspace", dt, int(given), rows, c_in, c_out)
     with _on(x.device, stream, (x, x_scale, w, w_scale, bias, residual, rows_dev, out, workspace)):
         x, w, w_scale, x_scale, bias, residual = (x.contiguous(), w.contiguous(), w_scale.contiguous(), _cont(x_scale),
                                                   _cont(bias), _cont(residual))
         out = _result(out, x, (rows, c_out), "out", dtype)
-        workspace = _scratch(workspace, need, x)
+        workspace = _scratch(workspace, _need(x.device.index, "linear_int8_fwd_workspace", dt, int(given), rows, c_in, c_out), x)
         _check(L, L.linear_int8_fwd(dt, _at(x), _at(x_scale), rows, _at(rows_dev), c_in, _at(w), _at(w_scale), _at(bias), c_out,
                                     code, _at(residual), _at(out), _at(workspace), _bytes(workspace), _current()))
     return out

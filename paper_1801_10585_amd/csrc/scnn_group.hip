@@ -1182,9 +1182,11 @@ static long long group_chunk(const GroupLayout& l, long long rows) {
 }
 
 // A workgroup a sample and slab, its values in registers: 16384 of them, in 256 threads, or in 512 where workgroups are few; samples of
-// up to twice that on the average.
+// up to twice that on the average.  Only the device knows how unequal the samples are, and one that holds all values of a call keeps its
+// workgroup for 0.3 us a thousand: calls of up to 2^24 values.  us of this / of blocks of rows, us in a graph: backward 64 samples of
+// 512 x 256 bf16 20 / 39, forward 512 x 24 fp32 7.5 / 14.
 constexpr int kOneFew = 512, kOneMany = 256;
-constexpr long long kOneHeld = 16384;
+constexpr long long kOneHeld = 16384, kOneAll = 1LL << 24;
 static bool group_one(long long rows, long long batch, int channels, int per, int dtype, GroupLayout& l, int& threads) {
     const int v = group_vec(dtype), least = 64 / (16 / v);  // (64 bytes of a row)
     const long long values = rows * channels / batch, cus = device_cu_count();
@@ -1201,7 +1203,7 @@ static bool group_one(long long rows, long long batch, int channels, int per, in
             if (wide < most) most = (int)wide;
         }
     }
-    if (rows * (channels < most ? channels : most) > 2 * kOneHeld * batch) return false;
+    if (rows * channels > kOneAll || rows * (channels < most ? channels : most) > 2 * kOneHeld * batch) return false;
     threads = kOneFew;
     l = group_layout(channels, per, dtype, threads, most);
     if (batch * l.slabs >= cus || one_lds(l, v, per) > 60000) {
