@@ -32,7 +32,7 @@ constexpr int kHereGroups = 64;     // most groups of a slab whose sums a workgr
 struct GroupLayout {
     int tv, reps, active, flat;
     int wide, slabs, pieces;  // a slab is whole groups (pieces 1), or one of `pieces` pieces of a group
-    int merged;               // a vector's columns are of one group
+    int merged;               // a vector's columns are of one group, and none is cut
     int sub;                  // 2^sub neighbouring values of a vector are of one group, whatever the vector
     float inv_tv, inv_per, inv_c;
     double inv_reps;
@@ -159,37 +159,39 @@ __device__ __forceinline__ Slab slab_of(const GroupArgs& p) {
     return a;
 }
 
-// This thread's place: its row among a step's, its first column in the slab.
-struct Place { int row, col; };
+// This thread's place: its row among a step's, its first column in the slab.  A vector that the slab's end cuts is the slab's last whole
+// one instead (it may begin before the slab), of which the first `other` values are another thread's: read, but neither
+// added nor written.  (Cut vectors taken value by value behind the others: forward 60000 x 517 bf16 in 11 groups WAS us.)
+struct Place { int row, col, other; };
 template <int V>
-__device__ __forceinline__ Place place_of(const GroupArgs& p) {
+__device__ __forceinline__ Place place_of(const GroupArgs& p, const Slab& a) {
     const int t = threadIdx.x;
-    if (p.l.flat) return {0, t * V};
-    const int k = quotient(t, p.l.inv_tv);
-    return {k, (t - k * p.l.tv) * V};
+    if (p.l.flat) return {0, t * V, 0};
+    const int k = quotient(t, p.l.inv_tv), c = (t - k * p.l.tv) * V, over = c + V - (a.c1 - a.c0);
+    return over <= 0 ? Place{k, c, 0} : Place{k, c - over, over < V ? over : V};
 }
-// Column in the slab of value i of this thread.  (Values past the slab's end take its last column.)
+// Column in the slab of value i of this thread, or one of the slab's where it has none.
 __device__ __forceinline__ int column_of(const GroupArgs& p, const Slab& a, const Place& t, int i) {
     int c = t.col + i;
     if (p.l.flat) c -= quotient(c, p.l.inv_c) * p.channels;
-    return c < a.c1 - a.c0 ? c : a.c1 - a.c0 - 1;
+    return c < 0 ? 0 : (c < a.c1 - a.c0 ? c : a.c1 - a.c0 - 1);
 }
 // Group in the slab of a column of it.
 __device__ __forceinline__ int group_of(const GroupArgs& p, int column) { return p.l.pieces > 1 ? 0 : quotient(column, p.l.inv_per); }
 
-// A thread's vectors among the rows lo .. hi - 1: `full` whole ones, then `part` of n values.  All threads that have any whole one have
-// `common` of them (the same in every lane).
+// A thread's vectors among the rows lo .. hi - 1: `full` whole ones, of which all threads that have any have `common` (the same in every
+// lane); behind those of rows that run on, n values.
 struct Walk {
     long long at, step;
-    int full, part, n, common;
+    int full, n, common, other;
 };
 template <int V>
 __device__ __forceinline__ Walk walk_of(const GroupArgs& p, const Slab& a, const Place& t, long long lo, long long hi) {
-    Walk w = {0, 0, 0, 0, 0, 0};
+    Walk w = {0, 0, 0, 0, 0, t.other};
     if (hi <= lo) return w;
     const int steps = __builtin_amdgcn_readfirstlane((int)quotient(hi - lo, p.l.inv_reps));
     w.common = steps;
-    if ((int)threadIdx.x >= p.l.active) return w;
+    if ((int)threadIdx.x >= p.l.active || t.other >= V) return w;
     const int left = (int)(hi - lo - (long long)steps * p.l.reps);
     w.step = (long long)p.l.reps * p.channels;
     w.full = steps;
@@ -197,16 +199,10 @@ __device__ __forceinline__ Walk walk_of(const GroupArgs& p, const Slab& a, const
         w.at = lo * p.channels + t.col;
         const int n = left * p.channels - t.col;  // (fewer than a step's values)
         if (n >= V) ++w.full;
-        else if (n > 0) w.part = 1, w.n = n;
+        else if (n > 0) w.n = n;
     } else {
         w.at = (lo + t.row) * p.channels + a.c0 + t.col;
         if (t.row < left) ++w.full;
-        const int n = a.c1 - a.c0 - t.col;
-        if (n < V) {
-            w.part = n > 0 ? w.full : 0;
-            w.n = n;
-            w.full = 0;
-        }
     }
     return w;
 }
@@ -214,7 +210,11 @@ __device__ __forceinline__ Walk walk_of(const GroupArgs& p, const Slab& a, const
 template <typename T> using Loose = VecOf<T, kVec<T>> __attribute__((aligned(sizeof(T))));  // (at any element's address)
 template <typename T> __device__ __forceinline__ VecOf<T, kVec<T>> take(const T* p) { return *(const Loose<T>*)p; }
 // Results are not read again soon: they leave the L2 to the rows.
-template <typename T> __device__ __forceinline__ void put(T* p, VecOf<T, kVec<T>> v) { __builtin_nontemporal_store(v, (Loose<T>*)p); }
+template <typename T> __device__ __forceinline__ void put(T* p, VecOf<T, kVec<T>> v, int other) {
+    typedef unsigned __int128 u128;
+    if (other == 0) __builtin_nontemporal_store(v, (Loose<T>*)p);
+    else store_raw<T>(p + other, kVec<T> - other, __builtin_bit_cast(VecOf<T, kVec<T>>, __builtin_bit_cast(u128, v) >> (other * 8 * (int)sizeof(T))));
+}
 
 // Vector number k of a thread, counted from its first one or, DOWN, from its last one (the last ones of a block are what the L2 still
 // has when its rows are read again).
@@ -298,11 +298,12 @@ __device__ __forceinline__ void sum_from(const T* __restrict__ x, const Walk& w,
                 for (int i = 0; i < V; ++i) add_value<T, M>((float)r[u][i], i, v);
             },
             [&](int u, int n) { r[u] = take(x + position<false>(w, n)); });
-    long long at = w.at + (long long)w.full * w.step;
-    for (k = 0; k < w.part; ++k, at += w.step)
+    if (w.n) {
+        const long long at = w.at + (long long)w.full * w.step;
 #pragma unroll
         for (int i = 0; i < V - 1; ++i)
             if (i < w.n) add_value<T, M>((float)x[at + i], i, v);
+    }
 }
 
 // Lanes that add the n values of each of `groups` sums, as a power of two: no more than there are values, threads for them all, or lanes
@@ -321,24 +322,27 @@ __device__ __forceinline__ int step_at(const GroupArgs& p, int v, int sub, int r
 
 // Sums over the slab's groups of the threads' pairs, then done(group, sums) by one lane a group.  All threads of the workgroup call it.
 template <typename T, bool M, typename F>
-__device__ __forceinline__ void add_groups(const GroupArgs& p, const Slab& a, const Sums<T, M>& v, Two* s_all, F done) {
+__device__ __forceinline__ void add_groups(const GroupArgs& p, const Slab& a, const Place& t, const Sums<T, M>& v, Two* s_all, F done) {
     constexpr int V = kVec<T>;
     constexpr int VB = V == 8 ? 3 : 2;
     const int sub = M ? VB : p.l.sub, w = (a.w + (1 << sub) - 1) >> sub, next = p.l.active + 1;
-    Two* const mine = s_all + threadIdx.x;
+    Two* const mine = s_all + threadIdx.x - (t.other >> sub) * next;
     if ((int)threadIdx.x < p.l.active) {
         if constexpr (M) {
-            mine[0] = {v.one[0] + v.one[1], v.two[0] + v.two[1]};
+            s_all[threadIdx.x] = {v.one[0] + v.one[1], v.two[0] + v.two[1]};
         } else if (sub == 0) {
 #pragma unroll
-            for (int i = 0; i < V; ++i) mine[i * next] = {v.one[i], v.two[i]};
+            for (int i = 0; i < V; ++i)
+                if (i >= t.other) mine[i * next] = {v.one[i], v.two[i]};
         } else if (sub == 1) {
 #pragma unroll
-            for (int i = 0; i < V; i += 2) mine[i / 2 * next] = {v.one[i] + v.one[i + 1], v.two[i] + v.two[i + 1]};
+            for (int i = 0; i < V; i += 2)
+                if (i >= t.other) mine[i / 2 * next] = {v.one[i] + v.one[i + 1], v.two[i] + v.two[i + 1]};
         } else if constexpr (V == 8) {
 #pragma unroll
             for (int i = 0; i < V; i += 4)
-                mine[i / 4 * next] = {(v.one[i] + v.one[i + 1]) + (v.one[i + 2] + v.one[i + 3]), (v.two[i] + v.two[i + 1]) + (v.two[i + 2] + v.two[i + 3])};
+                if (i >= t.other)
+                    mine[i / 4 * next] = {(v.one[i] + v.one[i + 1]) + (v.one[i + 2] + v.one[i + 3]), (v.two[i] + v.two[i + 1]) + (v.two[i + 2] + v.two[i + 3])};
         }
     }
     __syncthreads();
@@ -423,23 +427,24 @@ __device__ __forceinline__ float forward_value(const Columns<V, A>& k, int i, fl
     return activate(__builtin_fmaf((x - k.mean[j]) - k.rest[j], k.scale[i], k.beta[i]), act);
 }
 template <typename T, int A>
-__device__ __forceinline__ void forward_vector(const GroupArgs& p, const Columns<kVec<T>, A>& k, long long at, VecOf<T, kVec<T>> r) {
+__device__ __forceinline__ void forward_vector(const GroupArgs& p, const Columns<kVec<T>, A>& k, const Walk& w, long long at, VecOf<T, kVec<T>> r) {
     VecOf<T, kVec<T>> y;
 #pragma unroll
     for (int i = 0; i < kVec<T>; ++i) y[i] = (T)forward_value<kVec<T>, A>(k, i, (float)r[i], p.act);
-    put((T*)p.out + at, y);
+    put((T*)p.out + at, y, A == 1 ? 0 : w.other);
 }
 // A thread's vectors from its last down to number `from`, of which the first U are there, and its odd values.
 template <typename T, int A, int U>
 __device__ __forceinline__ void forward_down(const GroupArgs& p, const Columns<kVec<T>, A>& c, const Walk& w, int from,
                                              VecOf<T, kVec<T>> (&r)[U]) {
-    walk<U>(w, 0, w.full - from, [&](int u, int n) { forward_vector<T, A>(p, c, position<true>(w, n), r[u]); },
+    walk<U>(w, 0, w.full - from, [&](int u, int n) { forward_vector<T, A>(p, c, w, position<true>(w, n), r[u]); },
             [&](int u, int n) { r[u] = take((const T*)p.x + position<true>(w, n)); });
-    long long at = w.at + (long long)w.full * w.step;
-    for (int k = 0; k < w.part; ++k, at += w.step)
+    if (w.n) {
+        const long long at = w.at + (long long)w.full * w.step;
 #pragma unroll
         for (int i = 0; i < kVec<T> - 1; ++i)
             if (i < w.n) ((T*)p.out)[at + i] = (T)forward_value<kVec<T>, A>(c, i, (float)((const T*)p.x)[at + i], p.act);
+    }
 }
 
 constexpr int kAhead = 4;  // vectors of x that a thread of the blocks' kernels has on their way
@@ -452,7 +457,7 @@ __global__ __launch_bounds__(kGroupThreads, 2) void k_group_sums(GroupArgs p) {
     if (i >= p.blocks) return;
     const Bounds s = bounds_of(p);
     const Slab a = slab_of(p);
-    const Place t = place_of<V>(p);
+    const Place t = place_of<V>(p, a);
     const Block k = block_of(p, s, i);
     const int to = p.l.pieces > 1 ? (int)blockIdx.y : a.j0;
     for (long long b = k.b0; b <= k.b1; ++b) {
@@ -472,7 +477,7 @@ __global__ __launch_bounds__(kGroupThreads, 2) void k_group_sums(GroupArgs p) {
         Sums<T, M> v;
         begin_sums<T, M>(near, v);
         sum_from<T, M, kAhead>((const T*)p.x, w, 0, x, v);
-        add_groups<T, M>(p, a, v, (Two*)s_step, [&](int j, Two sum) { part[j] = sum; });
+        add_groups<T, M>(p, a, t, v, (Two*)s_step, [&](int j, Two sum) { part[j] = sum; });
         if (b < k.b1) __syncthreads();
     }
 }
@@ -609,7 +614,7 @@ __global__ __launch_bounds__(kGroupThreads, 2) void k_group_apply(GroupArgs p) {
     if (i >= p.blocks) return;
     const Bounds s = bounds_of(p);
     const Slab a = slab_of(p);
-    const Place t = place_of<V>(p);
+    const Place t = place_of<V>(p, a);
     const Affine<T> f = affine_of<T>(p, a, t);
     const Joiner o = joiner_of(a);
     const Block k = block_of(p, s, i);
@@ -659,7 +664,7 @@ __global__ __launch_bounds__(B, 2) void k_group_one(GroupArgs p) {
     if (b >= p.batch) return;
     const Bounds s = {p.offsets, p.each, p.rows, p.batch, 0, p.inv_each, false};
     const Slab a = slab_of(p);
-    const Place t = place_of<V>(p);
+    const Place t = place_of<V>(p, a);
     const Rows r = rows_of_sample(s, b);
     const long long id = b * p.groups + a.j0;
     if (r.end == r.first) {
@@ -688,7 +693,7 @@ __global__ __launch_bounds__(B, 2) void k_group_one(GroupArgs p) {
     VecOf<T, V> more[2];
     fetch<T, 2, false>(x, w, H, more);
     sum_from<T, M, 2>(x, w, H, more, v);
-    add_groups<T, M>(p, a, v, s_all, [&](int j, Two sum) {
+    add_groups<T, M>(p, a, t, v, s_all, [&](int j, Two sum) {
         const GroupStat g = stat_of(near_value<T>(p, r, a.j0 + j), sum, (double)(r.end - r.first) * p.per, p.eps);
         s_stat[j] = g;
         if (p.mean) p.mean[id + j] = g.mean;
@@ -699,7 +704,7 @@ __global__ __launch_bounds__(B, 2) void k_group_one(GroupArgs p) {
 #pragma unroll
     for (int h = 0; h < H; ++h)
         if (h < w.full) {
-            forward_vector<T, A>(p, c, position<false>(w, h), held[h]);
+            forward_vector<T, A>(p, c, w, position<false>(w, h), held[h]);
             __builtin_amdgcn_sched_barrier(0);
         }
     if (w.full > H) fetch<T, 2, true>(x, w, 0, more);
@@ -793,8 +798,8 @@ __device__ __forceinline__ void back_sum_from(const GroupArgs& p, const BackColu
                 r[u] = take(x + position<false>(w, n));
                 q[u] = take(g + position<false>(w, n));
             });
-    long long at = w.at + (long long)w.full * w.step;
-    for (k = 0; k < w.part; ++k, at += w.step)
+    if (w.n) {
+        const long long at = w.at + (long long)w.full * w.step;
 #pragma unroll
         for (int i = 0; i < V - 1; ++i)
             if (i < w.n) {
@@ -802,16 +807,18 @@ __device__ __forceinline__ void back_sum_from(const GroupArgs& p, const BackColu
                 float dz[1];
                 back_add<V, A, 1>(c, i, xs, gs, p.act, v, dz);
             }
+    }
 }
 
 // Sums over a step's rows, given to s_col [2][wide].  All threads call it and meet at its end; s_all: a step's numbers, as in add_groups.
 // (Rows one behind the other, all lanes of a sum in one bank: 64 samples of 512 x 256 bf16 10 us longer.)
 template <int V>
-__device__ __forceinline__ void add_columns(const GroupArgs& p, const Slab& a, const BackSums<V>& v, float2* s_all, float* s_col) {
+__device__ __forceinline__ void add_columns(const GroupArgs& p, const Slab& a, const Place& t, const BackSums<V>& v, float2* s_all, float* s_col) {
     const int wide = a.c1 - a.c0;
     if ((int)threadIdx.x < p.l.active)
 #pragma unroll
-        for (int i = 0; i < V; ++i) s_all[i * (p.l.active + 1) + threadIdx.x] = make_float2(v.a[i], v.b[i]);
+        for (int i = 0; i < V; ++i)
+            if (i >= t.other) s_all[(i - t.other) * (p.l.active + 1) + threadIdx.x] = make_float2(v.a[i], v.b[i]);
     __syncthreads();
     const int bits = lane_bits(p.l.reps, wide), q = 1 << bits, sets = blockDim.x >> bits, in = threadIdx.x & (q - 1);
     for (int c0 = 0; c0 < wide; c0 += sets) {
@@ -890,14 +897,14 @@ __device__ __forceinline__ void back_down(const GroupArgs& p, const BackColumns<
                 back_values<V, A, V>(c, 0, xs, gs, p.act, xh, dz);
 #pragma unroll
                 for (int i = 0; i < V; ++i) y[i] = (T)back_result<V, A>(c, m, i, xh[i], dz[i]);
-                put((T*)p.out + position<true>(w, n), y);
+                put((T*)p.out + position<true>(w, n), y, A == 1 ? 0 : w.other);
             },
             [&](int u, int n) {
                 r[u] = take(x + position<true>(w, n));
                 q[u] = take(g + position<true>(w, n));
             });
-    long long at = w.at + (long long)w.full * w.step;
-    for (int k = 0; k < w.part; ++k, at += w.step)
+    if (w.n) {
+        const long long at = w.at + (long long)w.full * w.step;
 #pragma unroll
         for (int i = 0; i < V - 1; ++i)
             if (i < w.n) {
@@ -906,6 +913,7 @@ __device__ __forceinline__ void back_down(const GroupArgs& p, const BackColumns<
                 back_values<V, A, 1>(c, i, xs, gs, p.act, xh, dz);
                 ((T*)p.out)[at + i] = (T)back_result<V, A>(c, m, i, xh[0], dz[0]);
             }
+    }
 }
 
 constexpr int kBackAhead = 2;  // vectors of x and of g
@@ -923,7 +931,7 @@ __global__ __launch_bounds__(kGroupThreads, 2) void k_group_back_sums(GroupArgs 
     if (i >= p.blocks) return;
     const Bounds s = bounds_of(p);
     const Slab a = slab_of(p);
-    const Place t = place_of<V>(p);
+    const Place t = place_of<V>(p, a);
     const Affine<T> f = affine_of<T>(p, a, t);
     const Block k = block_of(p, s, i);
     const int wide = a.c1 - a.c0, to = p.l.pieces > 1 ? (int)blockIdx.y : a.j0;
@@ -944,7 +952,7 @@ __global__ __launch_bounds__(kGroupThreads, 2) void k_group_back_sums(GroupArgs 
         fetch<T, U, false>((const T*)p.g, w, 0, g);
         BackSums<V> v = {};
         back_sum_from<T, A, U>(p, back_columns<T, M>(p, a, t, f, b), w, 0, x, g, v);
-        add_columns<V>(p, a, v, s_all, s_col);
+        add_columns<V>(p, a, t, v, s_all, s_col);
         if (p.cols)
             for (int c = threadIdx.x; c < wide; c += blockDim.x) {
                 cols[c] = s_col[c];
@@ -1009,7 +1017,7 @@ __global__ __launch_bounds__(kGroupThreads, 2) void k_group_back(GroupArgs p) {
     }
     const Bounds s = bounds_of(p);
     const Slab a = slab_of(p);
-    const Place t = place_of<V>(p);
+    const Place t = place_of<V>(p, a);
     const Affine<T> f = affine_of<T>(p, a, t);
     const Joiner o = joiner_of(a);
     const Block k = block_of(p, s, i);
@@ -1048,7 +1056,7 @@ __global__ __launch_bounds__(B, 2) void k_group_back_one(GroupArgs p) {
     if (b >= p.batch) return;
     const Bounds s = {p.offsets, p.each, p.rows, p.batch, 0, p.inv_each, false};
     const Slab a = slab_of(p);
-    const Place t = place_of<V>(p);
+    const Place t = place_of<V>(p, a);
     const Rows r = rows_of_sample(s, b);
     const int wide = a.c1 - a.c0;
     auto give = [&](int c, float da, float db) {
@@ -1086,7 +1094,7 @@ __global__ __launch_bounds__(B, 2) void k_group_back_one(GroupArgs p) {
     fetch<T, 2, false>(x, w, H, more);
     fetch<T, 2, false>(g, w, H, more_g);
     back_sum_from<T, A, 2>(p, k, w, H, more, more_g, v);
-    add_columns<V>(p, a, v, s_all, s_col);
+    add_columns<V>(p, a, t, v, s_all, s_col);
     for (int c = threadIdx.x; c < wide; c += blockDim.x) give(c, s_col[c], s_col[wide + c]);
     if (!p.out) return;
     const double inv = 1.0 / ((double)(r.end - r.first) * p.per);
@@ -1102,7 +1110,7 @@ __global__ __launch_bounds__(B, 2) void k_group_back_one(GroupArgs p) {
                 const int j = A == 1 ? 0 : i;
                 y[i] = (T)back_result<V, A>(k, m, i, ((float)held[h][i] - k.mean[j]) * k.rstd[j], dz[h][i]);
             }
-            put((T*)p.out + w.at + h * w.step, y);
+            put((T*)p.out + w.at + h * w.step, y, A == 1 ? 0 : w.other);
             __builtin_amdgcn_sched_barrier(0);
         }
     if (w.full > H) {
@@ -1155,7 +1163,7 @@ static GroupLayout group_layout(int channels, int per, int dtype, int threads, i
         l.tv = (l.wide + v - 1) / v;
         l.reps = l.tv >= threads ? 1 : threads / l.tv;
         l.active = l.tv * l.reps;
-        l.merged = l.pieces > 1 || per % v == 0;
+        l.merged = per % v == 0;
         while (1 << l.sub < v && per % (2 << l.sub) == 0) ++l.sub;
     }
     l.inv_tv = 1.0f / (float)l.tv;

@@ -91,6 +91,30 @@ def test_activations_and_what_is_left_out(case, act):
         check(d, case, act, None, d["beta"], dtype, eps=0.1)
 
 
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("case", [(4000, 517, 11, [0, 7, 2500, 4000]), (30, 2051, 2051, 1), (30, 1027, 1027, [0, 11, 29]), (700, 4099, 1, 1),
+                                  (600, 6150, 3, [1, 50, 599]), (1500, 1999, 1, 3), (2500, 1026, 9, 5), (90, 2050, 1025, 1)], ids=str)
+def test_rows_that_end_inside_a_vector(case, dtype):
+    """Of one group and many, of several slabs, the last narrower than a vector, and of groups in pieces; a NaN stays in its group."""
+    rows, channels, groups, offsets = case
+    d = make(41, rows, channels, dtype)
+    check(d, case, "silu", d["gamma"], d["beta"], dtype)
+    row = offsets[1] - 1 if not isinstance(offsets, int) else rows - 1
+    fwd, bwd = where(offsets)
+    if groups > 1:
+        per = channels // groups
+        for j in (0, groups - 2, groups - 1):
+            x = d["x"].clone()
+            x[row, (j + 1) * per - 1] = float("nan")
+            out, mean, rstd = scnn.group_norm_fwd(x, groups, d["gamma"], d["beta"], **fwd)
+            bad = torch.zeros(groups, dtype=torch.bool, device=DEV)
+            bad[j] = True
+            b = 0 if not isinstance(offsets, int) else offsets - 1
+            assert torch.equal(mean[b].isnan(), bad) and torch.equal(out[row].isnan(), bad.repeat_interleave(per))
+            dx, dgamma, _ = scnn.group_norm_bwd(x, d["g"], groups, d["gamma"], d["beta"], mean, rstd, **bwd)
+            assert torch.equal(dx[row].isnan(), bad.repeat_interleave(per)) and torch.equal(dgamma.isnan(), bad.repeat_interleave(per))
+
+
 def test_gradients_match_differences():
     rows, channels, groups, samples = 7, 6, 3, [(0, 3), (3, 7)]
     d = {k: v.cpu().double() for k, v in make(3, rows, channels, torch.float32).items()}
