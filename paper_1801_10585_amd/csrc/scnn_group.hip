@@ -161,7 +161,7 @@ __device__ __forceinline__ Slab slab_of(const GroupArgs& p) {
 
 // This thread's place: its row among a step's, its first column in the slab.  A vector that the slab's end cuts is the slab's last whole
 // one instead (it may begin before the slab), of which the first `other` values are another thread's: read, but neither
-// added nor written.  (Cut vectors taken value by value behind the others: forward 60000 x 517 bf16 in 11 groups WAS us.)
+// added nor written.  (Cut vectors taken value by value behind the others: forward 60000 x 517 bf16 in 11 groups 122 us, so 59.)
 struct Place { int row, col, other; };
 template <int V>
 __device__ __forceinline__ Place place_of(const GroupArgs& p, const Slab& a) {
@@ -227,7 +227,8 @@ __device__ __forceinline__ void fetch(const T* __restrict__ x, const Walk& w, in
         if (k + u < w.full) r[u] = take(x + position<DOWN>(w, k + u));
 }
 // Calls use(slot, k) for a thread's vectors from number k up to `end`; the first U are there, and each slot is loaded again as soon as it
-// was used: load(slot, k).  (Loaded all at once behind the last use, sums of 643072 x 64 bf16 in 64 groups took 27 us.)
+// was used: load(slot, k).  Steps that all threads have run without a condition, so that a wait counts the loads behind it.  (Loaded all at
+// once behind the last use: forward 643072 x 64 fp32 82.6 us, so 78.5; backward 209645 x 25 fp32 37, so 33.)
 template <int U, typename Use, typename Load>
 __device__ __forceinline__ void walk(const Walk& w, int k, int end, Use use, Load load) {
     if (k >= end) return;
@@ -449,6 +450,8 @@ __device__ __forceinline__ void forward_down(const GroupArgs& p, const Columns<k
 
 constexpr int kAhead = 4;  // vectors of x that a thread of the blocks' kernels has on their way
 
+// Sums of a block's rows.  643072 x 64 fp32 in 8 groups: 25 us, 6.5 TB/s of x (caches hold some of it), bound by memory; the fp64 sums of
+// 23651 x 16 bf16 take 9 us, where a workgroup has one step: its start, two loads behind one another, LDS.
 template <typename T, bool M>
 __global__ __launch_bounds__(kGroupThreads, 2) void k_group_sums(GroupArgs p) {
     constexpr int V = kVec<T>;
@@ -605,6 +608,7 @@ __device__ __forceinline__ Two join_here(const GroupArgs& p, const Slab& a, cons
     return lanes_two(sum, o.q);
 }
 
+// Results of a block's rows, its last ones first.  643072 x 64 fp32: 52 us, 6.3 TB/s read and written, bound by memory.
 template <typename T, bool M>
 __global__ __launch_bounds__(kGroupThreads, 2) void k_group_apply(GroupArgs p) {
     constexpr int V = kVec<T>, A = M ? 1 : V;
@@ -653,7 +657,7 @@ __global__ __launch_bounds__(kGroupThreads, 2) void k_group_apply(GroupArgs p) {
 }
 
 // A sample's slab of whole groups by one workgroup of up to B threads, H vectors a thread in registers; what a larger sample has
-// more is read again.
+// more is read again.  One launch and one reading: 512 x 24 fp32 in 8 groups 8 us, bound by latency (a load, LDS, a store).
 template <typename T, bool M, int B, int H>
 __global__ __launch_bounds__(B, 2) void k_group_one(GroupArgs p) {
     constexpr int V = kVec<T>, A = M ? 1 : V;
@@ -811,7 +815,7 @@ __device__ __forceinline__ void back_sum_from(const GroupArgs& p, const BackColu
 }
 
 // Sums over a step's rows, given to s_col [2][wide].  All threads call it and meet at its end; s_all: a step's numbers, as in add_groups.
-// (Rows one behind the other, all lanes of a sum in one bank: 64 samples of 512 x 256 bf16 10 us longer.)
+// (Rows one behind the other put all lanes of a sum in one bank: 64 samples of 512 x 256 bf16 took 36.9 us, so 26.6 at the time.)
 template <int V>
 __device__ __forceinline__ void add_columns(const GroupArgs& p, const Slab& a, const Place& t, const BackSums<V>& v, float2* s_all, float* s_col) {
     const int wide = a.c1 - a.c0;
@@ -921,6 +925,8 @@ constexpr int kBackAhead = 2;  // vectors of x and of g
 // LDS: a step's numbers, then the columns' sums.
 __host__ __device__ __forceinline__ int step_values(const GroupLayout& l, int v) { return v * (l.active + 1); }
 
+// Sums of a block's rows, of columns first: dgamma and dbeta want these, and those of a group's h and h xh follow from them by gamma.
+// 209645 x 25 fp32 in 5 groups, relu: 16 us, 2.6 TB/s of x and g: eleven steps a workgroup with a start and an end around them.
 template <typename T, bool M>
 __global__ __launch_bounds__(kGroupThreads, 2) void k_group_back_sums(GroupArgs p) {
     constexpr int V = kVec<T>, A = M ? 1 : V, U = kBackAhead;
@@ -1004,7 +1010,7 @@ __device__ __forceinline__ void back_columns_sum(const GroupArgs& p, long long a
 
 constexpr int kSumColumns = 16;  // (64 bytes of a place)
 
-// Workgroups past the blocks add the columns' sums.
+// Gradients of a block's rows; workgroups past the blocks add the columns' sums.  209645 x 25 fp32 in 5 groups, relu: 16 us, 3.9 TB/s.
 template <typename T, bool M>
 __global__ __launch_bounds__(kGroupThreads, 2) void k_group_back(GroupArgs p) {
     constexpr int V = kVec<T>, A = M ? 1 : V, U = kBackAhead;
@@ -1044,7 +1050,9 @@ __global__ __launch_bounds__(kGroupThreads, 2) void k_group_back(GroupArgs p) {
     }
 }
 
-// cols [batch][2][channels]; with one sample dgamma and dbeta themselves.
+// Backward by a workgroup a sample and slab, x, g and dz in registers.  cols [batch][2][channels]; with one sample dgamma and dbeta
+// themselves.  64 samples of 512 x 256 bf16 in 32 groups, silu: 17 us, 3 TB/s, bound by the instructions of silu and its slope and by
+// what a workgroup does between its loads and its stores; k_column_sums behind it 4 us.
 template <typename T, bool M, int B, int H>
 __global__ __launch_bounds__(B, 2) void k_group_back_one(GroupArgs p) {
     constexpr int V = kVec<T>, A = M ? 1 : V;
@@ -1143,7 +1151,11 @@ static GroupLayout group_layout(int channels, int per, int dtype, int threads, i
     int even = 1;  // the largest power of two that both the vector and a row are a multiple of
     while (even < v && channels % (2 * even) == 0) even *= 2;
     const int period = channels / even;  // vectors after which a run of rows meets the same columns
-    if (even < v && period <= threads && channels <= most) {
+    // Values of a step: of rows that run on, and of rows that each begin with a vector (loads at any address, a cut vector a row).  The
+    // first where they are as many, or nearly.  us of the first / second, bf16, relu: backward 60000 x 516 112 / 88, 100000 x 260
+    // 78 / 70, 100000 x 165 66 / 55; fp32: 100000 x 258 116 / 96.
+    const int row = (channels + v - 1) / v, runs = threads / period * period * v, rows = (row >= threads ? 1 : threads / row) * channels;
+    if (even < v && period <= threads && channels <= most && 8LL * runs >= 7LL * rows) {
         l.flat = 1;
         l.active = threads / period * period;
         l.reps = (int)((long long)l.active * v / channels);

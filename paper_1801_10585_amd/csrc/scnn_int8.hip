@@ -44,7 +44,8 @@ __device__ __forceinline__ int quantized(float v, const Quantizer& q) {
 }
 
 // P threads a row (a group of lanes of a wave, or a workgroup of whole waves), H vectors of the row in a thread's registers; what a
-// longer row has more is read again.
+// longer row has more is read again.  Bound by memory, one reading of rows of up to 2 P vectors: 8192 x 4096 bf16 19 us (5.3 TB/s),
+// 200000 x 64 bf16 9.5 us by 4 threads a row (16.4 by 16), 64 x 12288 fp16 4.2 us by 1024.
 template <typename T, int P, int H>
 __global__ __launch_bounds__(P < 256 ? 256 : P) void k_quantize_rows(const T* __restrict__ x, long long rows_cap,
                                                                      const long long* __restrict__ rows_dev, long long channels,
@@ -102,38 +103,70 @@ __global__ __launch_bounds__(P < 256 ? 256 : P) void k_quantize_rows(const T* __
     if (t == 0) scale[row] = q.scale;
 }
 
-// 32 columns of w [c_in, c_out] a workgroup: their largest magnitudes, then their values as rows of q by way of LDS.
+// Once for a layer.  32 columns of w [c_in, c_out] a workgroup, V of a row a thread: their largest magnitudes, then k_span rows of them as
+// rows of q by way of LDS; workgroups along y each look at all of the columns, which the L2 has by then.  12288 x 1024 bf16 30 us (one
+// workgroup a strip, value by value: 203).
 template <typename T>
 __global__ __launch_bounds__(1024) void k_quantize_weight(const T* __restrict__ w, long long c_in, long long c_out, long long width,
-                                                          signed char* __restrict__ out, float* __restrict__ scale) {
-    __shared__ unsigned s_most[32][33];
-    __shared__ signed char s_q[32][64 + 4];
-    const int tc = threadIdx.x & 31, tr = threadIdx.x >> 5;
-    const long long c0 = block_id<1024>() * 32, c = c0 + tc;
+                                                          long long k_span, signed char* __restrict__ out, float* __restrict__ scale) {
+    constexpr int V = kVec<T>, C = 32, TR = C / V, R = 1024 / TR, B = R / 32;  // R rows a step, B bytes of q a thread
+    typedef signed char Q __attribute__((ext_vector_type(B)));
+    __shared__ unsigned s_most[16][C];
+    __shared__ float s_inverse[C];
+    __shared__ __align__(16) signed char s_q[C][R + 16];
+    const int tid = threadIdx.x, lane = tid & 63, tc = tid % TR * V, tr = tid / TR;
+    const long long c0 = block_id<1024>() * C;
     if (c0 >= c_out) return;
-    unsigned most = 0;
-    if (c < c_out)
-#pragma unroll 4
-        for (long long k = tr; k < c_in; k += 32) {
-            const unsigned m = magnitude((float)w[k * c_out + c]);
-            most = m > most ? m : most;
+    const int n = (int)(c_out - c0 - tc < V ? c_out - c0 - tc : V);  // (0 and less: no column of this thread's is there)
+    const T* __restrict__ from = w + c0 + tc;
+    auto take = [&](long long k) { return load_raw<T>(from + k * c_out, n, c_out >= V); };
+    unsigned most[V] = {};
+    for (long long k = tr; k < c_in; k += 4 * R) {
+        VecOf<T, V> v[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) v[u] = take(k + u * R < c_in ? k + u * R : k);
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const unsigned m = magnitude((float)v[u][i]);
+                most[i] = m > most[i] ? m : most[i];
+            }
+    }
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+#pragma unroll
+        for (int d = TR; d < 64; d <<= 1) {
+            const unsigned o = __shfl_xor(most[i], d, 64);
+            most[i] = o > most[i] ? o : most[i];
         }
-    s_most[tr][tc] = most;
+        if (lane < TR) s_most[tid >> 6][tc + i] = most[i];
+    }
     __syncthreads();
+    if (tid < C) {
+        unsigned m = 0;
 #pragma unroll
-    for (int k = 0; k < 32; ++k) most = s_most[k][tc] > most ? s_most[k][tc] : most;
-    const Quantizer q = quantizer(most);
-    if (tr == 0 && c < c_out) scale[c] = q.scale;
-    for (long long k0 = 0; k0 < width; k0 += 64) {
-        __syncthreads();
+        for (int k = 0; k < 16; ++k) m = s_most[k][tid] > m ? s_most[k][tid] : m;
+        const Quantizer q = quantizer(m);
+        s_inverse[tid] = q.inverse;
+        if (blockIdx.y == 0 && c0 + tid < c_out) scale[c0 + tid] = q.scale;
+    }
+    __syncthreads();
+    Quantizer q[V];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const long long k = k0 + h * 32 + tr;
-            s_q[tc][h * 32 + tr] = (signed char)(k < c_in && c < c_out ? quantized((float)w[k * c_out + c], q) : 0);
-        }
+    for (int i = 0; i < V; ++i) q[i].inverse = s_inverse[tc + i];
+    const long long k_first = (long long)blockIdx.y * k_span, k_end = k_first + k_span < width ? k_first + k_span : width;
+    VecOf<T, V> next = {};
+    if (k_first + tr < c_in) next = take(k_first + tr);
+    for (long long k0 = k_first; k0 < k_end; k0 += R) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) s_q[tc + i][tr] = (signed char)quantized((float)next[i], q[i]);
+        next = VecOf<T, V>{};
+        if (k0 + R + tr < c_in) next = take(k0 + R + tr);
         __syncthreads();
-        const int row = threadIdx.x >> 4, four = threadIdx.x & 15;
-        if (row < 32 && c0 + row < c_out) *(int*)(out + (c0 + row) * width + k0 + four * 4) = *(const int*)&s_q[row][four * 4];
+        const int col = tid >> 5, at = (tid & 31) * B;
+        if (c0 + col < c_out && k0 + at < k_end) *(Q*)(out + (c0 + col) * width + k0 + at) = *(const Q*)&s_q[col][at];
+        __syncthreads();
     }
 }
 
@@ -186,12 +219,16 @@ __device__ __forceinline__ void finish(const Int8Args& p, long long m, long long
 }
 
 // BM x BN outputs a workgroup; a step is 128 bytes of every row, copied from memory to LDS without passing through registers, the
-// next step's while this one's is multiplied.  (Steps of 64 bytes in three, four and five places: 3 to 12 per cent longer.)  Rows of a step are pieces of 16 bytes; piece c of row r lies at place c ^ spread(r), so that the lanes of a read
-// meet different banks (the copy puts pieces down in the order of the lanes, whose addresses carry the permutation).  Rows past the
-// arrays' ends are read from the last one, what they add up to is not stored; a row that ends in the middle of a step
-// has its first half copied twice and multiplied once.  The operands swap places at the instruction: its rows are the tile's
+// next step's while this one's is multiplied.  (Steps of 64 bytes in three, four and five places: 3 to 12 per cent longer.)  Rows of a
+// step are pieces of 16 bytes; piece c of row r lies at place c ^ spread(r), so that the lanes of a read meet different banks (the copy
+// puts pieces down in the order of the lanes, whose addresses carry the permutation).  Rows past the arrays' ends are read from the last
+// one, what they add up to is not stored; a row that ends in the middle of a step has its first half copied twice and multiplied once.  The operands swap places at the instruction: its rows are the tile's
 // columns n, in pairs of blocks (block b of a pair takes columns 8 (i / 4) + 4 b + i % 4, i < 16), so that a lane ends with
 // eight neighbouring columns of one row.
+// 8192 x 4096 x 4096 bf16 out, tiles of 256: 153 us, with gelu and a residual 173, 1800 and 1590 TOP/s (the library's bare product 2070).
+// LDS has no conflict; the matrix cores are busy 39 per cent of the cycles: one workgroup a unit, whose waves wait at a barrier a step,
+// and an epilogue that nothing overlaps.  (Four waves of 128 x 128 225 us; without s_setprio 164; both halves' operands read
+// ahead: no change.)  3001 x 1001 x 1303 fp32 out, tiles of 64: 14 us, four workgroups a unit, mostly their starts and ends.
 template <bool PAIR>
 __device__ __forceinline__ int spread(int r) { return PAIR ? (r & 3) | ((r >> 1) & 4) : r & 7; }  // (eight lanes read rows 0 to 7, PAIR: 0 to 3 and 8 to 11)
 
@@ -302,7 +339,8 @@ __global__ __launch_bounds__(64 * WM * WN) void k_int8_ring(Int8Args p) {
 }
 
 // Up to 16 MB rows: bound by reading w once.  Eight waves share the k of 16 NB columns, operands straight from memory to the
-// registers that the instruction wants, a lane 16 bytes of one row; their sums meet in LDS.
+// registers that the instruction wants, a lane 16 bytes of one row; their sums meet in LDS.  8 x 4096 -> 4096 in 8 bits: 6.8 us, 2.5 TB/s;
+// 32 x 4096 -> 4096 9.1 (tiles of 64 longer than that up to 32 rows).
 template <typename T, int MB, int NB>
 __global__ __launch_bounds__(512) void k_int8_skinny(Int8Args p) {
     constexpr int W = 8, U = 4;
@@ -404,7 +442,8 @@ __global__ __launch_bounds__(256) void k_int8_join(Int8Args p, int splits) {
 
 // One row, brought to 8 bits by every workgroup for itself: bound by reading w once.  A wave takes R columns (rows of w), its first
 // pieces of them on their way while the row is quantised; a lane multiplies 16 bytes at a time, four products an instruction.
-// GIVEN: the row is there in 8 bits.
+// GIVEN: the row is there in 8 bits.  4096 -> 4096 bf16: 6.4 us, 2.6 TB/s of w, where the row's own reading, maximum and rounding come
+// before the first product; one launch (as a quantisation and a product it took 26 us).
 constexpr int kRowThreads = 256, kRowLds = 16384;  // bytes of the row in LDS at a time
 template <typename T, int R, bool GIVEN>
 __global__ __launch_bounds__(kRowThreads) void k_int8_row(Int8Args p, const T* __restrict__ x, int c_in) {
@@ -526,8 +565,14 @@ hipError_t launch_quantize_rows(int dtype, const void* x, long long rows, const 
 
 template <typename T>
 static hipError_t quantize_weight(const void* w, long long c_in, long long c_out, signed char* q, float* scale, hipStream_t s) {
-    hipLaunchKernelGGL((k_quantize_weight<T>), grid_of<1024>((c_out + 31) / 32), dim3(1024), 0, s, (const T*)w, c_in, c_out,
-                       int8_width(c_in), q, scale);
+    // as many workgroups as compute units, where the rows are enough for some steps each
+    const long long width = int8_width(c_in), strips = (c_out + 31) / 32, least = 1024;
+    long long splits = device_cu_count() / strips;
+    if (splits > width / least) splits = width / least;
+    if (splits < 1) splits = 1;
+    const long long span = round_up((width + splits - 1) / splits, 256);
+    hipLaunchKernelGGL((k_quantize_weight<T>), grid_of<1024>(strips, (unsigned)((width + span - 1) / span)), dim3(1024), 0, s, (const T*)w,
+                       c_in, c_out, width, span, q, scale);
     return hipGetLastError();
 }
 
