@@ -222,9 +222,9 @@ __device__ __forceinline__ void finish(const Int8Args& p, long long m, long long
 // next step's while this one's is multiplied.  (Steps of 64 bytes in three, four and five places: 3 to 12 per cent longer.)  Rows of a
 // step are pieces of 16 bytes; piece c of row r lies at place c ^ spread(r), so that the lanes of a read meet different banks (the copy
 // puts pieces down in the order of the lanes, whose addresses carry the permutation).  Rows past the arrays' ends are read from the last
-// one, what they add up to is not stored; a row that ends in the middle of a step has its first half copied twice and multiplied once.  The operands swap places at the instruction: its rows are the tile's
-// columns n, in pairs of blocks (block b of a pair takes columns 8 (i / 4) + 4 b + i % 4, i < 16), so that a lane ends with
-// eight neighbouring columns of one row.
+// one, what they add up to is not stored; a row that ends in the middle of a step has its first half copied twice and multiplied once.
+// The operands swap places at the instruction: its rows are the tile's columns n, in pairs of blocks (block b of a pair takes columns
+// 8 (i / 4) + 4 b + i % 4, i < 16), so that a lane ends with eight neighbouring columns of one row.
 // 8192 x 4096 x 4096 bf16 out, tiles of 256: 153 us, with gelu and a residual 173, 1800 and 1590 TOP/s (the library's bare product 2070).
 // LDS has no conflict; the matrix cores are busy 39 per cent of the cycles: one workgroup a unit, whose waves wait at a barrier a step,
 // and an epilogue that nothing overlaps.  (Four waves of 128 x 128 225 us; without s_setprio 164; both halves' operands read
