@@ -1202,12 +1202,14 @@ static long long group_chunk(const GroupLayout& l, long long rows) {
 }
 
 // A workgroup a sample and slab, its values in registers: 16384 of them, in 256 threads, or in 512 where workgroups are few; samples of
-// up to twice that on the average.  Only the device knows how unequal the samples are, and one that holds all values of a call keeps its
-// workgroup for 0.3 us a thousand: calls of up to 2^24 values.  us of this / of blocks of rows, us in a graph: backward 64 samples of
-// 512 x 256 bf16 20 / 39, forward 512 x 24 fp32 7.5 / 14.
+// up to twice that on the average.  Only the device knows how unequal samples are that offsets name, and a large one keeps its
+// workgroup for 0.3 us a thousand values: they are up to half of it in calls of more than 2^24 values, and these up to 2^28.
+// us of this / of blocks of rows, in a graph: backward 64 samples of 512 x 256 bf16 20 / 39, forward 512 x 24 fp32 7.5 / 14; forward and
+// backward 4096 samples of about 128 x 64 bf16 39 / 105 and 87 / 141, of 16 x 512 fp32 49 / 107 and 105 / 187; 1024 equal ones of
+// 512 x 64 fp32 52 / 80 and 88 / 124.
 constexpr int kOneFew = 512, kOneMany = 256;
-constexpr long long kOneHeld = 16384, kOneAll = 1LL << 24;
-static bool group_one(long long rows, long long batch, int channels, int per, int dtype, GroupLayout& l, int& threads) {
+constexpr long long kOneHeld = 16384, kOneAny = 1LL << 24, kOneAll = 1LL << 28;
+static bool group_one(long long rows, long long batch, int channels, int per, int dtype, bool equal, GroupLayout& l, int& threads) {
     const int v = group_vec(dtype), least = 64 / (16 / v);  // (64 bytes of a row)
     const long long values = rows * channels / batch, cus = device_cu_count();
     int most = kOneMany * v / 2;
@@ -1223,21 +1225,23 @@ static bool group_one(long long rows, long long batch, int channels, int per, in
             if (wide < most) most = (int)wide;
         }
     }
-    if (rows * channels > kOneAll || rows * (channels < most ? channels : most) > 2 * kOneHeld * batch) return false;
+    const long long held = rows * (channels < most ? channels : most);
+    if (held > 2 * kOneHeld * batch) return false;
+    if (!equal && rows * channels > kOneAny && (rows * channels > kOneAll || 2 * held > kOneHeld * batch)) return false;
     threads = kOneFew;
     l = group_layout(channels, per, dtype, threads, most);
     if (batch * l.slabs >= cus || one_lds(l, v, per) > 60000) {
         threads = kOneMany;
         l = group_layout(channels, per, dtype, threads, most);
     }
-    return l.pieces == 1;
+    return l.pieces == 1 && l.slabs <= 65535;  // (a launch's second axis)
 }
 
 struct GroupSpace { GroupLayout l; long long blocks, chunk, places; size_t part, cols, stat, total; bool one, joined; int threads; };
-static GroupSpace group_space(long long rows, long long batch, int channels, int groups, int dtype, bool back) {
+static GroupSpace group_space(long long rows, long long batch, int channels, int groups, int dtype, bool equal, bool back) {
     GroupSpace s = {};
     const int per = channels / groups;
-    s.one = group_one(rows, batch, channels, per, dtype, s.l, s.threads);
+    s.one = group_one(rows, batch, channels, per, dtype, equal, s.l, s.threads);
     if (s.one) {
         s.places = batch;
         if (back && batch > 1) s.total = (size_t)round_up(batch * channels * 8, 256);
@@ -1256,7 +1260,9 @@ static GroupSpace group_space(long long rows, long long batch, int channels, int
 }
 
 size_t group_norm_bytes(int dtype, long long rows, long long batch, int channels, int groups, bool back) {
-    return group_space(rows, batch, channels, groups, dtype, back).total;
+    const size_t equal = group_space(rows, batch, channels, groups, dtype, true, back).total;
+    const size_t any = group_space(rows, batch, channels, groups, dtype, false, back).total;
+    return equal > any ? equal : any;
 }
 
 static GroupArgs group_args(int dtype, const GroupCall& c, bool back, GroupSpace& s) {
@@ -1270,7 +1276,7 @@ static GroupArgs group_args(int dtype, const GroupCall& c, bool back, GroupSpace
     p.each = c.rows / c.batch;
     p.channels = c.channels; p.groups = c.groups; p.per = c.channels / c.groups; p.act = c.act;
     p.eps = c.eps;
-    s = group_space(c.rows, c.batch, c.channels, c.groups, dtype, back);
+    s = group_space(c.rows, c.batch, c.channels, c.groups, dtype, c.offsets == nullptr, back);
     p.l = s.l;
     p.chunk = s.chunk; p.blocks = s.blocks; p.places = s.places;
     p.inv_each = p.each > 0 ? 1.0 / (double)p.each : 0.0;

@@ -125,3 +125,27 @@ def test_refusals_of_the_binding():
                  lambda: scnn.dropout_fwd(x, float("nan")), lambda: scnn.group_norm_fwd(x, 2, out=(x, mean[:1], rstd[:1]))):
         with pytest.raises(scnn.ScnnError):
             call()
+
+
+@pytest.mark.parametrize("dtype", (torch.float32, torch.bfloat16), ids=str)
+def test_calls_of_many_samples(dtype):
+    """Calls of more than 2^24 values, of equal samples with and without offsets, of short ones whole and in two halves."""
+    e = torch.finfo(dtype).eps
+    x, g, gamma = normal(15, 300000, 64, dtype=dtype), normal(16, 300000, 64, dtype=dtype), normal(17, 64, dtype=dtype)
+
+    def both(x, g, batch=None, offsets=None):
+        y, m, r = scnn.group_norm_fwd(x, 8, gamma, batch=batch, offsets=offsets, act="silu")
+        return [y, m, r, *scnn.group_norm_bwd(x, g, 8, gamma, None, m, r, offsets=offsets, act="silu")]
+
+    same = both(x, g, batch=600), both(x, g, offsets=torch.arange(0, 300001, 500, device=DEV))
+    for k, (a, b) in enumerate(zip(*same)):
+        # sums in other orders: steps of fp32 apart before the rounding (64 of them where a term cancels or 300000 are added), then one step of the type
+        near = (64 if k < 4 else 4096) * ref.U32 * float(b.float().abs().max())
+        assert torch.allclose(a.float(), b.float(), rtol=e if k != 1 and k != 2 else 8 * ref.U32, atol=near), k
+    cuts = torch.sort(torch.randint(0, 150001, (1, 3000), generator=torch.Generator().manual_seed(1)), 1)[0][0].to(DEV)
+    half = torch.cat([torch.zeros(1, dtype=torch.int64, device=DEV), cuts, torch.full((1,), 150000, device=DEV)])
+    whole = both(x, g, offsets=torch.cat([half, half[1:] + 150000]))
+    for k, one in enumerate((both(x[:150000], g[:150000], offsets=half), both(x[150000:], g[150000:], offsets=half))):
+        at = slice(k * 150000, (k + 1) * 150000), slice(k * 3001, (k + 1) * 3001)
+        for a, b, rows in ((whole[0], one[0], 0), (whole[3], one[3], 0), (whole[1], one[1], 1), (whole[2], one[2], 1)):
+            assert torch.equal(a[at[rows]], b)
