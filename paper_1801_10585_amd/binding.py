@@ -526,7 +526,7 @@ _HERE = _Here()
 def _on(dev, stream, tensors):
     """Makes `dev`, and `stream` where one is given, current while a call allocates and launches."""
     if stream is None:
-        return _HERE if dev.index == torch.cuda.current_device() else torch.cuda.device(dev)
+        return _HERE if dev.index == torch._C._cuda_getDevice() else torch.cuda.device(dev)
     if stream.device != dev:
         raise ValueError("the stream belongs to another device than the tensors")
     if stream != torch.cuda.current_stream(dev):
@@ -619,7 +619,7 @@ def _bytes(workspace) -> int:
 
 def _current() -> int:
     """The current device's current stream."""
-    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
 
 
 def _cont(t: Optional[torch.Tensor]) -> Optional[torch.Tensor]:
@@ -784,9 +784,10 @@ def group_norm_fwd(x, groups, gamma=None, beta=None, *, offsets=None, batch=None
     with _on(x.device, stream, (x, gamma, beta, offsets, y, mean, rstd, workspace)):
         x, gamma, beta, offsets = x.contiguous(), _cont(gamma), _cont(beta), _cont(offsets)
         y = _result(y, x, (rows, ch), "out")
+        need = _need(x.device.index, "group_norm_fwd_workspace", dt, rows, batch, ch, groups)
         mean = _result(mean, x, (batch, groups), "mean", torch.float32)
         rstd = _result(rstd, mean, (batch, groups), "rstd")
-        workspace = _scratch(workspace, _need(x.device.index, "group_norm_fwd_workspace", dt, rows, batch, ch, groups), x)
+        workspace = _scratch(workspace, need, x)
         _check(L, L.group_norm_fwd(dt, _at(x), rows, _at(offsets), batch, ch, groups, _at(gamma), _at(beta), float(eps), code,
                                    _at(y), _at(mean), _at(rstd), _at(workspace), _bytes(workspace), _current()))
     return y, mean, rstd

@@ -121,7 +121,7 @@ def test_refusals_of_the_binding():
             call()
             pytest.fail(f"call {k} was taken")
     for call in (lambda: scnn.group_norm_fwd(x, 3), lambda: scnn.group_norm_fwd(x, 2, batch=5), lambda: scnn.group_norm_fwd(x, 2, eps=-1.0),
-                 lambda: scnn.group_norm_fwd(x, 0), lambda: scnn.group_norm_fwd(x, 2, batch=0), lambda: scnn.dropout_fwd(x, 1.5),
+                 lambda: scnn.group_norm_fwd(x, 0), lambda: scnn.group_norm_fwd(x, 2, batch=0), lambda: scnn.group_norm_fwd(x, 2, batch=-1), lambda: scnn.group_norm_fwd(x, -2), lambda: scnn.dropout_fwd(x, 1.5),
                  lambda: scnn.dropout_fwd(x, float("nan")), lambda: scnn.group_norm_fwd(x, 2, out=(x, mean[:1], rstd[:1]))):
         with pytest.raises(scnn.ScnnError):
             call()
