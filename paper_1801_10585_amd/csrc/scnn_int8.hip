@@ -182,40 +182,78 @@ struct Int8Args {
     long long k_split;  // bytes of a row that a workgroup sums, a multiple of 64
 };
 
+// One choice of the activation for C values, whose chains of instructions then run side by side.
+template <int C>
+__device__ __forceinline__ void activate_all(float (&z)[C], int act) {
+    if (act == SCNN_ACT_GELU) {
+#pragma unroll
+        for (int j = 0; j < C; ++j) z[j] = activate(z[j], SCNN_ACT_GELU);
+    } else if (act == SCNN_ACT_SILU) {
+#pragma unroll
+        for (int j = 0; j < C; ++j) z[j] = activate(z[j], SCNN_ACT_SILU);
+    } else if (act == SCNN_ACT_RELU) {
+#pragma unroll
+        for (int j = 0; j < C; ++j) z[j] = activate(z[j], SCNN_ACT_RELU);
+    }
+}
+
 // Epilogue of C neighbouring columns of which w are there; everything is read before the first is written (out may be residual).
 template <typename T, int C>
-__device__ __forceinline__ void finish(const Int8Args& p, long long m, long long n, int w, float xs, const int (&sum)[C]) {
-    typedef VecOf<T, C> V;
-    float ws[C];
-    V bias = {}, residual = {}, y;
-    const long long at = m * p.n + n;
+struct Beside { float scale[C]; VecOf<T, C> bias; };
+template <typename T, int C>
+__device__ __forceinline__ VecOf<T, C> some(const void* from, long long at, int w) {
+    VecOf<T, C> v = {};
+    if (!from) return v;
+    const T* p = (const T*)from + at;
     if (w >= C) {
-        __builtin_memcpy(ws, p.w_scale + n, sizeof(ws));
-        if (p.bias) __builtin_memcpy(&bias, (const T*)p.bias + n, sizeof(V));
-        if (p.residual) __builtin_memcpy(&residual, (const T*)p.residual + at, sizeof(V));
+        __builtin_memcpy(&v, p, sizeof(v));
     } else {
 #pragma unroll
-        for (int j = 0; j < C; ++j) {
-            ws[j] = j < w ? p.w_scale[n + j] : 0.0f;
-            if (p.bias && j < w) bias[j] = ((const T*)p.bias)[n + j];
-            if (p.residual && j < w) residual[j] = ((const T*)p.residual)[at + j];
-        }
+        for (int j = 0; j < C; ++j)
+            if (j < w) v[j] = p[j];
     }
+    return v;
+}
+template <typename T, int C>
+__device__ __forceinline__ Beside<T, C> beside(const Int8Args& p, long long n, int w) {
+    Beside<T, C> b;
+    if (w >= C) {
+        __builtin_memcpy(b.scale, p.w_scale + n, sizeof(b.scale));
+    } else {
+#pragma unroll
+        for (int j = 0; j < C; ++j) b.scale[j] = j < w ? p.w_scale[n + j] : 0.0f;
+    }
+    b.bias = some<T, C>(p.bias, n, w);
+    return b;
+}
+template <typename T, int C>
+__device__ __forceinline__ void finish(const Int8Args& p, long long m, long long n, int w, float xs, const int (&sum)[C],
+                                       const Beside<T, C>& b, const VecOf<T, C>& residual) {
+    VecOf<T, C> y;
+    const long long at = m * p.n + n;
+    float z[C];
 #pragma unroll
     for (int j = 0; j < C; ++j) {
-        float z = (float)sum[j] * xs * ws[j];
-        if (p.bias) z += (float)bias[j];
-        z = activate(z, p.act);
-        if (p.residual) z += (float)residual[j];
-        y[j] = (T)z;
+        z[j] = (float)sum[j] * xs * b.scale[j];
+        if (p.bias) z[j] += (float)b.bias[j];
+    }
+    activate_all<C>(z, p.act);
+#pragma unroll
+    for (int j = 0; j < C; ++j) {
+        if (p.residual) z[j] += (float)residual[j];
+        y[j] = (T)z[j];
     }
     if (w >= C) {
-        __builtin_memcpy((T*)p.out + at, &y, sizeof(V));
+        __builtin_memcpy((T*)p.out + at, &y, sizeof(y));
     } else {
 #pragma unroll
         for (int j = 0; j < C; ++j)
             if (j < w) ((T*)p.out)[at + j] = y[j];
     }
+}
+template <typename T, int C>
+__device__ __forceinline__ void finish(const Int8Args& p, long long m, long long n, int w, float xs, const int (&sum)[C]) {
+    finish<T, C>(p, m, n, w, xs, sum, beside<T, C>(p, n, w), some<T, C>(p.residual, m * p.n + n, w));
 }
 
 // BM x BN outputs a workgroup; a step is 128 bytes of every row, copied from memory to LDS without passing through registers, the
@@ -310,29 +348,51 @@ __global__ __launch_bounds__(64 * WM * WN) void k_int8_ring(Int8Args p) {
         multiply(s, s + A8 * 16, 0);
         if (!odd || step + 1 < steps) multiply(s, s + A8 * 16, 1);
     }
+    const long long m_lane = m0 + wm + i16;
+    if (p.part) {
 #pragma unroll
-    for (int i = 0; i < TM; ++i) {
-        const long long m = m0 + wm + i * 16 + i16;
-        if (m >= m_end) continue;
-        const float xs = p.part ? 0.0f : p.x_scale[m];
+        for (int i = 0; i < TM; ++i)
 #pragma unroll
-        for (int j = 0; j < TN; j += 2) {
-            const long long n = n0 + wn + j * 16 + 8 * q;
-            if (n >= p.n) continue;
-            const int sum[8] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3],
-                                acc[i][j + 1][0], acc[i][j + 1][1], acc[i][j + 1][2], acc[i][j + 1][3]};
-            const int w = (int)(p.n - n < 8 ? p.n - n : 8);
-            if (p.part) {
+            for (int j = 0; j < TN; j += 2) {
+                const long long m = m_lane + i * 16, n = n0 + wn + j * 16 + 8 * q;
+                if (m >= m_end || n >= p.n) continue;
                 int* to = p.part + ((long long)blockIdx.y * p.m + m) * p.n + n;
-                if (w == 8) {
-                    __builtin_memcpy(to, sum, sizeof(sum));
+                if (p.n - n >= 8) {
+                    __builtin_memcpy(to, &acc[i][j], 16);
+                    __builtin_memcpy(to + 4, &acc[i][j + 1], 16);
                 } else {
 #pragma unroll
                     for (int c = 0; c < 8; ++c)
-                        if (c < w) to[c] = sum[c];
+                        if (c < p.n - n) to[c] = acc[i][j + c / 4][c % 4];
                 }
-            } else {
-                finish<T, 8>(p, m, n, w, xs, sum);
+            }
+        return;
+    }
+    // what stands beside the sums is read for R rows at once
+    constexpr int R = TM < 4 ? TM : 4;
+    float xs[TM];
+#pragma unroll
+    for (int i = 0; i < TM; ++i) xs[i] = p.x_scale[m_lane + i * 16 < m_end ? m_lane + i * 16 : m_end - 1];
+#pragma unroll
+    for (int j = 0; j < TN; j += 2) {
+        const long long n = n0 + wn + j * 16 + 8 * q;
+        if (n >= p.n) continue;
+        const int w = (int)(p.n - n < 8 ? p.n - n : 8);
+        const Beside<T, 8> b = beside<T, 8>(p, n, w);
+#pragma unroll
+        for (int i0 = 0; i0 < TM; i0 += R) {
+            VecOf<T, 8> residual[R];
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                const long long m = m_lane + (i0 + r) * 16;
+                residual[r] = some<T, 8>(p.residual, (m < m_end ? m : m_end - 1) * p.n + n, w);
+            }
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                const int i = i0 + r;
+                const int sum[8] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3],
+                                    acc[i][j + 1][0], acc[i][j + 1][1], acc[i][j + 1][2], acc[i][j + 1][3]};
+                if (m_lane + i * 16 < m_end) finish<T, 8>(p, m_lane + i * 16, n, w, xs[i], sum, b, residual[r]);
             }
         }
     }
