@@ -244,7 +244,10 @@ __device__ __forceinline__ void finish(const Int8Args& p, long long m, long long
         y[j] = (T)z[j];
     }
     if (w >= C) {
-        __builtin_memcpy((T*)p.out + at, &y, sizeof(y));
+        // (tiles' results, where rows are whole vectors, leave the L2 to the operands: 8192 x 4096 x 4096 bf16 with silu and a residual
+        // 150 us else, so 131; of 1303 columns it takes 2 per cent longer)
+        if (C == 8 && (p.n & 7) == 0) __builtin_nontemporal_store(y, (VecOf<T, C> __attribute__((aligned(sizeof(T))))*)((T*)p.out + at));
+        else __builtin_memcpy((T*)p.out + at, &y, sizeof(y));
     } else {
 #pragma unroll
         for (int j = 0; j < C; ++j)
@@ -263,10 +266,10 @@ __device__ __forceinline__ void finish(const Int8Args& p, long long m, long long
 // one, what they add up to is not stored; a row that ends in the middle of a step has its first half copied twice and multiplied once.
 // The operands swap places at the instruction: its rows are the tile's columns n, in pairs of blocks (block b of a pair takes columns
 // 8 (i / 4) + 4 b + i % 4, i < 16), so that a lane ends with eight neighbouring columns of one row.
-// 8192 x 4096 x 4096 bf16 out, tiles of 256: 153 us, with gelu and a residual 173, 1800 and 1590 TOP/s (the library's bare product 2070).
-// LDS has no conflict; the matrix cores are busy 39 per cent of the cycles: one workgroup a unit, whose waves wait at a barrier a step,
-// and an epilogue that nothing overlaps.  (Four waves of 128 x 128 225 us; without s_setprio 164; both halves' operands read
-// ahead: no change.)  3001 x 1001 x 1303 fp32 out, tiles of 64: 14 us, four workgroups a unit, mostly their starts and ends.
+// 8192 x 4096 x 4096 bf16 out, tiles of 256: 129 us, with gelu and a residual 142, 2130 and 1940 TOP/s (the library's bare product 2070).
+// LDS has no conflict; one workgroup a unit, whose waves wait at a barrier a step, and an epilogue that nothing overlaps.  (Four waves
+// of 128 x 128 one and a half times as long; without s_setprio 7 per cent longer; both halves' operands read ahead: no change.)
+// 3001 x 1001 x 1303 fp32 out, tiles of 64: 14 us, four workgroups a unit, mostly their starts and ends.
 template <bool PAIR>
 __device__ __forceinline__ int spread(int r) { return PAIR ? (r & 3) | ((r >> 1) & 4) : r & 7; }  // (eight lanes read rows 0 to 7, PAIR: 0 to 3 and 8 to 11)
 
