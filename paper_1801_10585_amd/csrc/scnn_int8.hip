@@ -269,7 +269,7 @@ __device__ __forceinline__ void finish(const Int8Args& p, long long m, long long
 // 8192 x 4096 x 4096 bf16 out, tiles of 256: 129 us, with gelu and a residual 142, 2130 and 1940 TOP/s (the library's bare product 2070).
 // LDS has no conflict; one workgroup a unit, whose waves wait at a barrier a step, and an epilogue that nothing overlaps.  (Four waves
 // of 128 x 128 one and a half times as long; without s_setprio 7 per cent longer; both halves' operands read ahead: no change.)
-// 3001 x 1001 x 1303 fp32 out, tiles of 64: 14 us, four workgroups a unit, mostly their starts and ends.
+// 3001 x 1001 x 1303 fp32 out, tiles of 64: 12 us, four workgroups a unit, mostly their starts and ends.
 template <bool PAIR>
 __device__ __forceinline__ int spread(int r) { return PAIR ? (r & 3) | ((r >> 1) & 4) : r & 7; }  // (eight lanes read rows 0 to 7, PAIR: 0 to 3 and 8 to 11)
 
@@ -648,13 +648,13 @@ hipError_t launch_quantize_weight(int dtype, const void* w, long long c_in, long
     }
 }
 
-// Kernel of a product: one row, up to 32 rows straight from memory, or tiles of 256, 128 or 64 squared.  bf16 with silu and residual,
-// us, of 256 / 128 / 64 / (64 x 128, left out) tiles, and of up to 32 rows by k_int8_skinny / tiles of 64:
-//   8192 x 4096 x 4096 (m, k, n)  168 / 184 / 229 / 205     4096 x 4096 x 4096   84 / 98 / 131 / 114
-//   6000 x 4096 x 4096  149 / 130 / 170 / 145 (384 tiles of 256 on 256 units)    2048 x 2048 x 2048   39 / 23.3 / 19.4 / 19.2
-//   8192 x 1024 x 1024   44 / 25.4 / 27.9 / 28.2 (512 of 128)                    5000 x 1000 x 1304   41 / 23.8 / 22.2 / 25.7 (440)
-//   1000 x 12288 x 1000  44 / 37 / 43 / 45 (k split four ways, 64: twice)        1024 x 1024 x 1024   21 / 12.5 / 9.3 / 11.3
-//   200000 x 64 x 64     93 / 51 / 24 / 39      300 x 300 x 3000   27 / 14.7 / 6.6 / 9.4      100 x 4096 x 4096   17.9 / 14.7 / 12.5 / 13.1
+// Kernel of a product: one row, up to 32 rows straight from memory, or tiles of 256, 128 or 64 squared.  bf16 with silu and residual, rows
+// given, us in a graph, of tiles of 256 / 128 / 64 (tiles of 64 x 128 lay between the last two, or above both):
+//   8192 x 4096 x 4096 (m, k, n)  130 / 152 / 204        4096 x 4096 x 4096   66 / 74 / 104       16384 x 2048 x 1024  40 / 45 / 60
+//   6000 x 4096 x 4096  117 / 111 / 155 (384 tiles of 256 on 256 units)     8192 x 1024 x 1024   25 / 17.0 / 19.9 (512 of 128)
+//   5000 x 1000 x 1304   26 / 20.3 / 18.3 (440)          2048 x 2048 x 2048   35 / 18.7 / 17.4    3000 x 4096 x 1024   38 / 27.4 / 21.6
+//   1000 x 12288 x 1000  38 / 31.4 / 31.5 (k split four ways, 64: twice)    1024 x 1024 x 1024   24 / 12.2 / 7.8
+//   512 x 4096 x 4096    33 / 25.1 / 19.5                200000 x 64 x 64     51 / 26.4 / 15.8    300 x 300 x 3000   17.9 / 9.6 / 5.7
 // The largest where their rounds over the units are 95 per cent full, 128 from two a unit on with k to hide their start and end, or where
 // k is long.  k is split where workgroups are few, down to 1024 bytes of it: one a unit (tiles of 64: two).
 enum class Int8Kind { kRow, kSkinny, kRing256, kRing128, kRing64 };
