@@ -174,6 +174,29 @@ __device__ __forceinline__ float activate_back(float g, float z, int act) {
     }
 }
 
+// Both for N values: one choice of the activation, whose chains of instructions then run side by side.
+template <int N>
+__device__ __forceinline__ void activate_all(float (&z)[N], int act) {
+    auto each = [&](int kind) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) z[i] = activate(z[i], kind);
+    };
+    if (act == SCNN_ACT_GELU) each(SCNN_ACT_GELU);
+    else if (act == SCNN_ACT_SILU) each(SCNN_ACT_SILU);
+    else if (act == SCNN_ACT_RELU) each(SCNN_ACT_RELU);
+}
+template <int N>
+__device__ __forceinline__ void activate_back_all(const float (&g)[N], const float (&z)[N], int act, float (&dz)[N]) {
+    auto each = [&](int kind) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) dz[i] = activate_back(g[i], z[i], kind);
+    };
+    if (act == SCNN_ACT_GELU) each(SCNN_ACT_GELU);
+    else if (act == SCNN_ACT_SILU) each(SCNN_ACT_SILU);
+    else if (act == SCNN_ACT_RELU) each(SCNN_ACT_RELU);
+    else each(SCNN_ACT_NONE);
+}
+
 // Sum over groups of P lanes of a wave (P a power of two), the same bits in each of the group's lanes.
 template <int P, typename F>
 __device__ __forceinline__ F lanes_add(F v) {

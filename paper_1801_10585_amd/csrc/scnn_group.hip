@@ -423,15 +423,20 @@ __device__ __forceinline__ Columns<kVec<T>, M ? 1 : kVec<T>> columns_of(const Gr
     return k;
 }
 template <int V, int A>
-__device__ __forceinline__ float forward_value(const Columns<V, A>& k, int i, float x, int act) {
+__device__ __forceinline__ float forward_value(const Columns<V, A>& k, int i, float x) {  // z
     const int j = A == 1 ? 0 : i;
-    return activate(__builtin_fmaf((x - k.mean[j]) - k.rest[j], k.scale[i], k.beta[i]), act);
+    return __builtin_fmaf((x - k.mean[j]) - k.rest[j], k.scale[i], k.beta[i]);
 }
 template <typename T, int A>
 __device__ __forceinline__ void forward_vector(const GroupArgs& p, const Columns<kVec<T>, A>& k, const Walk& w, long long at, VecOf<T, kVec<T>> r) {
-    VecOf<T, kVec<T>> y;
+    constexpr int V = kVec<T>;
+    VecOf<T, V> y;
+    float z[V];
 #pragma unroll
-    for (int i = 0; i < kVec<T>; ++i) y[i] = (T)forward_value<kVec<T>, A>(k, i, (float)r[i], p.act);
+    for (int i = 0; i < V; ++i) z[i] = forward_value<V, A>(k, i, (float)r[i]);
+    activate_all<V>(z, p.act);
+#pragma unroll
+    for (int i = 0; i < V; ++i) y[i] = (T)z[i];
     put((T*)p.out + at, y, A == 1 ? 0 : w.other);
 }
 // A thread's vectors from its last down to number `from`, of which the first U are there, and its odd values.
@@ -444,7 +449,7 @@ __device__ __forceinline__ void forward_down(const GroupArgs& p, const Columns<k
         const long long at = w.at + (long long)w.full * w.step;
 #pragma unroll
         for (int i = 0; i < kVec<T> - 1; ++i)
-            if (i < w.n) ((T*)p.out)[at + i] = (T)forward_value<kVec<T>, A>(c, i, (float)((const T*)p.x)[at + i], p.act);
+            if (i < w.n) ((T*)p.out)[at + i] = (T)activate(forward_value<kVec<T>, A>(c, i, (float)((const T*)p.x)[at + i]), p.act);
     }
 }
 
@@ -764,8 +769,7 @@ __device__ __forceinline__ void back_values(const BackColumns<V, A>& k, int i0, 
                 z[i] = far <= 0.0 ? 0.0f : 1.0f;  // (a NaN's slope is 1, as with activate_back)
             }
     }
-#pragma unroll
-    for (int i = 0; i < N; ++i) dz[i] = activate_back(g[i], z[i], act);
+    activate_back_all<N>(g, z, act, dz);
 }
 template <int V>
 struct BackSums { float a[V], b[V]; };  // of dz xh and dz

@@ -182,21 +182,6 @@ struct Int8Args {
     long long k_split;  // bytes of a row that a workgroup sums, a multiple of 64
 };
 
-// One choice of the activation for C values, whose chains of instructions then run side by side.
-template <int C>
-__device__ __forceinline__ void activate_all(float (&z)[C], int act) {
-    if (act == SCNN_ACT_GELU) {
-#pragma unroll
-        for (int j = 0; j < C; ++j) z[j] = activate(z[j], SCNN_ACT_GELU);
-    } else if (act == SCNN_ACT_SILU) {
-#pragma unroll
-        for (int j = 0; j < C; ++j) z[j] = activate(z[j], SCNN_ACT_SILU);
-    } else if (act == SCNN_ACT_RELU) {
-#pragma unroll
-        for (int j = 0; j < C; ++j) z[j] = activate(z[j], SCNN_ACT_RELU);
-    }
-}
-
 // Epilogue of C neighbouring columns of which w are there; everything is read before the first is written (out may be residual).
 template <typename T, int C>
 struct Beside { float scale[C]; VecOf<T, C> bias; };
