@@ -173,11 +173,11 @@ __device__ __forceinline__ Place place_of(const GroupArgs& p, const Slab& a) {
 // Column in the slab of value i of this thread, or one of the slab's where it has none.
 __device__ __forceinline__ int column_of(const GroupArgs& p, const Slab& a, const Place& t, int i) {
     int c = t.col + i;
-    if (p.l.flat) c -= quotient(c, p.l.inv_c) * p.channels;
+    c -= quotient(c, p.l.inv_c) * p.channels;  // (inv_c is 0 where rows do not run on)
     return c < 0 ? 0 : (c < a.c1 - a.c0 ? c : a.c1 - a.c0 - 1);
 }
 // Group in the slab of a column of it.
-__device__ __forceinline__ int group_of(const GroupArgs& p, int column) { return p.l.pieces > 1 ? 0 : quotient(column, p.l.inv_per); }
+__device__ __forceinline__ int group_of(const GroupArgs& p, int column) { return quotient(column, p.l.inv_per); }  // (inv_per is 0 in pieces)
 
 // A thread's vectors among the rows lo .. hi - 1: `full` whole ones, of which all threads that have any have `common` (the same in every
 // lane); behind those of rows that run on, n values.
@@ -388,11 +388,14 @@ template <typename T>
 __device__ __forceinline__ VecOf<T, kVec<T>> column_values(const GroupArgs& p, const Slab& a, const Place& t, const void* from, float none) {
     constexpr int V = kVec<T>;
     VecOf<T, V> v;
-    if (from && !p.l.flat && t.col + V <= a.c1 - a.c0) {
+    if (!from) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[i] = (T)none;
+    } else if (!p.l.flat) {
         v = take((const T*)from + a.c0 + t.col);
     } else {
 #pragma unroll
-        for (int i = 0; i < V; ++i) v[i] = from ? ((const T*)from)[a.c0 + column_of(p, a, t, i)] : (T)none;
+        for (int i = 0; i < V; ++i) v[i] = ((const T*)from)[a.c0 + column_of(p, a, t, i)];
     }
     return v;
 }
@@ -1183,8 +1186,8 @@ static GroupLayout group_layout(int channels, int per, int dtype, int threads, i
         while (1 << l.sub < v && per % (2 << l.sub) == 0) ++l.sub;
     }
     l.inv_tv = 1.0f / (float)l.tv;
-    l.inv_per = 1.0f / (float)per;
-    l.inv_c = 1.0f / (float)channels;
+    l.inv_per = l.pieces > 1 ? 0.0f : 1.0f / (float)per;
+    l.inv_c = l.flat ? 1.0f / (float)channels : 0.0f;
     l.inv_reps = 1.0 / (double)l.reps;
     return l;
 }
