@@ -161,7 +161,7 @@ __device__ __forceinline__ Slab slab_of(const GroupArgs& p) {
 
 // This thread's place: its row among a step's, its first column in the slab.  A vector that the slab's end cuts is the slab's last whole
 // one instead (it may begin before the slab), of which the first `other` values are another thread's: read, but neither
-// added nor written.  (Cut vectors taken value by value behind the others: forward 60000 x 517 bf16 in 11 groups 122 us, so 59.)
+// added nor written.  (Cut vectors taken value by value behind the others: forward 60000 x 517 bf16 in 11 groups 122 us, so 59 at the time.)
 struct Place { int row, col, other; };
 template <int V>
 __device__ __forceinline__ Place place_of(const GroupArgs& p, const Slab& a) {
@@ -616,7 +616,7 @@ __device__ __forceinline__ Two join_here(const GroupArgs& p, const Slab& a, cons
     return lanes_two(sum, o.q);
 }
 
-// Results of a block's rows, its last ones first.  643072 x 64 fp32: 52 us, 6.3 TB/s read and written, bound by memory.
+// Results of a block's rows, its last ones first.  643072 x 64 fp32: 51 us, 6.5 TB/s read and written, bound by memory.
 template <typename T, bool M>
 __global__ __launch_bounds__(kGroupThreads, 2) void k_group_apply(GroupArgs p) {
     constexpr int V = kVec<T>, A = M ? 1 : V;
@@ -665,7 +665,7 @@ __global__ __launch_bounds__(kGroupThreads, 2) void k_group_apply(GroupArgs p) {
 }
 
 // A sample's slab of whole groups by one workgroup of up to B threads, H vectors a thread in registers; what a larger sample has
-// more is read again.  One launch and one reading: 512 x 24 fp32 in 8 groups 8 us, bound by latency (a load, LDS, a store).
+// more is read again.  One launch and one reading: 512 x 24 fp32 in 8 groups 7 us, bound by latency (a load, LDS, a store).
 template <typename T, bool M, int B, int H>
 __global__ __launch_bounds__(B, 2) void k_group_one(GroupArgs p) {
     constexpr int V = kVec<T>, A = M ? 1 : V;
@@ -933,7 +933,7 @@ constexpr int kBackAhead = 2;  // vectors of x and of g
 __host__ __device__ __forceinline__ int step_values(const GroupLayout& l, int v) { return v * (l.active + 1); }
 
 // Sums of a block's rows, of columns first: dgamma and dbeta want these, and those of a group's h and h xh follow from them by gamma.
-// 209645 x 25 fp32 in 5 groups, relu: 16 us, 2.6 TB/s of x and g: eleven steps a workgroup with a start and an end around them.
+// 209645 x 25 fp32 in 5 groups, relu: 14 us, 2.9 TB/s of x and g: eleven steps a workgroup with a start and an end around them.
 template <typename T, bool M>
 __global__ __launch_bounds__(kGroupThreads, 2) void k_group_back_sums(GroupArgs p) {
     constexpr int V = kVec<T>, A = M ? 1 : V, U = kBackAhead;
@@ -1017,7 +1017,7 @@ __device__ __forceinline__ void back_columns_sum(const GroupArgs& p, long long a
 
 constexpr int kSumColumns = 16;  // (64 bytes of a place)
 
-// Gradients of a block's rows; workgroups past the blocks add the columns' sums.  209645 x 25 fp32 in 5 groups, relu: 16 us, 3.9 TB/s.
+// Gradients of a block's rows; workgroups past the blocks add the columns' sums.  209645 x 25 fp32 in 5 groups, relu: 15 us, 4.3 TB/s.
 template <typename T, bool M>
 __global__ __launch_bounds__(kGroupThreads, 2) void k_group_back(GroupArgs p) {
     constexpr int V = kVec<T>, A = M ? 1 : V, U = kBackAhead;
@@ -1058,7 +1058,7 @@ __global__ __launch_bounds__(kGroupThreads, 2) void k_group_back(GroupArgs p) {
 }
 
 // Backward by a workgroup a sample and slab, x, g and dz in registers.  cols [batch][2][channels]; with one sample dgamma and dbeta
-// themselves.  64 samples of 512 x 256 bf16 in 32 groups, silu: 17 us, 3 TB/s, bound by the instructions of silu and its slope and by
+// themselves.  64 samples of 512 x 256 bf16 in 32 groups, silu: 16 us, 3.2 TB/s, bound by the instructions of silu and its slope and by
 // what a workgroup does between its loads and its stores; k_column_sums behind it 4 us.
 template <typename T, bool M, int B, int H>
 __global__ __launch_bounds__(B, 2) void k_group_back_one(GroupArgs p) {
@@ -1160,7 +1160,7 @@ static GroupLayout group_layout(int channels, int per, int dtype, int threads, i
     const int period = channels / even;  // vectors after which a run of rows meets the same columns
     // Values of a step: of rows that run on, and of rows that each begin with a vector (loads at any address, a cut vector a row).  The
     // first where they are as many, or nearly.  us of the first / second, bf16, relu: backward 60000 x 516 112 / 88, 100000 x 260
-    // 78 / 70, 100000 x 165 66 / 55; fp32: 100000 x 258 116 / 96.
+    // 78 / 70, 100000 x 165 66 / 55; fp32: 100000 x 258 116 / 96 (all some 10 per cent shorter since).
     const int row = (channels + v - 1) / v, runs = threads / period * period * v, rows = (row >= threads ? 1 : threads / row) * channels;
     if (even < v && period <= threads && channels <= most && 8LL * runs >= 7LL * rows) {
         l.flat = 1;
@@ -1211,9 +1211,9 @@ static long long group_chunk(const GroupLayout& l, long long rows) {
 // A workgroup a sample and slab, its values in registers: 16384 of them, in 256 threads, or in 512 where workgroups are few; samples of
 // up to twice that on the average.  Only the device knows how unequal samples are that offsets name, and a large one keeps its
 // workgroup for 0.3 us a thousand values: they are up to half of it in calls of more than 2^24 values, and these up to 2^28.
-// us of this / of blocks of rows, in a graph: backward 64 samples of 512 x 256 bf16 20 / 39, forward 512 x 24 fp32 7.5 / 14; forward and
-// backward 4096 samples of about 128 x 64 bf16 39 / 105 and 87 / 141, of 16 x 512 fp32 49 / 107 and 105 / 187; 1024 equal ones of
-// 512 x 64 fp32 52 / 80 and 88 / 124.
+// us of this / of blocks of rows, in a graph, at the time: backward 64 samples of 512 x 256 bf16 20 / 39, forward 512 x 24 fp32 7.5 / 14;
+// forward and backward 4096 samples of about 128 x 64 bf16 39 / 105 and 87 / 141, of 16 x 512 fp32 49 / 107 and 105 / 187; 1024 equal
+// ones of 512 x 64 fp32 52 / 80 and 88 / 124.
 constexpr int kOneFew = 512, kOneMany = 256;
 constexpr long long kOneHeld = 16384, kOneAny = 1LL << 24, kOneAll = 1LL << 28;
 static bool group_one(long long rows, long long batch, int channels, int per, int dtype, bool equal, GroupLayout& l, int& threads) {
