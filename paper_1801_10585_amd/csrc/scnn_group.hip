@@ -793,28 +793,53 @@ __device__ __forceinline__ void apart(VecOf<T, kVec<T>> r, float (&v)[kVec<T>]) 
     for (int i = 0; i < kVec<T>; ++i) v[i] = (float)r[i];
 }
 
+// A thread's sums are fp32 over runs of kRun of its vectors and fp64 over the runs: what a sum is off by does not grow with the rows.
+// (16384 additions of 0.1 behind each other in fp32 are off by 1.5e-4 of their sum, and a gradient of equal values, whose dx is 0, has as
+// much in every dx.)
+constexpr int kRun = 32;
+
+// Sums over a thread's vectors from number k on, of which the first U are there; U divides k and kRun.
 template <typename T, int A, int U>
 __device__ __forceinline__ void back_sum_from(const GroupArgs& p, const BackColumns<kVec<T>, A>& c, const Walk& w, int k,
                                               VecOf<T, kVec<T>> (&r)[U], VecOf<T, kVec<T>> (&q)[U], BackSums<kVec<T>>& v) {
     constexpr int V = kVec<T>;
     const T *__restrict__ x = (const T*)p.x, *__restrict__ g = (const T*)p.g;
+    double a[V] = {}, b[V] = {};
     walk<U>(w, k, w.full,
-            [&](int u, int) {
+            [&](int u, int n) {
                 float xs[V], gs[V], dz[V];
                 apart<T>(r[u], xs);
                 apart<T>(q[u], gs);
                 back_add<V, A, V>(c, 0, xs, gs, p.act, v, dz);
+                if (u == U - 1 && (n & (kRun - 1)) == kRun - 1)
+#pragma unroll
+                    for (int i = 0; i < V; ++i) {
+                        a[i] += (double)v.a[i];
+                        b[i] += (double)v.b[i];
+                        v.a[i] = v.b[i] = 0.0f;
+                    }
             },
             [&](int u, int n) {
                 r[u] = take(x + position<false>(w, n));
                 q[u] = take(g + position<false>(w, n));
             });
+    if (w.full >= kRun)
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            v.a[i] = (float)(a[i] + (double)v.a[i]);
+            v.b[i] = (float)(b[i] + (double)v.b[i]);
+        }
+}
+// And over its odd values.
+template <typename T, int A>
+__device__ __forceinline__ void back_sum_odd(const GroupArgs& p, const BackColumns<kVec<T>, A>& c, const Walk& w, BackSums<kVec<T>>& v) {
+    constexpr int V = kVec<T>;
     if (w.n) {
         const long long at = w.at + (long long)w.full * w.step;
 #pragma unroll
         for (int i = 0; i < V - 1; ++i)
             if (i < w.n) {
-                const float xs[1] = {(float)x[at + i]}, gs[1] = {(float)g[at + i]};
+                const float xs[1] = {(float)((const T*)p.x)[at + i]}, gs[1] = {(float)((const T*)p.g)[at + i]};
                 float dz[1];
                 back_add<V, A, 1>(c, i, xs, gs, p.act, v, dz);
             }
@@ -964,7 +989,9 @@ __global__ __launch_bounds__(kGroupThreads, 2) void k_group_back_sums(GroupArgs 
         fetch<T, U, false>((const T*)p.x, w, 0, x);
         fetch<T, U, false>((const T*)p.g, w, 0, g);
         BackSums<V> v = {};
-        back_sum_from<T, A, U>(p, back_columns<T, M>(p, a, t, f, b), w, 0, x, g, v);
+        const BackColumns<V, A> c = back_columns<T, M>(p, a, t, f, b);
+        back_sum_from<T, A, U>(p, c, w, 0, x, g, v);
+        back_sum_odd<T, A>(p, c, w, v);
         add_columns<V>(p, a, t, v, s_all, s_col);
         if (p.cols)
             for (int c = threadIdx.x; c < wide; c += blockDim.x) {
@@ -1092,9 +1119,15 @@ __global__ __launch_bounds__(B, 2) void k_group_back_one(GroupArgs p) {
     VecOf<T, V> held[H], grad[H];
     const Affine<T> f = affine_of<T>(p, a, t);
     const BackColumns<V, A> k = back_columns<T, M>(p, a, t, f, b);
+    BackSums<V> v = {};
+    VecOf<T, V> more[2], more_g[2];
+    if (w.full > H) {  // (what is read again comes first: its sums in fp64 and the held values would not both fit the registers)
+        fetch<T, 2, false>(x, w, H, more);
+        fetch<T, 2, false>(g, w, H, more_g);
+        back_sum_from<T, A, 2>(p, k, w, H, more, more_g, v);
+    }
     fetch<T, H, false>(x, w, 0, held);
     fetch<T, H, false>(g, w, 0, grad);
-    BackSums<V> v = {};
     float dz[H][V];
 #pragma unroll
     for (int h = 0; h < H; ++h)
@@ -1105,10 +1138,7 @@ __global__ __launch_bounds__(B, 2) void k_group_back_one(GroupArgs p) {
             back_add<V, A, V>(k, 0, xs, gs, p.act, v, dz[h]);
             __builtin_amdgcn_sched_barrier(0);
         }
-    VecOf<T, V> more[2], more_g[2];
-    fetch<T, 2, false>(x, w, H, more);
-    fetch<T, 2, false>(g, w, H, more_g);
-    back_sum_from<T, A, 2>(p, k, w, H, more, more_g, v);
+    back_sum_odd<T, A>(p, k, w, v);
     add_columns<V>(p, a, t, v, s_all, s_col);
     for (int c = threadIdx.x; c < wide; c += blockDim.x) give(c, s_col[c], s_col[wide + c]);
     if (!p.out) return;
