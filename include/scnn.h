@@ -401,9 +401,10 @@ int quantize_rows(int dtype, const void* x, int64_t rows, const int64_t* rows_de
 int quantize_weight(int dtype, const void* w, int64_t c_in, int64_t c_out, int8_t* q, float* scale, void* hip_stream);
 
 /* The layer:  z = (sum over k of q[r, k] w[n, k]) x_scale[r] w_scale[n] + bias,
- * out = act(z) + residual, the sums exact.  w, w_scale as quantize_weight gave
- * them; bias [c_out], residual [rows, c_out] (nullable) and out [rows, c_out] of
- * `dtype`; out and residual may be the same array.  With x_scale x holds 8-bit
+ * out = act(z) + residual, the sums exact.  z is fp32: infinite where its value
+ * is past fp32's range, and only there (gelu and silu of -infinity give NaN).
+ * w, w_scale as quantize_weight gave them; bias [c_out], residual [rows, c_out]
+ * (nullable) and out [rows, c_out] of `dtype`; out and residual may be the same array.  With x_scale x holds 8-bit
  * rows and their steps, as quantize_rows gave them; with x_scale null x is
  * [rows, c_in] of `dtype` and is brought to 8 bits within the call, with the same
  * result.  `given` of the query: 1 with x_scale, else 0.  Repeated calls give

@@ -217,9 +217,12 @@ __device__ __forceinline__ void finish(const Int8Args& p, long long m, long long
     VecOf<T, C> y;
     const long long at = m * p.n + n;
     float z[C];
+    // (|sum| < 2^31: times a scale above 2^96 it may leave fp32 where z does not; by powers of two, so that every rounding is as before)
+    const bool far = __builtin_fabsf(xs) > 0x1p96f;
+    const float down = far ? xs * 0x1p-64f : xs, up = far ? 0x1p64f : 1.0f;
 #pragma unroll
     for (int j = 0; j < C; ++j) {
-        z[j] = (float)sum[j] * xs * b.scale[j];
+        z[j] = (float)sum[j] * down * b.scale[j] * up;
         if (p.bias) z[j] += (float)b.bias[j];
     }
     activate_all<C>(z, p.act);
