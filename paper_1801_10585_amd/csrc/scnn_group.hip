@@ -10,7 +10,8 @@
 // read twice, in two launches: sums over blocks of rows (k_group_sums, k_group_back_sums), then results (k_group_apply,
 // k_group_back), every workgroup joining the sums of the samples that it meets; where these are many a launch between
 // joins them (k_group_join).  Samples of few values are done by a workgroup each, which keeps its rows in registers
-// (k_group_one, k_group_back_one).
+// (k_group_one, k_group_back_one).  Only the device knows the sizes of samples that offsets name: where one of them could hold a workgroup
+// up, it leaves those above `over` rows to the blocks of rows, which then take no others.
 //
 // Blocks of rows are cut without regard to the samples, whose sizes only the device knows: block i keeps one set of sums for
 // every sample that it meets, in place i + b (along the rows either i or b grows by one, so that no place is taken twice), and
@@ -45,11 +46,12 @@ struct GroupArgs {
     const long long* offsets;
     long long each;              // rows of a sample where offsets is null
     long long rows, chunk;       // chunk: rows of a block
+    long long over;              // samples of more rows are the blocks', the others a workgroup's each; 0: no such division
     long long batch, blocks, places, sum_blocks;
     double inv_each, inv_chunk;
     int channels, groups, per, act;
     float eps;
-    float* cols;                 // backward: [places][2][channels], sums of dz xh and dz over a place's rows; null: not wanted
+    float* cols;                 // backward: [places][2][channels], sums of dz xh and dz over a place's rows ([blocks] with `over`); null: not wanted
     void* part;                  // [places][groups * pieces]: forward {sum d, sum d^2} in fp64, backward {sum h, sum h xh} in fp32
     void* stat;                  // [batch][groups] of k_group_join; null: joined where they are used
     GroupLayout l;
@@ -126,21 +128,28 @@ __device__ __forceinline__ long long sample_at(const Bounds& s, long long r) {
     return uniform(b < s.batch ? b : s.batch - 1);
 }
 
-// Rows of block i, and the samples whose sums it keeps.
+// Rows of block i, and the samples whose sums it keeps.  (Of those above `over` rows, which is no less than a block's, a block holds an end
+// at least: only the samples of its first and its last row are looked at.)
 struct Block { long long r0, r1, b0, b1; };
+template <bool OVER>
 __device__ __forceinline__ Block block_of(const GroupArgs& p, const Bounds& s, long long i) {
     Block k;
     k.r0 = i * p.chunk;
     k.r1 = k.r0 + p.chunk < p.rows ? k.r0 + p.chunk : p.rows;
-    k.b0 = i == 0 ? 0 : sample_at(s, k.r0);
-    k.b1 = i + 1 == p.blocks ? p.batch - 1 : sample_at(s, k.r1);
+    k.b0 = i == 0 && !OVER ? 0 : sample_at(s, k.r0);
+    k.b1 = OVER ? sample_at(s, k.r1 - 1) : (i + 1 == p.blocks ? p.batch - 1 : sample_at(s, k.r1));
     return k;
 }
+__device__ __forceinline__ bool any_over(const GroupArgs& p, const Bounds& s, const Block& k) {
+    const Rows a = rows_of_sample(s, k.b0), b = rows_of_sample(s, k.b1);
+    return a.end - a.first > p.over || b.end - b.first > p.over;
+}
+template <bool OVER>
+__device__ __forceinline__ long long next_sample(const Block& k, long long b) { return OVER && b < k.b1 ? k.b1 : b + 1; }
 
-// Columns of this workgroup's slab, its first group, the number of its groups and their width in it.
+// Columns of slab s, its first group, the number of its groups and their width in it.
 struct Slab { int c0, c1, j0, ng, w; };
-__device__ __forceinline__ Slab slab_of(const GroupArgs& p) {
-    const int s = blockIdx.y;
+__device__ __forceinline__ Slab slab_of(const GroupArgs& p, int s) {
     if (p.l.slabs == 1) return {0, p.channels, 0, p.groups, p.per};
     Slab a;
     if (p.l.pieces > 1) {
@@ -460,19 +469,19 @@ constexpr int kAhead = 4;  // vectors of x that a thread of the blocks' kernels 
 
 // Sums of a block's rows.  643072 x 64 fp32 in 8 groups: 25 us, 6.5 TB/s of x (caches hold some of it), bound by memory; the fp64 sums of
 // 23651 x 16 bf16 take 9 us, where a workgroup has one step: its start, two loads behind one another, LDS.
-template <typename T, bool M>
-__global__ __launch_bounds__(kGroupThreads, 2) void k_group_sums(GroupArgs p) {
+template <typename T, bool M, bool OVER>
+__device__ __forceinline__ void block_sums(const GroupArgs& p, long long i, int slab, char* s_step) {
     constexpr int V = kVec<T>;
-    extern __shared__ __align__(16) char s_step[];
-    const long long i = block_id<kGroupThreads>();
     if (i >= p.blocks) return;
     const Bounds s = bounds_of(p);
-    const Slab a = slab_of(p);
+    const Block k = block_of<OVER>(p, s, i);
+    if (OVER && !any_over(p, s, k)) return;
+    const Slab a = slab_of(p, slab);
     const Place t = place_of<V>(p, a);
-    const Block k = block_of(p, s, i);
-    const int to = p.l.pieces > 1 ? (int)blockIdx.y : a.j0;
-    for (long long b = k.b0; b <= k.b1; ++b) {
+    const int to = p.l.pieces > 1 ? slab : a.j0;
+    for (long long b = k.b0; b <= k.b1; b = next_sample<OVER>(k, b)) {
         const Rows r = rows_of_sample(s, b);
+        if (OVER && r.end - r.first <= p.over) continue;
         const long long lo = r.first > k.r0 ? r.first : k.r0, hi = r.end < k.r1 ? r.end : k.r1;
         Two* const part = (Two*)p.part + (i + b) * p.groups * p.l.pieces + to;
         if (hi <= lo) {
@@ -491,6 +500,11 @@ __global__ __launch_bounds__(kGroupThreads, 2) void k_group_sums(GroupArgs p) {
         add_groups<T, M>(p, a, t, v, (Two*)s_step, [&](int j, Two sum) { part[j] = sum; });
         if (b < k.b1) __syncthreads();
     }
+}
+template <typename T, bool M>
+__global__ __launch_bounds__(kGroupThreads, 2) void k_group_sums(GroupArgs p) {
+    extern __shared__ __align__(16) char s_step[];
+    block_sums<T, M, false>(p, block_id<kGroupThreads>(), blockIdx.y, s_step);
 }
 
 // Sum over the Q threads (a power of two up to 256) of each of a workgroup's sets; all 256 threads call it.
@@ -526,12 +540,13 @@ __global__ __launch_bounds__(256) void k_group_join(GroupArgs p, int q) {
     __shared__ Two s_wave[4];
     const long long id = block_id<256>() * (256 / q) + threadIdx.x / q;
     const int in = threadIdx.x & (q - 1);
-    const bool live = id < p.batch * p.groups;
+    bool live = id < p.batch * p.groups;
     const long long b = live ? id / p.groups : 0;
     const int j = (int)(live ? id - b * p.groups : 0);
     const Bounds s = {p.offsets, p.each, p.rows, p.batch, 0, p.inv_each, false};  // (b differs from lane to lane)
     Rows r = {first_row(s, b), first_row(s, b + 1)};
     if (r.end < r.first) r.end = r.first;
+    live = live && (p.over == 0 || r.end - r.first > p.over);
     Two sum = {0.0, 0.0};
     if (live && r.end > r.first) {
         int count;
@@ -617,7 +632,7 @@ __device__ __forceinline__ Two join_here(const GroupArgs& p, const Slab& a, cons
 }
 
 // Results of a block's rows, its last ones first.  643072 x 64 fp32: 51 us, 6.5 TB/s read and written, bound by memory.
-template <typename T, bool M>
+template <typename T, bool M, bool OVER>
 __global__ __launch_bounds__(kGroupThreads, 2) void k_group_apply(GroupArgs p) {
     constexpr int V = kVec<T>, A = M ? 1 : V;
     __shared__ Two s_two[kGroupThreads];
@@ -625,13 +640,15 @@ __global__ __launch_bounds__(kGroupThreads, 2) void k_group_apply(GroupArgs p) {
     const long long i = block_id<kGroupThreads>();
     if (i >= p.blocks) return;
     const Bounds s = bounds_of(p);
-    const Slab a = slab_of(p);
+    const Block k = block_of<OVER>(p, s, i);
+    if (OVER && !any_over(p, s, k)) return;
+    const Slab a = slab_of(p, blockIdx.y);
     const Place t = place_of<V>(p, a);
     const Affine<T> f = affine_of<T>(p, a, t);
     const Joiner o = joiner_of(a);
-    const Block k = block_of(p, s, i);
-    for (long long b = k.b0; b <= k.b1; ++b) {
+    for (long long b = k.b0; b <= k.b1; b = next_sample<OVER>(k, b)) {
         const Rows r = rows_of_sample(s, b);
+        if (OVER && r.end - r.first <= p.over) continue;
         const long long lo = r.first > k.r0 ? r.first : k.r0, hi = r.end < k.r1 ? r.end : k.r1, id = b * p.groups + a.j0;
         if (!p.stat && r.end == r.first)  // (by every workgroup that passes the empty sample)
             for (int j = threadIdx.x; j < a.ng; j += blockDim.x) {
@@ -666,16 +683,14 @@ __global__ __launch_bounds__(kGroupThreads, 2) void k_group_apply(GroupArgs p) {
 
 // A sample's slab of whole groups by one workgroup of up to B threads, H vectors a thread in registers; what a larger sample has
 // more is read again.  One launch and one reading: 512 x 24 fp32 in 8 groups 7 us, bound by latency (a load, LDS, a store).
-template <typename T, bool M, int B, int H>
-__global__ __launch_bounds__(B, 2) void k_group_one(GroupArgs p) {
+template <typename T, bool M, int H, bool OVER>
+__device__ __forceinline__ void one_forward(const GroupArgs& p, long long b, char* s_step) {
     constexpr int V = kVec<T>, A = M ? 1 : V;
-    extern __shared__ __align__(16) char s_step[];
     GroupStat* const s_stat = (GroupStat*)s_step;
     Two* const s_all = (Two*)(s_stat + p.l.wide / p.per);
-    const long long b = block_id<B>();
     if (b >= p.batch) return;
     const Bounds s = {p.offsets, p.each, p.rows, p.batch, 0, p.inv_each, false};
-    const Slab a = slab_of(p);
+    const Slab a = slab_of(p, blockIdx.y);
     const Place t = place_of<V>(p, a);
     const Rows r = rows_of_sample(s, b);
     const long long id = b * p.groups + a.j0;
@@ -686,6 +701,7 @@ __global__ __launch_bounds__(B, 2) void k_group_one(GroupArgs p) {
         }
         return;
     }
+    if (OVER && r.end - r.first > p.over) return;
     const T* __restrict__ x = (const T*)p.x;
     const Walk w = walk_of<V>(p, a, t, r.first, r.end);
     float near[kSums<T, M>];
@@ -721,6 +737,26 @@ __global__ __launch_bounds__(B, 2) void k_group_one(GroupArgs p) {
         }
     if (w.full > H) fetch<T, 2, true>(x, w, 0, more);
     forward_down<T, A, 2>(p, c, w, H, more);
+}
+template <typename T, bool M, int B, int H>
+__global__ __launch_bounds__(B, 2) void k_group_one(GroupArgs p) {
+    extern __shared__ __align__(16) char s_step[];
+    one_forward<T, M, H, false>(p, block_id<B>(), s_step);
+}
+// Number of a workgroup among those behind the ones that take a sample and slab each, which lie along the grid's x and y: in further columns
+// of the grid or in further rows; below 0: it is one of these.
+__device__ __forceinline__ long long number_behind(const GroupArgs& p, long long id) {
+    const int y = blockIdx.y;
+    if (y >= p.l.slabs) return (y - p.l.slabs) * p.batch + id;
+    return id < p.batch ? -1 : (id - p.batch) * p.l.slabs + y;
+}
+// Samples of up to `over` rows; workgroups behind theirs add the blocks' sums of the others.
+template <typename T, bool M, int B, int H>
+__global__ __launch_bounds__(B, 2) void k_group_one_sums(GroupArgs p, GroupArgs blocks) {
+    extern __shared__ __align__(16) char s_step[];
+    const long long id = block_id<B>(), at = number_behind(p, id);
+    if (at < 0) one_forward<T, M, H, true>(p, id, s_step);
+    else if (at < blocks.blocks * blocks.l.slabs) block_sums<T, M, true>(blocks, (unsigned)at / blocks.l.slabs, (unsigned)at % blocks.l.slabs, s_step);
 }
 
 // ------------------------------------------------------------------ backward
@@ -959,26 +995,27 @@ __host__ __device__ __forceinline__ int step_values(const GroupLayout& l, int v)
 
 // Sums of a block's rows, of columns first: dgamma and dbeta want these, and those of a group's h and h xh follow from them by gamma.
 // 209645 x 25 fp32 in 5 groups, relu: 14 us, 2.9 TB/s of x and g: eleven steps a workgroup with a start and an end around them.
-template <typename T, bool M>
-__global__ __launch_bounds__(kGroupThreads, 2) void k_group_back_sums(GroupArgs p) {
+template <typename T, bool M, bool OVER>
+__device__ __forceinline__ void block_back_sums(const GroupArgs& p, long long i, int slab, char* s_step) {
     constexpr int V = kVec<T>, A = M ? 1 : V, U = kBackAhead;
-    extern __shared__ __align__(16) char s_step[];
     float2* const s_all = (float2*)s_step;
     float* const s_col = (float*)(s_all + step_values(p.l, V));
-    const long long i = block_id<kGroupThreads>();
     if (i >= p.blocks) return;
     const Bounds s = bounds_of(p);
-    const Slab a = slab_of(p);
+    const Slab a = slab_of(p, slab);
     const Place t = place_of<V>(p, a);
     const Affine<T> f = affine_of<T>(p, a, t);
-    const Block k = block_of(p, s, i);
-    const int wide = a.c1 - a.c0, to = p.l.pieces > 1 ? (int)blockIdx.y : a.j0;
-    for (long long b = k.b0; b <= k.b1; ++b) {
+    const Block k = block_of<OVER>(p, s, i);
+    const int wide = a.c1 - a.c0, to = p.l.pieces > 1 ? slab : a.j0;
+    bool first = true;
+    for (long long b = k.b0; b <= k.b1; b = next_sample<OVER>(k, b)) {
         const Rows r = rows_of_sample(s, b);
+        if (OVER && r.end - r.first <= p.over) continue;
         const long long lo = r.first > k.r0 ? r.first : k.r0, hi = r.end < k.r1 ? r.end : k.r1;
-        float* const cols = p.cols + (i + b) * 2 * p.channels + a.c0;
+        float* const cols = p.cols + (OVER ? i : i + b) * 2 * p.channels + a.c0;
         float2* const part = (float2*)p.part + (i + b) * p.groups * p.l.pieces + to;
         if (hi <= lo) {
+            if (OVER) continue;
             if (p.cols)
                 for (int c = threadIdx.x; c < wide; c += blockDim.x) cols[c] = cols[p.channels + c] = 0.0f;
             for (int j = threadIdx.x; j < a.ng; j += blockDim.x) part[j] = make_float2(0.0f, 0.0f);
@@ -995,12 +1032,20 @@ __global__ __launch_bounds__(kGroupThreads, 2) void k_group_back_sums(GroupArgs 
         add_columns<V>(p, a, t, v, s_all, s_col);
         if (p.cols)
             for (int c = threadIdx.x; c < wide; c += blockDim.x) {
-                cols[c] = s_col[c];
-                cols[p.channels + c] = s_col[wide + c];
+                cols[c] = OVER && !first ? cols[c] + s_col[c] : s_col[c];
+                cols[p.channels + c] = OVER && !first ? cols[p.channels + c] + s_col[wide + c] : s_col[wide + c];
             }
+        first = false;
         if (p.out) back_groups<T>(p, a, s_col, [&](int j, Two sum) { part[j] = make_float2((float)sum.a, (float)sum.b); });
         if (b < k.b1) __syncthreads();
     }
+    if (OVER && p.cols && first)
+        for (int c = threadIdx.x; c < wide; c += blockDim.x) p.cols[i * 2 * p.channels + a.c0 + c] = p.cols[(i * 2 + 1) * p.channels + a.c0 + c] = 0.0f;
+}
+template <typename T, bool M>
+__global__ __launch_bounds__(kGroupThreads, 2) void k_group_back_sums(GroupArgs p) {
+    extern __shared__ __align__(16) char s_step[];
+    block_back_sums<T, M, false>(p, block_id<kGroupThreads>(), blockIdx.y, s_step);
 }
 
 // 4 N columns of the places' sums of dz xh and dz by one workgroup, four neighbours a thread.
@@ -1042,27 +1087,30 @@ __device__ __forceinline__ void back_columns_sum(const GroupArgs& p, long long a
     if (to) to[out < p.channels ? out : out - p.channels] = (T)(float)all;
 }
 
-constexpr int kSumColumns = 16;  // (64 bytes of a place)
+// Columns of a workgroup that adds them: 64 bytes of a place, or 16 where these are many.
+template <bool OVER> constexpr int kSumColumns = OVER ? 4 : 16;
 
 // Gradients of a block's rows; workgroups past the blocks add the columns' sums.  209645 x 25 fp32 in 5 groups, relu: 15 us, 4.3 TB/s.
-template <typename T, bool M>
+template <typename T, bool M, bool OVER>
 __global__ __launch_bounds__(kGroupThreads, 2) void k_group_back(GroupArgs p) {
     constexpr int V = kVec<T>, A = M ? 1 : V, U = kBackAhead;
     __shared__ Two s_two[kGroupThreads];
     __shared__ float2 s_stat[kHereGroups];
     const long long i = block_id<kGroupThreads>();
     if (i >= p.blocks) {
-        if (blockIdx.y == 0 && i - p.blocks < p.sum_blocks) back_columns_sum<T, kSumColumns / 4>(p, i - p.blocks, (double*)s_two);
+        if (blockIdx.y == 0 && i - p.blocks < p.sum_blocks) back_columns_sum<T, kSumColumns<OVER> / 4>(p, i - p.blocks, (double*)s_two);
         return;
     }
     const Bounds s = bounds_of(p);
-    const Slab a = slab_of(p);
+    const Block k = block_of<OVER>(p, s, i);
+    if (OVER && !any_over(p, s, k)) return;
+    const Slab a = slab_of(p, blockIdx.y);
     const Place t = place_of<V>(p, a);
     const Affine<T> f = affine_of<T>(p, a, t);
     const Joiner o = joiner_of(a);
-    const Block k = block_of(p, s, i);
-    for (long long b = k.b0; b <= k.b1; ++b) {
+    for (long long b = k.b0; b <= k.b1; b = next_sample<OVER>(k, b)) {
         const Rows r = rows_of_sample(s, b);
+        if (OVER && r.end - r.first <= p.over) continue;
         const long long lo = r.first > k.r0 ? r.first : k.r0, hi = r.end < k.r1 ? r.end : k.r1;
         if (hi <= lo) continue;
         const Walk w = walk_of<V>(p, a, t, lo, hi);
@@ -1087,17 +1135,15 @@ __global__ __launch_bounds__(kGroupThreads, 2) void k_group_back(GroupArgs p) {
 // Backward by a workgroup a sample and slab, x, g and dz in registers.  cols [batch][2][channels]; with one sample dgamma and dbeta
 // themselves.  64 samples of 512 x 256 bf16 in 32 groups, silu: 16 us, 3.2 TB/s, bound by the instructions of silu and its slope and by
 // what a workgroup does between its loads and its stores; k_column_sums behind it 4 us.
-template <typename T, bool M, int B, int H>
-__global__ __launch_bounds__(B, 2) void k_group_back_one(GroupArgs p) {
+template <typename T, bool M, int H, bool OVER>
+__device__ __forceinline__ void one_back(const GroupArgs& p, long long b, char* s_step) {
     constexpr int V = kVec<T>, A = M ? 1 : V;
-    extern __shared__ __align__(16) char s_step[];
     float2* const s_all = (float2*)s_step;
     float* const s_col = (float*)(s_all + step_values(p.l, V));
     float2* const s_stat = s_all;  // (when the columns' sums are done)
-    const long long b = block_id<B>();
     if (b >= p.batch) return;
     const Bounds s = {p.offsets, p.each, p.rows, p.batch, 0, p.inv_each, false};
-    const Slab a = slab_of(p);
+    const Slab a = slab_of(p, blockIdx.y);
     const Place t = place_of<V>(p, a);
     const Rows r = rows_of_sample(s, b);
     const int wide = a.c1 - a.c0;
@@ -1110,7 +1156,7 @@ __global__ __launch_bounds__(B, 2) void k_group_back_one(GroupArgs p) {
             p.cols[(b * 2 + 1) * p.channels + a.c0 + c] = db;
         }
     };
-    if (r.end == r.first) {
+    if (r.end == r.first || (OVER && r.end - r.first > p.over)) {
         for (int c = threadIdx.x; c < wide; c += blockDim.x) give(c, 0.0f, 0.0f);
         return;
     }
@@ -1163,6 +1209,19 @@ __global__ __launch_bounds__(B, 2) void k_group_back_one(GroupArgs p) {
         fetch<T, 2, true>(g, w, 0, more_g);
     }
     back_down<T, A, 2>(p, k, m, w, H, more, more_g);
+}
+template <typename T, bool M, int B, int H>
+__global__ __launch_bounds__(B, 2) void k_group_back_one(GroupArgs p) {
+    extern __shared__ __align__(16) char s_step[];
+    one_back<T, M, H, false>(p, block_id<B>(), s_step);
+}
+// As k_group_one_sums.
+template <typename T, bool M, int B, int H>
+__global__ __launch_bounds__(B, 2) void k_group_back_one_sums(GroupArgs p, GroupArgs blocks) {
+    extern __shared__ __align__(16) char s_step[];
+    const long long id = block_id<B>(), at = number_behind(p, id);
+    if (at < 0) one_back<T, M, H, true>(p, id, s_step);
+    else if (at < blocks.blocks * blocks.l.slabs) block_back_sums<T, M, true>(blocks, (unsigned)at / blocks.l.slabs, (unsigned)at % blocks.l.slabs, s_step);
 }
 
 // offsets[b]: the rows whose sample index is below b, a wave a sample.
@@ -1239,8 +1298,8 @@ static long long group_chunk(const GroupLayout& l, long long rows) {
 }
 
 // A workgroup a sample and slab, its values in registers: 16384 of them, in 256 threads, or in 512 where workgroups are few; samples of
-// up to twice that on the average.  Only the device knows how unequal samples are that offsets name, and a large one keeps its
-// workgroup for 0.3 us a thousand values: they are up to half of it in calls of more than 2^24 values, and these up to 2^28.
+// up to twice that on the average.  Only the device knows how unequal samples are that offsets name, and a workgroup takes 0.3 us a
+// thousand values: they are up to half of it in calls of more than 2^24 values, and these up to 2^28 (and see kOneMost).
 // us of this / of blocks of rows, in a graph, at the time: backward 64 samples of 512 x 256 bf16 20 / 39, forward 512 x 24 fp32 7.5 / 14;
 // forward and backward 4096 samples of about 128 x 64 bf16 39 / 105 and 87 / 141, of 16 x 512 fp32 49 / 107 and 105 / 187; 1024 equal
 // ones of 512 x 64 fp32 52 / 80 and 88 / 124.
@@ -1274,13 +1333,27 @@ static bool group_one(long long rows, long long batch, int channels, int per, in
     return l.pieces == 1 && l.slabs <= 65535;  // (a launch's second axis)
 }
 
-struct GroupSpace { GroupLayout l; long long blocks, chunk, places; size_t part, cols, stat, total; bool one, joined; int threads; };
+// With offsets, samples above `over` rows are left to the blocks: their sums are added beside the others' work, and one more launch ends at
+// once where there are none.  A workgroup keeps up to kOneMost values, 20 us of it, or as many as a block's rows; calls of up to twice as many
+// are not divided.  us in a graph of one sample with all rows (a workgroup for it) / of equal ones (undivided): 64 samples in 131072 x 16
+// fp32 forward 16 (442) / 15 (12.7), backward 22 (679) / 23 (19.9); 512 in 262144 x 64 bf16 29 (2770) / 23 (19.7) and 42 (3630) / 44 (39.6);
+// 32768 in 4194304 x 64 bf16 348 (85700) / 263 (230) and 652 (136600) / 615 (584).
+constexpr long long kOneMost = 65536;
+
+struct GroupSpace {
+    GroupLayout one_l, l;  // of a workgroup a sample, of blocks
+    long long blocks, chunk, places, over;
+    size_t part, cols, stat, total;
+    bool one, joined;
+    int threads;
+    bool any_blocks() const { return !one || over; }
+};
 static GroupSpace group_space(long long rows, long long batch, int channels, int groups, int dtype, bool equal, bool back) {
     GroupSpace s = {};
     const int per = channels / groups;
-    s.one = group_one(rows, batch, channels, per, dtype, equal, s.l, s.threads);
-    if (s.one) {
-        s.places = batch;
+    s.one = group_one(rows, batch, channels, per, dtype, equal, s.one_l, s.threads);
+    const bool divided = s.one && !equal && rows * s.one_l.wide > 2 * kOneMost;
+    if (s.one && !divided) {
         if (back && batch > 1) s.total = (size_t)round_up(batch * channels * 8, 256);
         return s;
     }
@@ -1288,10 +1361,12 @@ static GroupSpace group_space(long long rows, long long batch, int channels, int
     s.chunk = group_chunk(s.l, rows);
     s.blocks = rows < 1 ? 1 : (rows + s.chunk - 1) / s.chunk;
     s.places = s.blocks + batch - 1;
+    if (divided) s.over = s.chunk > kOneMost / s.one_l.wide ? s.chunk : kOneMost / s.one_l.wide;
     const int ng = s.l.wide / per;  // (of a slab)
-    s.joined = s.l.pieces > 1 || ng > kHereGroups || (s.blocks / batch + 1) * ng > 2048;
-    s.cols = (size_t)round_up(s.places * groups * s.l.pieces * (back ? 8LL : 16LL), 256);
-    s.stat = s.cols + (back ? (size_t)round_up(s.places * channels * 8LL, 256) : 0);
+    s.joined = s.l.pieces > 1 || ng > kHereGroups || (!divided && (s.blocks / batch + 1) * ng > 2048);
+    // (divided, the columns' sums of samples and of blocks lie behind each other)
+    if (back) s.part = (size_t)round_up((divided ? batch + s.blocks : s.places) * channels * 8LL, 256);
+    s.stat = s.part + (size_t)round_up(s.places * groups * s.l.pieces * (back ? 8LL : 16LL), 256);
     s.total = s.stat + (s.joined ? (size_t)round_up(batch * groups * (back ? 8LL : 16LL), 256) : 0);
     return s;
 }
@@ -1302,7 +1377,9 @@ size_t group_norm_bytes(int dtype, long long rows, long long batch, int channels
     return equal > any ? equal : any;
 }
 
-static GroupArgs group_args(int dtype, const GroupCall& c, bool back, GroupSpace& s) {
+// Arguments of the workgroups that take a sample each, and of the blocks'.
+struct GroupBoth { GroupArgs one, blocks; };
+static GroupBoth group_args(const GroupCall& c, bool back, const GroupSpace& s) {
     GroupArgs p = {};
     p.x = c.x; p.g = c.g; p.gamma = c.gamma; p.beta = c.beta;
     p.out = back ? c.dx : c.out;
@@ -1313,15 +1390,19 @@ static GroupArgs group_args(int dtype, const GroupCall& c, bool back, GroupSpace
     p.each = c.rows / c.batch;
     p.channels = c.channels; p.groups = c.groups; p.per = c.channels / c.groups; p.act = c.act;
     p.eps = c.eps;
-    s = group_space(c.rows, c.batch, c.channels, c.groups, dtype, c.offsets == nullptr, back);
-    p.l = s.l;
-    p.chunk = s.chunk; p.blocks = s.blocks; p.places = s.places;
+    p.over = s.over;
     p.inv_each = p.each > 0 ? 1.0 / (double)p.each : 0.0;
-    p.inv_chunk = s.one ? 0.0 : 1.0 / (double)s.chunk;
-    p.part = (char*)c.workspace + s.part;
-    if (c.dgamma || c.dbeta) p.cols = (float*)((char*)c.workspace + s.cols);
-    if (s.joined) p.stat = (char*)c.workspace + s.stat;
-    return p;
+    if (c.dgamma || c.dbeta) p.cols = (float*)c.workspace;
+    GroupBoth a = {p, p};
+    a.one.l = s.one_l;
+    if (!s.any_blocks()) return a;
+    a.blocks.l = s.l;
+    a.blocks.chunk = s.chunk; a.blocks.blocks = s.blocks; a.blocks.places = s.places;
+    a.blocks.inv_chunk = 1.0 / (double)s.chunk;
+    a.blocks.part = (char*)c.workspace + s.part;
+    if (p.cols && s.over) a.blocks.cols = p.cols + c.batch * 2 * c.channels;
+    if (s.joined) a.blocks.stat = (char*)c.workspace + s.stat;
+    return a;
 }
 
 // A launch that joins the places' sums, about as many threads for a sample's group as it has places.
@@ -1333,55 +1414,89 @@ static void group_join(const GroupArgs& p, hipStream_t s) {
     hipLaunchKernelGGL((k_group_join<T, BACK>), grid_of<256>((p.batch * p.groups + 256 / q - 1) / (256 / q)), dim3(256), 0, s, p, q);
 }
 
-template <typename T, bool M>
-static hipError_t group_fwd(int dtype, const GroupCall& c, const GroupArgs& p, const GroupSpace& at, hipStream_t s) {
+// The first launch where a workgroup takes a sample: alone, or with the blocks' sums of longer ones behind it (in rows of the grid, which are
+// started last, where there are several already: 64 samples in 19200 x 64 fp32 backward 13.3 us, in columns 15.2).
+template <typename F>
+static void one_launch(const GroupBoth& p, const GroupSpace& at, unsigned one, unsigned sums, F launch) {
+    const unsigned t1 = group_threads(p.one.l);
+    const long long batch = p.one.batch;
+    const int y = p.one.l.slabs;
+    if (!at.over) return launch(batch, y, dim3(t1), one);
+    const unsigned t2 = group_threads(p.blocks.l);
+    const long long more = at.blocks * p.blocks.l.slabs, rows = (more + batch - 1) / batch;
+    const bool below = y > 1 && y + rows <= 65535 && batch <= 1 << 20;
+    launch(batch + (below ? 0 : (more + y - 1) / y), below ? y + (int)rows : y, dim3(t1 > t2 ? t1 : t2), sums > one ? sums : one);
+}
+template <typename T, bool M, int B, int H>
+static void one_fwd(const GroupBoth& p, const GroupSpace& at, hipStream_t s) {
     constexpr int V = kVec<T>;
-    const dim3 threads(group_threads(p.l));
+    one_launch(p, at, one_lds(p.one.l, V, p.one.per), at.over ? sums_lds(p.blocks.l, V) : 0, [&](long long n, int y, dim3 threads, unsigned lds) {
+        if (at.over) hipLaunchKernelGGL((k_group_one_sums<T, M, B, H>), grid_of<B>(n, y), threads, lds, s, p.one, p.blocks);
+        else hipLaunchKernelGGL((k_group_one<T, M, B, H>), grid_of<B>(n, y), threads, lds, s, p.one);
+    });
+}
+template <typename T, bool M, int B, int H>
+static void one_bwd(const GroupBoth& p, const GroupSpace& at, hipStream_t s) {
+    constexpr int V = kVec<T>;
+    one_launch(p, at, back_lds(p.one.l, V), at.over ? back_lds(p.blocks.l, V) : 0, [&](long long n, int y, dim3 threads, unsigned lds) {
+        if (at.over) hipLaunchKernelGGL((k_group_back_one_sums<T, M, B, H>), grid_of<B>(n, y), threads, lds, s, p.one, p.blocks);
+        else hipLaunchKernelGGL((k_group_back_one<T, M, B, H>), grid_of<B>(n, y), threads, lds, s, p.one);
+    });
+}
+
+template <typename T, bool M>
+static hipError_t group_fwd(const GroupBoth& p, const GroupSpace& at, hipStream_t s) {
+    constexpr int V = kVec<T>;
     if (at.one) {
-        const unsigned lds = one_lds(p.l, V, p.per);
-        if (at.threads == kOneFew) hipLaunchKernelGGL((k_group_one<T, M, kOneFew, 32 / V>), grid_of<kOneFew>(c.batch, p.l.slabs), threads, lds, s, p);
-        else hipLaunchKernelGGL((k_group_one<T, M, kOneMany, 64 / V>), grid_of<kOneMany>(c.batch, p.l.slabs), threads, lds, s, p);
-        return hipGetLastError();
+        if (at.threads == kOneFew) one_fwd<T, M, kOneFew, 32 / V>(p, at, s);
+        else one_fwd<T, M, kOneMany, 64 / V>(p, at, s);
+        if (!at.over) return hipGetLastError();
     }
-    const dim3 grid = grid_of<kGroupThreads>(p.blocks, p.l.slabs);
-    hipLaunchKernelGGL((k_group_sums<T, M>), grid, threads, sums_lds(p.l, V), s, p);
-    if (p.stat) group_join<T, false>(p, s);
-    hipLaunchKernelGGL((k_group_apply<T, M>), grid, threads, 0, s, p);
+    const GroupArgs& b = p.blocks;
+    const dim3 threads(group_threads(b.l)), grid = grid_of<kGroupThreads>(b.blocks, b.l.slabs);
+    if (!at.one) hipLaunchKernelGGL((k_group_sums<T, M>), grid, threads, sums_lds(b.l, V), s, b);
+    if (b.stat) group_join<T, false>(b, s);
+    if (at.over) hipLaunchKernelGGL((k_group_apply<T, M, true>), grid, threads, 0, s, b);
+    else hipLaunchKernelGGL((k_group_apply<T, M, false>), grid, threads, 0, s, b);
     return hipGetLastError();
 }
 
 template <typename T, bool M>
-static hipError_t group_bwd(int dtype, const GroupCall& c, const GroupArgs& p, const GroupSpace& at, hipStream_t s) {
+static hipError_t group_bwd(int dtype, const GroupBoth& p, const GroupSpace& at, hipStream_t s) {
     constexpr int V = kVec<T>;
-    const dim3 threads(group_threads(p.l));
-    const unsigned lds = back_lds(p.l, V);
-    hipError_t e;
+    GroupArgs b = p.blocks;
     if (at.one) {
-        if (at.threads == kOneFew) hipLaunchKernelGGL((k_group_back_one<T, M, kOneFew, 32 / V>), grid_of<kOneFew>(c.batch, p.l.slabs), threads, lds, s, p);
-        else hipLaunchKernelGGL((k_group_back_one<T, M, kOneMany, 64 / V>), grid_of<kOneMany>(c.batch, p.l.slabs), threads, lds, s, p);
-        e = hipGetLastError();
-        if (c.batch == 1) return e;
+        if (at.threads == kOneFew) one_bwd<T, M, kOneFew, 32 / V>(p, at, s);
+        else one_bwd<T, M, kOneMany, 64 / V>(p, at, s);
     } else {
-        hipLaunchKernelGGL((k_group_back_sums<T, M>), grid_of<kGroupThreads>(p.blocks, p.l.slabs), threads, lds, s, p);
-        if (p.out) {
-            if (p.stat) group_join<T, true>(p, s);
-            GroupArgs b = p;
-            b.sum_blocks = p.cols ? (2LL * p.channels + kSumColumns - 1) / kSumColumns : 0;
-            hipLaunchKernelGGL((k_group_back<T, M>), grid_of<kGroupThreads>(p.blocks + b.sum_blocks, p.l.slabs), threads, 0, s, b);
-            return hipGetLastError();
-        }
-        e = hipGetLastError();
+        hipLaunchKernelGGL((k_group_back_sums<T, M>), grid_of<kGroupThreads>(b.blocks, b.l.slabs), dim3(group_threads(b.l)), back_lds(b.l, V), s, b);
     }
-    if (e != hipSuccess || !p.cols) return e;
-    return launch_column_sums(p.cols, (int)p.places, 2LL * p.channels, p.channels, c.dgamma, c.dbeta, dtype, s);
+    // the columns' sums, of samples and blocks behind each other where both took some
+    const long long parts = at.one ? b.batch + (at.over ? b.blocks : 0) : b.places;
+    b.cols = p.one.cols;
+    if (b.out && (!at.one || at.over)) {
+        if (b.stat) group_join<T, true>(b, s);
+        b.places = parts;
+        const int wide = at.over ? kSumColumns<true> : kSumColumns<false>;
+        const bool here = b.cols && (!at.over || parts <= 1024);  // (4608 places of 128: 17 us here, so 8 in a launch of their own)
+        b.sum_blocks = here ? (2LL * b.channels + wide - 1) / wide : 0;
+        const dim3 grid = grid_of<kGroupThreads>(b.blocks + b.sum_blocks, b.l.slabs), threads(group_threads(b.l));
+        if (at.over) hipLaunchKernelGGL((k_group_back<T, M, true>), grid, threads, 0, s, b);
+        else hipLaunchKernelGGL((k_group_back<T, M, false>), grid, threads, 0, s, b);
+        if (here || !b.cols) return hipGetLastError();
+    }
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || !b.cols || (at.one && b.batch == 1)) return e;
+    return launch_column_sums(b.cols, (int)parts, 2LL * b.channels, b.channels, b.dgamma, b.dbeta, dtype, s);
 }
 
 template <typename T>
 static hipError_t group_norm(int dtype, const GroupCall& c, bool back, hipStream_t s) {
-    GroupSpace at;
-    const GroupArgs p = group_args(dtype, c, back, at);
-    if (back) return p.l.merged ? group_bwd<T, true>(dtype, c, p, at, s) : group_bwd<T, false>(dtype, c, p, at, s);
-    return p.l.merged ? group_fwd<T, true>(dtype, c, p, at, s) : group_fwd<T, false>(dtype, c, p, at, s);
+    const GroupSpace at = group_space(c.rows, c.batch, c.channels, c.groups, dtype, c.offsets == nullptr, back);
+    const GroupBoth p = group_args(c, back, at);
+    const bool merged = at.one ? p.one.l.merged : p.blocks.l.merged;  // (of both the same: whether a group is whole vectors)
+    if (back) return merged ? group_bwd<T, true>(dtype, p, at, s) : group_bwd<T, false>(dtype, p, at, s);
+    return merged ? group_fwd<T, true>(p, at, s) : group_fwd<T, false>(p, at, s);
 }
 static hipError_t group_norm(int dtype, const GroupCall& c, bool back, hipStream_t s) {
     switch (dtype) {
