@@ -341,6 +341,8 @@ int sample_offsets(int ndim, int batch, const int32_t* coords, int64_t rows, con
  * empty sample.  Sums are fp64; deviations are taken from the unrounded mean.  A
  * NaN or infinity reaches its sample's group and nothing else.  eps >= 0, held in
  * fp32; with eps 0 a group of equal values gives NaN, as the formula does.
+ * Deviations and rstd gamma are fp32: a value 2^128 away from the mean gives an
+ * infinity, and where rstd gamma is below 2^-126 results lose digits.
  * channels up to 2^24.  Repeated calls give identical bits. */
 size_t group_norm_fwd_workspace(int dtype, int64_t rows, int64_t batch, int64_t channels, int64_t groups);
 int group_norm_fwd(int dtype, const void* x, int64_t rows, const int64_t* offsets, int64_t batch, int64_t channels,

@@ -41,7 +41,8 @@ struct DropoutArgs {
 };
 
 // Eight values a thread and step, of one counter: ten rounds of two 32-bit products each are ten instructions a value, which memory hides.
-// 8192 x 4096 bf16 with a residual: 30 us, 6.6 TB/s; 643072 x 35 fp16: 16 us, 5.5 TB/s (both partly from caches); 64 x 1024 fp32: 2.4 us.
+// Under the profiler, on the same arrays again and again (the last-level cache holds them): 8192 x 4096 bf16 with a residual 30 us, 6.6 TB/s;
+// 643072 x 35 fp16 16 us, 5.5 TB/s; 64 x 1024 fp32 2.6 us.  The first on arrays that change from call to call: 38.7 us, 5.2 TB/s.
 template <typename T>
 __global__ __launch_bounds__(256) void k_dropout(DropoutArgs p) {
     constexpr int V = kVec<T>, H = 8 / V;

@@ -467,7 +467,7 @@ __device__ __forceinline__ void forward_down(const GroupArgs& p, const Columns<k
 
 constexpr int kAhead = 4;  // vectors of x that a thread of the blocks' kernels has on their way
 
-// Sums of a block's rows.  643072 x 64 fp32 in 8 groups: 25 us, 6.5 TB/s of x (caches hold some of it), bound by memory; the fp64 sums of
+// Sums of a block's rows.  643072 x 64 fp32 in 8 groups: 26 us, 6.4 TB/s of x (caches hold some of it), bound by memory; the fp64 sums of
 // 23651 x 16 bf16 take 9 us, where a workgroup has one step: its start, two loads behind one another, LDS.
 template <typename T, bool M, bool OVER>
 __device__ __forceinline__ void block_sums(const GroupArgs& p, long long i, int slab, char* s_step) {
@@ -631,7 +631,7 @@ __device__ __forceinline__ Two join_here(const GroupArgs& p, const Slab& a, cons
     return lanes_two(sum, o.q);
 }
 
-// Results of a block's rows, its last ones first.  643072 x 64 fp32: 51 us, 6.5 TB/s read and written, bound by memory.
+// Results of a block's rows, its last ones first.  643072 x 64 fp32: 50 us, 6.5 TB/s read and written, bound by memory.
 template <typename T, bool M, bool OVER>
 __global__ __launch_bounds__(kGroupThreads, 2) void k_group_apply(GroupArgs p) {
     constexpr int V = kVec<T>, A = M ? 1 : V;
@@ -994,7 +994,7 @@ constexpr int kBackAhead = 2;  // vectors of x and of g
 __host__ __device__ __forceinline__ int step_values(const GroupLayout& l, int v) { return v * (l.active + 1); }
 
 // Sums of a block's rows, of columns first: dgamma and dbeta want these, and those of a group's h and h xh follow from them by gamma.
-// 209645 x 25 fp32 in 5 groups, relu: 14 us, 2.9 TB/s of x and g: eleven steps a workgroup with a start and an end around them.
+// 209645 x 25 fp32 in 5 groups, relu: 15 us, 2.9 TB/s of x and g: eleven steps a workgroup with a start and an end around them.
 template <typename T, bool M, bool OVER>
 __device__ __forceinline__ void block_back_sums(const GroupArgs& p, long long i, int slab, char* s_step) {
     constexpr int V = kVec<T>, A = M ? 1 : V, U = kBackAhead;
@@ -1133,7 +1133,7 @@ __global__ __launch_bounds__(kGroupThreads, 2) void k_group_back(GroupArgs p) {
 }
 
 // Backward by a workgroup a sample and slab, x, g and dz in registers.  cols [batch][2][channels]; with one sample dgamma and dbeta
-// themselves.  64 samples of 512 x 256 bf16 in 32 groups, silu: 16 us, 3.2 TB/s, bound by the instructions of silu and its slope and by
+// themselves.  64 samples of 512 x 256 bf16 in 32 groups, silu: 15 us, 3.4 TB/s, bound by the instructions of silu and its slope and by
 // what a workgroup does between its loads and its stores; k_column_sums behind it 4 us.
 template <typename T, bool M, int H, bool OVER>
 __device__ __forceinline__ void one_back(const GroupArgs& p, long long b, char* s_step) {

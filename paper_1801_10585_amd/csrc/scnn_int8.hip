@@ -45,7 +45,7 @@ __device__ __forceinline__ int quantized(float v, const Quantizer& q) {
 
 // P threads a row (a group of lanes of a wave, or a workgroup of whole waves), H vectors of the row in a thread's registers; what a
 // longer row has more is read again.  Bound by memory, one reading of rows of up to 2 P vectors: 8192 x 4096 bf16 19 us (5.3 TB/s),
-// 200000 x 64 bf16 9.5 us by 4 threads a row (16.4 by 16), 64 x 12288 fp16 4.2 us by 1024.
+// 200000 x 64 bf16 8.4 us by 4 threads a row (16.4 by 16), 64 x 12288 fp16 4.2 us by 1024.
 template <typename T, int P, int H>
 __global__ __launch_bounds__(P < 256 ? 256 : P) void k_quantize_rows(const T* __restrict__ x, long long rows_cap,
                                                                      const long long* __restrict__ rows_dev, long long channels,
@@ -254,10 +254,11 @@ __device__ __forceinline__ void finish(const Int8Args& p, long long m, long long
 // one, what they add up to is not stored; a row that ends in the middle of a step has its first half copied twice and multiplied once.
 // The operands swap places at the instruction: its rows are the tile's columns n, in pairs of blocks (block b of a pair takes columns
 // 8 (i / 4) + 4 b + i % 4, i < 16), so that a lane ends with eight neighbouring columns of one row.
-// 8192 x 4096 x 4096 bf16 out, tiles of 256: 129 us, with gelu and a residual 142, 2130 and 1940 TOP/s (the library's bare product 2070).
+// 8192 x 4096 x 4096 bf16 out, tiles of 256, in a graph: 123 us, with gelu and a residual 148, 2230 and 1860 TOP/s (the library's bare product
+// 2030 to 2070); under the profiler the second 165, the least of 21 149.
 // LDS has no conflict; one workgroup a unit, whose waves wait at a barrier a step, and an epilogue that nothing overlaps.  (Four waves
 // of 128 x 128 one and a half times as long; without s_setprio 7 per cent longer; both halves' operands read ahead: no change.)
-// 3001 x 1001 x 1303 fp32 out, tiles of 64: 12 us, four workgroups a unit, mostly their starts and ends.
+// 3001 x 1001 x 1303 fp32 out, tiles of 64: 13 us, four workgroups a unit, mostly their starts and ends.
 template <bool PAIR>
 __device__ __forceinline__ int spread(int r) { return PAIR ? (r & 3) | ((r >> 1) & 4) : r & 7; }  // (eight lanes read rows 0 to 7, PAIR: 0 to 3 and 8 to 11)
 
@@ -390,8 +391,8 @@ __global__ __launch_bounds__(64 * WM * WN) void k_int8_ring(Int8Args p) {
 }
 
 // Up to 16 MB rows: bound by reading w once.  Eight waves share the k of 16 NB columns, operands straight from memory to the
-// registers that the instruction wants, a lane 16 bytes of one row; their sums meet in LDS.  8 x 4096 -> 4096 in 8 bits: 6.8 us, 2.5 TB/s;
-// 32 x 4096 -> 4096 9.1 (tiles of 64 longer than that up to 32 rows).
+// registers that the instruction wants, a lane 16 bytes of one row; their sums meet in LDS.  8 x 4096 -> 4096 in 8 bits: 6.4 us, 2.6 TB/s;
+// 32 x 4096 -> 4096 8.9 (tiles of 64 longer than that up to 32 rows).
 template <typename T, int MB, int NB>
 __global__ __launch_bounds__(512) void k_int8_skinny(Int8Args p) {
     constexpr int W = 8, U = 4;
