@@ -356,10 +356,10 @@ int group_norm_fwd(int dtype, const void* x, int64_t rows, const int64_t* offset
  * mean, rstd as group_norm_fwd gave them (mean is fp32 here: where a group's mean
  * is m times its spread, xh is off by up to 2^-24 m); offsets, batch, gamma, beta
  * as there.  dx, dgamma, dbeta: each nullable.  Rows outside the samples are
- * neither read nor written in dx; without any dgamma and dbeta are 0.  A sum is
- * fp32 over a run of up to 32 values and over the runs' neighbours in a workgroup
- * (up to 120 roundings of 2^-24 of the magnitudes added in all, whatever the
- * number of rows), fp64 beyond.  Repeated calls give identical bits. */
+ * neither read nor written in dx; without any dgamma and dbeta are 0.  Sums
+ * are fp32 over runs of up to 32 values of a thread and across a workgroup's
+ * threads (up to 120 roundings of 2^-24 of the magnitudes added in all, whatever
+ * the number of rows), fp64 beyond.  Repeated calls give identical bits. */
 size_t group_norm_bwd_workspace(int dtype, int64_t rows, int64_t batch, int64_t channels, int64_t groups);
 int group_norm_bwd(int dtype, const void* x, const void* g, int64_t rows, const int64_t* offsets, int64_t batch,
                    int64_t channels, int64_t groups, const void* gamma, const void* beta, const float* mean,

@@ -1343,7 +1343,7 @@ constexpr long long kOneMost = 65536;
 struct GroupSpace {
     GroupLayout one_l, l;  // of a workgroup a sample, of blocks
     long long blocks, chunk, places, over;
-    size_t part, cols, stat, total;
+    size_t part, stat, total;  // (the columns' sums, where there are some, come first)
     bool one, joined;
     int threads;
     bool any_blocks() const { return !one || over; }

@@ -117,6 +117,51 @@ def test_a_nan_stays_in_its_sample_and_group():
         assert bool(dx[hit].isnan().all()) and bool(dx[~hit].isfinite().all()) and torch.equal(dgamma.isnan(), hit.any(0))
 
 
+@pytest.mark.parametrize("k", (0, 3, 6, 9))
+def test_a_workspace_of_the_size_asked_for(k):
+    """Nothing is written beside it, and what it held before does not matter."""
+    rows, channels, groups, offsets = CASES[k]
+    d = make(3, rows, channels, torch.float32)
+    where, batch = torch.tensor(offsets, device=DEV), len(offsets) - 1
+
+    def both(rooms):
+        y, m, r = scnn.group_norm_fwd(d["x"], groups, d["gamma"], d["beta"], offsets=where, act="silu", workspace=rooms[0])
+        dx, dgamma, dbeta = scnn.group_norm_bwd(d["x"], d["g"], groups, d["gamma"], d["beta"], m, r, offsets=where, act="silu", workspace=rooms[1])
+        return [y[offsets[0]:offsets[-1]], m, r, dx[offsets[0]:offsets[-1]], dgamma, dbeta]
+
+    want = both((None, None))
+    for fill in (0xA5, 0xFF):
+        held, rooms = [], []
+        for query in (scnn.group_norm_fwd_workspace, scnn.group_norm_bwd_workspace):
+            need = query(torch.float32, rows, batch, channels, groups)
+            held.append(torch.full((need + 1024,), fill, dtype=torch.uint8, device=DEV))
+            rooms.append(held[-1][512:512 + need])
+        assert all(torch.equal(a, b) for a, b in zip(both(rooms), want))
+        for whole, room in zip(held, rooms):
+            assert bool((whole[:512] == fill).all()) and bool((whole[512 + room.numel():] == fill).all())
+
+
+def test_calls_on_two_streams_at_once():
+    rows, channels, groups, offsets = CASES[4]
+    d = make(4, rows, channels, torch.bfloat16)
+    cuts = [offsets, one_long(rows, len(offsets) - 1)]
+    where = [torch.tensor(c, device=DEV) for c in cuts]
+
+    def calls(k, stream=None):
+        y, m, r = scnn.group_norm_fwd(d["x"], groups, d["gamma"], offsets=where[k], act="gelu", stream=stream)
+        dx, *rest = scnn.group_norm_bwd(d["x"], d["g"], groups, d["gamma"], None, m, r, offsets=where[k], act="gelu", stream=stream)
+        return [y[:cuts[k][-1]], m, r, dx[:cuts[k][-1]], *rest]  # (rows behind the last sample are not written)
+
+    want = [calls(k) for k in range(2)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(5):
+        got = [calls(k, streams[k]) for k in range(2)]
+        torch.cuda.synchronize()
+        for a, b in zip(got, want):
+            assert all(torch.equal(p, q) for p, q in zip(a, b))
+
+
 def test_numbers_that_do_not_ascend_end():
     """No defined result, but an end to the call."""
     rows, channels = 40000, 16
